@@ -341,6 +341,156 @@ int32_t d3_stall_next_step(d3_model *m);
 void d3_free(d3_model *m);    /* host bookkeeping only */
 const char *d3_strerror(int32_t code);
 
+/* ---------------------------------------------------------------- paged key-value operators
+ *
+ * The cache side of a decode step as operators of its own, for a caller that runs a block itself
+ * (an adapter, a drafted block, a step captured into a graph) over a paged cache of the layout
+ * D3_KV_PAGED describes, or over the cache of a loaded model (d3_paged_view):
+ *   d3_page_plan        pages, block table rows and the slot map of a step from request lengths
+ *   d3_paged_append     the step's K (rotated) and V into their slots, q rotated beside them
+ *   d3_paged_attention  one new token per row over its pages
+ * All lengths, tables, maps and page ids are DEVICE data: nothing is read back, so the three can be
+ * captured into a graph and replayed with other lengths.  They need no model handle.  Each depth-decayed
+ * block can have a table and lengths of its own (Sec. 3.2: a dropped block's entries are never
+ * written).
+ *
+ * Common rules.  Work goes to `cuda_stream` on the CURRENT device, which must own every buffer.
+ * Sizes, strides (in elements) and alignment are checked on the host (D3_EINVAL, nothing enqueued).
+ * Device data is checked where it is used, against the bounds the host gave: a value out of range is
+ * never used as an index; the call skips what it stands for, as said below, and stores D3_EINVAL to
+ * `status_dev` (int32, never cleared by these calls; nullable except where noted).  One workspace
+ * serves one call at a time: calls that may overlap need a workspace each. */
+#define D3_BF16 0
+#define D3_FP16 1
+#define D3_FP32 2
+#define D3_E4M3 3            /* 8-bit float of 4 exponent and 3 mantissa bits, no infinity, largest 448 */
+#define D3_MAX_REQUESTS 4096 /* requests of one d3_page_plan */
+
+/* A pool of pages: entry (page, kv head, position in the page, dim) of K sits at
+ * k_dev[page * page_stride + head * head_stride + position * token_stride + dim], of V likewise.
+ * D3_KV_PAGED's own layout is token_stride = head_dim, head_stride = page_size * head_dim.
+ * Both bases and all strides in bytes are multiples of 16. */
+typedef struct d3_paged_kv {
+  uint32_t struct_size;      /* sizeof(d3_paged_kv), checked                             */
+  int32_t dtype;             /* D3_BF16, D3_FP16 or D3_E4M3                              */
+  int32_t n_pages;
+  int32_t page_size;         /* a power of two, 16..1024                                 */
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 32, 64 or 128                                            */
+  int64_t page_stride, head_stride, token_stride;
+  void *k_dev, *v_dev;
+  const float *k_scale_dev, *v_scale_dev; /* E4M3 only: fp32 [n_kv_heads], the stored number times
+                                the scale is the value; NULL = 1                         */
+} d3_paged_kv;
+
+/* Block tables and slot maps of one step.  Request b has cached[b] tokens in the pages its table
+ * row names and gets new_tokens[b] more; a NEGATIVE count ends the request and gives its pages back.
+ * In order: the pages of ended requests are pushed on the free stack (request by request, page by
+ * page), then the pages the new tokens need beyond those in place are popped from its top (request
+ * by request) into the table.  Table entries of ended requests are left as they are.
+ *   cached_out [n_requests]   cached + new; 0 for an ended request (may be cached_dev itself)
+ *   n_free_out [1]            (may be n_free_dev itself)
+ *   first      [n_requests+1] where each request's tokens start in the maps below
+ *   slots      [max_tokens] int64   page * page_size + position in the page, tokens request by request
+ *   row, context [max_tokens]       the token's request; the tokens it attends to (its position + 1)
+ * Map entries behind the last token are padding: slot -1, row -1, context 0.
+ * All or nothing: with too few free pages, a request longer than table_width pages, more tokens than
+ * max_tokens (D3_ECAPACITY), or cached, n_free or the count of pages given back out of range
+ * (D3_EINVAL), status_dev gets the code, table, stack and lengths stay, and every map entry is
+ * padding.  A token whose page id is not in [0, n_pages) gets slot -1, and D3_EINVAL is stored. */
+typedef struct d3_page_plan_args {
+  uint32_t struct_size;
+  int32_t n_requests;        /* 1..D3_MAX_REQUESTS                                       */
+  int32_t page_size;         /* a power of two, 16..1024                                 */
+  int32_t n_pages;           /* pages in the pool = entries of the free stack            */
+  int32_t table_width;       /* entries of a table row that may be used                  */
+  int32_t max_tokens;        /* entries of slots, row and context                        */
+  int64_t table_stride;      /* entries from one row to the next, >= table_width         */
+  const int32_t *cached_dev, *new_tokens_dev;
+  int32_t *table_dev, *free_dev;
+  const int32_t *n_free_dev;
+  int32_t *cached_out_dev, *n_free_out_dev, *first_dev;
+  int64_t *slots_dev;
+  int32_t *row_dev, *context_dev;
+  int32_t *status_dev;
+} d3_page_plan_args;
+int32_t d3_page_plan(const d3_page_plan_args *a, void *cuda_stream);
+
+/* K and V of n_tokens tokens [token][kv head][head_dim] to the slots of `slots`; with `rope_dev`, K
+ * is rotated first and the queries [token][q head][head_dim] go rotated to q_out (q itself allowed).
+ * rope_dev: fp32 [rope_len][head_dim / 2] pairs (cos, sin) (d3_rope_table); a token's position is
+ * context - 1; pairs are (j, j + head_dim / 2).  Products and sums are fp32, each rounded once; the
+ * result is rounded once to the cache's type (E4M3: after division by the scale, saturating).
+ * Types: dtype of q, k, v, q_out / of the cache: BF16 / BF16, FP32 / BF16, FP16 / FP16, BF16 / E4M3,
+ * FP16 / E4M3.  A token with a negative slot is padding: nothing of it is read or written.  A slot
+ * beyond the pool or a position beyond rope_len: the token is skipped, D3_EINVAL is stored.  The
+ * slots of one call are distinct; of a repeated one it is open, number by number, which token's stays. */
+typedef struct d3_paged_append_args {
+  uint32_t struct_size;
+  int32_t dtype;
+  int32_t n_tokens;          /* >= 0                                                     */
+  int32_t n_q_heads;         /* with q_dev                                               */
+  int32_t rope_len;
+  const void *k_dev, *v_dev;
+  int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  const void *q_dev;         /* nullable; needs rope_dev                                 */
+  void *q_out_dev;
+  int64_t q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride;
+  const int64_t *slots_dev;
+  const int32_t *context_dev; /* with rope_dev                                           */
+  const float *rope_dev;     /* nullable: K is stored as it comes                        */
+  int32_t *status_dev;
+} d3_paged_append_args;
+int32_t d3_paged_append(const d3_paged_kv *kv, const d3_paged_append_args *a, void *cuda_stream);
+
+/* The rotary table of the model path (fp64 angles position * base^(-2j / head_dim), rounded to fp32
+ * (cos, sin)) for positions 0..n_positions-1, to table_dev fp32 [n_positions][head_dim / 2][2]. */
+int32_t d3_rope_table(int32_t n_positions, int32_t head_dim, float rope_base, float *table_dev,
+                      void *cuda_stream);
+
+/* Attention of one new token per row: query head h of row b over the first context[b] positions of
+ * the pages that table row rows[b] names (rows_dev NULL: row b itself), kv head h / (Hq / Hkv):
+ *   out = sum_t softmax_t(scale q . k_t) v_t,   lse = log sum_t exp(scale q . k_t)  (nullable)
+ * Scores, softmax and sums are fp32; out is rounded once to dtype.  Types as in d3_paged_append (q
+ * and out / cache).  The length is cut into equal shares over the SMs, whichever rows they fall in,
+ * and a second kernel joins the rows that were cut; the order of the sums is fixed by the lengths, so
+ * equal inputs give equal bits.
+ * context 0: out = 0, lse = -inf.  rows[b] = -1: padding, the row's outputs stay as they are.  What
+ * the pages hold behind the context is never used, NaN included.  Out-of-range data stores D3_EINVAL:
+ * a context beyond table_width pages (or negative) counts as 0, another bad rows[b] as padding, and
+ * the positions of a bad page id are left out.  status_dev also gets D3_ETIMEOUT when a bounded wait ran out (out and
+ * lse are then undefined).  workspace_dev: d3_paged_attention_workspace bytes, 256-byte aligned,
+ * contents need no set-up and are used only during the call. */
+typedef struct d3_paged_attention_args {
+  uint32_t struct_size;
+  int32_t dtype;
+  int32_t n_rows;            /* 0..65535                                                 */
+  int32_t n_q_heads;         /* a multiple of n_kv_heads                                 */
+  int32_t table_rows, table_width;
+  int64_t table_stride;
+  float scale;               /* finite                                                   */
+  const void *q_dev;         /* base and strides in bytes: multiples of 16               */
+  int64_t q_row_stride, q_head_stride;
+  void *out_dev;
+  int64_t out_row_stride, out_head_stride;
+  float *lse_dev;            /* nullable, fp32 [n_rows][n_q_heads]                       */
+  const int32_t *table_dev, *context_dev;
+  const int32_t *rows_dev;   /* nullable                                                 */
+  void *workspace_dev;
+  size_t workspace_bytes;
+  int32_t *status_dev;
+} d3_paged_attention_args;
+int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args *a, void *cuda_stream);
+/* Workspace bytes for any call over `kv` with n_q_heads query heads (k_dev, v_dev are not looked at). */
+int32_t d3_paged_attention_workspace(const d3_paged_kv *kv, int32_t n_q_heads, size_t *bytes);
+
+/* The pool and the table of one block of a loaded PAGED model, for the calls above (read-only use: the
+ * model keeps its own bookkeeping): *table_dev is int32 [*table_rows = max_slots][*table_width], row =
+ * slot, entries 0 where nothing was written.  A slot's context is d3_slot_pos.  Calls on another
+ * stream than the model's must be ordered after its steps by the caller. */
+int32_t d3_paged_view(const d3_model *m, int32_t layer, d3_paged_kv *kv, const int32_t **table_dev,
+                      int32_t *table_rows, int32_t *table_width);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,7 +28,9 @@ EXPORTS = ("d3_depth", "d3_schedule", "d3_workspace_bytes", "d3_load", "d3_prefi
            "d3_set_exec", "d3_profile", "d3_read_profile", "d3_profile_name", "d3_read_fused_phases",
            "d3_decode_step_noalloc", "d3_noalloc_status", "d3_set_policy", "d3_set_wait_ns",
            "d3_stall_next_step", "d3_slot_pos",
-           "d3_kv_pages_used", "d3_reset_slot", "d3_sync", "d3_free", "d3_strerror")
+           "d3_kv_pages_used", "d3_reset_slot", "d3_sync", "d3_free", "d3_strerror",
+           "d3_page_plan", "d3_paged_append", "d3_rope_table", "d3_paged_attention",
+           "d3_paged_attention_workspace", "d3_paged_view")
 
 
 class Config(C.Structure):
@@ -98,6 +100,13 @@ def _load() -> C.CDLL:
     lib.d3_free.restype = None
     lib.d3_strerror.argtypes = [I32]
     lib.d3_strerror.restype = C.c_char_p
+    # paged key-value operators: the argument structs are in paged.py
+    lib.d3_page_plan.argtypes = [P, P]
+    lib.d3_paged_append.argtypes = [P, P, P]
+    lib.d3_rope_table.argtypes = [I32, I32, C.c_float, P, P]
+    lib.d3_paged_attention.argtypes = [P, P, P]
+    lib.d3_paged_attention_workspace.argtypes = [P, I32, C.POINTER(C.c_size_t)]
+    lib.d3_paged_view.argtypes = [P, I32, P, C.POINTER(P), C.POINTER(I32), C.POINTER(I32)]
     return lib
 
 
@@ -388,6 +397,12 @@ class D3Model:
         if rc < 0:
             raise D3Error(rc, "d3_kv_pages_used")
         return rc
+
+    def d3_paged_view(self, layer: int):
+        """(pool, table) of one block of a paged model, for paged.d3_paged_append / d3_paged_attention:
+        a paged.PagedKV over the model's cache and its int32 table [max_slots][pages per slot]."""
+        from . import paged
+        return paged.model_view(self, layer)
 
     def d3_reset_slot(self, slot: int) -> None:
         rc = LIB.d3_reset_slot(self.h, slot)

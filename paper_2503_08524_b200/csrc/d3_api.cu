@@ -891,6 +891,26 @@ int32_t d3_slot_pos(const d3_model *m, int32_t slot) {
   return m->pos[slot] < 0 ? D3_ESTATE : m->pos[slot];
 }
 
+int32_t d3_paged_view(const d3_model *m, int32_t layer, d3_paged_kv *kv, const int32_t **table_dev,
+                      int32_t *table_rows, int32_t *table_width) {
+  if (!m || !kv || !table_dev || !table_rows || !table_width || layer < 0 || layer >= m->cfg.n_layers ||
+      m->cfg.kv_layout != D3_KV_PAGED)
+    return D3_EINVAL;
+  const d3_config &c = m->cfg;
+  memset(kv, 0, sizeof(*kv));
+  kv->struct_size = sizeof(*kv);
+  kv->dtype = D3_BF16;
+  kv->n_pages = c.n_pages; kv->page_size = c.page_size; kv->n_kv_heads = c.n_kv_heads; kv->head_dim = c.head_dim;
+  kv->token_stride = c.head_dim;
+  kv->head_stride = (int64_t)c.page_size * c.head_dim;
+  kv->page_stride = kv->head_stride * c.n_kv_heads;
+  kv->k_dev = m->Kc; kv->v_dev = m->Vc;
+  *table_dev = m->bt_dev() + (size_t)layer * c.max_slots * (c.max_seq / c.page_size);
+  *table_rows = c.max_slots;
+  *table_width = c.max_seq / c.page_size;
+  return D3_OK;
+}
+
 int32_t d3_reset_slot(d3_model *m, int32_t slot) {
   if (!m || slot < 0 || slot >= m->cfg.max_slots) return D3_EINVAL;
   m->pos[slot] = -1;

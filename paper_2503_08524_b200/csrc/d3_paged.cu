@@ -1,0 +1,607 @@
+// Paged key-value operators: block tables and slot maps, append, and the C ABI of the three calls.
+#include <cuda.h>   // CUtensorMap and its enums; the encoder is fetched at run time
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <math.h>
+
+#include "d3_paged.cuh"
+
+namespace d3 {
+
+namespace {
+
+// ------------------------------------------------------------------ plan
+// Latency decides: the whole plan is one launch.  Every CTA of one cluster reads the R lengths and
+// keeps the three running sums (tokens, pages needed, pages given back) of all requests in shared
+// memory; after the cluster barrier no input length is read any more, so the outputs may be the inputs
+// themselves, and the CTAs share the page and token entries between them.  A page that is taken is
+// looked up by its rank in (old stack ++ pages given back), so nothing waits for the stack to be written.
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanMaxPer = D3_MAX_REQUESTS / kPlanThreads;   // requests of one thread
+
+struct PlanArgs {
+  int R, page_shift, n_pages, width, T;
+  long long table_stride;
+  const int32_t *cached, *added;
+  int32_t *table, *free_pages;
+  const int32_t *n_free;
+  int32_t *cached_out, *n_free_out, *first;
+  long long *slots;
+  int32_t *row, *context, *status;
+};
+
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ unsigned cluster_size() {
+  unsigned r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// the request whose half-open range [sum[b], sum[b + 1]) holds x  (sum[0] = 0 <= x < sum[R])
+__device__ __forceinline__ int owner(const int *sum, int R, int x) {
+  int lo = 0, hi = R;          // sum[lo] <= x < sum[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (sum[mid] <= x) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) k_page_plan(const __grid_constant__ PlanArgs a) {
+  extern __shared__ int s_plan[];
+  int *s_first = s_plan, *s_need = s_first + (a.R + 1), *s_back = s_need + (a.R + 1), *s_cached = s_back + (a.R + 1);
+  __shared__ long long s_warp[3][kPlanThreads / 32];
+  __shared__ int s_bad;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int page_mask = (1 << a.page_shift) - 1;
+  const long long max_len = (long long)a.width << a.page_shift;
+  if (tid == 0) s_bad = 0;
+  pdl_wait();
+  pdl_trigger();
+  __syncthreads();
+
+  const int n_free = *a.n_free;
+  const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
+  long long sum[3] = {0, 0, 0};                       // this thread's tokens, pages needed, pages given back
+  int c_[kPlanMaxPer], add_[kPlanMaxPer], need_[kPlanMaxPer], back_[kPlanMaxPer];
+  int bad = (n_free < 0 || n_free > a.n_pages) ? 2 : 0;
+#pragma unroll
+  for (int i = 0; i < kPlanMaxPer; ++i) {
+    const int b = tid * per + i;
+    c_[i] = add_[i] = need_[i] = back_[i] = 0;
+    if (i < per && b < a.R) {
+      const int c = a.cached[b], n = a.added[b];
+      const long long grown = (long long)c + (n > 0 ? n : 0);
+      if (c < 0 || c > max_len) { bad |= 2; }
+      else if (grown > max_len) { bad |= 1; }
+      else {
+        const int have = (int)(((long long)c + page_mask) >> a.page_shift);
+        c_[i] = c;
+        if (n < 0) back_[i] = have;
+        else {
+          add_[i] = n;
+          need_[i] = (int)((grown + page_mask) >> a.page_shift) - have;
+        }
+      }
+      sum[0] += add_[i]; sum[1] += need_[i]; sum[2] += back_[i];
+    }
+  }
+  if (bad) atomicOr(&s_bad, bad);
+  long long inc[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    long long v = sum[k];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane >= d) v += u;
+    }
+    inc[k] = v;
+    if (lane == 31) s_warp[k][warp] = v;
+  }
+  __syncthreads();
+  long long total[3], before[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    long long v = s_warp[k][lane];                    // one value per warp
+    const long long own = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane >= d) v += u;
+    }
+    total[k] = __shfl_sync(0xffffffffu, v, 31);
+    before[k] = __shfl_sync(0xffffffffu, v - own, warp) + inc[k] - sum[k];
+  }
+  bad = s_bad;
+  if ((long long)n_free + total[2] > a.n_pages) bad |= 2;      // more pages than there are came back
+  if (total[0] > a.T || total[1] > n_free + total[2]) bad |= 1;
+  if (!bad) {
+#pragma unroll
+    for (int i = 0; i < kPlanMaxPer; ++i) {
+      const int b = tid * per + i;
+      if (i < per && b < a.R) {
+        s_first[b] = (int)before[0]; s_need[b] = (int)before[1]; s_back[b] = (int)before[2];
+        s_cached[b] = c_[i];
+        before[0] += add_[i]; before[1] += need_[i]; before[2] += back_[i];
+      }
+    }
+    if (tid == 0) { s_first[a.R] = (int)total[0]; s_need[a.R] = (int)total[1]; s_back[a.R] = (int)total[2]; }
+  }
+  // all CTAs have read the lengths and the stack's height: they may be overwritten from here on
+  cluster_barrier();
+  __syncthreads();
+
+  const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
+  const int gid = rank * kPlanThreads + tid, step = ctas * kPlanThreads;
+  if (rank == 0) {
+#pragma unroll
+    for (int i = 0; i < kPlanMaxPer; ++i) {
+      const int b = tid * per + i;
+      if (i < per && b < a.R) {
+        if (!bad) {
+          a.cached_out[b] = back_[i] ? 0 : c_[i] + add_[i];
+          a.first[b] = s_first[b];
+        } else {
+          if (a.cached_out != a.cached) a.cached_out[b] = a.cached[b];
+          a.first[b] = 0;
+        }
+      }
+    }
+    if (tid == 0) {
+      a.first[a.R] = bad ? 0 : (int)total[0];
+      if (!bad) *a.n_free_out = (int)(n_free + total[2] - total[1]);
+      else if (a.n_free_out != a.n_free) *a.n_free_out = n_free;
+      if (bad && a.status) *a.status = (bad & 2) ? D3_EINVAL : D3_ECAPACITY;
+    }
+  }
+  const int n_tok = bad ? 0 : (int)total[0], n_need = bad ? 0 : (int)total[1], n_back = bad ? 0 : (int)total[2];
+  const int top = n_free + n_back;
+  // entry i of (old stack ++ pages given back)
+  auto stack = [&](int i) -> int {
+    if (i < n_free) return a.free_pages[i];
+    const int b = owner(s_back, a.R, i - n_free);
+    return a.table[b * a.table_stride + (i - n_free - s_back[b])];
+  };
+  auto pages_of = [&](int len) { return (len + page_mask) >> a.page_shift; };   // len <= 2^31 - 1024 (checked on the host)
+
+  for (int e = gid; e < n_back; e += step) {
+    const int b = owner(s_back, a.R, e);
+    a.free_pages[n_free + e] = a.table[b * a.table_stride + (e - s_back[b])];
+  }
+  for (int e = gid; e < n_need; e += step) {
+    const int b = owner(s_need, a.R, e);
+    a.table[b * a.table_stride + pages_of(s_cached[b]) + (e - s_need[b])] = stack(top - 1 - e);
+  }
+  // four consecutive tokens per thread: one search, the map entries in 16-byte pieces
+  bool strange = false;
+  for (long long t0 = (long long)gid * 4; t0 < a.T; t0 += (long long)step * 4) {
+    long long slot[4];
+    int row[4], ctx[4];
+    int b = t0 < n_tok ? owner(s_first, a.R, (int)t0) : a.R;
+    int last_page = -1, id = -1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const long long t = t0 + i;
+      slot[i] = -1; row[i] = -1; ctx[i] = 0;
+      if (t < n_tok) {
+        while (t >= s_first[b + 1]) { ++b; last_page = -1; }
+        const int pos = s_cached[b] + (int)(t - s_first[b]);
+        const int pg = pos >> a.page_shift, have = pages_of(s_cached[b]);
+        if (pg != last_page) {
+          // a page taken by this call is read from the stack: its table entry may not be written yet
+          id = pg < have ? a.table[b * a.table_stride + pg] : stack(top - 1 - (s_need[b] + pg - have));
+          last_page = pg;
+        }
+        row[i] = b;
+        ctx[i] = pos + 1;
+        if (id >= 0 && id < a.n_pages) slot[i] = ((long long)id << a.page_shift) | (pos & page_mask);
+        else strange = true;
+      }
+    }
+    if (t0 + 4 <= a.T) {
+      reinterpret_cast<longlong2 *>(a.slots + t0)[0] = make_longlong2(slot[0], slot[1]);
+      reinterpret_cast<longlong2 *>(a.slots + t0)[1] = make_longlong2(slot[2], slot[3]);
+      *reinterpret_cast<int4 *>(a.row + t0) = make_int4(row[0], row[1], row[2], row[3]);
+      *reinterpret_cast<int4 *>(a.context + t0) = make_int4(ctx[0], ctx[1], ctx[2], ctx[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (t0 + i < a.T) { a.slots[t0 + i] = slot[i]; a.row[t0 + i] = row[i]; a.context[t0 + i] = ctx[i]; }
+    }
+  }
+  if (strange && a.status) *a.status = D3_EINVAL;
+}
+
+// ------------------------------------------------------------------ append
+// Bandwidth: every number once in and once out.  A thread takes the pairs (8 numbers of a head's lower
+// half, the 8 that they are paired with), so the rotation needs no exchange and all traffic is in
+// 16-byte pieces (8 for the 8-bit cache); it keeps the 8 (cos, sin) of its piece for H heads of the token.
+struct AppendArgs {
+  long long n_tokens;
+  int hq, rope_len, chunks;     // chunks: groups of H heads per token
+  const void *k, *v, *q;
+  void *q_out;
+  long long kt, kh, vt, vh, qt, qh, ot, oh;   // token and head strides
+  const long long *slots;
+  const int32_t *context;
+  const float *rope;
+  int32_t *status;
+  KvPool kv;
+};
+
+template <typename T> struct Vec8 { float f[8]; };
+
+__device__ __forceinline__ void load8(const float *p, float *f) {
+  const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16 *p, float *f) {
+  const uint4 u = *reinterpret_cast<const uint4 *>(p);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(w[i] << 16);
+    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8(const __half *p, float *f) {
+  const uint4 u = *reinterpret_cast<const uint4 *>(p);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+    f[2 * i] = v.x; f[2 * i + 1] = v.y;
+  }
+}
+__device__ __forceinline__ void store8(float *p, const float *f) {
+  reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+  reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+}
+__device__ __forceinline__ void store8(bf16 *p, const float *f) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t *>(&v);
+  }
+  *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store8(__half *p, const float *f) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 v = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t *>(&v);
+  }
+  *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store8(__nv_fp8_e4m3 *p, const float *f) {
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i], f[4 * i + 1]), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i + 2], f[4 * i + 3]), __NV_SATFINITE, __NV_E4M3);
+    w[i] = lo | (hi << 16);
+  }
+  *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+}
+
+template <typename X, typename C, int DH, int H>
+__global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ AppendArgs a) {
+  constexpr int HALF = DH / 2, PIECES = HALF / 8;
+  pdl_wait();
+  pdl_trigger();
+  const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int j = (int)(id % PIECES);
+  const long long u = id / PIECES;
+  const int chunk = (int)(u % a.chunks);
+  const long long t = u / a.chunks;
+  if (t >= a.n_tokens) return;
+  const long long slot = a.slots[t];
+  if (slot < 0) return;
+  int pos = 0;
+  bool bad = slot >= ((long long)a.kv.n_pages << a.kv.page_shift);
+  if (a.rope) {
+    pos = a.context[t] - 1;
+    bad = bad || pos < 0 || pos >= a.rope_len;
+  }
+  if (bad) {
+    if (a.status) *a.status = D3_EINVAL;
+    return;
+  }
+  const int heads = a.hq + 2 * a.kv.n_kv_heads, h0 = chunk * H;
+  const long long in_page = slot & ((1 << a.kv.page_shift) - 1);
+  const long long entry = (slot >> a.kv.page_shift) * a.kv.page_stride + in_page * a.kv.token_stride;
+
+  // all loads of the thread are issued before the first is used
+  float lo[H][8], hi[H][8];
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    const int h = h0 + i;
+    if (h < heads) {
+      const X *p = h < a.hq ? static_cast<const X *>(a.q) + t * a.qt + (long long)h * a.qh
+                   : h < a.hq + a.kv.n_kv_heads ? static_cast<const X *>(a.k) + t * a.kt + (long long)(h - a.hq) * a.kh
+                   : static_cast<const X *>(a.v) + t * a.vt + (long long)(h - a.hq - a.kv.n_kv_heads) * a.vh;
+      load8(p + 8 * j, lo[i]);
+      load8(p + HALF + 8 * j, hi[i]);
+    }
+  }
+  float cs[16];
+  if (a.rope && h0 < a.hq + a.kv.n_kv_heads) {
+    const float *r = a.rope + ((long long)pos * HALF + 8 * j) * 2;
+    load8(r, cs);
+    load8(r + 8, cs + 8);
+  }
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    const int h = h0 + i;
+    if (h >= heads) continue;
+    if (a.rope && h < a.hq + a.kv.n_kv_heads) {
+      // products and sums rounded one by one: no contraction, so every store rounds the same number
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float c = cs[2 * e], s = cs[2 * e + 1], x = lo[i][e], y = hi[i][e];
+        lo[i][e] = __fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s));
+        hi[i][e] = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
+      }
+    }
+    if (h < a.hq) {
+      X *p = static_cast<X *>(a.q_out) + t * a.ot + (long long)h * a.oh;
+      store8(p + 8 * j, lo[i]);
+      store8(p + HALF + 8 * j, hi[i]);
+    } else {
+      const bool is_v = h >= a.hq + a.kv.n_kv_heads;
+      const int kh = h - a.hq - (is_v ? a.kv.n_kv_heads : 0);
+      C *p = static_cast<C *>(is_v ? a.kv.v : a.kv.k) + entry + (long long)kh * a.kv.head_stride;
+      if (sizeof(C) == 1) {
+        const float *sc = is_v ? a.kv.v_scale : a.kv.k_scale;
+        if (sc) {
+          const float d = sc[kh];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { lo[i][e] = __fdiv_rn(lo[i][e], d); hi[i][e] = __fdiv_rn(hi[i][e], d); }
+        }
+      }
+      store8(p + 8 * j, lo[i]);
+      store8(p + HALF + 8 * j, hi[i]);
+    }
+  }
+}
+
+template <typename X, typename C, int DH>
+void launch_append_dh(AppendArgs &a, cudaStream_t st) {
+  constexpr int PIECES = DH / 16;
+  const int heads = a.hq + 2 * a.kv.n_kv_heads;
+  // Several heads per thread keep more loads in flight and read (cos, sin) once for all of them; with few tokens one
+  // head per thread spreads the call over more SMs.
+  const bool wide = a.n_tokens * heads * PIECES >= 4ll * 148 * 1024;
+  a.chunks = wide ? (heads + 3) / 4 : heads;
+  const long long threads = a.n_tokens * a.chunks * PIECES;
+  const unsigned grid = (unsigned)((threads + 255) / 256);
+  if (wide) launch_pdl(k_paged_append<X, C, DH, 4>, dim3(grid), dim3(256), 0, st, a);
+  else launch_pdl(k_paged_append<X, C, DH, 1>, dim3(grid), dim3(256), 0, st, a);
+}
+template <typename X, typename C>
+void launch_append(AppendArgs &a, int dh, cudaStream_t st) {
+  if (dh == 128) launch_append_dh<X, C, 128>(a, st);
+  else if (dh == 64) launch_append_dh<X, C, 64>(a, st);
+  else launch_append_dh<X, C, 32>(a, st);
+}
+
+bool int_span_ok(const void *p, unsigned align) { return p && ((uintptr_t)p & (align - 1)) == 0; }
+
+// ------------------------------------------------------------------ tensor maps
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+EncodeTiledFn pool_encoder() {
+  static EncodeTiledFn fn = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+
+// one float4-aligned region behind the other
+struct AttnWorkspace {
+  size_t part_o, part_ml, join, total;
+};
+AttnWorkspace attn_workspace(int dh) {
+  AttnWorkspace w;
+  const size_t parts = 2 * (size_t)kFusedMaxCtas * 16;   // two cut pieces per CTA, up to 16 heads each
+  w.part_o = 0;
+  w.part_ml = parts * dh * sizeof(float);
+  w.join = w.part_ml + parts * 2 * sizeof(float);
+  w.total = (w.join + kFusedMaxCtas * sizeof(int4) + 255) / 256 * 256;
+  return w;
+}
+
+}  // namespace
+
+bool encode_pool_map(TMap *out, const d3_paged_kv &kv, void *base) {
+  EncodeTiledFn fn = pool_encoder();
+  if (!fn) return false;
+  const int es = bytes_of(kv.dtype), row = kv.head_dim * es, box_bytes = row < 128 ? row : 128;
+  cuuint64_t dims[4] = {(cuuint64_t)kv.head_dim, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};
+  cuuint64_t strides[3] = {(cuuint64_t)(kv.token_stride * es), (cuuint64_t)(kv.head_stride * es),
+                           (cuuint64_t)(kv.page_stride * es)};
+  cuuint32_t box[4] = {(cuuint32_t)(box_bytes / es), 16, 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  const CUtensorMapDataType type = kv.dtype == D3_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                   : kv.dtype == D3_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+  const CUtensorMapSwizzle sw = box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B
+                                : box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
+  return fn(reinterpret_cast<CUtensorMap *>(out), type, 4, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace d3
+
+using namespace d3;
+
+extern "C" {
+
+int32_t d3_page_plan(const d3_page_plan_args *a, void *cuda_stream) {
+  if (!a || a->struct_size != sizeof(d3_page_plan_args)) return D3_EINVAL;
+  if (a->n_requests < 1 || a->n_requests > D3_MAX_REQUESTS || !page_size_ok(a->page_size)) return D3_EINVAL;
+  if (a->n_pages < 1 || a->table_width < 1 || a->max_tokens < 1 || a->table_stride < a->table_width) return D3_EINVAL;
+  if (a->table_stride > ((int64_t)1 << 40) ||
+      (int64_t)a->table_width * a->page_size > 0x7fffffff - 1024)   // lengths and positions fit 32 bits
+    return D3_EINVAL;
+  if (!int_span_ok(a->cached_dev, 4) || !int_span_ok(a->new_tokens_dev, 4) || !int_span_ok(a->table_dev, 4) ||
+      !int_span_ok(a->free_dev, 4) || !int_span_ok(a->n_free_dev, 4) || !int_span_ok(a->cached_out_dev, 4) ||
+      !int_span_ok(a->n_free_out_dev, 4) || !int_span_ok(a->first_dev, 4) || !int_span_ok(a->slots_dev, 16) ||
+      !int_span_ok(a->row_dev, 16) || !int_span_ok(a->context_dev, 16) || ((uintptr_t)a->status_dev & 3))
+    return D3_EINVAL;
+  PlanArgs p;
+  p.R = a->n_requests; p.page_shift = log2_of(a->page_size); p.n_pages = a->n_pages; p.width = a->table_width;
+  p.T = a->max_tokens; p.table_stride = a->table_stride;
+  p.cached = a->cached_dev; p.added = a->new_tokens_dev; p.table = a->table_dev; p.free_pages = a->free_dev;
+  p.n_free = a->n_free_dev; p.cached_out = a->cached_out_dev; p.n_free_out = a->n_free_out_dev; p.first = a->first_dev;
+  p.slots = reinterpret_cast<long long *>(a->slots_dev); p.row = a->row_dev; p.context = a->context_dev; p.status = a->status_dev;
+  const size_t smem = ((size_t)4 * a->n_requests + 3) * sizeof(int);
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return D3_ECUDA;
+  static bool ready[64];   // the shared-memory attribute is per device; setting it twice is harmless
+  if (!ready[dev]) {
+    if (cudaFuncSetAttribute(k_page_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (4 * D3_MAX_REQUESTS + 4) * (int)sizeof(int)) !=
+        cudaSuccess)
+      return D3_ECUDA;
+    ready[dev] = true;
+  }
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  // one CTA while its threads take at most one group of four tokens each; a cluster of eight for prompts
+  const unsigned ctas = a->max_tokens <= 4 * kPlanThreads ? 1 : 8;
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(kPlanThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = static_cast<cudaStream_t>(cuda_stream);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, k_page_plan, p) == cudaSuccess ? D3_OK : D3_ECUDA;
+}
+
+int32_t d3_paged_append(const d3_paged_kv *kv, const d3_paged_append_args *a, void *cuda_stream) {
+  if (!kv_ok(kv, true) || !a || a->struct_size != sizeof(d3_paged_append_args)) return D3_EINVAL;
+  if (!types_ok(a->dtype, kv->dtype) || a->n_tokens < 0) return D3_EINVAL;
+  const int xs = bytes_of(a->dtype), dh = kv->head_dim;
+  if (!a->k_dev || !a->v_dev || !aligned16(a->k_dev) || !aligned16(a->v_dev) || !a->slots_dev ||
+      ((uintptr_t)a->slots_dev & 7) || ((uintptr_t)a->status_dev & 3))
+    return D3_EINVAL;
+  if (!stride_ok(a->k_token_stride, xs, 0) || !stride_ok(a->k_head_stride, xs, 0) || !stride_ok(a->v_token_stride, xs, 0) ||
+      !stride_ok(a->v_head_stride, xs, 0))
+    return D3_EINVAL;
+  if (a->rope_dev) {
+    if (!aligned16(a->rope_dev) || a->rope_len < 1 || !a->context_dev || ((uintptr_t)a->context_dev & 3)) return D3_EINVAL;
+  }
+  if (a->q_dev) {
+    if (!a->rope_dev || a->n_q_heads < 1 || a->n_q_heads > 65535 || !a->q_out_dev || !aligned16(a->q_dev) || !aligned16(a->q_out_dev) ||
+        !stride_ok(a->q_token_stride, xs, 0) || !stride_ok(a->q_head_stride, xs, 0) ||
+        !stride_ok(a->q_out_token_stride, xs, dh) || !stride_ok(a->q_out_head_stride, xs, dh))
+      return D3_EINVAL;
+  }
+  if (a->n_tokens == 0) return D3_OK;
+  AppendArgs p;
+  memset(&p, 0, sizeof(p));
+  p.n_tokens = a->n_tokens; p.hq = a->q_dev ? a->n_q_heads : 0; p.rope_len = a->rope_len;
+  p.k = a->k_dev; p.v = a->v_dev; p.q = a->q_dev; p.q_out = a->q_out_dev;
+  p.kt = a->k_token_stride; p.kh = a->k_head_stride; p.vt = a->v_token_stride; p.vh = a->v_head_stride;
+  p.qt = a->q_token_stride; p.qh = a->q_head_stride; p.ot = a->q_out_token_stride; p.oh = a->q_out_head_stride;
+  p.slots = reinterpret_cast<const long long *>(a->slots_dev); p.context = a->context_dev; p.rope = a->rope_dev; p.status = a->status_dev;
+  p.kv = pool_of(*kv);
+  // threads of the launch: the grid has to fit 31 bits
+  if ((double)a->n_tokens * (p.hq + 2.0 * kv->n_kv_heads) * (dh / 16) / 256 > 2.0e9) return D3_EINVAL;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (kv->dtype == D3_BF16) {
+    if (a->dtype == D3_BF16) launch_append<bf16, bf16>(p, dh, st);
+    else launch_append<float, bf16>(p, dh, st);
+  } else if (kv->dtype == D3_FP16) {
+    launch_append<__half, __half>(p, dh, st);
+  } else {
+    if (a->dtype == D3_BF16) launch_append<bf16, __nv_fp8_e4m3>(p, dh, st);
+    else launch_append<__half, __nv_fp8_e4m3>(p, dh, st);
+  }
+  return cudaGetLastError() == cudaSuccess ? D3_OK : D3_ECUDA;
+}
+
+int32_t d3_rope_table(int32_t n_positions, int32_t head_dim, float rope_base, float *table_dev, void *cuda_stream) {
+  if (n_positions < 1 || (head_dim != 32 && head_dim != 64 && head_dim != 128) || !(rope_base > 0.f) || isinf(rope_base) ||
+      !table_dev || !aligned16(table_dev) || (int64_t)n_positions * (head_dim / 2) > 0x7fffff00)
+    return D3_EINVAL;
+  launch_rope_table(reinterpret_cast<float2 *>(table_dev), n_positions, head_dim, rope_base, static_cast<cudaStream_t>(cuda_stream));
+  return cudaGetLastError() == cudaSuccess ? D3_OK : D3_ECUDA;
+}
+
+int32_t d3_paged_attention_workspace(const d3_paged_kv *kv, int32_t n_q_heads, size_t *bytes) {
+  if (!kv_ok(kv, false) || !bytes || n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return D3_EINVAL;
+  *bytes = attn_workspace(kv->head_dim).total;
+  return D3_OK;
+}
+
+int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args *a, void *cuda_stream) {
+  if (!kv_ok(kv, true) || !a || a->struct_size != sizeof(d3_paged_attention_args)) return D3_EINVAL;
+  if (!types_ok(a->dtype, kv->dtype)) return D3_EINVAL;
+  const int xs = bytes_of(a->dtype), dh = kv->head_dim;
+  if (a->n_rows < 0 || a->n_rows > 65535 || a->n_q_heads < 1 || a->n_q_heads % kv->n_kv_heads || a->n_q_heads > 65535) return D3_EINVAL;
+  if (a->table_rows < 1 || a->table_width < 1 || a->table_stride < a->table_width || a->table_stride > ((int64_t)1 << 40) ||
+      (int64_t)a->table_width * kv->page_size > 0x7fffffff - 1024)
+    return D3_EINVAL;
+  if (!a->rows_dev && a->table_rows < a->n_rows) return D3_EINVAL;
+  if (!isfinite(a->scale)) return D3_EINVAL;
+  if (!a->q_dev || !a->out_dev || !aligned16(a->q_dev) || ((uintptr_t)a->out_dev & (xs - 1)) || ((uintptr_t)a->lse_dev & 3) ||
+      !a->table_dev || ((uintptr_t)a->table_dev & 3) || !a->context_dev || ((uintptr_t)a->context_dev & 3) ||
+      ((uintptr_t)a->rows_dev & 3) || ((uintptr_t)a->status_dev & 3))
+    return D3_EINVAL;
+  if (!stride_ok(a->q_row_stride, xs, 0) || !stride_ok(a->q_head_stride, xs, 0)) return D3_EINVAL;
+  if (a->out_row_stride < dh || a->out_head_stride < dh || a->out_row_stride > ((int64_t)1 << 38) || a->out_head_stride > ((int64_t)1 << 38))
+    return D3_EINVAL;
+  const AttnWorkspace w = attn_workspace(dh);
+  if (!a->workspace_dev || ((uintptr_t)a->workspace_dev & 255) || a->workspace_bytes < w.total) return D3_EINVAL;
+  if (a->n_rows == 0) return D3_OK;
+  TMap mk, mv;
+  if (!encode_pool_map(&mk, *kv, kv->k_dev) || !encode_pool_map(&mv, *kv, kv->v_dev)) return D3_ECUDA;
+  PagedAttnArgs p;
+  memset(&p, 0, sizeof(p));
+  p.n_rows = a->n_rows; p.hq = a->n_q_heads; p.hkv = kv->n_kv_heads; p.group = a->n_q_heads / kv->n_kv_heads;
+  // Query heads that share one reading of K and V: up to 8, and up to 16 where 8 rows of the score tile
+  // would not do (16-bit queries; fp32 ones use those rows for their third term).
+  const int most = a->dtype != D3_FP32 && p.group > 8 ? 16 : 8;
+  p.tiles_per_head = (p.group + most - 1) / most;
+  p.heads_per_tile = (p.group + p.tiles_per_head - 1) / p.tiles_per_head;
+  p.table_rows = a->table_rows; p.table_width = a->table_width; p.page_shift = log2_of(kv->page_size); p.n_pages = kv->n_pages;
+  p.table_stride = a->table_stride; p.q_row_stride = a->q_row_stride; p.q_head_stride = a->q_head_stride;
+  p.out_row_stride = a->out_row_stride; p.out_head_stride = a->out_head_stride;
+  p.scale = a->scale; p.q = a->q_dev; p.out = a->out_dev; p.lse = a->lse_dev;
+  p.table = a->table_dev; p.context = a->context_dev; p.rows = a->rows_dev;
+  p.k_scale = kv->k_scale_dev; p.v_scale = kv->v_scale_dev;
+  char *ws = static_cast<char *>(a->workspace_dev);
+  p.part_o = reinterpret_cast<float *>(ws + w.part_o); p.part_ml = reinterpret_cast<float *>(ws + w.part_ml);
+  p.join = reinterpret_cast<int4 *>(ws + w.join);
+  p.status = a->status_dev;
+  p.wait_ns = 2000000000ull;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const int rc = dh == 128 ? launch_paged_attention_128(mk, mv, p, kv->dtype, a->dtype, st)
+                 : dh == 64 ? launch_paged_attention_64(mk, mv, p, kv->dtype, a->dtype, st)
+                            : launch_paged_attention_32(mk, mv, p, kv->dtype, a->dtype, st);
+  return rc == 0 && cudaGetLastError() == cudaSuccess ? D3_OK : D3_ECUDA;
+}
+
+}  // extern "C"

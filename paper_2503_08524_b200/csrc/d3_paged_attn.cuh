@@ -1,0 +1,777 @@
+// Attention of one new token per row over a paged cache: the kernel, compiled per head dimension.
+//
+// Mathematics.  For a tile of up to 8 query heads of one kv head (16 with two score tiles) and a piece of 16
+// positions: S = Q K^T, the running maximum m and sum l of exp2(S scale log2 e - m), O = O exp2(m_old - m) + P V.
+// O, m and l are additive over any cut of the positions once brought to a common maximum, which is all that the
+// split over the length needs.
+//
+// What bounds it.  K and V are read once: 2 G flops per byte (G query heads per kv head, 16-bit cache), far
+// below the ~260 of this GPU's tensor cores, so HBM decides and the kernel is built to keep copies in flight:
+//   * one CTA per SM; a producer warp walks the CTA's share of all positions of all rows and fills a ring of up to
+//     ~170 KB of 64-position stages by TMA (4-D tensor map over the pool: dim, position, kv head, page; boxes of
+//     16 positions, so any page size and both layouts cost the same); it looks page ids up 32 at a time, one
+//     window ahead, and never waits for the arithmetic until the ring is full;
+//   * the share is cut by positions, not by rows: row lengths are read on the device, every CTA sums them up and takes
+//     the same number of 64-position units, so ragged batches and one long row load all SMs alike;
+//   * a consumer warp takes one piece of 16 positions of a stage at a time (mma.sync m16n8k16, fragments by
+//     ldmatrix from the 128-byte-swizzled rows).  The 16 rows of a score tile hold the 8 heads twice: for P V the
+//     upper 8 rows carry P - round(P), which keeps P to 16 (bf16) or 22 (fp16) bits for nothing.  tcgen05.mma would
+//     put 8 rows into a 128-row tile and its operands and results through shared and tensor memory; with the
+//     pipe as idle as it is here that only adds steps.
+//   * rows that end inside a CTA are written at once; of a row that is cut every CTA leaves (m, l, O) of its piece and
+//     k_paged_join adds them up in the order of the CTAs: bits depend on the lengths alone, no atomics.
+//
+// fp32 queries (bf16 cache): q is three bf16 terms by truncation (8 + 8 + 8 bits: exact), P too; two score tiles carry
+// (hi, mid) and (lo, 0) of 8 heads.  8-bit cache: the stored numbers are widened to fp16 (exact), bf16 queries are
+// scaled by a power of two per head so that fp16 holds them.  Where P is fp16, it is exp2(.. + 15): 2^-29 of the
+// largest stays a normal number.
+//
+// Every wait is bounded; when one runs out the CTA stores D3_ETIMEOUT, stops issuing, lets its copies land and ends.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include "d3_paged.cuh"
+
+namespace d3 {
+namespace paged_attn {
+
+constexpr int kUnit = 64;             // positions of a stage
+constexpr int kPiece = 16;            // positions of a warp's trip, and of a TMA box
+constexpr int kMaxStages = 12;
+constexpr int kSmemMost = 212 * 1024; // of 227 KB: leaves room for the joining kernel's CTAs beside this one
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+template <int CACHE> struct CacheBytes { static constexpr int v = CACHE == D3_E4M3 ? 1 : 2; };
+template <int X> struct QBytes { static constexpr int v = X == D3_FP32 ? 4 : 2; };
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint64_t now_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+__device__ __forceinline__ void mb_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mb_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mb_arrive_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mb_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Bounded wait; false once it, or another wait of the CTA, has run out.
+__device__ __forceinline__ bool mb_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, unsigned long long wait_ns,
+                                        bool check_abort = true) {
+  if (mb_try(bar, parity)) return true;
+  const uint64_t t0 = now_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (mb_try(bar, parity)) return true;
+    if ((it & 31u) == 0u) {
+      if (check_abort && *abort_flag) return false;
+      if (now_ns() - t0 > wait_ns) break;
+    }
+  }
+  *abort_flag = 1;
+  return false;
+}
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap *map, int dim, int pos, int head, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(dim), "r"(pos), "r"(head), "r"(page), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+template <bool F16>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if (F16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_fast(float x) {   // 2^x to 2^-22 relative; 0 for -inf
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  uint32_t r;
+  if (F16) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <bool F16>
+__device__ __forceinline__ void unpack(uint32_t r, float &lo, float &hi) {
+  if (F16) {
+    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&r));
+    lo = v.x; hi = v.y;
+  } else {
+    lo = __uint_as_float(r << 16);
+    hi = __uint_as_float(r & 0xffff0000u);
+  }
+}
+// two e4m3 numbers (low 16 bits of v) as two fp16 numbers, exactly
+__device__ __forceinline__ uint32_t widen(uint32_t v) {
+  uint32_t r;
+  const unsigned short h = (unsigned short)v;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(h));
+  return r;
+}
+// x, y by truncation to their upper 16 bits, packed; and what is left of them
+__device__ __forceinline__ uint32_t cut(float &x, float &y) {
+  const uint32_t a = __float_as_uint(x) & 0xffff0000u, b = __float_as_uint(y) & 0xffff0000u;
+  x -= __uint_as_float(a);
+  y -= __uint_as_float(b);
+  return (a >> 16) | b;
+}
+
+// The share of CTA i of n among U units starts here.
+__device__ __forceinline__ long long share(long long U, int i, int n) { return U * i / n; }
+
+enum { STAGE_FIRST = 1, STAGE_LAST = 2 };   // of the item within this CTA
+enum { OUT_WHOLE = 0, OUT_HEAD = 1, OUT_TAIL = 2 };   // an item lies in this CTA / started before it / starts in it and goes on
+
+// What the producer tells the consumers about a stage.
+struct StageInfo {
+  int row, tile;        // tile = kv head * tiles_per_head + tile of its query heads
+  int n;                // positions in the stage (0 .. 64)
+  int flags;            // STAGE_* | pieces that hold positions << 4 | OUT_* << 8
+};
+
+template <int DH, int CACHE, int X, int MT>
+struct Cfg {
+  static constexpr int kEs = CacheBytes<CACHE>::v;
+  static constexpr int kRow = DH * kEs;                      // bytes of a cache row
+  static constexpr int kBox = kRow < 128 ? kRow : 128;       // bytes of a box row = swizzle width
+  static constexpr int kBoxes = kRow / kBox;                 // boxes per piece of K (or V)
+  static constexpr int kHeads = X == D3_FP32 ? 8 : 8 * MT;   // query heads of a tile
+  static constexpr int kHalfBytes = kUnit * kRow;            // K (or V) of a stage
+  static constexpr int kQBytes = kHeads * DH * QBytes<X>::v;
+  static constexpr int kStageBytes = 2 * kHalfBytes;
+  // Consumer warps.  Registers are dealt out to four warps at a time: with the producer 12 warps of 168 or 8 of 255,
+  // which the 64 (128) accumulator and 32 (64) query registers fit into without spills.
+  static constexpr int kWarps = MT == 1 ? 11 : 7;
+  static constexpr int kThreads = 32 * (kWarps + 1);
+  static constexpr bool kF16 = CACHE != D3_BF16;
+  static constexpr bool kThree = X == D3_FP32;
+};
+
+template <int DH, int CACHE, int X, int MT>
+__global__ void __launch_bounds__(Cfg<DH, CACHE, X, MT>::kThreads, 1)
+k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                  const __grid_constant__ PagedAttnArgs a) {
+  using C = Cfg<DH, CACHE, X, MT>;
+  constexpr int NT = DH / 8, KK = DH / 16;
+  constexpr bool F16 = C::kF16, THREE = C::kThree;
+  constexpr int KT = THREE ? 1 : MT;       // score tiles that belong to different heads
+  extern __shared__ unsigned char s_dyn[];
+  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_merge[2];
+  __shared__ StageInfo s_info[kMaxStages];
+  __shared__ float s_m[C::kWarps][C::kHeads], s_l[C::kWarps][C::kHeads];
+  __shared__ long long s_sum[32];
+  __shared__ int s_abort, s_start_row;
+  __shared__ long long s_start_before;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int S = a.n_stages;
+  const uint32_t ring = (smem_u32(s_dyn) + 1023u) & ~1023u;
+  unsigned char *ring_p = s_dyn + (ring - smem_u32(s_dyn));
+  unsigned char *q_slots = ring_p + (size_t)S * C::kStageBytes;
+  float *s_o = reinterpret_cast<float *>(q_slots + (size_t)S * C::kQBytes);   // [warp][head][DH]
+  const int HG = a.hkv * a.tiles_per_head;
+
+  if (tid == 0) {
+    for (int i = 0; i < S; ++i) {
+      mb_init(smem_u32(&s_full[i]), 1);
+      mb_init(smem_u32(&s_empty[i]), C::kWarps);
+    }
+    mb_init(smem_u32(&s_merge[0]), C::kWarps);
+    mb_init(smem_u32(&s_merge[1]), C::kWarps);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    s_abort = 0;
+    s_start_row = a.n_rows;
+  }
+  pdl_wait();
+  pdl_trigger();
+
+  // ---- the rows' unit counts, summed over all rows by every CTA
+  auto row_of = [&](int b, bool &bad) -> int {   // table row, -1 = padding
+    if (!a.rows) return b;
+    const int r = a.rows[b];
+    if (r >= 0 && r < a.table_rows) return r;
+    if (r != -1) bad = true;
+    return -1;
+  };
+  auto length_of = [&](int b, bool &bad) -> int {
+    const int c = a.context[b];
+    if (c < 0 || c > ((long long)a.table_width << a.page_shift)) { bad = true; return 0; }
+    return c;
+  };
+  auto units_of = [&](int len) -> int { return len > 0 ? (len + kUnit - 1) / kUnit : 1; };   // a row without context still gets its zeros
+  const int per = (a.n_rows + C::kThreads - 1) / C::kThreads;
+  long long mine = 0;
+  bool bad = false;
+  for (int i = 0; i < per; ++i) {
+    const int b = tid * per + i;
+    if (b < a.n_rows && row_of(b, bad) >= 0) mine += units_of(length_of(b, bad));
+  }
+  if (bad && blockIdx.x == 0 && a.status) *a.status = D3_EINVAL;
+  long long inc = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, inc, d);
+    if (lane >= d) inc += u;
+  }
+  if (lane == 31) s_sum[warp] = inc;
+  __syncthreads();
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < C::kThreads / 32; ++w) {
+    const long long v = s_sum[w];
+    if (w < warp) before += v;
+    total += v;
+  }
+  before += inc - mine;
+  const long long U = total * HG;
+  const int n_cta = (int)(U < (long long)gridDim.x ? U : (long long)gridDim.x);   // every one of them has work
+  if ((int)blockIdx.x >= n_cta) {
+    if (tid == 0) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
+    return;
+  }
+  const long long u0 = share(U, blockIdx.x, n_cta), u1 = share(U, blockIdx.x + 1, n_cta);
+  {
+    const long long t0 = u0 / HG;   // the row whose range of the unit sums holds t0 is the first one
+    if (t0 >= before && t0 < before + mine) {
+      long long p = before;
+      for (int i = 0; i < per; ++i) {
+        const int b = tid * per + i;
+        bool dummy = false;
+        if (b < a.n_rows && row_of(b, dummy) >= 0) {
+          const int n = units_of(length_of(b, dummy));
+          if (t0 < p + n) { s_start_row = b; s_start_before = p; break; }
+          p += n;
+        }
+      }
+    }
+  }
+  __syncthreads();
+
+  if (warp == C::kWarps) {
+    // ------------------------------------------------------------ producer
+    int row = s_start_row;
+    bool dummy = false;
+    int trow = row_of(row, dummy), len = length_of(row, dummy), nu = units_of(len);
+    long long at = u0 - s_start_before * HG;     // unit inside the row's (tile, unit) range
+    int tile = (int)(at / nu), unit = (int)(at % nu);
+    int win0 = -1, win = 0, win_next = 0;        // page ids of the row: [win0, +32) in win, the next 32 in win_next
+    long long u = u0;
+    int issued = 0;
+    bool first = true, ok = true;
+    int joins = 0;
+    int4 join = make_int4(0, 0, 0, 0);
+    for (; u < u1; ++u) {
+      const int s = issued % S;
+      const uint32_t parity = (uint32_t)((issued / S) & 1) ^ 1u;
+      const int p0 = unit * kUnit, n = min(kUnit, len - p0);   // n <= 0 only for a row without context
+      // page ids, one per lane, 32 pages at a time and one window ahead
+      const int pg0 = p0 >> a.page_shift, pg_last = len > 0 ? (min(len, p0 + kUnit) - 1) >> a.page_shift : 0;
+      if (len > 0) {
+        const int32_t *t = a.table + (long long)trow * a.table_stride;
+        auto fetch = [&](int base) -> int {
+          const int i = base + lane;
+          return i < a.table_width ? __ldg(t + i) : -1;
+        };
+        if (win0 < 0) { win0 = pg0 & ~31; win = fetch(win0); win_next = fetch(win0 + 32); }
+        else if (pg0 >= win0 + 32) { win0 += 32; win = win_next; win_next = fetch(win0 + 32); }
+      }
+      // this lane's copy: piece (16 positions), K or V, 128-byte column
+      const int piece = lane & 3, is_v = (lane >> 2) & 1, col = lane >> 3;
+      const int pos = p0 + piece * kPiece;
+      bool want = pos < p0 + n && col < C::kBoxes;
+      const int pg = min(pos >> a.page_shift, pg_last);
+      // windows are 32 pages aligned to 32 and a unit is 64 positions = at most 4 aligned pages: it never straddles
+      const int id = __shfl_sync(0xffffffffu, win, pg & 31);
+      const bool good = id >= 0 && id < a.n_pages;
+      if (want && !good && a.status) *a.status = D3_EINVAL;
+      const bool present = pos < p0 + n && good;
+      const unsigned pieces = __ballot_sync(0xffffffffu, present) & 0xfu;
+      want = want && good;
+      const bool last = u + 1 == u1 || unit + 1 == nu;
+      if (!mb_wait(smem_u32(&s_empty[s]), parity, &s_abort, a.wait_ns)) { ok = false; }
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const uint32_t full = smem_u32(&s_full[s]);
+      if (lane == 0) {
+        StageInfo info;
+        info.row = row; info.tile = tile; info.n = max(n, 0);
+        int kind = OUT_WHOLE;
+        if (unit + 1 < nu && last) {   // the item goes on in the next CTA
+          const bool starts_here = u - unit >= u0;
+          kind = starts_here ? OUT_TAIL : OUT_HEAD;
+          if (starts_here) {
+            const long long end = u - unit + nu;   // CTAs up to the one that holds unit end - 1
+            const int jl = (int)((end * n_cta + U - 1) / U) - 1;
+            join = make_int4(1 + jl - (int)blockIdx.x, row, tile, 0);
+            joins = 1;
+          }
+        } else if (last && u - unit < u0) {
+          kind = OUT_HEAD;             // its last piece: the rest is in CTAs before this one
+        }
+        info.flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (int)(pieces << 4) | (kind << 8);
+        s_info[s] = info;
+        const uint32_t bytes = (uint32_t)__popc(pieces) * 2u * kPiece * C::kRow +
+                               (first ? (uint32_t)min(a.heads_per_tile, a.group - (tile % a.tiles_per_head) * a.heads_per_tile) * DH * QBytes<X>::v : 0u);
+        mb_arrive_tx(full, bytes);
+      }
+      __syncwarp();
+      if (want) {
+        const uint32_t dst = ring + s * C::kStageBytes + is_v * C::kHalfBytes + col * (kUnit * C::kBox) + piece * (kPiece * C::kBox);
+        tma_box(dst, is_v ? &map_v : &map_k, col * (C::kBox / C::kEs), pos & ((1 << a.page_shift) - 1), tile / a.tiles_per_head, id, full);
+      }
+      if (first) {
+        const int g0 = (tile % a.tiles_per_head) * a.heads_per_tile, nh = min(a.heads_per_tile, a.group - g0);
+        if (lane < nh) {
+          const long long h = (long long)(tile / a.tiles_per_head) * a.group + g0 + lane;
+          bulk_copy(smem_u32(q_slots) + s * C::kQBytes + lane * DH * QBytes<X>::v,
+                    static_cast<const char *>(a.q) + (row * a.q_row_stride + h * a.q_head_stride) * QBytes<X>::v, DH * QBytes<X>::v, full);
+        }
+      }
+      ++issued;
+      first = last;
+      if (++unit == nu) {   // next tile of the row, or next row
+        unit = 0; win0 = -1;
+        if (++tile == HG) {
+          tile = 0;
+          if (u + 1 < u1) {
+            do { ++row; trow = row < a.n_rows ? row_of(row, dummy) : 0; } while (trow < 0);
+            len = length_of(row, dummy);
+            nu = units_of(len);
+          }
+        }
+      }
+    }
+    if (lane == 0) a.join[blockIdx.x] = joins ? join : make_int4(0, 0, 0, 0);
+    if (!ok) {   // copies in flight end by themselves: wait for them before the shared memory goes
+      const unsigned long long drain = a.wait_ns > kDrainFloorNs ? a.wait_ns : kDrainFloorNs;
+      for (int k = max(0, issued - S); k < issued; ++k)
+        mb_wait(smem_u32(&s_full[k % S]), (uint32_t)((k / S) & 1), &s_abort, drain, false);
+      if (lane == 0 && a.status) *a.status = D3_ETIMEOUT;
+    }
+    return;
+  }
+
+  // -------------------------------------------------------------- consumers
+  const int g = lane >> 2, t = lane & 3;
+  uint32_t qa[MT][KK][4];
+  float o[MT][NT][4], mx[KT], sum[KT], mul[KT];
+#pragma unroll
+  for (int i = 0; i < KT; ++i) { mx[i] = -INFINITY; sum[i] = 0.f; mul[i] = 0.f; }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+  int piece_turn = 0;       // pieces of the CTA so far, mod kWarps: whose turn it is
+  int items = 0;
+  const long long n_units = u1 - u0;
+  bool ok = true;
+  for (long long k = 0; k < n_units; ++k) {
+    const int s = (int)(k % S);
+    if (!mb_wait(smem_u32(&s_full[s]), (uint32_t)((k / S) & 1), &s_abort, a.wait_ns)) ok = false;
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) break;
+    const StageInfo info = s_info[s];
+    const int kvh = info.tile / a.tiles_per_head, g0 = (info.tile % a.tiles_per_head) * a.heads_per_tile;
+    const int nh = min(a.heads_per_tile, a.group - g0);
+    if (info.flags & STAGE_FIRST) {
+      // ---- this thread's fragments of Q, and what a raw score is multiplied by
+      const float ks = a.k_scale ? __ldg(a.k_scale + kvh) : 1.f;
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        const int h = g + 8 * i;
+        const bool live = h < nh;
+        const unsigned char *qp = q_slots + (size_t)s * C::kQBytes + (size_t)(live ? h : 0) * DH * QBytes<X>::v;
+        mul[i] = a.scale * kLog2e * ks;
+        if constexpr (X == D3_FP32) {
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float2 v = *reinterpret_cast<const float2 *>(qp + (16 * kk + 8 * j + 2 * t) * 4);
+              float x = live ? v.x : 0.f, y = live ? v.y : 0.f;
+              qa[0][kk][2 * j] = cut(x, y);
+              qa[0][kk][2 * j + 1] = cut(x, y);
+              qa[MT - 1][kk][2 * j] = cut(x, y);
+              qa[MT - 1][kk][2 * j + 1] = 0u;
+            }
+        } else {
+          // position of the pairs: dims 16kk + 2t, +8 (16-bit cache); 16kk + 4t, +2 (8-bit cache, whose
+          // four bytes of a fragment register are four neighbouring dims)
+          constexpr int kA = CACHE == D3_E4M3 ? 4 : 2, kB = CACHE == D3_E4M3 ? 2 : 8;
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t v = *reinterpret_cast<const uint32_t *>(qp + (16 * kk + kB * j + kA * t) * 2);
+              qa[i][kk][2 * j] = live ? v : 0u;
+              qa[i][kk][2 * j + 1] = 0u;
+            }
+          if constexpr (CACHE == D3_E4M3 && X == D3_BF16) {
+            // to fp16: the head's largest |q| scaled to [1, 2); what falls under fp16's range is under 2^-24 of it
+            float top = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                float x, y;
+                unpack<false>(qa[i][kk][2 * j], x, y);
+                top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
+              }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = (top >= 1.17549435e-38f && top < INFINITY) ? min((int)(__float_as_uint(top) >> 23) - 127, 126) : 0;
+            const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
+            mul[i] *= up;
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                float x, y;
+                unpack<false>(qa[i][kk][2 * j], x, y);
+                qa[i][kk][2 * j] = pack<true>(x * down, y * down);
+              }
+          }
+        }
+      }
+    }
+    const int n_pieces = (info.n + kPiece - 1) / kPiece;
+    // pieces go round the warps; of a stage a warp has at most one (4 pieces, 7 or 11 warps)
+    int p = warp - piece_turn;
+    if (p < 0) p += C::kWarps;
+    piece_turn += n_pieces;
+    if (piece_turn >= C::kWarps) piece_turn -= C::kWarps;
+    if (p < n_pieces && (info.flags >> (4 + p)) & 1) {
+      const uint32_t kbase = ring + s * C::kStageBytes, vbase = kbase + C::kHalfBytes;
+      const int valid = info.n - p * kPiece;   // positions of the piece (>= 1)
+      // byte address of 16-byte chunk c of row r (0..15) of the piece
+      auto chunk = [&](uint32_t base, int r, int c) -> uint32_t {
+        constexpr int per_row = C::kBox / 16;
+        const int half = c / per_row, cc = c % per_row;
+        return base + half * (kUnit * C::kBox) + (p * kPiece + r) * C::kBox + ((cc ^ (((r * C::kBox) >> 7) & (per_row - 1))) << 4);
+      };
+      float sc[MT][2][4];
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) sc[i][j][0] = sc[i][j][1] = sc[i][j][2] = sc[i][j][3] = 0.f;
+      const int mat = lane >> 3;
+      if constexpr (CACHE != D3_E4M3) {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          uint32_t b[4];   // (positions 0-7, dims 16kk..+7), (0-7, +8..+15), (8-15, ..), (8-15, ..)
+          ldsm4(b, chunk(kbase, (lane & 7) + 8 * (mat >> 1), 2 * kk + (mat & 1)));
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            mma<F16>(sc[i][0], qa[i][kk], b[0], b[1]);
+            mma<F16>(sc[i][1], qa[i][kk], b[2], b[3]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < KK; kk += 2) {
+          uint32_t b[4];   // (positions 0-7, dims 16kk..+15), (8-15, same), then the next 16 dims
+          ldsm4(b, chunk(kbase, (lane & 7) + 8 * (mat & 1), kk + (mat >> 1)));
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t b0 = widen(b[2 * q + j]), b1 = widen(b[2 * q + j] >> 16);
+#pragma unroll
+              for (int i = 0; i < MT; ++i) mma<F16>(sc[i][j], qa[i][kk + q], b0, b1);
+            }
+        }
+      }
+      // ---- softmax of the piece: this thread has head g (+ 8 i), positions 2t, 2t+1, 8+2t, 8+2t+1
+      uint32_t pa[MT][4];
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float x = THREE ? (sc[MT - 1][j][e] + sc[0][j][2 + e]) + sc[0][j][e] : sc[i][j][e];
+            x *= mul[i];
+            v[2 * j + e] = 8 * j + 2 * t + e < valid ? x : -INFINITY;
+          }
+        float cm = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+        cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 1));
+        cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 2));
+        const float mn = fmaxf(mx[i], cm);
+        if (__any_sync(0xffffffffu, mn > mx[i])) {
+          const float corr = mn > mx[i] ? exp2_fast(mx[i] - mn) : 1.f;   // 0 at the first piece
+          sum[i] *= corr;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            o[i][n][0] *= corr; o[i][n][1] *= corr; o[i][n][2] *= corr; o[i][n][3] *= corr;
+            if (THREE) { o[MT - 1][n][0] *= corr; o[MT - 1][n][1] *= corr; }
+          }
+        }
+        mx[i] = mn;
+        const float ref = mn == -INFINITY ? 0.f : (F16 ? mn - 15.f : mn);
+        float pr[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { pr[e] = exp2_fast(v[e] - ref); sum[i] += pr[e]; }
+        if constexpr (THREE) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            pa[0][2 * j] = cut(pr[2 * j], pr[2 * j + 1]);
+            pa[0][2 * j + 1] = cut(pr[2 * j], pr[2 * j + 1]);
+            pa[MT - 1][2 * j] = cut(pr[2 * j], pr[2 * j + 1]);
+            pa[MT - 1][2 * j + 1] = 0u;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t hi = pack<F16>(pr[2 * j], pr[2 * j + 1]);
+            float x, y;
+            unpack<F16>(hi, x, y);
+            pa[i][2 * j] = hi;
+            pa[i][2 * j + 1] = pack<F16>(pr[2 * j] - x, pr[2 * j + 1] - y);
+          }
+        }
+      }
+      // ---- O += P V.  What the page holds behind the row's end must not reach a product (0 x NaN is NaN).
+      uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
+      const bool partial = valid < kPiece;
+      if (partial) {
+        keep0 = (2 * t < valid ? 0xffffu : 0u) | (2 * t + 1 < valid ? 0xffff0000u : 0u);
+        keep1 = (2 * t + 8 < valid ? 0xffffu : 0u) | (2 * t + 9 < valid ? 0xffff0000u : 0u);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; n += 2) {
+        if constexpr (CACHE != D3_E4M3) {
+          uint32_t b[4];   // (positions 0-7, dims 8n..), (8-15, same), (0-7, dims 8n+8..), (8-15, same)
+          ldsm4t(b, chunk(vbase, (lane & 7) + 8 * (mat & 1), n + (mat >> 1)));
+          if (partial) { b[0] &= keep0; b[1] &= keep1; b[2] &= keep0; b[3] &= keep1; }
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            mma<F16>(o[i][n], pa[i], b[0], b[1]);
+            mma<F16>(o[i][n + 1], pa[i], b[2], b[3]);
+          }
+        } else if (n % 4 == 0) {
+          // 16-byte chunks n/2 and n/2 + 1: a register holds positions 2t, 2t+1 of dims 2g, 2g+1 of the chunk;
+          // even dims make one 8-wide tile, odd dims the next
+          uint32_t b[4];
+          ldsm4t(b, chunk(vbase, (lane & 7) + 8 * (mat & 1), n / 2 + (mat >> 1)));
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const uint32_t u0_ = __byte_perm(b[2 * q], 0, 0x3120), u1_ = __byte_perm(b[2 * q + 1], 0, 0x3120);
+            uint32_t e0 = widen(u0_), e1 = widen(u1_), d0 = widen(u0_ >> 16), d1 = widen(u1_ >> 16);
+            if (partial) { e0 &= keep0; d0 &= keep0; e1 &= keep1; d1 &= keep1; }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              mma<F16>(o[i][n + 2 * q], pa[i], e0, e1);
+              mma<F16>(o[i][n + 2 * q + 1], pa[i], d0, d1);
+            }
+          }
+        }
+      }
+    }
+    __syncwarp();
+    if (lane == 0) mb_arrive(smem_u32(&s_empty[s]));
+
+    if (info.flags & STAGE_LAST) {
+      // ---- the item's end in this CTA: add the warps up
+      // the previous item's sums have been read by every warp
+      if (items > 0 && !mb_wait(smem_u32(&s_merge[1]), (uint32_t)((items - 1) & 1), &s_abort, a.wait_ns)) ok = false;
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        float l = sum[i];
+        l += __shfl_xor_sync(0xffffffffu, l, 1);
+        l += __shfl_xor_sync(0xffffffffu, l, 2);
+        const int h = g + 8 * i;
+        if (h < nh) {
+          float *dst = s_o + ((size_t)warp * a.heads_per_tile + h) * DH;
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float val = THREE ? (o[MT - 1][n][e] + o[0][n][2 + e]) + o[0][n][e] : o[i][n][2 + e] + o[i][n][e];
+              const int dim = CACHE == D3_E4M3 ? 16 * (n >> 1) + 2 * (2 * t + e) + (n & 1) : 8 * n + 2 * t + e;
+              dst[dim] = val;
+            }
+          if (t == 0) { s_m[warp][h] = mx[i]; s_l[warp][h] = l; }
+        }
+        mx[i] = -INFINITY; sum[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+      __syncwarp();
+      if (lane == 0) mb_arrive(smem_u32(&s_merge[0]));
+      if (!mb_wait(smem_u32(&s_merge[0]), (uint32_t)(items & 1), &s_abort, a.wait_ns)) ok = false;
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const int kind = (info.flags >> 8) & 3;
+      const float vs = a.v_scale ? __ldg(a.v_scale + kvh) : 1.f;
+      for (int i = tid; i < nh * DH; i += C::kWarps * 32) {
+        const int h = i / DH, e = i % DH;
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < C::kWarps; ++w) M = fmaxf(M, s_m[w][h]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        float L = 0.f, O = 0.f;
+#pragma unroll
+        for (int w = 0; w < C::kWarps; ++w) {
+          const float l = s_l[w][h];
+          if (l != 0.f) {   // the warp had positions of the item
+            const float c = exp2_fast(s_m[w][h] - ref);
+            L += l * c;
+            O += s_o[((size_t)w * a.heads_per_tile + h) * DH + e] * c;
+          }
+        }
+        const long long head = (long long)kvh * a.group + g0 + h;
+        if (kind == OUT_WHOLE) {
+          const float val = L == 0.f ? 0.f : O / L * vs;
+          const long long at = info.row * a.out_row_stride + head * a.out_head_stride + e;
+          if (X == D3_FP32) static_cast<float *>(a.out)[at] = val;
+          else if (X == D3_BF16) static_cast<bf16 *>(a.out)[at] = __float2bfloat16_rn(val);
+          else static_cast<__half *>(a.out)[at] = __float2half_rn(val);
+          if (e == 0 && a.lse) a.lse[(long long)info.row * a.hq + head] = L == 0.f ? -INFINITY : (M + (log2f(L) - (F16 ? 15.f : 0.f))) * kLn2;
+        } else {
+          const size_t part = (size_t)(2 * blockIdx.x + (kind == OUT_TAIL ? 1 : 0)) * 16 + h;
+          a.part_o[part * DH + e] = O;
+          if (e == 0) { a.part_ml[2 * part] = M; a.part_ml[2 * part + 1] = L; }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mb_arrive(smem_u32(&s_merge[1]));
+      ++items;
+    }
+  }
+  if (!ok && lane == 0 && a.status) *a.status = D3_ETIMEOUT;
+}
+
+// Joins the pieces of the item that starts in CTA blockIdx.x and goes on behind it; blockIdx.y: head of the tile.
+// Parts: this CTA's second slot, then the first slots of the CTAs that follow, in that order.  8 warps take parts
+// w, w + 8, ..; a lane has DH / 32 neighbouring dims.
+template <int DH, int X, bool F16>
+__global__ void __launch_bounds__(256) k_paged_join(const __grid_constant__ PagedAttnArgs a) {
+  constexpr int V = DH / 32;
+  __shared__ float s_o[8][DH], s_l[8], s_max[8];
+  pdl_wait();
+  pdl_trigger();
+  const int4 job = a.join[blockIdx.x];
+  if (job.x == 0) return;
+  const int parts = job.x, row = job.y, tile = job.z, h = blockIdx.y;
+  const int kvh = tile / a.tiles_per_head, g0 = (tile % a.tiles_per_head) * a.heads_per_tile;
+  if (h >= min(a.heads_per_tile, a.group - g0)) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto part = [&](int k) -> size_t { return (size_t)(k == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + k)) * 16 + h; };
+  float M = -INFINITY;
+  for (int k = threadIdx.x; k < parts; k += 256) M = fmaxf(M, a.part_ml[2 * part(k)]);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+  if (lane == 0) s_max[warp] = M;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) M = fmaxf(M, s_max[w]);
+  const float ref = M == -INFINITY ? 0.f : M;
+  float o[V], L = 0.f;
+#pragma unroll
+  for (int e = 0; e < V; ++e) o[e] = 0.f;
+#pragma unroll 4
+  for (int k = warp; k < parts; k += 8) {
+    const size_t p = part(k);
+    const float l = a.part_ml[2 * p + 1];
+    if (l != 0.f) {
+      const float c = exp2_fast(a.part_ml[2 * p] - ref);
+      L += l * c;
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[e] += a.part_o[p * DH + lane * V + e] * c;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) s_o[warp][lane * V + e] = o[e];
+  if (lane == 0) s_l[warp] = L;
+  __syncthreads();
+  const int e = threadIdx.x;
+  if (e >= DH) return;
+  float O = 0.f;
+  L = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) { O += s_o[w][e]; L += s_l[w]; }
+  const float vs = a.v_scale ? __ldg(a.v_scale + kvh) : 1.f;
+  const float val = L == 0.f ? 0.f : O / L * vs;
+  const long long head = (long long)kvh * a.group + g0 + h;
+  const long long at = row * a.out_row_stride + head * a.out_head_stride + e;
+  if (X == D3_FP32) static_cast<float *>(a.out)[at] = val;
+  else if (X == D3_BF16) static_cast<bf16 *>(a.out)[at] = __float2bfloat16_rn(val);
+  else static_cast<__half *>(a.out)[at] = __float2half_rn(val);
+  if (e == 0 && a.lse) a.lse[(long long)row * a.hq + head] = L == 0.f ? -INFINITY : (M + (log2f(L) - (F16 ? 15.f : 0.f))) * kLn2;
+}
+
+// ---------------------------------------------------------------- launch
+template <int DH, int CACHE, int X, int MT>
+int launch(const TMap &k, const TMap &v, PagedAttnArgs a, cudaStream_t st) {
+  using C = Cfg<DH, CACHE, X, MT>;
+  const int merge = C::kWarps * a.heads_per_tile * DH * (int)sizeof(float);
+  int stages = (kSmemMost - 1024 - merge) / (C::kStageBytes + C::kQBytes);
+  if (stages > kMaxStages) stages = kMaxStages;
+  if (stages < 2) return -1;
+  a.n_stages = stages;
+  const size_t smem = 1024 + (size_t)stages * (C::kStageBytes + C::kQBytes) + merge;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
+  static int sms[64];   // per device: its SM count once the kernel's attribute is set there
+  if (sms[dev] == 0) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return -1;
+    if (cudaFuncSetAttribute(k_paged_attention<DH, CACHE, X, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost) != cudaSuccess)
+      return -1;
+    sms[dev] = n < kFusedMaxCtas ? n : kFusedMaxCtas;
+  }
+  const CUtensorMap *mk = reinterpret_cast<const CUtensorMap *>(&k), *mv = reinterpret_cast<const CUtensorMap *>(&v);
+  if (launch_pdl(k_paged_attention<DH, CACHE, X, MT>, dim3(sms[dev]), dim3(C::kThreads), smem, st, *mk, *mv, a) != cudaSuccess) return -1;
+  // a table of at most one unit's positions cannot be cut
+  if (((long long)a.table_width << a.page_shift) > kUnit)
+    if (launch_pdl(k_paged_join<DH, X, C::kF16>, dim3(sms[dev], a.heads_per_tile), dim3(256), 0, st, a) != cudaSuccess) return -1;
+  return 0;
+}
+
+template <int DH>
+int launch_types(const TMap &k, const TMap &v, const PagedAttnArgs &a, int cache, int x, cudaStream_t st) {
+  const bool wide = a.heads_per_tile > 8;
+  if (cache == D3_BF16 && x == D3_FP32) return launch<DH, D3_BF16, D3_FP32, 2>(k, v, a, st);
+  if (cache == D3_BF16) return wide ? launch<DH, D3_BF16, D3_BF16, 2>(k, v, a, st) : launch<DH, D3_BF16, D3_BF16, 1>(k, v, a, st);
+  if (cache == D3_FP16) return wide ? launch<DH, D3_FP16, D3_FP16, 2>(k, v, a, st) : launch<DH, D3_FP16, D3_FP16, 1>(k, v, a, st);
+  if (x == D3_BF16) return wide ? launch<DH, D3_E4M3, D3_BF16, 2>(k, v, a, st) : launch<DH, D3_E4M3, D3_BF16, 1>(k, v, a, st);
+  return wide ? launch<DH, D3_E4M3, D3_FP16, 2>(k, v, a, st) : launch<DH, D3_E4M3, D3_FP16, 1>(k, v, a, st);
+}
+
+}  // namespace paged_attn
+}  // namespace d3
