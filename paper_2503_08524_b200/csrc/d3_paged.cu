@@ -430,14 +430,14 @@ AttnWorkspace attn_workspace(int dh) {
 
 }  // namespace
 
-bool encode_pool_map(TMap *out, const d3_paged_kv &kv, void *base) {
+bool encode_pool_map(TMap *out, const d3_paged_kv &kv, void *base, int box_rows) {
   EncodeTiledFn fn = pool_encoder();
   if (!fn) return false;
   const int es = bytes_of(kv.dtype), row = kv.head_dim * es, box_bytes = row < 128 ? row : 128;
   cuuint64_t dims[4] = {(cuuint64_t)kv.head_dim, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};
   cuuint64_t strides[3] = {(cuuint64_t)(kv.token_stride * es), (cuuint64_t)(kv.head_stride * es),
                            (cuuint64_t)(kv.page_stride * es)};
-  cuuint32_t box[4] = {(cuuint32_t)(box_bytes / es), 16, 1, 1};
+  cuuint32_t box[4] = {(cuuint32_t)(box_bytes / es), (cuuint32_t)box_rows, 1, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
   const CUtensorMapDataType type = kv.dtype == D3_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                    : kv.dtype == D3_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
@@ -565,6 +565,8 @@ int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args 
       (int64_t)a->table_width * kv->page_size > 0x7fffffff - 1024)
     return D3_EINVAL;
   if (!a->rows_dev && a->table_rows < a->n_rows) return D3_EINVAL;
+  // a CTA counts its units in 32 bits (far beyond what any pool holds; rows may share pages)
+  if ((double)a->n_rows * ((double)a->table_width * kv->page_size / 64 + 1) * a->n_q_heads > 1.0e11) return D3_EINVAL;
   if (!isfinite(a->scale)) return D3_EINVAL;
   if (!a->q_dev || !a->out_dev || !aligned16(a->q_dev) || ((uintptr_t)a->out_dev & (xs - 1)) || ((uintptr_t)a->lse_dev & 3) ||
       !a->table_dev || ((uintptr_t)a->table_dev & 3) || !a->context_dev || ((uintptr_t)a->context_dev & 3) ||
@@ -576,8 +578,6 @@ int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args 
   const AttnWorkspace w = attn_workspace(dh);
   if (!a->workspace_dev || ((uintptr_t)a->workspace_dev & 255) || a->workspace_bytes < w.total) return D3_EINVAL;
   if (a->n_rows == 0) return D3_OK;
-  TMap mk, mv;
-  if (!encode_pool_map(&mk, *kv, kv->k_dev) || !encode_pool_map(&mv, *kv, kv->v_dev)) return D3_ECUDA;
   PagedAttnArgs p;
   memset(&p, 0, sizeof(p));
   p.n_rows = a->n_rows; p.hq = a->n_q_heads; p.hkv = kv->n_kv_heads; p.group = a->n_q_heads / kv->n_kv_heads;
@@ -598,9 +598,9 @@ int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args 
   p.status = a->status_dev;
   p.wait_ns = 2000000000ull;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int rc = dh == 128 ? launch_paged_attention_128(mk, mv, p, kv->dtype, a->dtype, st)
-                 : dh == 64 ? launch_paged_attention_64(mk, mv, p, kv->dtype, a->dtype, st)
-                            : launch_paged_attention_32(mk, mv, p, kv->dtype, a->dtype, st);
+  const int rc = dh == 128 ? launch_paged_attention_128(*kv, p, a->dtype, st)
+                 : dh == 64 ? launch_paged_attention_64(*kv, p, a->dtype, st)
+                            : launch_paged_attention_32(*kv, p, a->dtype, st);
   return rc == 0 && cudaGetLastError() == cudaSuccess ? D3_OK : D3_ECUDA;
 }
 

@@ -53,8 +53,8 @@ inline KvPool pool_of(const d3_paged_kv &kv) {
 }
 
 // tensor map of a pool's K or V (encoded by the driver; false when it refuses or is absent):
-// (dim, position, kv head, page), boxes of 16 positions x min(128 bytes, a row)
-bool encode_pool_map(TMap *out, const d3_paged_kv &kv, void *base);
+// (dim, position, kv head, page), boxes of box_rows positions x min(128 bytes, a row)
+bool encode_pool_map(TMap *out, const d3_paged_kv &kv, void *base, int box_rows);
 
 // What the attention launch gets (device pointers; strides in elements).
 struct PagedAttnArgs {
@@ -75,8 +75,8 @@ struct PagedAttnArgs {
   unsigned long long wait_ns;
 };
 // one translation unit per head dimension (each compiles every type pair)
-int launch_paged_attention_32(const TMap &k, const TMap &v, PagedAttnArgs a, int cache, int x, cudaStream_t st);
-int launch_paged_attention_64(const TMap &k, const TMap &v, PagedAttnArgs a, int cache, int x, cudaStream_t st);
-int launch_paged_attention_128(const TMap &k, const TMap &v, PagedAttnArgs a, int cache, int x, cudaStream_t st);
+int launch_paged_attention_32(const d3_paged_kv &kv, const PagedAttnArgs &a, int x, cudaStream_t st);
+int launch_paged_attention_64(const d3_paged_kv &kv, const PagedAttnArgs &a, int x, cudaStream_t st);
+int launch_paged_attention_128(const d3_paged_kv &kv, const PagedAttnArgs &a, int x, cudaStream_t st);
 
 }  // namespace d3

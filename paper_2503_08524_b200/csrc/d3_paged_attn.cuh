@@ -37,8 +37,8 @@
 namespace d3 {
 namespace paged_attn {
 
-constexpr int kUnit = 64;             // positions of a stage
-constexpr int kPiece = 16;            // positions of a warp's trip, and of a TMA box
+constexpr int kPiece = 16;            // positions of a warp's trip, and of the smallest TMA box
+constexpr int kProducers = 2;         // warps that issue copies, stage by stage in turn
 constexpr int kMaxStages = 12;
 constexpr int kSmemMost = 212 * 1024; // of 227 KB: leaves room for the joining kernel's CTAs beside this one
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -156,8 +156,8 @@ enum { OUT_WHOLE = 0, OUT_HEAD = 1, OUT_TAIL = 2 };   // an item lies in this CT
 // What the producer tells the consumers about a stage.
 struct StageInfo {
   int row, tile;        // tile = kv head * tiles_per_head + tile of its query heads
-  int n;                // positions in the stage (0 .. 64)
-  int flags;            // STAGE_* | pieces that hold positions << 4 | OUT_* << 8
+  int n;                // positions in the stage (0 .. kUnit)
+  int flags;            // STAGE_* | pieces that hold positions << 4 | OUT_* << 12
 };
 
 template <int DH, int CACHE, int X, int MT>
@@ -167,13 +167,14 @@ struct Cfg {
   static constexpr int kBox = kRow < 128 ? kRow : 128;       // bytes of a box row = swizzle width
   static constexpr int kBoxes = kRow / kBox;                 // boxes per piece of K (or V)
   static constexpr int kHeads = X == D3_FP32 ? 8 : 8 * MT;   // query heads of a tile
+  static constexpr int kUnit = kRow > 128 ? 64 : 128;        // positions of a stage (of up to 32 KB)
   static constexpr int kHalfBytes = kUnit * kRow;            // K (or V) of a stage
   static constexpr int kQBytes = kHeads * DH * QBytes<X>::v;
   static constexpr int kStageBytes = 2 * kHalfBytes;
-  // Consumer warps.  Registers are dealt out to four warps at a time: with the producer 12 warps of 168 or 8 of 255,
+  // Consumer warps.  Registers are dealt out to four warps at a time: with the producers 12 warps of 168 or 8 of 255,
   // which the 64 (128) accumulator and 32 (64) query registers fit into without spills.
-  static constexpr int kWarps = MT == 1 ? 11 : 7;
-  static constexpr int kThreads = 32 * (kWarps + 1);
+  static constexpr int kWarps = MT == 1 ? 10 : 6;
+  static constexpr int kThreads = 32 * (kWarps + kProducers);
   static constexpr bool kF16 = CACHE != D3_BF16;
   static constexpr bool kThree = X == D3_FP32;
 };
@@ -181,8 +182,10 @@ struct Cfg {
 template <int DH, int CACHE, int X, int MT>
 __global__ void __launch_bounds__(Cfg<DH, CACHE, X, MT>::kThreads, 1)
 k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                  const __grid_constant__ CUtensorMap map_k16, const __grid_constant__ CUtensorMap map_v16,
                   const __grid_constant__ PagedAttnArgs a) {
   using C = Cfg<DH, CACHE, X, MT>;
+  constexpr int kUnit = C::kUnit;
   constexpr int NT = DH / 8, KK = DH / 16;
   constexpr bool F16 = C::kF16, THREE = C::kThree;
   constexpr int KT = THREE ? 1 : MT;       // score tiles that belong to different heads
@@ -277,105 +280,110 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   }
   __syncthreads();
 
-  if (warp == C::kWarps) {
-    // ------------------------------------------------------------ producer
+  if (warp >= C::kWarps) {
+    // ------------------------------------------------------------ producers
+    const int me = warp - C::kWarps;
     int row = s_start_row;
     bool dummy = false;
     int trow = row_of(row, dummy), len = length_of(row, dummy), nu = units_of(len);
-    long long at = u0 - s_start_before * HG;     // unit inside the row's (tile, unit) range
+    const long long at = u0 - s_start_before * HG;     // unit inside the row's (tile, unit) range
     int tile = (int)(at / nu), unit = (int)(at % nu);
-    int win0 = -1, win = 0, win_next = 0;        // page ids of the row: [win0, +32) in win, the next 32 in win_next
-    long long u = u0;
-    int issued = 0;
+    int kvh = tile / a.tiles_per_head, sub = tile % a.tiles_per_head;
+    const int32_t *pages = a.table + (long long)trow * a.table_stride;
+    auto fetch = [&](int base) -> int { return base + lane < a.table_width ? __ldg(pages + base + lane) : -1; };
+    // page ids of the row, one per lane: 32 aligned pages in `win`, the next 32 in `win_next`.  A unit is at most 8
+    // aligned pages and never straddles a window.
+    int win0 = -1, win = 0, win_next = 0;
+    const int box_rows = min(1 << a.page_shift, kUnit), page_mask = (1 << a.page_shift) - 1;
+    const int full_boxes = kUnit / box_rows, full_shift = 31 - __clz(full_boxes);
+    int s = 0, issued = 0;
+    uint32_t parity = 1;
     bool first = true, ok = true;
-    int joins = 0;
-    int4 join = make_int4(0, 0, 0, 0);
-    for (; u < u1; ++u) {
-      const int s = issued % S;
-      const uint32_t parity = (uint32_t)((issued / S) & 1) ^ 1u;
-      const int p0 = unit * kUnit, n = min(kUnit, len - p0);   // n <= 0 only for a row without context
-      // page ids, one per lane, 32 pages at a time and one window ahead
-      const int pg0 = p0 >> a.page_shift, pg_last = len > 0 ? (min(len, p0 + kUnit) - 1) >> a.page_shift : 0;
-      if (len > 0) {
-        const int32_t *t = a.table + (long long)trow * a.table_stride;
-        auto fetch = [&](int base) -> int {
-          const int i = base + lane;
-          return i < a.table_width ? __ldg(t + i) : -1;
-        };
-        if (win0 < 0) { win0 = pg0 & ~31; win = fetch(win0); win_next = fetch(win0 + 32); }
-        else if (pg0 >= win0 + 32) { win0 += 32; win = win_next; win_next = fetch(win0 + 32); }
-      }
-      // this lane's copy: piece (16 positions), K or V, 128-byte column
-      const int piece = lane & 3, is_v = (lane >> 2) & 1, col = lane >> 3;
-      const int pos = p0 + piece * kPiece;
-      bool want = pos < p0 + n && col < C::kBoxes;
-      const int pg = min(pos >> a.page_shift, pg_last);
-      // windows are 32 pages aligned to 32 and a unit is 64 positions = at most 4 aligned pages: it never straddles
-      const int id = __shfl_sync(0xffffffffu, win, pg & 31);
-      const bool good = id >= 0 && id < a.n_pages;
-      if (want && !good && a.status) *a.status = D3_EINVAL;
-      const bool present = pos < p0 + n && good;
-      const unsigned pieces = __ballot_sync(0xffffffffu, present) & 0xfu;
-      want = want && good;
-      const bool last = u + 1 == u1 || unit + 1 == nu;
-      if (!mb_wait(smem_u32(&s_empty[s]), parity, &s_abort, a.wait_ns)) { ok = false; }
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      const uint32_t full = smem_u32(&s_full[s]);
-      if (lane == 0) {
-        StageInfo info;
-        info.row = row; info.tile = tile; info.n = max(n, 0);
-        int kind = OUT_WHOLE;
-        if (unit + 1 < nu && last) {   // the item goes on in the next CTA
-          const bool starts_here = u - unit >= u0;
-          kind = starts_here ? OUT_TAIL : OUT_HEAD;
-          if (starts_here) {
-            const long long end = u - unit + nu;   // CTAs up to the one that holds unit end - 1
-            const int jl = (int)((end * n_cta + U - 1) / U) - 1;
-            join = make_int4(1 + jl - (int)blockIdx.x, row, tile, 0);
-            joins = 1;
+    const int n_units = (int)(u1 - u0);
+    int left = n_units;
+    long long item = u0 - unit;        // where the item's units start
+    for (int k = 0; k < n_units; ++k, --left) {
+      const bool last = left == 1 || unit + 1 == nu;
+      if ((k & (kProducers - 1)) == me) {
+        const int p0 = unit * kUnit, n = max(0, min(kUnit, len - p0));   // n = 0 only for a row without context
+        const int pg0 = p0 >> a.page_shift;
+        if (n > 0) {
+          if (win0 < 0) { win0 = pg0 & ~31; win = fetch(win0); win_next = fetch(win0 + 32); }
+          else if (pg0 >= win0 + 32) {
+            // the other producers' units may have moved past the whole next window only if a unit had more than 16 pages
+            win0 += 32; win = win_next; win_next = fetch(win0 + 32);
           }
-        } else if (last && u - unit < u0) {
-          kind = OUT_HEAD;             // its last piece: the rest is in CTAs before this one
         }
-        info.flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (int)(pieces << 4) | (kind << 8);
-        s_info[s] = info;
-        const uint32_t bytes = (uint32_t)__popc(pieces) * 2u * kPiece * C::kRow +
-                               (first ? (uint32_t)min(a.heads_per_tile, a.group - (tile % a.tiles_per_head) * a.heads_per_tile) * DH * QBytes<X>::v : 0u);
-        mb_arrive_tx(full, bytes);
-      }
-      __syncwarp();
-      if (want) {
-        const uint32_t dst = ring + s * C::kStageBytes + is_v * C::kHalfBytes + col * (kUnit * C::kBox) + piece * (kPiece * C::kBox);
-        tma_box(dst, is_v ? &map_v : &map_k, col * (C::kBox / C::kEs), pos & ((1 << a.page_shift) - 1), tile / a.tiles_per_head, id, full);
-      }
-      if (first) {
-        const int g0 = (tile % a.tiles_per_head) * a.heads_per_tile, nh = min(a.heads_per_tile, a.group - g0);
-        if (lane < nh) {
-          const long long h = (long long)(tile / a.tiles_per_head) * a.group + g0 + lane;
+        // which pieces are there: lane p looks at piece p
+        const int id_p = __shfl_sync(0xffffffffu, win, ((p0 + lane * kPiece) >> a.page_shift) & 31);
+        const bool inside = lane * kPiece < n, good = id_p >= 0 && id_p < a.n_pages;
+        const unsigned pieces = __ballot_sync(0xffffffffu, inside && good);
+        if (inside && !good && a.status) *a.status = D3_EINVAL;
+        // this lane's copy: box of positions, K or V, 128-byte column.  Whole units go in boxes of up to a page, the
+        // last unit of a row in boxes of 16 positions (nothing is fetched behind the piece the row ends in).
+        const bool whole = n == kUnit;
+        const int bs = whole ? full_shift : (kUnit == 64 ? 2 : 3);
+        const int box = lane & ((1 << bs) - 1), is_v = (lane >> bs) & 1, col = lane >> (bs + 1);
+        const int off = box * (kUnit >> bs), pos = p0 + off;
+        const int id = __shfl_sync(0xffffffffu, win, (pos >> a.page_shift) & 31);
+        const bool want = col < C::kBoxes && off < n && id >= 0 && id < a.n_pages;
+        if (!mb_wait(smem_u32(&s_empty[s]), parity, &s_abort, a.wait_ns)) ok = false;
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t full = smem_u32(&s_full[s]);
+        const int nh = min(a.heads_per_tile, a.group - sub * a.heads_per_tile);
+        if (lane == 0) {
+          StageInfo info;
+          info.row = row; info.tile = tile; info.n = n;
+          int kind = OUT_WHOLE;
+          if (last && unit + 1 < nu) kind = item >= u0 ? OUT_TAIL : OUT_HEAD;   // the item goes on in the next CTA
+          else if (last && item < u0) kind = OUT_HEAD;                          // its last piece
+          info.flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (int)(pieces << 4) | (kind << 12);
+          s_info[s] = info;
+          mb_arrive_tx(full, (uint32_t)__popc(pieces) * 2u * kPiece * C::kRow + (first ? (uint32_t)nh * DH * QBytes<X>::v : 0u));
+        }
+        __syncwarp();
+        if (want) {
+          const uint32_t dst = ring + s * C::kStageBytes + is_v * C::kHalfBytes + col * (kUnit * C::kBox) + off * C::kBox;
+          const CUtensorMap *map = whole ? (is_v ? &map_v : &map_k) : (is_v ? &map_v16 : &map_k16);
+          tma_box(dst, map, col * (C::kBox / C::kEs), pos & page_mask, kvh, id, full);
+        }
+        if (first && lane < nh) {
+          const long long h = (long long)kvh * a.group + sub * a.heads_per_tile + lane;
           bulk_copy(smem_u32(q_slots) + s * C::kQBytes + lane * DH * QBytes<X>::v,
                     static_cast<const char *>(a.q) + (row * a.q_row_stride + h * a.q_head_stride) * QBytes<X>::v, DH * QBytes<X>::v, full);
         }
       }
-      ++issued;
+      issued = k + 1;
       first = last;
-      if (++unit == nu) {   // next tile of the row, or next row
+      if (++s == S) { s = 0; parity ^= 1u; }
+      if (++unit == nu && left > 1) {   // next tile of the row, or next row
         unit = 0; win0 = -1;
-        if (++tile == HG) {
-          tile = 0;
-          if (u + 1 < u1) {
-            do { ++row; trow = row < a.n_rows ? row_of(row, dummy) : 0; } while (trow < 0);
-            len = length_of(row, dummy);
-            nu = units_of(len);
-          }
+        item += nu;
+        ++tile;
+        if (++sub == a.tiles_per_head) { sub = 0; ++kvh; }
+        if (tile == HG) {
+          tile = kvh = 0;
+          do { ++row; trow = row < a.n_rows ? row_of(row, dummy) : 0; } while (trow < 0);
+          len = length_of(row, dummy);
+          nu = units_of(len);
+          pages = a.table + (long long)trow * a.table_stride;
         }
       }
     }
-    if (lane == 0) a.join[blockIdx.x] = joins ? join : make_int4(0, 0, 0, 0);
+    if (me == 0 && lane == 0) {
+      // the last item, if it starts here and goes on: what the joining kernel adds up
+      int4 join = make_int4(0, 0, 0, 0);
+      if (ok && unit < nu && item >= u0) {   // (unit counts the units passed)
+        const long long end = item + nu;     // CTAs up to the one that holds unit end - 1
+        join = make_int4((int)((end * n_cta + U - 1) / U) - (int)blockIdx.x, row, tile, 0);
+      }
+      a.join[blockIdx.x] = join;
+    }
     if (!ok) {   // copies in flight end by themselves: wait for them before the shared memory goes
       const unsigned long long drain = a.wait_ns > kDrainFloorNs ? a.wait_ns : kDrainFloorNs;
       for (int k = max(0, issued - S); k < issued; ++k)
-        mb_wait(smem_u32(&s_full[k % S]), (uint32_t)((k / S) & 1), &s_abort, drain, false);
+        if ((k & (kProducers - 1)) == me) mb_wait(smem_u32(&s_full[k % S]), (uint32_t)((k / S) & 1), &s_abort, drain, false);
       if (lane == 0 && a.status) *a.status = D3_ETIMEOUT;
     }
     return;
@@ -393,11 +401,12 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     for (int n = 0; n < NT; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
   int piece_turn = 0;       // pieces of the CTA so far, mod kWarps: whose turn it is
   int items = 0;
-  const long long n_units = u1 - u0;
+  const int n_units = (int)(u1 - u0);
   bool ok = true;
-  for (long long k = 0; k < n_units; ++k) {
-    const int s = (int)(k % S);
-    if (!mb_wait(smem_u32(&s_full[s]), (uint32_t)((k / S) & 1), &s_abort, a.wait_ns)) ok = false;
+  int s = 0;
+  uint32_t parity = 0;
+  for (int k = 0; k < n_units; ++k) {
+    if (!mb_wait(smem_u32(&s_full[s]), parity, &s_abort, a.wait_ns)) ok = false;
     ok = __all_sync(0xffffffffu, ok);
     if (!ok) break;
     const StageInfo info = s_info[s];
@@ -465,12 +474,13 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       }
     }
     const int n_pieces = (info.n + kPiece - 1) / kPiece;
-    // pieces go round the warps; of a stage a warp has at most one (4 pieces, 7 or 11 warps)
+    // pieces go round the warps
     int p = warp - piece_turn;
     if (p < 0) p += C::kWarps;
     piece_turn += n_pieces;
-    if (piece_turn >= C::kWarps) piece_turn -= C::kWarps;
-    if (p < n_pieces && (info.flags >> (4 + p)) & 1) {
+    while (piece_turn >= C::kWarps) piece_turn -= C::kWarps;
+    for (; p < n_pieces; p += C::kWarps) {
+      if (!((info.flags >> (4 + p)) & 1)) continue;   // its page id was out of range
       const uint32_t kbase = ring + s * C::kStageBytes, vbase = kbase + C::kHalfBytes;
       const int valid = info.n - p * kPiece;   // positions of the piece (>= 1)
       // byte address of 16-byte chunk c of row r (0..15) of the piece
@@ -600,6 +610,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     }
     __syncwarp();
     if (lane == 0) mb_arrive(smem_u32(&s_empty[s]));
+    if (++s == S) { s = 0; parity ^= 1u; }
 
     if (info.flags & STAGE_LAST) {
       // ---- the item's end in this CTA: add the warps up
@@ -636,7 +647,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       if (!mb_wait(smem_u32(&s_merge[0]), (uint32_t)(items & 1), &s_abort, a.wait_ns)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      const int kind = (info.flags >> 8) & 3;
+      const int kind = (info.flags >> 12) & 3;
       const float vs = a.v_scale ? __ldg(a.v_scale + kvh) : 1.f;
       for (int i = tid; i < nh * DH; i += C::kWarps * 32) {
         const int h = i / DH, e = i % DH;
@@ -737,8 +748,13 @@ __global__ void __launch_bounds__(256) k_paged_join(const __grid_constant__ Page
 
 // ---------------------------------------------------------------- launch
 template <int DH, int CACHE, int X, int MT>
-int launch(const TMap &k, const TMap &v, PagedAttnArgs a, cudaStream_t st) {
+int launch(const d3_paged_kv &kv, PagedAttnArgs a, cudaStream_t st) {
   using C = Cfg<DH, CACHE, X, MT>;
+  TMap k, v, k16, v16;
+  const int rows = kv.page_size < C::kUnit ? kv.page_size : C::kUnit;
+  if (!encode_pool_map(&k, kv, kv.k_dev, rows) || !encode_pool_map(&v, kv, kv.v_dev, rows) ||
+      !encode_pool_map(&k16, kv, kv.k_dev, kPiece) || !encode_pool_map(&v16, kv, kv.v_dev, kPiece))
+    return -1;
   const int merge = C::kWarps * a.heads_per_tile * DH * (int)sizeof(float);
   int stages = (kSmemMost - 1024 - merge) / (C::kStageBytes + C::kQBytes);
   if (stages > kMaxStages) stages = kMaxStages;
@@ -755,22 +771,25 @@ int launch(const TMap &k, const TMap &v, PagedAttnArgs a, cudaStream_t st) {
       return -1;
     sms[dev] = n < kFusedMaxCtas ? n : kFusedMaxCtas;
   }
-  const CUtensorMap *mk = reinterpret_cast<const CUtensorMap *>(&k), *mv = reinterpret_cast<const CUtensorMap *>(&v);
-  if (launch_pdl(k_paged_attention<DH, CACHE, X, MT>, dim3(sms[dev]), dim3(C::kThreads), smem, st, *mk, *mv, a) != cudaSuccess) return -1;
+  auto map = [](const TMap &m) -> const CUtensorMap & { return *reinterpret_cast<const CUtensorMap *>(&m); };
+  if (launch_pdl(k_paged_attention<DH, CACHE, X, MT>, dim3(sms[dev]), dim3(C::kThreads), smem, st, map(k), map(v), map(k16), map(v16), a) !=
+      cudaSuccess)
+    return -1;
   // a table of at most one unit's positions cannot be cut
-  if (((long long)a.table_width << a.page_shift) > kUnit)
+  if (((long long)a.table_width << a.page_shift) > C::kUnit)
     if (launch_pdl(k_paged_join<DH, X, C::kF16>, dim3(sms[dev], a.heads_per_tile), dim3(256), 0, st, a) != cudaSuccess) return -1;
   return 0;
 }
 
 template <int DH>
-int launch_types(const TMap &k, const TMap &v, const PagedAttnArgs &a, int cache, int x, cudaStream_t st) {
+int launch_types(const d3_paged_kv &kv, const PagedAttnArgs &a, int x, cudaStream_t st) {
+  const int cache = kv.dtype;
   const bool wide = a.heads_per_tile > 8;
-  if (cache == D3_BF16 && x == D3_FP32) return launch<DH, D3_BF16, D3_FP32, 2>(k, v, a, st);
-  if (cache == D3_BF16) return wide ? launch<DH, D3_BF16, D3_BF16, 2>(k, v, a, st) : launch<DH, D3_BF16, D3_BF16, 1>(k, v, a, st);
-  if (cache == D3_FP16) return wide ? launch<DH, D3_FP16, D3_FP16, 2>(k, v, a, st) : launch<DH, D3_FP16, D3_FP16, 1>(k, v, a, st);
-  if (x == D3_BF16) return wide ? launch<DH, D3_E4M3, D3_BF16, 2>(k, v, a, st) : launch<DH, D3_E4M3, D3_BF16, 1>(k, v, a, st);
-  return wide ? launch<DH, D3_E4M3, D3_FP16, 2>(k, v, a, st) : launch<DH, D3_E4M3, D3_FP16, 1>(k, v, a, st);
+  if (cache == D3_BF16 && x == D3_FP32) return launch<DH, D3_BF16, D3_FP32, 2>(kv, a, st);
+  if (cache == D3_BF16) return wide ? launch<DH, D3_BF16, D3_BF16, 2>(kv, a, st) : launch<DH, D3_BF16, D3_BF16, 1>(kv, a, st);
+  if (cache == D3_FP16) return wide ? launch<DH, D3_FP16, D3_FP16, 2>(kv, a, st) : launch<DH, D3_FP16, D3_FP16, 1>(kv, a, st);
+  if (x == D3_BF16) return wide ? launch<DH, D3_E4M3, D3_BF16, 2>(kv, a, st) : launch<DH, D3_E4M3, D3_BF16, 1>(kv, a, st);
+  return wide ? launch<DH, D3_E4M3, D3_FP16, 2>(kv, a, st) : launch<DH, D3_E4M3, D3_FP16, 1>(kv, a, st);
 }
 
 }  // namespace paged_attn

@@ -3,8 +3,8 @@
 
 namespace d3 {
 
-int launch_paged_attention_128(const TMap &k, const TMap &v, PagedAttnArgs a, int cache, int x, cudaStream_t st) {
-  return paged_attn::launch_types<128>(k, v, a, cache, x, st);
+int launch_paged_attention_128(const d3_paged_kv &kv, const PagedAttnArgs &a, int x, cudaStream_t st) {
+  return paged_attn::launch_types<128>(kv, a, x, st);
 }
 
 }  // namespace d3
