@@ -1,30 +1,30 @@
 // Attention of one new token per row over a paged cache: the kernel, compiled per head dimension.
 //
 // Mathematics.  For a tile of up to 8 query heads of one kv head (16 with two score tiles) and a piece of 16
-// positions: S = Q K^T, the running maximum m and sum l of exp2(S scale log2 e - m), O = O exp2(m_old - m) + P V.
-// O, m and l are additive over any cut of the positions once brought to a common maximum, which is all that the
-// split over the length needs.
+// positions: S^T = K Q^T, the running maximum m and sum l of exp2(S scale log2 e - m), O^T = O^T exp2(m_old - m) +
+// V^T P^T.  O, m and l are additive over any cut of the positions once brought to a common maximum, which is all that
+// the split over the length needs.
 //
 // What bounds it.  K and V are read once: 2 G flops per byte (G query heads per kv head, 16-bit cache), far
 // below the ~260 of this GPU's tensor cores, so HBM decides and the kernel is built to keep copies in flight:
-//   * one CTA per SM; a producer warp walks the CTA's share of all positions of all rows and fills a ring of up to
-//     ~170 KB of 64-position stages by TMA (4-D tensor map over the pool: dim, position, kv head, page; boxes of
-//     16 positions, so any page size and both layouts cost the same); it looks page ids up 32 at a time, one
-//     window ahead, and never waits for the arithmetic until the ring is full;
+//   * one CTA per SM; two producer warps walk the CTA's share of all positions of all rows and fill a ring of up to
+//     ~170 KB of 32 KB stages by TMA (4-D tensor map over the pool: dim, position, kv head, page; boxes of up to a
+//     page, of 16 positions where a row ends), so both layouts cost the same; page ids are looked up 32 at a time, one
+//     window ahead; they never wait for the arithmetic until the ring is full;
 //   * the share is cut by positions, not by rows: row lengths are read on the device, every CTA sums them up and takes
-//     the same number of 64-position units, so ragged batches and one long row load all SMs alike;
-//   * a consumer warp takes one piece of 16 positions of a stage at a time (mma.sync m16n8k16, fragments by
-//     ldmatrix from the 128-byte-swizzled rows).  The 16 rows of a score tile hold the 8 heads twice: for P V the
-//     upper 8 rows carry P - round(P), which keeps P to 16 (bf16) or 22 (fp16) bits for nothing.  tcgen05.mma would
-//     put 8 rows into a 128-row tile and its operands and results through shared and tensor memory; with the
-//     pipe as idle as it is here that only adds steps.
-//   * rows that end inside a CTA are written at once; of a row that is cut every CTA leaves (m, l, O) of its piece and
+//     the same number of units (stages), so ragged batches and one long row load all SMs alike;
+//   * a consumer warp takes one piece of 16 positions at a time (mma.sync m16n8k16).  Positions (dims) are the 16 rows
+//     of a product and heads its 8 columns: K and V come from the swizzled stage by ldmatrix as they lie there, no row
+//     is wasted on G <= 8 heads, and 8 heads x 128 dims of O take 32 registers.  P is used as two terms, P - round(P) in a
+//     second product: 16 (bf16) or 22 (fp16) bits of it count.  tcgen05.mma would need P, a few hundred numbers, written to
+//     shared memory and results fetched from tensor memory for every piece; the legacy pipe is a quarter busy here;
+//   * epilogue warps add the consumers' (m, l, O) up at the end of a row, while the consumers go on with the next row.
+//     Rows that end inside a CTA are written at once; of a row that is cut every CTA leaves (m, l, O) of its piece and
 //     k_paged_join adds them up in the order of the CTAs: bits depend on the lengths alone, no atomics.
 //
-// fp32 queries (bf16 cache): q is three bf16 terms by truncation (8 + 8 + 8 bits: exact), P too; two score tiles carry
-// (hi, mid) and (lo, 0) of 8 heads.  8-bit cache: the stored numbers are widened to fp16 (exact), bf16 queries are
-// scaled by a power of two per head so that fp16 holds them.  Where P is fp16, it is exp2(.. + 15): 2^-29 of the
-// largest stays a normal number.
+// fp32 queries (bf16 cache): q and P are three bf16 terms by truncation (8 + 8 + 8 bits: exact).  8-bit cache: the
+// stored numbers are widened to fp16 (exact), bf16 queries are scaled by a power of two per head so that fp16 holds
+// them.  Where P is fp16, it is exp2(.. + 15): 2^-29 of the largest stays a normal number.
 //
 // Every wait is bounded; when one runs out the CTA stores D3_ETIMEOUT, stops issuing, lets its copies land and ends.
 #pragma once
@@ -40,7 +40,7 @@ namespace paged_attn {
 constexpr int kPiece = 16;            // positions of a warp's trip, and of the smallest TMA box
 constexpr int kProducers = 2;         // warps that issue copies, stage by stage in turn
 constexpr int kMaxStages = 12;
-constexpr int kSmemMost = 212 * 1024; // of 227 KB: leaves room for the joining kernel's CTAs beside this one
+constexpr int kSmemMost = 224 * 1024; // of 227 KB
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <int CACHE> struct CacheBytes { static constexpr int v = CACHE == D3_E4M3 ? 1 : 2; };
@@ -97,6 +97,12 @@ __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
+// transpose of an 8 x 8 matrix of 16-bit numbers held by the warp
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
 __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
@@ -147,6 +153,11 @@ __device__ __forceinline__ uint32_t cut(float &x, float &y) {
   return (a >> 16) | b;
 }
 
+// What the consumers tell the epilogue warps about an item.
+struct ItemInfo {
+  int row, tile, kind, final;
+};
+
 // The share of CTA i of n among U units starts here.
 __device__ __forceinline__ long long share(long long U, int i, int n) { return U * i / n; }
 
@@ -171,12 +182,15 @@ struct Cfg {
   static constexpr int kHalfBytes = kUnit * kRow;            // K (or V) of a stage
   static constexpr int kQBytes = kHeads * DH * QBytes<X>::v;
   static constexpr int kStageBytes = 2 * kHalfBytes;
-  // Consumer warps.  Registers are dealt out to four warps at a time: with the producers 12 warps of 168 or 8 of 255,
-  // which the 64 (128) accumulator and 32 (64) query registers fit into without spills.
-  static constexpr int kWarps = MT == 1 ? 10 : 6;
-  static constexpr int kThreads = 32 * (kWarps + kProducers);
+  // Registers are dealt out to four warps at a time: 16 warps of 128 (which 32 accumulator and 16 query registers fit
+  // into), or 12 of 168 for 16 heads or three-term queries.
+  static constexpr int kWarps = MT == 1 ? 10 : 8;            // consumers
+  static constexpr int kEpilogue = MT == 1 ? 4 : 2;
+  static constexpr int kThreads = 32 * (kWarps + kProducers + kEpilogue);
+  static constexpr int kHeadFloats = DH + 4;                 // of a head's sums in shared memory (padded: no bank conflicts)
   static constexpr bool kF16 = CACHE != D3_BF16;
-  static constexpr bool kThree = X == D3_FP32;
+  static constexpr int kTiles = X == D3_FP32 ? 1 : MT;       // 8-head tiles
+  static constexpr int kQTerms = X == D3_FP32 ? 3 : 1, kPTerms = X == D3_FP32 ? 3 : 2;
 };
 
 template <int DH, int CACHE, int X, int MT>
@@ -186,13 +200,13 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                   const __grid_constant__ PagedAttnArgs a) {
   using C = Cfg<DH, CACHE, X, MT>;
   constexpr int kUnit = C::kUnit;
-  constexpr int NT = DH / 8, KK = DH / 16;
-  constexpr bool F16 = C::kF16, THREE = C::kThree;
-  constexpr int KT = THREE ? 1 : MT;       // score tiles that belong to different heads
+  constexpr int KK = DH / 16, KT = C::kTiles, TQ = C::kQTerms, TP = C::kPTerms;
+  constexpr bool F16 = C::kF16;
   extern __shared__ unsigned char s_dyn[];
-  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_merge[2];
+  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sums_full, s_sums_free;
   __shared__ StageInfo s_info[kMaxStages];
   __shared__ float s_m[C::kWarps][C::kHeads], s_l[C::kWarps][C::kHeads];
+  __shared__ ItemInfo s_item;
   __shared__ long long s_sum[32];
   __shared__ int s_abort, s_start_row;
   __shared__ long long s_start_before;
@@ -201,7 +215,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   const uint32_t ring = (smem_u32(s_dyn) + 1023u) & ~1023u;
   unsigned char *ring_p = s_dyn + (ring - smem_u32(s_dyn));
   unsigned char *q_slots = ring_p + (size_t)S * C::kStageBytes;
-  float *s_o = reinterpret_cast<float *>(q_slots + (size_t)S * C::kQBytes);   // [warp][head][DH]
+  float *s_o = reinterpret_cast<float *>(q_slots + (size_t)S * C::kQBytes);   // [warp][head][kHeadFloats]
   const int HG = a.hkv * a.tiles_per_head;
 
   if (tid == 0) {
@@ -209,11 +223,15 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       mb_init(smem_u32(&s_full[i]), 1);
       mb_init(smem_u32(&s_empty[i]), C::kWarps);
     }
-    mb_init(smem_u32(&s_merge[0]), C::kWarps);
-    mb_init(smem_u32(&s_merge[1]), C::kWarps);
+    mb_init(smem_u32(&s_sums_full), C::kWarps);
+    mb_init(smem_u32(&s_sums_free), C::kEpilogue);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s_abort = 0;
     s_start_row = a.n_rows;
+  }
+  if (warp == C::kWarps + C::kEpilogue && lane < 4) {
+    const CUtensorMap *m = lane == 0 ? &map_k : lane == 1 ? &map_v : lane == 2 ? &map_k16 : &map_v16;
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
   }
   pdl_wait();
   pdl_trigger();
@@ -280,9 +298,9 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   }
   __syncthreads();
 
-  if (warp >= C::kWarps) {
+  if (warp >= C::kWarps + C::kEpilogue) {
     // ------------------------------------------------------------ producers
-    const int me = warp - C::kWarps;
+    const int me = warp - C::kWarps - C::kEpilogue;
     int row = s_start_row;
     bool dummy = false;
     int trow = row_of(row, dummy), len = length_of(row, dummy), nu = units_of(len);
@@ -389,16 +407,94 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     return;
   }
 
+  auto write_out = [&](long long at, float val) {
+    if (X == D3_FP32) static_cast<float *>(a.out)[at] = val;
+    else if (X == D3_BF16) static_cast<bf16 *>(a.out)[at] = __float2bfloat16_rn(val);
+    else static_cast<__half *>(a.out)[at] = __float2half_rn(val);
+  };
+
+  if (warp >= C::kWarps) {
+    // ------------------------------------------------------------ epilogue: a head per warp, DH / 32 dims per lane
+    constexpr int V = DH / 32;
+    const int me = warp - C::kWarps;
+    for (uint32_t parity = 0;; parity ^= 1u) {
+      if (!__all_sync(0xffffffffu, mb_wait(smem_u32(&s_sums_full), parity, &s_abort, a.wait_ns))) break;
+      const ItemInfo item = s_item;
+      const int kvh = item.tile / a.tiles_per_head, g0 = (item.tile % a.tiles_per_head) * a.heads_per_tile;
+      const int nh = min(a.heads_per_tile, a.group - g0);
+      for (int h = me; h < nh; h += C::kEpilogue) {
+        const float l = lane < C::kWarps ? s_l[lane][h] : 0.f;
+        const float m = lane < C::kWarps ? s_m[lane][h] : -INFINITY;
+        float M = m;
+#pragma unroll
+        for (int d = 8; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+        M = __shfl_sync(0xffffffffu, M, 0);
+        // a warp that had no position of the item counts with factor 0, whatever lies in its sums
+        const float c = l != 0.f ? exp2_fast(m - (M == -INFINITY ? 0.f : M)) : 0.f;
+        float L = l != 0.f ? l * c : 0.f;
+#pragma unroll
+        for (int d = 8; d; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
+        L = __shfl_sync(0xffffffffu, L, 0);
+        const unsigned took_part = __ballot_sync(0xffffffffu, l != 0.f);
+        float o[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < C::kWarps; ++w) {
+          const float cw = __shfl_sync(0xffffffffu, c, w);
+          const float *src = s_o + (w * a.heads_per_tile + h) * C::kHeadFloats + lane * V;
+          const uint32_t there = 0u - (took_part >> w & 1u);   // a mask: sums that were not written may be anything
+          uint32_t x[V];
+          if constexpr (V == 4) { const uint4 v = *reinterpret_cast<const uint4 *>(src); x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+          else if constexpr (V == 2) { const uint2 v = *reinterpret_cast<const uint2 *>(src); x[0] = v.x; x[1] = v.y; }
+          else x[0] = *reinterpret_cast<const uint32_t *>(src);
+#pragma unroll
+          for (int e = 0; e < V; ++e) o[e] += cw * __uint_as_float(x[e] & there);
+        }
+        const long long head = (long long)kvh * a.group + g0 + h;
+        if (item.kind == OUT_WHOLE) {
+          const float f = L == 0.f ? 0.f : (a.v_scale ? __ldg(a.v_scale + kvh) : 1.f) / L;
+          const long long at = item.row * a.out_row_stride + head * a.out_head_stride + lane * V;
+#pragma unroll
+          for (int e = 0; e < V; ++e) write_out(at + e, o[e] * f);
+          if (lane == 0 && a.lse)
+            a.lse[(long long)item.row * a.hq + head] = L == 0.f ? -INFINITY : (M + (log2f(L) - (F16 ? 15.f : 0.f))) * kLn2;
+        } else {
+          const size_t part = (size_t)(2 * blockIdx.x + (item.kind == OUT_TAIL ? 1 : 0)) * 16 + h;
+#pragma unroll
+          for (int e = 0; e < V; ++e) a.part_o[part * DH + lane * V + e] = o[e];
+          if (lane == 0) { a.part_ml[2 * part] = M; a.part_ml[2 * part + 1] = L; }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mb_arrive(smem_u32(&s_sums_free));
+      if (item.final) break;
+    }
+    return;
+  }
+
   // -------------------------------------------------------------- consumers
-  const int g = lane >> 2, t = lane & 3;
-  uint32_t qa[MT][KK][4];
-  float o[MT][NT][4], mx[KT], sum[KT], mul[KT];
+  // Fragments (g = lane / 4, t = lane % 4).  Scores: A = K (rows = positions), B = Q^T (column g = head), result: positions
+  // g, g + 8 of heads 2t, 2t + 1.  Sums: A = V^T (rows = dims), B = P^T, result: dims g, g + 8 of heads 2t, 2t + 1.
+  const int g = lane >> 2, t = lane & 3, mat = lane >> 3;
+  // 16-bit cache: row and 16-byte chunk of this lane's ldmatrix row; 8-bit: the same for two chunks of 16 dims
+  constexpr int kPerRow = C::kBox / 16;
+  const int k_row = (lane & 7) + 8 * (mat & 1), k_chunk = mat >> 1;                      // K: (0-7), (8-15), then the next chunk
+  const int v_row = CACHE == D3_E4M3 ? k_row : (lane & 7) + 8 * (mat >> 1);              // V: 16-bit: dims first, then positions
+  const int v_chunk = CACHE == D3_E4M3 ? k_chunk : mat & 1;
+  auto lane_part = [](int r, int c) -> uint32_t {   // of an address; the swizzle XORs the chunk with the row's 128-byte line
+    return (uint32_t)(r * C::kBox + ((c ^ (((r * C::kBox) >> 7) & (kPerRow - 1))) << 4));
+  };
+  const uint32_t k_lane = lane_part(k_row, k_chunk), v_lane = lane_part(v_row, v_chunk);
+  uint32_t qb[KT][TQ][KK][2];
+  float o[KT][KK][4], mx[KT][2], sum[KT][2], mul[KT][2];
 #pragma unroll
-  for (int i = 0; i < KT; ++i) { mx[i] = -INFINITY; sum[i] = 0.f; mul[i] = 0.f; }
+  for (int i = 0; i < KT; ++i) {
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
+    for (int e = 0; e < 2; ++e) { mx[i][e] = -INFINITY; sum[i][e] = 0.f; mul[i][e] = 0.f; }
 #pragma unroll
-    for (int n = 0; n < NT; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+    for (int n = 0; n < KK; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+  }
   int piece_turn = 0;       // pieces of the CTA so far, mod kWarps: whose turn it is
   int items = 0;
   const int n_units = (int)(u1 - u0);
@@ -410,17 +506,17 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     ok = __all_sync(0xffffffffu, ok);
     if (!ok) break;
     const StageInfo info = s_info[s];
-    const int kvh = info.tile / a.tiles_per_head, g0 = (info.tile % a.tiles_per_head) * a.heads_per_tile;
-    const int nh = min(a.heads_per_tile, a.group - g0);
     if (info.flags & STAGE_FIRST) {
       // ---- this thread's fragments of Q, and what a raw score is multiplied by
+      const int kvh = info.tile / a.tiles_per_head, g0 = (info.tile % a.tiles_per_head) * a.heads_per_tile;
+      const int nh = min(a.heads_per_tile, a.group - g0);
       const float ks = a.k_scale ? __ldg(a.k_scale + kvh) : 1.f;
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
         const int h = g + 8 * i;
         const bool live = h < nh;
         const unsigned char *qp = q_slots + (size_t)s * C::kQBytes + (size_t)(live ? h : 0) * DH * QBytes<X>::v;
-        mul[i] = a.scale * kLog2e * ks;
+        float factor = a.scale * kLog2e * ks;
         if constexpr (X == D3_FP32) {
 #pragma unroll
           for (int kk = 0; kk < KK; ++kk)
@@ -428,22 +524,19 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             for (int j = 0; j < 2; ++j) {
               const float2 v = *reinterpret_cast<const float2 *>(qp + (16 * kk + 8 * j + 2 * t) * 4);
               float x = live ? v.x : 0.f, y = live ? v.y : 0.f;
-              qa[0][kk][2 * j] = cut(x, y);
-              qa[0][kk][2 * j + 1] = cut(x, y);
-              qa[MT - 1][kk][2 * j] = cut(x, y);
-              qa[MT - 1][kk][2 * j + 1] = 0u;
+#pragma unroll
+              for (int q = 0; q < TQ; ++q) qb[i][q][kk][j] = cut(x, y);
             }
         } else {
-          // position of the pairs: dims 16kk + 2t, +8 (16-bit cache); 16kk + 4t, +2 (8-bit cache, whose
-          // four bytes of a fragment register are four neighbouring dims)
+          // the pairs: dims 16kk + 2t, +8 (16-bit cache); 16kk + 4t, +2 (8-bit cache, whose four bytes of a
+          // fragment register are four neighbouring dims)
           constexpr int kA = CACHE == D3_E4M3 ? 4 : 2, kB = CACHE == D3_E4M3 ? 2 : 8;
 #pragma unroll
           for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               const uint32_t v = *reinterpret_cast<const uint32_t *>(qp + (16 * kk + kB * j + kA * t) * 2);
-              qa[i][kk][2 * j] = live ? v : 0u;
-              qa[i][kk][2 * j + 1] = 0u;
+              qb[i][0][kk][j] = live ? v : 0u;
             }
           if constexpr (CACHE == D3_E4M3 && X == D3_BF16) {
             // to fp16: the head's largest |q| scaled to [1, 2); what falls under fp16's range is under 2^-24 of it
@@ -453,24 +546,26 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
                 float x, y;
-                unpack<false>(qa[i][kk][2 * j], x, y);
+                unpack<false>(qb[i][0][kk][j], x, y);
                 top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
               }
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const int e = (top >= 1.17549435e-38f && top < INFINITY) ? min((int)(__float_as_uint(top) >> 23) - 127, 126) : 0;
             const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
-            mul[i] *= up;
+            factor *= up;
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
                 float x, y;
-                unpack<false>(qa[i][kk][2 * j], x, y);
-                qa[i][kk][2 * j] = pack<true>(x * down, y * down);
+                unpack<false>(qb[i][0][kk][j], x, y);
+                qb[i][0][kk][j] = pack<true>(x * down, y * down);
               }
           }
         }
+        mul[i][0] = __shfl_sync(0xffffffffu, factor, 8 * t);       // of heads 2t and 2t + 1
+        mul[i][1] = __shfl_sync(0xffffffffu, factor, 8 * t + 4);
       }
     }
     const int n_pieces = (info.n + kPiece - 1) / kPiece;
@@ -481,129 +576,118 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     while (piece_turn >= C::kWarps) piece_turn -= C::kWarps;
     for (; p < n_pieces; p += C::kWarps) {
       if (!((info.flags >> (4 + p)) & 1)) continue;   // its page id was out of range
-      const uint32_t kbase = ring + s * C::kStageBytes, vbase = kbase + C::kHalfBytes;
+      const uint32_t kbase = ring + s * C::kStageBytes + p * (kPiece * C::kBox) + k_lane;
+      const uint32_t vbase = ring + s * C::kStageBytes + C::kHalfBytes + p * (kPiece * C::kBox) + v_lane;
       const int valid = info.n - p * kPiece;   // positions of the piece (>= 1)
-      // byte address of 16-byte chunk c of row r (0..15) of the piece
-      auto chunk = [&](uint32_t base, int r, int c) -> uint32_t {
-        constexpr int per_row = C::kBox / 16;
-        const int half = c / per_row, cc = c % per_row;
-        return base + half * (kUnit * C::kBox) + (p * kPiece + r) * C::kBox + ((cc ^ (((r * C::kBox) >> 7) & (per_row - 1))) << 4);
-      };
-      float sc[MT][2][4];
+      // 16-byte chunk c (even) past the lane's own: an XOR inside the 128-byte line, the next column behind it
+      auto chunk = [&](uint32_t base, int c) -> uint32_t { return (base ^ ((c % kPerRow) << 4)) + (c / kPerRow) * (kUnit * C::kBox); };
+      float sc[KT][4];
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) sc[i][j][0] = sc[i][j][1] = sc[i][j][2] = sc[i][j][3] = 0.f;
-      const int mat = lane >> 3;
+      for (int i = 0; i < KT; ++i) sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
       if constexpr (CACHE != D3_E4M3) {
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-          uint32_t b[4];   // (positions 0-7, dims 16kk..+7), (0-7, +8..+15), (8-15, ..), (8-15, ..)
-          ldsm4(b, chunk(kbase, (lane & 7) + 8 * (mat >> 1), 2 * kk + (mat & 1)));
+          uint32_t f[4];
+          ldsm4(f, chunk(kbase, 2 * kk));
 #pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            mma<F16>(sc[i][0], qa[i][kk], b[0], b[1]);
-            mma<F16>(sc[i][1], qa[i][kk], b[2], b[3]);
-          }
+          for (int i = 0; i < KT; ++i)
+#pragma unroll
+            for (int q = TQ - 1; q >= 0; --q) mma<F16>(sc[i], f, qb[i][q][kk][0], qb[i][q][kk][1]);
         }
       } else {
 #pragma unroll
         for (int kk = 0; kk < KK; kk += 2) {
-          uint32_t b[4];   // (positions 0-7, dims 16kk..+15), (8-15, same), then the next 16 dims
-          ldsm4(b, chunk(kbase, (lane & 7) + 8 * (mat & 1), kk + (mat >> 1)));
+          uint32_t b[4];   // chunk kk of positions 0-7, of 8-15, then chunk kk + 1: four dims 4t.. of position g
+          ldsm4(b, chunk(kbase, kk));
 #pragma unroll
-          for (int q = 0; q < 2; ++q)
+          for (int q = 0; q < 2; ++q) {
+            const uint32_t f[4] = {widen(b[2 * q]), widen(b[2 * q + 1]), widen(b[2 * q] >> 16), widen(b[2 * q + 1] >> 16)};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const uint32_t b0 = widen(b[2 * q + j]), b1 = widen(b[2 * q + j] >> 16);
-#pragma unroll
-              for (int i = 0; i < MT; ++i) mma<F16>(sc[i][j], qa[i][kk + q], b0, b1);
-            }
+            for (int i = 0; i < KT; ++i) mma<F16>(sc[i], f, qb[i][0][kk + q][0], qb[i][0][kk + q][1]);
+          }
         }
       }
-      // ---- softmax of the piece: this thread has head g (+ 8 i), positions 2t, 2t+1, 8+2t, 8+2t+1
-      uint32_t pa[MT][4];
+      // ---- softmax of the piece: [0] head 2t, [1] head 2t + 1 of position g; [2], [3] of position g + 8
+      const bool partial = valid < kPiece;
+      uint32_t pb[KT][TP][2];
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
         float v[4];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float x = THREE ? (sc[MT - 1][j][e] + sc[0][j][2 + e]) + sc[0][j][e] : sc[i][j][e];
-            x *= mul[i];
-            v[2 * j + e] = 8 * j + 2 * t + e < valid ? x : -INFINITY;
-          }
-        float cm = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
-        cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 1));
-        cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 2));
-        const float mn = fmaxf(mx[i], cm);
-        if (__any_sync(0xffffffffu, mn > mx[i])) {
-          const float corr = mn > mx[i] ? exp2_fast(mx[i] - mn) : 1.f;   // 0 at the first piece
-          sum[i] *= corr;
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            o[i][n][0] *= corr; o[i][n][1] *= corr; o[i][n][2] *= corr; o[i][n][3] *= corr;
-            if (THREE) { o[MT - 1][n][0] *= corr; o[MT - 1][n][1] *= corr; }
-          }
+        for (int e = 0; e < 4; ++e) v[e] = sc[i][e] * mul[i][e & 1];
+        if (partial) {
+          if (g >= valid) v[0] = v[1] = -INFINITY;
+          if (g + 8 >= valid) v[2] = v[3] = -INFINITY;
         }
-        mx[i] = mn;
-        const float ref = mn == -INFINITY ? 0.f : (F16 ? mn - 15.f : mn);
+        float cm[2] = {fmaxf(v[0], v[2]), fmaxf(v[1], v[3])};
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+          cm[0] = fmaxf(cm[0], __shfl_xor_sync(0xffffffffu, cm[0], d));
+          cm[1] = fmaxf(cm[1], __shfl_xor_sync(0xffffffffu, cm[1], d));
+        }
+        if (__any_sync(0xffffffffu, cm[0] > mx[i][0] || cm[1] > mx[i][1])) {   // a new maximum: rescale (by 0 at the first piece)
+          const float m0 = fmaxf(mx[i][0], cm[0]), m1 = fmaxf(mx[i][1], cm[1]);
+          const float c0 = m0 > mx[i][0] ? exp2_fast(mx[i][0] - m0) : 1.f, c1 = m1 > mx[i][1] ? exp2_fast(mx[i][1] - m1) : 1.f;
+          mx[i][0] = m0; mx[i][1] = m1;
+          sum[i][0] *= c0; sum[i][1] *= c1;
+#pragma unroll
+          for (int n = 0; n < KK; ++n) { o[i][n][0] *= c0; o[i][n][1] *= c1; o[i][n][2] *= c0; o[i][n][3] *= c1; }
+        }
         float pr[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { pr[e] = exp2_fast(v[e] - ref); sum[i] += pr[e]; }
-        if constexpr (THREE) {
+        for (int e = 0; e < 4; ++e) {
+          const float m = mx[i][e & 1], ref = m == -INFINITY ? 0.f : (F16 ? m - 15.f : m);
+          pr[e] = exp2_fast(v[e] - ref);
+          sum[i][e & 1] += pr[e];
+        }
+        // P^T fragments: positions 2t, 2t + 1 (+ 8) of head g, the transpose of what this thread holds
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            pa[0][2 * j] = cut(pr[2 * j], pr[2 * j + 1]);
-            pa[0][2 * j + 1] = cut(pr[2 * j], pr[2 * j + 1]);
-            pa[MT - 1][2 * j] = cut(pr[2 * j], pr[2 * j + 1]);
-            pa[MT - 1][2 * j + 1] = 0u;
-          }
-        } else {
+        for (int j = 0; j < 2; ++j) {
+          float x = pr[2 * j], y = pr[2 * j + 1];
+          if constexpr (TP == 3) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t hi = pack<F16>(pr[2 * j], pr[2 * j + 1]);
-            float x, y;
-            unpack<F16>(hi, x, y);
-            pa[i][2 * j] = hi;
-            pa[i][2 * j + 1] = pack<F16>(pr[2 * j] - x, pr[2 * j + 1] - y);
+            for (int q = 0; q < 3; ++q) pb[i][q][j] = transpose8(cut(x, y));
+          } else {
+            const uint32_t hi = pack<F16>(x, y);
+            float hx, hy;
+            unpack<F16>(hi, hx, hy);
+            pb[i][0][j] = transpose8(hi);
+            pb[i][1][j] = transpose8(pack<F16>(x - hx, y - hy));
           }
         }
       }
-      // ---- O += P V.  What the page holds behind the row's end must not reach a product (0 x NaN is NaN).
+      // ---- O^T += V^T P^T.  What the page holds behind the row's end must not reach a product (0 x NaN is NaN).
       uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
-      const bool partial = valid < kPiece;
       if (partial) {
         keep0 = (2 * t < valid ? 0xffffu : 0u) | (2 * t + 1 < valid ? 0xffff0000u : 0u);
         keep1 = (2 * t + 8 < valid ? 0xffffu : 0u) | (2 * t + 9 < valid ? 0xffff0000u : 0u);
       }
+      auto add = [&](int n, uint32_t (&f)[4]) {
+        if (partial) { f[0] &= keep0; f[1] &= keep0; f[2] &= keep1; f[3] &= keep1; }
 #pragma unroll
-      for (int n = 0; n < NT; n += 2) {
-        if constexpr (CACHE != D3_E4M3) {
-          uint32_t b[4];   // (positions 0-7, dims 8n..), (8-15, same), (0-7, dims 8n+8..), (8-15, same)
-          ldsm4t(b, chunk(vbase, (lane & 7) + 8 * (mat & 1), n + (mat >> 1)));
-          if (partial) { b[0] &= keep0; b[1] &= keep1; b[2] &= keep0; b[3] &= keep1; }
+        for (int i = 0; i < KT; ++i)
 #pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            mma<F16>(o[i][n], pa[i], b[0], b[1]);
-            mma<F16>(o[i][n + 1], pa[i], b[2], b[3]);
-          }
-        } else if (n % 4 == 0) {
-          // 16-byte chunks n/2 and n/2 + 1: a register holds positions 2t, 2t+1 of dims 2g, 2g+1 of the chunk;
-          // even dims make one 8-wide tile, odd dims the next
+          for (int q = TP - 1; q >= 0; --q) mma<F16>(o[i][n], f, pb[i][q][0], pb[i][q][1]);
+      };
+      if constexpr (CACHE != D3_E4M3) {
+#pragma unroll
+        for (int n = 0; n < KK; ++n) {
+          uint32_t f[4];   // dims 16n.. / +8 of positions 0-7, then of 8-15
+          ldsm4t(f, chunk(vbase, 2 * n));
+          add(n, f);
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < KK; n += 2) {
+          // chunk n of positions 0-7, of 8-15, then chunk n + 1: positions 2t, 2t + 1 of dims 2g, 2g + 1.  Even
+          // dims make rows 0-7 of the product, odd ones rows 8-15
           uint32_t b[4];
-          ldsm4t(b, chunk(vbase, (lane & 7) + 8 * (mat & 1), n / 2 + (mat >> 1)));
+          ldsm4t(b, chunk(vbase, n));
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
-            const uint32_t u0_ = __byte_perm(b[2 * q], 0, 0x3120), u1_ = __byte_perm(b[2 * q + 1], 0, 0x3120);
-            uint32_t e0 = widen(u0_), e1 = widen(u1_), d0 = widen(u0_ >> 16), d1 = widen(u1_ >> 16);
-            if (partial) { e0 &= keep0; d0 &= keep0; e1 &= keep1; d1 &= keep1; }
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-              mma<F16>(o[i][n + 2 * q], pa[i], e0, e1);
-              mma<F16>(o[i][n + 2 * q + 1], pa[i], d0, d1);
-            }
+            const uint32_t lo = __byte_perm(b[2 * q], 0, 0x3120), hi = __byte_perm(b[2 * q + 1], 0, 0x3120);
+            uint32_t f[4] = {widen(lo), widen(lo >> 16), widen(hi), widen(hi >> 16)};
+            add(n + q, f);
           }
         }
       }
@@ -613,137 +697,134 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (++s == S) { s = 0; parity ^= 1u; }
 
     if (info.flags & STAGE_LAST) {
-      // ---- the item's end in this CTA: add the warps up
-      // the previous item's sums have been read by every warp
-      if (items > 0 && !mb_wait(smem_u32(&s_merge[1]), (uint32_t)((items - 1) & 1), &s_abort, a.wait_ns)) ok = false;
+      // ---- the item's end in this CTA: this warp's sums to shared memory, for the epilogue warps to add up
+      if (items > 0 && !mb_wait(smem_u32(&s_sums_free), (uint32_t)((items - 1) & 1), &s_abort, a.wait_ns)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
-        float l = sum[i];
-        l += __shfl_xor_sync(0xffffffffu, l, 1);
-        l += __shfl_xor_sync(0xffffffffu, l, 2);
-        const int h = g + 8 * i;
-        if (h < nh) {
-          float *dst = s_o + ((size_t)warp * a.heads_per_tile + h) * DH;
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+        for (int e = 0; e < 2; ++e) {
+          const int h = 2 * t + e + 8 * i;
+          float l = sum[i][e];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float val = THREE ? (o[MT - 1][n][e] + o[0][n][2 + e]) + o[0][n][e] : o[i][n][2 + e] + o[i][n][e];
-              const int dim = CACHE == D3_E4M3 ? 16 * (n >> 1) + 2 * (2 * t + e) + (n & 1) : 8 * n + 2 * t + e;
-              dst[dim] = val;
+          for (int d = 4; d < 32; d <<= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+          if (h < a.heads_per_tile) {
+            float *dst = s_o + (warp * a.heads_per_tile + h) * C::kHeadFloats;
+            if (l != 0.f) {
+#pragma unroll
+              for (int n = 0; n < KK; ++n) {
+                if constexpr (CACHE == D3_E4M3) {
+                  *reinterpret_cast<float2 *>(dst + 16 * n + 2 * g) = make_float2(o[i][n][e], o[i][n][2 + e]);
+                } else {
+                  dst[16 * n + g] = o[i][n][e];
+                  dst[16 * n + 8 + g] = o[i][n][2 + e];
+                }
+              }
             }
-          if (t == 0) { s_m[warp][h] = mx[i]; s_l[warp][h] = l; }
-        }
-        mx[i] = -INFINITY; sum[i] = 0.f;
-      }
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
-      __syncwarp();
-      if (lane == 0) mb_arrive(smem_u32(&s_merge[0]));
-      if (!mb_wait(smem_u32(&s_merge[0]), (uint32_t)(items & 1), &s_abort, a.wait_ns)) ok = false;
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      const int kind = (info.flags >> 12) & 3;
-      const float vs = a.v_scale ? __ldg(a.v_scale + kvh) : 1.f;
-      for (int i = tid; i < nh * DH; i += C::kWarps * 32) {
-        const int h = i / DH, e = i % DH;
-        float M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < C::kWarps; ++w) M = fmaxf(M, s_m[w][h]);
-        const float ref = M == -INFINITY ? 0.f : M;
-        float L = 0.f, O = 0.f;
-#pragma unroll
-        for (int w = 0; w < C::kWarps; ++w) {
-          const float l = s_l[w][h];
-          if (l != 0.f) {   // the warp had positions of the item
-            const float c = exp2_fast(s_m[w][h] - ref);
-            L += l * c;
-            O += s_o[((size_t)w * a.heads_per_tile + h) * DH + e] * c;
+            if (g == 0) { s_m[warp][h] = mx[i][e]; s_l[warp][h] = l; }
           }
+          mx[i][e] = -INFINITY; sum[i][e] = 0.f;
         }
-        const long long head = (long long)kvh * a.group + g0 + h;
-        if (kind == OUT_WHOLE) {
-          const float val = L == 0.f ? 0.f : O / L * vs;
-          const long long at = info.row * a.out_row_stride + head * a.out_head_stride + e;
-          if (X == D3_FP32) static_cast<float *>(a.out)[at] = val;
-          else if (X == D3_BF16) static_cast<bf16 *>(a.out)[at] = __float2bfloat16_rn(val);
-          else static_cast<__half *>(a.out)[at] = __float2half_rn(val);
-          if (e == 0 && a.lse) a.lse[(long long)info.row * a.hq + head] = L == 0.f ? -INFINITY : (M + (log2f(L) - (F16 ? 15.f : 0.f))) * kLn2;
-        } else {
-          const size_t part = (size_t)(2 * blockIdx.x + (kind == OUT_TAIL ? 1 : 0)) * 16 + h;
-          a.part_o[part * DH + e] = O;
-          if (e == 0) { a.part_ml[2 * part] = M; a.part_ml[2 * part + 1] = L; }
-        }
+#pragma unroll
+        for (int n = 0; n < KK; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
       }
+      if (warp == 0 && lane == 0) s_item = ItemInfo{info.row, info.tile, (info.flags >> 12) & 3, k + 1 == n_units};
       __syncwarp();
-      if (lane == 0) mb_arrive(smem_u32(&s_merge[1]));
+      if (lane == 0) mb_arrive(smem_u32(&s_sums_full));
       ++items;
     }
   }
   if (!ok && lane == 0 && a.status) *a.status = D3_ETIMEOUT;
 }
 
-// Joins the pieces of the item that starts in CTA blockIdx.x and goes on behind it; blockIdx.y: head of the tile.
-// Parts: this CTA's second slot, then the first slots of the CTAs that follow, in that order.  8 warps take parts
-// w, w + 8, ..; a lane has DH / 32 neighbouring dims.
+// Joins the pieces of the item that starts in CTA blockIdx.x and goes on behind it.  Parts: this CTA's second slot, then the
+// first slots of the CTAs that follow, in that order.  16 warps: 16 / heads of them share a head's parts, a lane
+// has DH / 32 neighbouring dims; the last sum runs over those warps in order.
+constexpr int kJoinWarps = 16;
 template <int DH, int X, bool F16>
-__global__ void __launch_bounds__(256) k_paged_join(const __grid_constant__ PagedAttnArgs a) {
+__global__ void __launch_bounds__(32 * kJoinWarps) k_paged_join(const __grid_constant__ PagedAttnArgs a) {
   constexpr int V = DH / 32;
-  __shared__ float s_o[8][DH], s_l[8], s_max[8];
+  __shared__ float s_o[kJoinWarps][DH], s_l[kJoinWarps], s_m[kJoinWarps];
   pdl_wait();
   pdl_trigger();
   const int4 job = a.join[blockIdx.x];
   if (job.x == 0) return;
-  const int parts = job.x, row = job.y, tile = job.z, h = blockIdx.y;
+  const int parts = job.x, row = job.y, tile = job.z;
   const int kvh = tile / a.tiles_per_head, g0 = (tile % a.tiles_per_head) * a.heads_per_tile;
-  if (h >= min(a.heads_per_tile, a.group - g0)) return;
+  const int nh = min(a.heads_per_tile, a.group - g0);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int share_of = kJoinWarps / nh, h = warp / share_of, first = warp % share_of;   // warps from nh * share_of on are idle
+  const bool busy = h < nh;
   auto part = [&](int k) -> size_t { return (size_t)(k == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + k)) * 16 + h; };
-  float M = -INFINITY;
-  for (int k = threadIdx.x; k < parts; k += 256) M = fmaxf(M, a.part_ml[2 * part(k)]);
-#pragma unroll
-  for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-  if (lane == 0) s_max[warp] = M;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 8; ++w) M = fmaxf(M, s_max[w]);
-  const float ref = M == -INFINITY ? 0.f : M;
-  float o[V], L = 0.f;
+  float M = -INFINITY, L = 0.f, o[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) o[e] = 0.f;
-#pragma unroll 4
-  for (int k = warp; k < parts; k += 8) {
-    const size_t p = part(k);
-    const float l = a.part_ml[2 * p + 1];
-    if (l != 0.f) {
-      const float c = exp2_fast(a.part_ml[2 * p] - ref);
-      L += l * c;
+  if (busy) {
+    // 32 parts at a time: their (m, l) by one load, then their sums, 8 loads in flight
+    for (int k0 = first; k0 < parts; k0 += 32 * share_of) {
+      const int mine = k0 + lane * share_of;
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (mine < parts) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * part(mine));
+      float m = ml.x;
 #pragma unroll
-      for (int e = 0; e < V; ++e) o[e] += a.part_o[p * DH + lane * V + e] * c;
+      for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+      m = fmaxf(m, M);
+      const float ref = m == -INFINITY ? 0.f : m;
+      const float keep = M == -INFINITY ? 0.f : exp2_fast(M - ref);
+      M = m;
+      const float c = ml.y != 0.f ? exp2_fast(ml.x - ref) : 0.f;
+      float l = ml.y != 0.f ? ml.y * c : 0.f;
+#pragma unroll
+      for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+      L = L * keep + l;
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[e] *= keep;
+      const unsigned there = __ballot_sync(0xffffffffu, ml.y != 0.f);
+      const int n = min(32, (parts - k0 + share_of - 1) / share_of);
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) {
+        const float ci = __shfl_sync(0xffffffffu, c, i);
+        const float *src = a.part_o + part(k0 + i * share_of) * DH + lane * V;
+        float x[V];
+        if constexpr (V == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+        else if constexpr (V == 2) { const float2 v = *reinterpret_cast<const float2 *>(src); x[0] = v.x; x[1] = v.y; }
+        else x[0] = *src;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] += (there >> i & 1) ? ci * x[e] : 0.f;
+      }
     }
   }
 #pragma unroll
   for (int e = 0; e < V; ++e) s_o[warp][lane * V + e] = o[e];
-  if (lane == 0) s_l[warp] = L;
+  if (lane == 0) { s_m[warp] = M; s_l[warp] = L; }
   __syncthreads();
-  const int e = threadIdx.x;
-  if (e >= DH) return;
-  float O = 0.f;
+  if (!busy || first != 0) return;
+  float top = -INFINITY;
+  for (int w = 0; w < share_of; ++w) top = fmaxf(top, s_m[warp + w]);
+  const float ref = top == -INFINITY ? 0.f : top;
   L = 0.f;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) { O += s_o[w][e]; L += s_l[w]; }
-  const float vs = a.v_scale ? __ldg(a.v_scale + kvh) : 1.f;
-  const float val = L == 0.f ? 0.f : O / L * vs;
+  for (int e = 0; e < V; ++e) o[e] = 0.f;
+  for (int w = 0; w < share_of; ++w) {
+    const float l = s_l[warp + w];
+    if (l == 0.f) continue;
+    const float c = exp2_fast(s_m[warp + w] - ref);
+    L += l * c;
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] += s_o[warp + w][lane * V + e] * c;
+  }
+  const float f = L == 0.f ? 0.f : (a.v_scale ? __ldg(a.v_scale + kvh) : 1.f) / L;
   const long long head = (long long)kvh * a.group + g0 + h;
-  const long long at = row * a.out_row_stride + head * a.out_head_stride + e;
-  if (X == D3_FP32) static_cast<float *>(a.out)[at] = val;
-  else if (X == D3_BF16) static_cast<bf16 *>(a.out)[at] = __float2bfloat16_rn(val);
-  else static_cast<__half *>(a.out)[at] = __float2half_rn(val);
-  if (e == 0 && a.lse) a.lse[(long long)row * a.hq + head] = L == 0.f ? -INFINITY : (M + (log2f(L) - (F16 ? 15.f : 0.f))) * kLn2;
+  const long long at = row * a.out_row_stride + head * a.out_head_stride + lane * V;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const float val = o[e] * f;
+    if (X == D3_FP32) static_cast<float *>(a.out)[at + e] = val;
+    else if (X == D3_BF16) static_cast<bf16 *>(a.out)[at + e] = __float2bfloat16_rn(val);
+    else static_cast<__half *>(a.out)[at + e] = __float2half_rn(val);
+  }
+  if (lane == 0 && a.lse) a.lse[(long long)row * a.hq + head] = L == 0.f ? -INFINITY : (top + (log2f(L) - (F16 ? 15.f : 0.f))) * kLn2;
 }
 
 // ---------------------------------------------------------------- launch
@@ -755,7 +836,7 @@ int launch(const d3_paged_kv &kv, PagedAttnArgs a, cudaStream_t st) {
   if (!encode_pool_map(&k, kv, kv.k_dev, rows) || !encode_pool_map(&v, kv, kv.v_dev, rows) ||
       !encode_pool_map(&k16, kv, kv.k_dev, kPiece) || !encode_pool_map(&v16, kv, kv.v_dev, kPiece))
     return -1;
-  const int merge = C::kWarps * a.heads_per_tile * DH * (int)sizeof(float);
+  const int merge = C::kWarps * a.heads_per_tile * C::kHeadFloats * (int)sizeof(float);
   int stages = (kSmemMost - 1024 - merge) / (C::kStageBytes + C::kQBytes);
   if (stages > kMaxStages) stages = kMaxStages;
   if (stages < 2) return -1;
@@ -777,7 +858,7 @@ int launch(const d3_paged_kv &kv, PagedAttnArgs a, cudaStream_t st) {
     return -1;
   // a table of at most one unit's positions cannot be cut
   if (((long long)a.table_width << a.page_shift) > C::kUnit)
-    if (launch_pdl(k_paged_join<DH, X, C::kF16>, dim3(sms[dev], a.heads_per_tile), dim3(256), 0, st, a) != cudaSuccess) return -1;
+    if (launch_pdl(k_paged_join<DH, X, C::kF16>, dim3(sms[dev]), dim3(32 * kJoinWarps), 0, st, a) != cudaSuccess) return -1;
   return 0;
 }
 
