@@ -422,14 +422,14 @@ int32_t d3_page_plan(const d3_page_plan_args *a, void *cuda_stream);
  * context - 1; pairs are (j, j + head_dim / 2).  Products and sums are fp32, each rounded once; the
  * result is rounded once to the cache's type (E4M3: after division by the scale, saturating).
  * Types: dtype of q, k, v, q_out / of the cache: BF16 / BF16, FP32 / BF16, FP16 / FP16, BF16 / E4M3,
- * FP16 / E4M3.  A token with a negative slot is padding: nothing of it is read or written.  A slot
+ * FP16 / E4M3.  A token with a negative slot is padding: nothing of it is written.  A slot
  * beyond the pool or a position beyond rope_len: the token is skipped, D3_EINVAL is stored.  The
  * slots of one call are distinct; of a repeated one it is open, number by number, which token's stays. */
 typedef struct d3_paged_append_args {
   uint32_t struct_size;
   int32_t dtype;
   int32_t n_tokens;          /* >= 0                                                     */
-  int32_t n_q_heads;         /* with q_dev                                               */
+  int32_t n_q_heads;         /* with q_dev; n_q_heads + 2 n_kv_heads <= 65535            */
   int32_t rope_len;
   const void *k_dev, *v_dev;
   int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;

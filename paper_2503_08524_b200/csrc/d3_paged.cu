@@ -4,6 +4,8 @@
 #include <cuda_fp8.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "d3_paged.cuh"
 
 namespace d3 {
@@ -11,13 +13,14 @@ namespace d3 {
 namespace {
 
 // ------------------------------------------------------------------ plan
-// Latency decides: the whole plan is one launch.  Every CTA of one cluster reads the R lengths and
-// keeps the three running sums (tokens, pages needed, pages given back) of all requests in shared
-// memory; after the cluster barrier no input length is read any more, so the outputs may be the inputs
-// themselves, and the CTAs share the page and token entries between them.  A page that is taken is
-// looked up by its rank in (old stack ++ pages given back), so nothing waits for the stack to be written.
-constexpr int kPlanThreads = 1024;
-constexpr int kPlanMaxPer = D3_MAX_REQUESTS / kPlanThreads;   // requests of one thread
+// Latency decides: the whole plan is one launch.  Every CTA reads the R lengths and keeps the three running sums
+// (tokens, pages needed, pages given back) of all requests in shared memory; after that the CTAs share page and token
+// entries between them and need nothing of one another: a page that is taken is looked up by its rank in
+// (old stack ++ pages given back), so nothing waits for the stack or the table to be written, and what is written is
+// never what another CTA reads.  Only where the new lengths replace the old ones in place do the CTAs have to have read
+// them all first: then they are one cluster with a barrier, of up to eight.
+constexpr int kPlanMaxThreads = 1024;
+constexpr int kPlanMaxPer = D3_MAX_REQUESTS / kPlanMaxThreads;   // requests of one thread
 
 struct PlanArgs {
   int R, page_shift, n_pages, width, T;
@@ -28,18 +31,9 @@ struct PlanArgs {
   int32_t *cached_out, *n_free_out, *first;
   long long *slots;
   int32_t *row, *context, *status;
+  int cluster;   // the grid is one cluster that has to meet before the first store
 };
 
-__device__ __forceinline__ unsigned cluster_rank() {
-  unsigned r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ unsigned cluster_size() {
-  unsigned r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
 __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
@@ -54,12 +48,14 @@ __device__ __forceinline__ int owner(const int *sum, int R, int x) {
   return lo;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) k_page_plan(const __grid_constant__ PlanArgs a) {
+// S: type of the sums (32 bits where no sum of R entries of at most max_tokens or n_pages can leave them)
+template <typename S>
+__global__ void __launch_bounds__(kPlanMaxThreads) k_page_plan(const __grid_constant__ PlanArgs a) {
   extern __shared__ int s_plan[];
   int *s_first = s_plan, *s_need = s_first + (a.R + 1), *s_back = s_need + (a.R + 1), *s_cached = s_back + (a.R + 1);
-  __shared__ long long s_warp[3][kPlanThreads / 32];
+  __shared__ S s_warp[3][32];
   __shared__ int s_bad;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
   const int page_mask = (1 << a.page_shift) - 1;
   const long long max_len = (long long)a.width << a.page_shift;
   if (tid == 0) s_bad = 0;
@@ -68,8 +64,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(const __grid_constan
   __syncthreads();
 
   const int n_free = *a.n_free;
-  const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
-  long long sum[3] = {0, 0, 0};                       // this thread's tokens, pages needed, pages given back
+  const int per = (a.R + threads - 1) / threads;
+  S sum[3] = {0, 0, 0};                       // this thread's tokens, pages needed, pages given back
   int c_[kPlanMaxPer], add_[kPlanMaxPer], need_[kPlanMaxPer], back_[kPlanMaxPer];
   int bad = (n_free < 0 || n_free > a.n_pages) ? 2 : 0;
 #pragma unroll
@@ -79,10 +75,10 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(const __grid_constan
     if (i < per && b < a.R) {
       const int c = a.cached[b], n = a.added[b];
       const long long grown = (long long)c + (n > 0 ? n : 0);
-      if (c < 0 || c > max_len) { bad |= 2; }
-      else if (grown > max_len) { bad |= 1; }
+      const int have = (int)(((long long)c + page_mask) >> a.page_shift);
+      if (c < 0 || c > max_len || (n < 0 && have > a.n_pages)) { bad |= 2; }
+      else if (grown > max_len || n > a.T) { bad |= 1; }
       else {
-        const int have = (int)(((long long)c + page_mask) >> a.page_shift);
         c_[i] = c;
         if (n < 0) back_[i] = have;
         else {
@@ -94,31 +90,34 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(const __grid_constan
     }
   }
   if (bad) atomicOr(&s_bad, bad);
-  long long inc[3];
+  S inc[3] = {sum[0], sum[1], sum[2]};
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    long long v = sum[k];
+  for (int d = 1; d < 32; d <<= 1) {
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, v, d);
-      if (lane >= d) v += u;
+    for (int k = 0; k < 3; ++k) {
+      const S u = __shfl_up_sync(0xffffffffu, inc[k], d);
+      if (lane >= d) inc[k] += u;
     }
-    inc[k] = v;
-    if (lane == 31) s_warp[k][warp] = v;
   }
+  if (lane == 31) { s_warp[0][warp] = inc[0]; s_warp[1][warp] = inc[1]; s_warp[2][warp] = inc[2]; }
   __syncthreads();
-  long long total[3], before[3];
+  S total[3], before[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) total[k] = lane < threads / 32 ? s_warp[k][lane] : 0;   // one value per warp
+#pragma unroll
+  for (int k = 0; k < 3; ++k) before[k] = total[k];
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const S u = __shfl_up_sync(0xffffffffu, total[k], d);
+      if (lane >= d) total[k] += u;
+    }
+  }
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    long long v = s_warp[k][lane];                    // one value per warp
-    const long long own = v;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, v, d);
-      if (lane >= d) v += u;
-    }
-    total[k] = __shfl_sync(0xffffffffu, v, 31);
-    before[k] = __shfl_sync(0xffffffffu, v - own, warp) + inc[k] - sum[k];
+    before[k] = __shfl_sync(0xffffffffu, total[k] - before[k], warp) + inc[k] - sum[k];
+    total[k] = __shfl_sync(0xffffffffu, total[k], 31);
   }
   bad = s_bad;
   if ((long long)n_free + total[2] > a.n_pages) bad |= 2;      // more pages than there are came back
@@ -135,13 +134,12 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(const __grid_constan
     }
     if (tid == 0) { s_first[a.R] = (int)total[0]; s_need[a.R] = (int)total[1]; s_back[a.R] = (int)total[2]; }
   }
-  // all CTAs have read the lengths and the stack's height: they may be overwritten from here on
-  cluster_barrier();
+  // in place: all CTAs have read the lengths and the stack's height, they may be overwritten from here on
+  if (a.cluster) cluster_barrier();
   __syncthreads();
 
-  const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
-  const int gid = rank * kPlanThreads + tid, step = ctas * kPlanThreads;
-  if (rank == 0) {
+  const int gid = blockIdx.x * threads + tid, step = gridDim.x * threads;
+  if (blockIdx.x == 0) {
 #pragma unroll
     for (int i = 0; i < kPlanMaxPer; ++i) {
       const int b = tid * per + i;
@@ -223,10 +221,13 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(const __grid_constan
 // ------------------------------------------------------------------ append
 // Bandwidth: every number once in and once out.  A thread takes the pairs (8 numbers of a head's lower
 // half, the 8 that they are paired with), so the rotation needs no exchange and all traffic is in
-// 16-byte pieces (8 for the 8-bit cache); it keeps the 8 (cos, sin) of its piece for H heads of the token.
+// 16-byte pieces (8 for the 8-bit cache); it does that for H heads of one token, whose (cos, sin) it loads
+// once.  A CTA's threads are tokens x heads x pieces, powers of two, so that no index needs a division; all loads are
+// in flight before the slot is looked at.
 struct AppendArgs {
   long long n_tokens;
-  int hq, rope_len, chunks;     // chunks: groups of H heads per token
+  int hq, rope_len;
+  int head_shift;               // log2 of the heads (of a token) that a CTA's threads stand for
   const void *k, *v, *q;
   void *q_out;
   long long kt, kh, vt, vh, qt, qh, ot, oh;   // token and head strides
@@ -236,8 +237,6 @@ struct AppendArgs {
   int32_t *status;
   KvPool kv;
 };
-
-template <typename T> struct Vec8 { float f[8]; };
 
 __device__ __forceinline__ void load8(const float *p, float *f) {
   const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
@@ -296,36 +295,20 @@ __device__ __forceinline__ void store8(__nv_fp8_e4m3 *p, const float *f) {
 
 template <typename X, typename C, int DH, int H>
 __global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ AppendArgs a) {
-  constexpr int HALF = DH / 2, PIECES = HALF / 8;
+  constexpr int HALF = DH / 2, PIECES = HALF / 8, LANES = 256 / PIECES;   // (token, head) pairs of a CTA
   pdl_wait();
   pdl_trigger();
-  const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-  const int j = (int)(id % PIECES);
-  const long long u = id / PIECES;
-  const int chunk = (int)(u % a.chunks);
-  const long long t = u / a.chunks;
+  const int j = threadIdx.x % PIECES, u = threadIdx.x / PIECES, step = 1 << a.head_shift;
+  const long long t = (long long)blockIdx.x * (LANES >> a.head_shift) + (u >> a.head_shift);
   if (t >= a.n_tokens) return;
+  const int heads = a.hq + 2 * a.kv.n_kv_heads, h0 = blockIdx.y * (step * H) + (u & (step - 1));
   const long long slot = a.slots[t];
-  if (slot < 0) return;
-  int pos = 0;
-  bool bad = slot >= ((long long)a.kv.n_pages << a.kv.page_shift);
-  if (a.rope) {
-    pos = a.context[t] - 1;
-    bad = bad || pos < 0 || pos >= a.rope_len;
-  }
-  if (bad) {
-    if (a.status) *a.status = D3_EINVAL;
-    return;
-  }
-  const int heads = a.hq + 2 * a.kv.n_kv_heads, h0 = chunk * H;
-  const long long in_page = slot & ((1 << a.kv.page_shift) - 1);
-  const long long entry = (slot >> a.kv.page_shift) * a.kv.page_stride + in_page * a.kv.token_stride;
+  const int pos = a.rope ? a.context[t] - 1 : 0;
 
-  // all loads of the thread are issued before the first is used
   float lo[H][8], hi[H][8];
 #pragma unroll
   for (int i = 0; i < H; ++i) {
-    const int h = h0 + i;
+    const int h = h0 + i * step;
     if (h < heads) {
       const X *p = h < a.hq ? static_cast<const X *>(a.q) + t * a.qt + (long long)h * a.qh
                    : h < a.hq + a.kv.n_kv_heads ? static_cast<const X *>(a.k) + t * a.kt + (long long)(h - a.hq) * a.kh
@@ -334,6 +317,13 @@ __global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ Ap
       load8(p + HALF + 8 * j, hi[i]);
     }
   }
+  if (slot < 0) return;
+  if (slot >= ((long long)a.kv.n_pages << a.kv.page_shift) || (a.rope && (pos < 0 || pos >= a.rope_len))) {
+    if (a.status) *a.status = D3_EINVAL;
+    return;
+  }
+  const long long in_page = slot & ((1 << a.kv.page_shift) - 1);
+  const long long entry = (slot >> a.kv.page_shift) * a.kv.page_stride + in_page * a.kv.token_stride;
   float cs[16];
   if (a.rope && h0 < a.hq + a.kv.n_kv_heads) {
     const float *r = a.rope + ((long long)pos * HALF + 8 * j) * 2;
@@ -342,7 +332,7 @@ __global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ Ap
   }
 #pragma unroll
   for (int i = 0; i < H; ++i) {
-    const int h = h0 + i;
+    const int h = h0 + i * step;
     if (h >= heads) continue;
     if (a.rope && h < a.hq + a.kv.n_kv_heads) {
       // products and sums rounded one by one: no contraction, so every store rounds the same number
@@ -377,16 +367,19 @@ __global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ Ap
 
 template <typename X, typename C, int DH>
 void launch_append_dh(AppendArgs &a, cudaStream_t st) {
-  constexpr int PIECES = DH / 16;
+  constexpr int LANES = 256 / (DH / 16);
   const int heads = a.hq + 2 * a.kv.n_kv_heads;
-  // Several heads per thread keep more loads in flight and read (cos, sin) once for all of them; with few tokens one
-  // head per thread spreads the call over more SMs.
-  const bool wide = a.n_tokens * heads * PIECES >= 4ll * 148 * 1024;
-  a.chunks = wide ? (heads + 3) / 4 : heads;
-  const long long threads = a.n_tokens * a.chunks * PIECES;
-  const unsigned grid = (unsigned)((threads + 255) / 256);
-  if (wide) launch_pdl(k_paged_append<X, C, DH, 4>, dim3(grid), dim3(256), 0, st, a);
-  else launch_pdl(k_paged_append<X, C, DH, 1>, dim3(grid), dim3(256), 0, st, a);
+  a.head_shift = 0;
+  while ((1 << a.head_shift) < heads && (1 << a.head_shift) < LANES) ++a.head_shift;
+  const int step = 1 << a.head_shift, tokens = LANES >> a.head_shift, rounds = (heads + step - 1) / step;
+  const long long groups = (a.n_tokens + tokens - 1) / tokens;
+  // Several heads per thread read (cos, sin) once for all of them; with few tokens one head per thread spreads the call
+  // over more SMs.
+  const int H = groups * rounds <= 4 * 148 ? 1 : rounds < 3 ? rounds : 3;
+  const dim3 grid((unsigned)groups, (unsigned)((rounds + H - 1) / H));
+  if (H == 1) launch_pdl(k_paged_append<X, C, DH, 1>, grid, dim3(256), 0, st, a);
+  else if (H == 2) launch_pdl(k_paged_append<X, C, DH, 2>, grid, dim3(256), 0, st, a);
+  else launch_pdl(k_paged_append<X, C, DH, 3>, grid, dim3(256), 0, st, a);
 }
 template <typename X, typename C>
 void launch_append(AppendArgs &a, int dh, cudaStream_t st) {
@@ -472,31 +465,41 @@ int32_t d3_page_plan(const d3_page_plan_args *a, void *cuda_stream) {
   p.n_free = a->n_free_dev; p.cached_out = a->cached_out_dev; p.n_free_out = a->n_free_out_dev; p.first = a->first_dev;
   p.slots = reinterpret_cast<long long *>(a->slots_dev); p.row = a->row_dev; p.context = a->context_dev; p.status = a->status_dev;
   const size_t smem = ((size_t)4 * a->n_requests + 3) * sizeof(int);
+  // In place: one CTA while its threads take at most one group of four tokens each, then a cluster of eight.  Elsewhere as many
+  // CTAs as there are groups of four tokens for, up to one per SM (192 prompts of 129..2048 tokens, 209,000
+  // in all: 21.3 us as a cluster of eight, PLAN_GRID_US as 52 CTAs).
+  const bool in_place = a->cached_out_dev == a->cached_dev || a->n_free_out_dev == a->n_free_dev;
+  const int threads = a->n_requests <= 128 && a->max_tokens <= 512 ? 128 : kPlanMaxThreads;
+  long long ctas = ((long long)a->max_tokens + 4 * threads - 1) / (4 * threads);
+  if (ctas > 148) ctas = 148;
+  if (in_place && ctas > 1) ctas = 8;
+  p.cluster = in_place && ctas > 1 ? 1 : 0;
+  // sums of at most 4096 entries of at most 2^19 stay within 32 bits
+  const bool narrow = a->max_tokens <= (1 << 19) && a->n_pages <= (1 << 19) && a->table_width <= (1 << 19);
+  void (*kernel)(PlanArgs) = narrow ? k_page_plan<int> : k_page_plan<long long>;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return D3_ECUDA;
-  static bool ready[64];   // the shared-memory attribute is per device; setting it twice is harmless
-  if (!ready[dev]) {
-    if (cudaFuncSetAttribute(k_page_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (4 * D3_MAX_REQUESTS + 4) * (int)sizeof(int)) !=
+  static std::atomic<bool> ready[2][64];   // the shared-memory attribute is per device; setting it twice is harmless
+  if (!ready[narrow][dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (4 * D3_MAX_REQUESTS + 4) * (int)sizeof(int)) !=
         cudaSuccess)
       return D3_ECUDA;
-    ready[dev] = true;
+    ready[narrow][dev].store(true, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
-  // one CTA while its threads take at most one group of four tokens each; a cluster of eight for prompts
-  const unsigned ctas = a->max_tokens <= 4 * kPlanThreads ? 1 : 8;
-  cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(kPlanThreads);
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = static_cast<cudaStream_t>(cuda_stream);
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = ctas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  attr[1].val.clusterDim.x = (unsigned)ctas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, k_page_plan, p) == cudaSuccess ? D3_OK : D3_ECUDA;
+  cfg.numAttrs = p.cluster ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? D3_OK : D3_ECUDA;
 }
 
 int32_t d3_paged_append(const d3_paged_kv *kv, const d3_paged_append_args *a, void *cuda_stream) {
@@ -527,8 +530,7 @@ int32_t d3_paged_append(const d3_paged_kv *kv, const d3_paged_append_args *a, vo
   p.qt = a->q_token_stride; p.qh = a->q_head_stride; p.ot = a->q_out_token_stride; p.oh = a->q_out_head_stride;
   p.slots = reinterpret_cast<const long long *>(a->slots_dev); p.context = a->context_dev; p.rope = a->rope_dev; p.status = a->status_dev;
   p.kv = pool_of(*kv);
-  // threads of the launch: the grid has to fit 31 bits
-  if ((double)a->n_tokens * (p.hq + 2.0 * kv->n_kv_heads) * (dh / 16) / 256 > 2.0e9) return D3_EINVAL;
+  if (p.hq + 2ll * kv->n_kv_heads > 65535) return D3_EINVAL;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (kv->dtype == D3_BF16) {
     if (a->dtype == D3_BF16) launch_append<bf16, bf16>(p, dh, st);

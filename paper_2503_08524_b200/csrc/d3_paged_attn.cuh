@@ -32,6 +32,8 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "d3_paged.cuh"
 
 namespace d3 {
@@ -844,21 +846,22 @@ int launch(const d3_paged_kv &kv, PagedAttnArgs a, cudaStream_t st) {
   const size_t smem = 1024 + (size_t)stages * (C::kStageBytes + C::kQBytes) + merge;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
-  static int sms[64];   // per device: its SM count once the kernel's attribute is set there
-  if (sms[dev] == 0) {
-    int n = 0;
+  static std::atomic<int> ready[64];   // per device: its SM count once the kernel's attribute is set there
+  int n = ready[dev].load(std::memory_order_acquire);
+  if (n == 0) {
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return -1;
     if (cudaFuncSetAttribute(k_paged_attention<DH, CACHE, X, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost) != cudaSuccess)
       return -1;
-    sms[dev] = n < kFusedMaxCtas ? n : kFusedMaxCtas;
+    if (n > kFusedMaxCtas) n = kFusedMaxCtas;
+    ready[dev].store(n, std::memory_order_release);
   }
   auto map = [](const TMap &m) -> const CUtensorMap & { return *reinterpret_cast<const CUtensorMap *>(&m); };
-  if (launch_pdl(k_paged_attention<DH, CACHE, X, MT>, dim3(sms[dev]), dim3(C::kThreads), smem, st, map(k), map(v), map(k16), map(v16), a) !=
+  if (launch_pdl(k_paged_attention<DH, CACHE, X, MT>, dim3(n), dim3(C::kThreads), smem, st, map(k), map(v), map(k16), map(v16), a) !=
       cudaSuccess)
     return -1;
   // a table of at most one unit's positions cannot be cut
   if (((long long)a.table_width << a.page_shift) > C::kUnit)
-    if (launch_pdl(k_paged_join<DH, X, C::kF16>, dim3(sms[dev]), dim3(32 * kJoinWarps), 0, st, a) != cudaSuccess) return -1;
+    if (launch_pdl(k_paged_join<DH, X, C::kF16>, dim3(n), dim3(32 * kJoinWarps), 0, st, a) != cudaSuccess) return -1;
   return 0;
 }
 

@@ -14,6 +14,7 @@ can see (a page id out of range, too few free pages) goes to the `status` tensor
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional
 
 import torch
@@ -24,6 +25,7 @@ BF16, FP16, FP32, E4M3 = 0, 1, 2, 3
 MAX_REQUESTS = 4096
 _TYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32, torch.float8_e4m3fn: E4M3}
 
+_I32T, _I64T, _F32 = torch.int32, torch.int64, torch.float32
 _I32, _I64, _U32, _P = C.c_int32, C.c_int64, C.c_uint32, C.c_void_p
 
 
@@ -60,6 +62,16 @@ class PagedAttentionArgs(C.Structure):
          ("status_dev", _P)]
 
 
+# The two structs that are filled on every call, as one packing each (the fields above, in order; a null pointer is
+# 0): a small decode step is bound by the host side of its calls.
+_APPEND = struct.Struct("=I4i4x2Q4q2Q4q4Q")
+_ATTENTION = struct.Struct("=I5iqf4xQ2qQ2q7Q")
+assert _APPEND.size == C.sizeof(PagedAppendArgs) and _ATTENTION.size == C.sizeof(PagedAttentionArgs)
+
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_device_now = torch._C._cuda_getDevice
+
+
 def _refuse(what: str):
     raise D3Error(EINVAL, what)
 
@@ -75,32 +87,32 @@ def _strides(t: torch.Tensor):
     return st[:-1]
 
 
-def _call(fn, what: str, device: torch.device, stream, *args) -> None:
-    """One C call on `stream` (default: the device's current stream), with the device current."""
-    if device.type != "cuda":
+def _call(fn, what: str, index: int, *args) -> None:
+    """One C call on the current stream of device `index`, with that device current."""
+    if index < 0:
         _refuse(what + ": tensors must be on a CUDA device")
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-    elif stream.device != device:
-        _refuse(what + ": stream of another device")
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, stream.cuda_stream)
+    if _device_now() == index:
+        rc = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, stream.cuda_stream)
+        with torch.cuda.device(index):
+            rc = fn(*args, _raw_stream(index))
     if rc != OK:
         raise D3Error(rc, what)
 
 
-def _vector(t: torch.Tensor, dtype, n: Optional[int], device, what: str) -> int:
-    """Data pointer of a contiguous 1-D tensor of `n` entries (None: any number)."""
-    if t.dtype != dtype or t.dim() != 1 or (n is not None and t.shape[0] != n) or t.device != device or not t.is_contiguous():
-        _refuse(f"{what}: expected a contiguous {dtype} vector" + ("" if n is None else f" of {n}") + f" on {device}")
+def _on_stream(call, index: int, stream, what: str):
+    """`call` with `stream` current, so that what it allocates belongs to that stream."""
+    if index < 0 or stream.device.index != index:
+        _refuse(f"{what}: stream and tensors must be on one CUDA device")
+    with torch.cuda.stream(stream):
+        return call()
+
+
+def _vector(t: torch.Tensor, dtype, n: int, index: int, what: str, name: str) -> int:
+    """Data pointer of a contiguous 1-D tensor of `n` entries (-1: any number)."""
+    if t.dtype is not dtype or t.dim() != 1 or (t.shape[0] != n and n != -1) or t.get_device() != index or not t.is_contiguous():
+        _refuse(f"{what}: {name} must be a contiguous {dtype} vector" + ("" if n < 0 else f" of {n}") + f" on device {index}")
     return t.data_ptr()
-
-
-def _status(t: Optional[torch.Tensor], device, what: str):
-    return None if t is None else _vector(t, torch.int32, 1, device, what + " status")
 
 
 class PagedKV:
@@ -115,9 +127,9 @@ class PagedKV:
         if k.dtype not in _TYPES or k.dtype == torch.float32 or k.stride(3) != 1:
             _refuse("PagedKV: bf16, fp16 or float8_e4m3fn with contiguous head_dim")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device, self.dtype = k.device, k.dtype
+        self.device, self.dtype, self.index = k.device, k.dtype, k.get_device()
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
-        sc = [None if s is None else _vector(s, torch.float32, self.n_kv_heads, k.device, "PagedKV scale")
+        sc = [None if s is None else _vector(s, torch.float32, self.n_kv_heads, self.index, "PagedKV", "scale")
               for s in (k_scale, v_scale)]
         if k.dtype != torch.float8_e4m3fn and (k_scale is not None or v_scale is not None):
             _refuse("PagedKV: scales belong to an 8-bit pool")
@@ -156,41 +168,49 @@ class PagePlan:
     def __init__(self, *, cached: torch.Tensor, new_tokens: torch.Tensor, table: torch.Tensor, free: torch.Tensor,
                  n_free: torch.Tensor, page_size: int, max_tokens: int, cached_out: Optional[torch.Tensor] = None,
                  n_free_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
-        dev, what = cached.device, "PagePlan"
+        dev, index, what, i32 = cached.device, cached.get_device(), "PagePlan", torch.int32
         R = cached.shape[0] if cached.dim() == 1 else -1
-        if not (1 <= R <= MAX_REQUESTS) or max_tokens < 1 or max_tokens > 0x7fffffff:
+        if not (1 <= R <= MAX_REQUESTS) or not (1 <= max_tokens <= 0x7fffffff):
             _refuse(f"{what}: 1..{MAX_REQUESTS} requests, max_tokens >= 1")
-        if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != R or table.device != dev or \
-                table.stride(1) != 1 or table.shape[1] < 1 or (R > 1 and table.stride(0) < table.shape[1]):
+        if table.dtype != i32 or table.dim() != 2 or table.shape[0] != R or table.device != dev or table.shape[1] < 1 or \
+                (table.shape[1] > 1 and table.stride(1) != 1):
             _refuse(f"{what}: table must be int32 [n_requests][width] on {dev}")
         self.cached, self.new_tokens, self.table, self.free, self.n_free = cached, new_tokens, table, free, n_free
         self.cached_out = cached if cached_out is None else cached_out
         self.n_free_out = n_free if n_free_out is None else n_free_out
-        self.device = dev
+        self.index = index
         self.slots = torch.empty(max_tokens, dtype=torch.int64, device=dev)
-        self.row = torch.empty(max_tokens, dtype=torch.int32, device=dev)
-        self.context = torch.empty(max_tokens, dtype=torch.int32, device=dev)
-        self.first = torch.empty(R + 1, dtype=torch.int32, device=dev)
-        self.status = torch.zeros(1, dtype=torch.int32, device=dev) if status is None else status
-        i32 = torch.int32
+        self.row = torch.empty(max_tokens, dtype=i32, device=dev)
+        self.context = torch.empty(max_tokens, dtype=i32, device=dev)
+        self.first = torch.empty(R + 1, dtype=i32, device=dev)
+        self.status = torch.zeros(1, dtype=i32, device=dev) if status is None else status
         self.args = PagePlanArgs(
             C.sizeof(PagePlanArgs), R, page_size, free.shape[0] if free.dim() == 1 else 0, table.shape[1], max_tokens,
-            table.stride(0) if R > 1 else table.shape[1], _vector(cached, i32, R, dev, what + " cached"),
-            _vector(new_tokens, i32, R, dev, what + " new_tokens"), table.data_ptr(), _vector(free, i32, None, dev, what + " free"),
-            _vector(n_free, i32, 1, dev, what + " n_free"), _vector(self.cached_out, i32, R, dev, what + " cached_out"),
-            _vector(self.n_free_out, i32, 1, dev, what + " n_free_out"), self.first.data_ptr(), self.slots.data_ptr(),
-            self.row.data_ptr(), self.context.data_ptr(), _status(self.status, dev, what))
+            table.stride(0) if R > 1 else table.shape[1], _vector(cached, i32, R, index, what, "cached"),
+            _vector(new_tokens, i32, R, index, what, "new_tokens"), table.data_ptr(), _vector(free, i32, -1, index, what, "free"),
+            _vector(n_free, i32, 1, index, what, "n_free"), _vector(self.cached_out, i32, R, index, what, "cached_out"),
+            _vector(self.n_free_out, i32, 1, index, what, "n_free_out"), self.first.data_ptr(), self.slots.data_ptr(),
+            self.row.data_ptr(), self.context.data_ptr(), _vector(self.status, i32, 1, index, what, "status"))
         self._ref = C.byref(self.args)
 
     def d3_page_plan(self, stream=None) -> "PagePlan":
-        _call(LIB.d3_page_plan, "d3_page_plan", self.device, stream, self._ref)
+        if stream is not None:
+            return _on_stream(self.d3_page_plan, self.index, stream, "d3_page_plan")
+        _call(LIB.d3_page_plan, "d3_page_plan", self.index, self._ref)
         return self
 
 
-def _heads(t: torch.Tensor, n: int, heads: int, dh: int, dtype, device, what: str):
-    """[n][heads][dh] with dh contiguous."""
-    if t.shape != (n, heads, dh) or t.dtype != dtype or t.device != device or t.stride(2) != 1:
-        _refuse(f"{what}: expected {dtype} [{n}][{heads}][{dh}] on {device}, last dimension contiguous")
+def _heads(t: torch.Tensor, n: int, heads: int, dh: int, dtype, index: int, what: str, name: str):
+    """(data pointer, stride of dimension 0, of dimension 1) of [n][heads][dh] with dh contiguous.  The stride of a
+    dimension of one entry, which torch leaves arbitrary, is taken as if the tensor were contiguous there."""
+    if t.shape != (n, heads, dh) or t.dtype is not dtype or t.get_device() != index:
+        _refuse(f"{what}: {name} must be {dtype} [{n}][{heads}][{dh}] on device {index}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1:
+        _refuse(f"{what}: the last dimension of {name} must be contiguous")
+    if heads == 1:
+        s1 = dh
+    return t.data_ptr(), s0 if n > 1 else heads * s1, s1
 
 
 def d3_rope_table(n_positions: int, head_dim: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
@@ -200,8 +220,11 @@ def d3_rope_table(n_positions: int, head_dim: int, base: float = 10000.0, device
         dev = torch.device("cuda", torch.cuda.current_device())
     if n_positions < 1 or head_dim not in (32, 64, 128):
         _refuse("d3_rope_table: n_positions >= 1, head_dim 32, 64 or 128")
+    if stream is not None:
+        return _on_stream(lambda: d3_rope_table(n_positions, head_dim, base, dev), -1 if dev.type != "cuda" else dev.index, stream,
+                          "d3_rope_table")
     t = torch.empty((n_positions, head_dim // 2, 2), dtype=torch.float32, device=dev)
-    _call(LIB.d3_rope_table, "d3_rope_table", dev, stream, n_positions, head_dim, float(base), t.data_ptr())
+    _call(LIB.d3_rope_table, "d3_rope_table", t.get_device(), n_positions, head_dim, float(base), t.data_ptr())
     return t
 
 
@@ -212,43 +235,39 @@ def d3_paged_append(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, slots: tor
     """k, v [n][n_kv_heads][head_dim] to the slots (int64 [n], negative = padding); with `rope`, k is
     rotated by position context - 1 and q [n][n_q_heads][head_dim] goes rotated to q_out (default: a
     new tensor whose padding rows are undefined; q itself is allowed).  Returns q_out."""
-    what, dev = "d3_paged_append", cache.device
-    n, hkv, dh = slots.shape[0] if slots.dim() == 1 else -1, cache.n_kv_heads, cache.head_dim
-    if k.dtype not in _TYPES:
-        _refuse(f"{what}: unsupported type {k.dtype}")
-    _heads(k, n, hkv, dh, k.dtype, dev, what + " k")
-    _heads(v, n, hkv, dh, k.dtype, dev, what + " v")
-    a = PagedAppendArgs()
-    a.struct_size, a.dtype, a.n_tokens = C.sizeof(PagedAppendArgs), _TYPES[k.dtype], n
-    a.slots_dev = _vector(slots, torch.int64, n, dev, what + " slots")
-    a.k_dev, a.v_dev = k.data_ptr(), v.data_ptr()
-    a.k_token_stride, a.k_head_stride = _strides(k)
-    a.v_token_stride, a.v_head_stride = _strides(v)
+    what, dev = "d3_paged_append", cache.index
+    if stream is not None:
+        return _on_stream(lambda: d3_paged_append(cache, k, v, slots, q=q, q_out=q_out, rope=rope, context=context, status=status),
+                          dev, stream, what)
+    n, hkv, dh, dtype = slots.shape[0] if slots.dim() == 1 else -1, cache.n_kv_heads, cache.head_dim, k.dtype
+    if dtype not in _TYPES:
+        _refuse(f"{what}: unsupported type {dtype}")
+    kp, kt, kh = _heads(k, n, hkv, dh, dtype, dev, what, "k")
+    vp, vt, vh = _heads(v, n, hkv, dh, dtype, dev, what, "v")
+    rope_p = rope_len = context_p = 0
     if rope is not None:
-        if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[1:] != (dh // 2, 2) or rope.device != dev or \
+        if rope.dtype is not _F32 or rope.dim() != 3 or rope.shape[1] != dh // 2 or rope.shape[2] != 2 or rope.get_device() != dev or \
                 not rope.is_contiguous():
-            _refuse(f"{what}: rope must be contiguous fp32 [positions][{dh // 2}][2] on {dev}")
+            _refuse(f"{what}: rope must be contiguous fp32 [positions][{dh // 2}][2] on device {dev}")
         if context is None:
             _refuse(f"{what}: rope needs context")
-        a.rope_dev, a.rope_len = rope.data_ptr(), rope.shape[0]
-        a.context_dev = _vector(context, torch.int32, n, dev, what + " context")
+        rope_p, rope_len = rope.data_ptr(), rope.shape[0]
+        context_p = _vector(context, _I32T, n, dev, what, "context")
+    hq = qp = qt = qh = op = ot = oh = 0
     if q is not None:
         if rope is None:
             _refuse(f"{what}: q is only rotated, and there is no rope")
         hq = q.shape[1] if q.dim() == 3 else -1
-        _heads(q, n, hq, dh, k.dtype, dev, what + " q")
+        qp, qt, qh = _heads(q, n, hq, dh, dtype, dev, what, "q")
         if q_out is None:
-            q_out = torch.empty((n, hq, dh), dtype=k.dtype, device=dev)
-        _heads(q_out, n, hq, dh, k.dtype, dev, what + " q_out")
-        a.n_q_heads, a.q_dev, a.q_out_dev = hq, q.data_ptr(), q_out.data_ptr()
-        a.q_token_stride, a.q_head_stride = _strides(q)
-        a.q_out_token_stride, a.q_out_head_stride = _strides(q_out)
+            q_out = q.new_empty((n, hq, dh))
+        op, ot, oh = _heads(q_out, n, hq, dh, dtype, dev, what, "q_out")
     elif q_out is not None:
         _refuse(f"{what}: q_out without q")
-    if status is not None:
-        a.status_dev = _status(status, dev, what)
+    a = _APPEND.pack(_APPEND.size, _TYPES[dtype], n, hq, rope_len, kp, vp, kt, kh, vt, vh, qp, op, qt, qh, ot, oh,
+                     _vector(slots, _I64T, n, dev, what, "slots"), context_p, rope_p, 0 if status is None else _vector(status, _I32T, 1, dev, what, "status"))
     if n > 0:
-        _call(LIB.d3_paged_append, what, dev, stream, cache._ref, C.byref(a))
+        _call(LIB.d3_paged_append, what, dev, cache._ref, a)
     return q_out
 
 
@@ -269,35 +288,41 @@ def d3_paged_attention(cache: PagedKV, q: torch.Tensor, table: torch.Tensor, con
     table[rows[b] or b] names (see include/d3.h).  scale: default head_dim^-0.5.  Returns out, or
     (out, lse) with `with_lse` or an `lse` tensor (fp32 [n][n_q_heads]).  Without `workspace` one is allocated for the
     call."""
-    what, dev = "d3_paged_attention", cache.device
-    if q.dim() != 3 or q.dtype not in _TYPES:
+    what, dev, dtype = "d3_paged_attention", cache.index, q.dtype
+    if stream is not None:
+        return _on_stream(lambda: d3_paged_attention(cache, q, table, context, rows=rows, scale=scale, out=out, lse=lse,
+                                                     with_lse=with_lse, workspace=workspace, status=status), dev, stream, what)
+    if q.dim() != 3 or dtype not in _TYPES:
         _refuse(f"{what}: q must be [n][n_q_heads][head_dim]")
     n, hq, dh = q.shape
-    _heads(q, n, hq, cache.head_dim, q.dtype, dev, what + " q")
-    if table.dtype != torch.int32 or table.dim() != 2 or table.device != dev or table.shape[0] < 1 or table.shape[1] < 1 or \
-            table.stride(1) != 1:
-        _refuse(f"{what}: table must be int32 [rows][width] on {dev}")
+    qp, qt, qh = _heads(q, n, hq, cache.head_dim, dtype, dev, what, "q")
+    if table.dtype is not _I32T or table.dim() != 2 or table.get_device() != dev:
+        _refuse(f"{what}: table must be int32 [rows][width] on device {dev}")
+    rows_n, width = table.shape
+    stride, inner = table.stride()
+    if rows_n < 1 or width < 1 or (inner != 1 and width > 1):
+        _refuse(f"{what}: table must have entries and contiguous rows")
     if out is None:
-        out = torch.empty((n, hq, dh), dtype=q.dtype, device=dev)
-    else:
-        _heads(out, n, hq, dh, q.dtype, dev, what + " out")
+        out = q.new_empty((n, hq, dh))
+    op, ot, oh = _heads(out, n, hq, dh, dtype, dev, what, "out")
+    if scale is None:
+        scale = dh ** -0.5
+    elif not -3e38 < scale < 3e38:
+        _refuse(f"{what}: scale must be finite")
     if lse is None:
         if with_lse:
-            lse = torch.empty((n, hq), dtype=torch.float32, device=dev)
-    elif lse.shape != (n, hq) or lse.dtype != torch.float32 or lse.device != dev or not lse.is_contiguous():
-        _refuse(f"{what}: lse must be contiguous fp32 [{n}][{hq}] on {dev}")
+            lse = q.new_empty((n, hq), dtype=_F32)
+    elif lse.shape != (n, hq) or lse.dtype is not _F32 or lse.get_device() != dev or not lse.is_contiguous():
+        _refuse(f"{what}: lse must be contiguous fp32 [{n}][{hq}] on device {dev}")
     if workspace is None:
         workspace = attention_workspace(cache, hq)
-    elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
-        _refuse(f"{what}: workspace must be contiguous uint8 on {dev}")
-    qs, os = _strides(q), _strides(out)
-    a = PagedAttentionArgs(
-        C.sizeof(PagedAttentionArgs), _TYPES[q.dtype], n, hq, table.shape[0], table.shape[1],
-        table.stride(0) if table.shape[0] > 1 else table.shape[1], dh ** -0.5 if scale is None else scale, q.data_ptr(), qs[0], qs[1],
-        out.data_ptr(), os[0], os[1], None if lse is None else lse.data_ptr(), table.data_ptr(),
-        _vector(context, torch.int32, n, dev, what + " context"),
-        None if rows is None else _vector(rows, torch.int32, n, dev, what + " rows"),
-        workspace.data_ptr(), workspace.numel(), _status(status, dev, what))
+    elif workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse(f"{what}: workspace must be contiguous uint8 on device {dev}")
+    a = _ATTENTION.pack(_ATTENTION.size, _TYPES[dtype], n, hq, rows_n, width, stride if rows_n > 1 else width,
+                        scale, qp, qt, qh, op, ot, oh, 0 if lse is None else lse.data_ptr(),
+                        table.data_ptr(), _vector(context, _I32T, n, dev, what, "context"),
+                        0 if rows is None else _vector(rows, _I32T, n, dev, what, "rows"),
+                        workspace.data_ptr(), workspace.numel(), 0 if status is None else _vector(status, _I32T, 1, dev, what, "status"))
     if n > 0:
-        _call(LIB.d3_paged_attention, what, dev, stream, cache._ref, C.byref(a))
+        _call(LIB.d3_paged_attention, what, dev, cache._ref, a)
     return out if lse is None else (out, lse)
