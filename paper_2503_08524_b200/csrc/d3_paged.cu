@@ -170,17 +170,22 @@ __global__ void __launch_bounds__(kPlanMaxThreads) k_page_plan(const __grid_cons
   };
   auto pages_of = [&](int len) { return (len + page_mask) >> a.page_shift; };   // len <= 2^31 - 1024 (checked on the host)
 
-  for (int e = gid; e < n_back; e += step) {
-    const int b = owner(s_back, a.R, e);
-    a.free_pages[n_free + e] = a.table[b * a.table_stride + (e - s_back[b])];
-  }
-  for (int e = gid; e < n_need; e += step) {
-    const int b = owner(s_need, a.R, e);
-    a.table[b * a.table_stride + pages_of(s_cached[b]) + (e - s_need[b])] = stack(top - 1 - e);
-  }
-  // four consecutive tokens per thread: one search, the map entries in 16-byte pieces
+  // one index over the pages given back, the pages taken and the tokens by fours (one search, map entries in 16-byte
+  // pieces): the three kinds run side by side
   bool strange = false;
-  for (long long t0 = (long long)gid * 4; t0 < a.T; t0 += (long long)step * 4) {
+  const long long n_all = (long long)n_back + n_need + ((long long)a.T + 3) / 4;
+  for (long long at = gid; at < n_all; at += step) {
+    if (at < n_back) {
+      const int e = (int)at, b = owner(s_back, a.R, e);
+      a.free_pages[n_free + e] = a.table[b * a.table_stride + (e - s_back[b])];
+      continue;
+    }
+    if (at < (long long)n_back + n_need) {
+      const int e = (int)(at - n_back), b = owner(s_need, a.R, e);
+      a.table[b * a.table_stride + pages_of(s_cached[b]) + (e - s_need[b])] = stack(top - 1 - e);
+      continue;
+    }
+    const long long t0 = (at - n_back - n_need) * 4;
     long long slot[4];
     int row[4], ctx[4];
     int b = t0 < n_tok ? owner(s_first, a.R, (int)t0) : a.R;
@@ -238,27 +243,44 @@ struct AppendArgs {
   KvPool kv;
 };
 
-__device__ __forceinline__ void load8(const float *p, float *f) {
-  const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+// eight numbers as they lie in memory, and widened
+template <typename T> struct Raw8 { uint4 u; };
+template <> struct Raw8<float> { uint4 u, w; };
+template <typename T>
+__device__ __forceinline__ void fetch(Raw8<T> &r, const T *p) { r.u = *reinterpret_cast<const uint4 *>(p); }
+__device__ __forceinline__ void fetch(Raw8<float> &r, const float *p) {
+  r.u = reinterpret_cast<const uint4 *>(p)[0];
+  r.w = reinterpret_cast<const uint4 *>(p)[1];
 }
-__device__ __forceinline__ void load8(const bf16 *p, float *f) {
-  const uint4 u = *reinterpret_cast<const uint4 *>(p);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ void widen8(const Raw8<float> &r, float *f) {
+  const uint32_t w[8] = {r.u.x, r.u.y, r.u.z, r.u.w, r.w.x, r.w.y, r.w.z, r.w.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
+}
+__device__ __forceinline__ void widen8(const Raw8<bf16> &r, float *f) {
+  const uint32_t w[4] = {r.u.x, r.u.y, r.u.z, r.u.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     f[2 * i] = __uint_as_float(w[i] << 16);
     f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ void load8(const __half *p, float *f) {
-  const uint4 u = *reinterpret_cast<const uint4 *>(p);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ void widen8(const Raw8<__half> &r, float *f) {
+  const uint32_t w[4] = {r.u.x, r.u.y, r.u.z, r.u.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
     f[2 * i] = v.x; f[2 * i + 1] = v.y;
   }
+}
+// x / d rounded once, for a d whose correctly rounded reciprocal r is known (2^-60 <= |d| <= 2^60): the remainder of the first
+// quotient is exact in one FMA, and adding it times r rounds like the division (Markstein 1990).  Quotients
+// beyond 10^4, infinities and NaN stay as the product has them: the 8-bit type saturates at 448.
+__device__ __forceinline__ float divide(float x, float d, float r) {
+  const float q = __fmul_rn(x, r);
+  const float better = __fmaf_rn(__fmaf_rn(-q, d, x), r, q);
+  const float v = fabsf(q) < 1.0e4f ? better : q;
+  return __uint_as_float(__float_as_uint(v) | (__float_as_uint(q) & 0x80000000u));   // -0 stays -0
 }
 __device__ __forceinline__ void store8(float *p, const float *f) {
   reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
@@ -305,7 +327,7 @@ __global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ Ap
   const long long slot = a.slots[t];
   const int pos = a.rope ? a.context[t] - 1 : 0;
 
-  float lo[H][8], hi[H][8];
+  Raw8<X> raw[H][2];
 #pragma unroll
   for (int i = 0; i < H; ++i) {
     const int h = h0 + i * step;
@@ -313,8 +335,8 @@ __global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ Ap
       const X *p = h < a.hq ? static_cast<const X *>(a.q) + t * a.qt + (long long)h * a.qh
                    : h < a.hq + a.kv.n_kv_heads ? static_cast<const X *>(a.k) + t * a.kt + (long long)(h - a.hq) * a.kh
                    : static_cast<const X *>(a.v) + t * a.vt + (long long)(h - a.hq - a.kv.n_kv_heads) * a.vh;
-      load8(p + 8 * j, lo[i]);
-      load8(p + HALF + 8 * j, hi[i]);
+      fetch(raw[i][0], p + 8 * j);
+      fetch(raw[i][1], p + HALF + 8 * j);
     }
   }
   if (slot < 0) return;
@@ -324,29 +346,32 @@ __global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ Ap
   }
   const long long in_page = slot & ((1 << a.kv.page_shift) - 1);
   const long long entry = (slot >> a.kv.page_shift) * a.kv.page_stride + in_page * a.kv.token_stride;
-  float cs[16];
+  float4 cs[4];   // (cos, sin) of the eight pairs
   if (a.rope && h0 < a.hq + a.kv.n_kv_heads) {
-    const float *r = a.rope + ((long long)pos * HALF + 8 * j) * 2;
-    load8(r, cs);
-    load8(r + 8, cs + 8);
+    const float4 *r = reinterpret_cast<const float4 *>(a.rope + ((long long)pos * HALF + 8 * j) * 2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) cs[i] = __ldg(r + i);
   }
 #pragma unroll
   for (int i = 0; i < H; ++i) {
     const int h = h0 + i * step;
     if (h >= heads) continue;
+    float lo[8], hi[8];
+    widen8(raw[i][0], lo);
+    widen8(raw[i][1], hi);
     if (a.rope && h < a.hq + a.kv.n_kv_heads) {
       // products and sums rounded one by one: no contraction, so every store rounds the same number
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float c = cs[2 * e], s = cs[2 * e + 1], x = lo[i][e], y = hi[i][e];
-        lo[i][e] = __fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s));
-        hi[i][e] = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
+        const float c = e & 1 ? cs[e / 2].z : cs[e / 2].x, s = e & 1 ? cs[e / 2].w : cs[e / 2].y, x = lo[e], y = hi[e];
+        lo[e] = __fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s));
+        hi[e] = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
       }
     }
     if (h < a.hq) {
       X *p = static_cast<X *>(a.q_out) + t * a.ot + (long long)h * a.oh;
-      store8(p + 8 * j, lo[i]);
-      store8(p + HALF + 8 * j, hi[i]);
+      store8(p + 8 * j, lo);
+      store8(p + HALF + 8 * j, hi);
     } else {
       const bool is_v = h >= a.hq + a.kv.n_kv_heads;
       const int kh = h - a.hq - (is_v ? a.kv.n_kv_heads : 0);
@@ -354,13 +379,19 @@ __global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ Ap
       if (sizeof(C) == 1) {
         const float *sc = is_v ? a.kv.v_scale : a.kv.k_scale;
         if (sc) {
-          const float d = sc[kh];
+          const float d = __ldg(sc + kh);
+          if (fabsf(d) >= 0x1p-60f && fabsf(d) <= 0x1p60f) {
+            const float r = __frcp_rn(d);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) { lo[i][e] = __fdiv_rn(lo[i][e], d); hi[i][e] = __fdiv_rn(hi[i][e], d); }
+            for (int e = 0; e < 8; ++e) { lo[e] = divide(lo[e], d, r); hi[e] = divide(hi[e], d, r); }
+          } else {
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) { lo[e] = __fdiv_rn(lo[e], d); hi[e] = __fdiv_rn(hi[e], d); }
+          }
         }
       }
-      store8(p + 8 * j, lo[i]);
-      store8(p + HALF + 8 * j, hi[i]);
+      store8(p + 8 * j, lo);
+      store8(p + HALF + 8 * j, hi);
     }
   }
 }
@@ -375,8 +406,8 @@ void launch_append_dh(AppendArgs &a, cudaStream_t st) {
   const long long groups = (a.n_tokens + tokens - 1) / tokens;
   // Several heads per thread read (cos, sin) once for all of them; with few tokens one head per thread spreads the call
   // over more SMs.
-  const int H = groups * rounds <= 4 * 148 ? 1 : rounds < 3 ? rounds : 3;
-  const dim3 grid((unsigned)groups, (unsigned)((rounds + H - 1) / H));
+  const int ny = groups * rounds <= 4 * 148 ? rounds : (rounds + 2) / 3, H = (rounds + ny - 1) / ny;
+  const dim3 grid((unsigned)groups, (unsigned)ny);
   if (H == 1) launch_pdl(k_paged_append<X, C, DH, 1>, grid, dim3(256), 0, st, a);
   else if (H == 2) launch_pdl(k_paged_append<X, C, DH, 2>, grid, dim3(256), 0, st, a);
   else launch_pdl(k_paged_append<X, C, DH, 3>, grid, dim3(256), 0, st, a);
@@ -469,8 +500,9 @@ int32_t d3_page_plan(const d3_page_plan_args *a, void *cuda_stream) {
   // CTAs as there are groups of four tokens for, up to one per SM (192 prompts of 129..2048 tokens, 209,000
   // in all: 21.3 us as a cluster of eight, PLAN_GRID_US as 52 CTAs).
   const bool in_place = a->cached_out_dev == a->cached_dev || a->n_free_out_dev == a->n_free_dev;
-  const int threads = a->n_requests <= 128 && a->max_tokens <= 512 ? 128 : kPlanMaxThreads;
-  long long ctas = ((long long)a->max_tokens + 4 * threads - 1) / (4 * threads);
+  const int threads = a->n_requests <= 128 && a->max_tokens <= 512 ? 128 : in_place || a->n_requests > 1024 ? 1024 : 256;
+  const long long entries = ((long long)a->max_tokens + 3) / 4 + (a->max_tokens > 512 ? a->n_pages / 4 : 0);
+  long long ctas = (entries + threads - 1) / threads;
   if (ctas > 148) ctas = 148;
   if (in_place && ctas > 1) ctas = 8;
   p.cluster = in_place && ctas > 1 ? 1 : 0;
