@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ Ap
 #pragma unroll
             for (int e = 0; e < 8; ++e) { lo[e] = divide(lo[e], d, r); hi[e] = divide(hi[e], d, r); }
           } else {
-#pragma unroll 1
+#pragma unroll
             for (int e = 0; e < 8; ++e) { lo[e] = __fdiv_rn(lo[e], d); hi[e] = __fdiv_rn(hi[e], d); }
           }
         }
