@@ -41,6 +41,7 @@ namespace paged_attn {
 
 constexpr int kPiece = 16;            // positions of a warp's trip, and of the smallest TMA box
 constexpr int kProducers = 2;         // warps that issue copies, stage by stage in turn
+constexpr int kFewRows = 128;         // rows that a producer warp sums up by itself
 constexpr int kMaxStages = 12;
 constexpr int kSmemMost = 224 * 1024; // of 227 KB
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -111,11 +112,11 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
 }
 template <bool F16>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if (F16)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  if (F16)   // (not volatile: a function of its registers, free to be scheduled between the loads)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float exp2_fast(float x) {   // 2^x to 2^-22 relative; 0 for -inf
@@ -160,11 +161,15 @@ struct ItemInfo {
   int row, tile, kind, final;
 };
 
-// The share of CTA i of n among U units starts here.
-__device__ __forceinline__ long long share(long long U, int i, int n) { return U * i / n; }
+// x / y and the start of CTA i's share of U units among n, without a 64-bit division where 32 bits do
+__device__ __forceinline__ long long divide(long long x, int y) {
+  return x < (1ll << 32) ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
+}
+__device__ __forceinline__ long long share(long long U, int i, int n) { return divide(U * i, n); }
 
-enum { STAGE_FIRST = 1, STAGE_LAST = 2 };   // of the item within this CTA
-enum { OUT_WHOLE = 0, OUT_HEAD = 1, OUT_TAIL = 2 };   // an item lies in this CTA / started before it / starts in it and goes on
+enum { STAGE_FIRST = 1, STAGE_LAST = 2, STAGE_FINAL = 4 };   // of the item within this CTA; of the CTA
+// an item lies in this CTA / started before it / starts in it and goes on; no item at all
+enum { OUT_WHOLE = 0, OUT_HEAD = 1, OUT_TAIL = 2, OUT_NONE = 3 };
 
 // What the producer tells the consumers about a stage.
 struct StageInfo {
@@ -210,7 +215,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   __shared__ float s_m[C::kWarps][C::kHeads], s_l[C::kWarps][C::kHeads];
   __shared__ ItemInfo s_item;
   __shared__ long long s_sum[32];
-  __shared__ int s_abort, s_start_row;
+  __shared__ int s_abort, s_start_row;   // (start: the first row's, where all threads look for it)
   __shared__ long long s_start_before;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int S = a.n_stages;
@@ -235,10 +240,9 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const CUtensorMap *m = lane == 0 ? &map_k : lane == 1 ? &map_v : lane == 2 ? &map_k16 : &map_v16;
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
   }
-  pdl_wait();
-  pdl_trigger();
 
-  // ---- the rows' unit counts, summed over all rows by every CTA
+  // ---- the rows' unit counts, summed over all rows by every CTA: up to 128 rows by each producer warp for itself, more of
+  // them by all threads
   auto row_of = [&](int b, bool &bad) -> int {   // table row, -1 = padding
     if (!a.rows) return b;
     const int r = a.rows[b];
@@ -252,62 +256,141 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     return c;
   };
   auto units_of = [&](int len) -> int { return len > 0 ? (len + kUnit - 1) / kUnit : 1; };   // a row without context still gets its zeros
-  const int per = (a.n_rows + C::kThreads - 1) / C::kThreads;
-  long long mine = 0;
-  bool bad = false;
-  for (int i = 0; i < per; ++i) {
-    const int b = tid * per + i;
-    if (b < a.n_rows && row_of(b, bad) >= 0) mine += units_of(length_of(b, bad));
-  }
-  if (bad && blockIdx.x == 0 && a.status) *a.status = D3_EINVAL;
-  long long inc = mine;
+  const bool few = a.n_rows <= kFewRows;
+  long long total = 0;
+  if (!few) {
+    pdl_wait();
+    pdl_trigger();
+    const int per = (a.n_rows + C::kThreads - 1) / C::kThreads;
+    long long mine = 0;
+    bool bad = false;
+    for (int i = 0; i < per; ++i) {
+      const int b = tid * per + i;
+      if (b < a.n_rows) {
+        const int len = length_of(b, bad);   // (padding may hold anything)
+        bool strange = false;
+        if (row_of(b, strange) >= 0) mine += units_of(len);
+        else bad = false;
+        bad = bad || strange;
+        if (bad && blockIdx.x == 0 && a.status) *a.status = D3_EINVAL;
+        bad = false;
+      }
+    }
+    long long inc = mine;
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long u = __shfl_up_sync(0xffffffffu, inc, d);
-    if (lane >= d) inc += u;
-  }
-  if (lane == 31) s_sum[warp] = inc;
-  __syncthreads();
-  long long before = 0, total = 0;
-#pragma unroll
-  for (int w = 0; w < C::kThreads / 32; ++w) {
-    const long long v = s_sum[w];
-    if (w < warp) before += v;
-    total += v;
-  }
-  before += inc - mine;
-  const long long U = total * HG;
-  const int n_cta = (int)(U < (long long)gridDim.x ? U : (long long)gridDim.x);   // every one of them has work
-  if ((int)blockIdx.x >= n_cta) {
-    if (tid == 0) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
-    return;
-  }
-  const long long u0 = share(U, blockIdx.x, n_cta), u1 = share(U, blockIdx.x + 1, n_cta);
-  {
-    const long long t0 = u0 / HG;   // the row whose range of the unit sums holds t0 is the first one
-    if (t0 >= before && t0 < before + mine) {
-      long long p = before;
-      for (int i = 0; i < per; ++i) {
-        const int b = tid * per + i;
-        bool dummy = false;
-        if (b < a.n_rows && row_of(b, dummy) >= 0) {
-          const int n = units_of(length_of(b, dummy));
-          if (t0 < p + n) { s_start_row = b; s_start_before = p; break; }
-          p += n;
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, inc, d);
+      if (lane >= d) inc += u;
+    }
+    if (lane == 31) s_sum[warp] = inc;
+    __syncthreads();
+    long long before = inc - mine;
+    for (int w = 0; w < C::kThreads / 32; ++w) {
+      const long long v = s_sum[w];
+      if (w < warp) before += v;
+      total += v;
+    }
+    const long long U = total * HG;
+    const int n_cta = (int)(U < (long long)gridDim.x ? U : (long long)gridDim.x);
+    if ((int)blockIdx.x < n_cta) {
+      const long long t0 = divide(share(U, blockIdx.x, n_cta), HG);   // the first row is the one whose range of the sums holds t0
+      if (t0 >= before && t0 < before + mine) {
+        long long p = before;
+        for (int i = 0; i < per; ++i) {
+          const int b = tid * per + i;
+          bool dummy = false;
+          if (b < a.n_rows && row_of(b, dummy) >= 0) {
+            const int n = units_of(length_of(b, dummy));
+            if (t0 < p + n) { s_start_row = b; s_start_before = p; break; }
+            p += n;
+          }
         }
       }
     }
   }
-  __syncthreads();
+  __syncthreads();   // the barriers, and the first row where it was looked for
 
   if (warp >= C::kWarps + C::kEpilogue) {
     // ------------------------------------------------------------ producers
     const int me = warp - C::kWarps - C::kEpilogue;
-    int row = s_start_row;
     bool dummy = false;
-    int trow = row_of(row, dummy), len = length_of(row, dummy), nu = units_of(len);
-    const long long at = u0 - s_start_before * HG;     // unit inside the row's (tile, unit) range
-    int tile = (int)(at / nu), unit = (int)(at % nu);
+    int row, trow, len;
+    long long start_before;
+    // few rows: their table rows and lengths stay in registers, row lane * per + i in entry i
+    constexpr int kPer = kFewRows / 32;
+    const int per = (a.n_rows + 31) / 32;
+    int r_[kPer], c_[kPer], at_lane = 0, at_entry = 0;
+    auto kept = [&](const int (&v)[kPer]) -> int {
+      int x = v[0];
+#pragma unroll
+      for (int i = 1; i < kPer; ++i) x = at_entry == i ? v[i] : x;
+      return __shfl_sync(0xffffffffu, x, at_lane);
+    };
+    if (few) {
+      pdl_wait();
+      pdl_trigger();
+      long long mine = 0;
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int b = lane * per + i;
+        r_[i] = -1; c_[i] = 0;
+        if (i < per && b < a.n_rows) {
+          bool strange = false;
+          c_[i] = length_of(b, strange);
+          r_[i] = row_of(b, bad);
+          if (r_[i] >= 0) { mine += units_of(c_[i]); bad = bad || strange; }
+        }
+      }
+      if (bad && blockIdx.x == 0 && a.status) *a.status = D3_EINVAL;
+      long long inc = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, inc, d);
+        if (lane >= d) inc += u;
+      }
+      total = __shfl_sync(0xffffffffu, inc, 31);
+      const long long U = total * HG;
+      const int n_cta = (int)(U < (long long)gridDim.x ? U : (long long)gridDim.x);
+      if ((int)blockIdx.x < n_cta) {
+        const long long t0 = divide(share(U, blockIdx.x, n_cta), HG);
+        long long p = inc - mine;
+        at_lane = __ffs(__ballot_sync(0xffffffffu, t0 >= p && t0 < inc)) - 1;
+        int entry = 0;
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const int n = r_[i] >= 0 ? units_of(c_[i]) : 0;
+          if (!found) {
+            if (t0 < p + n) { entry = i; found = true; }
+            else p += n;
+          }
+        }
+        at_entry = __shfl_sync(0xffffffffu, entry, at_lane);
+        start_before = __shfl_sync(0xffffffffu, p, at_lane);
+        row = at_lane * per + at_entry;
+        trow = kept(r_);
+        len = kept(c_);
+      }
+    } else {
+      row = s_start_row;
+      start_before = s_start_before;
+      if (row < a.n_rows) { trow = row_of(row, dummy); len = length_of(row, dummy); }
+    }
+    const long long U = total * HG;
+    const int n_cta = (int)(U < (long long)gridDim.x ? U : (long long)gridDim.x);   // every one of them has work
+    if ((int)blockIdx.x >= n_cta) {
+      if (me == 0 && lane == 0) {
+        a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
+        s_info[0] = StageInfo{0, 0, 0, STAGE_LAST | STAGE_FINAL | (OUT_NONE << 12)};
+        mb_arrive(smem_u32(&s_full[0]));
+      }
+      return;
+    }
+    const long long u0 = share(U, blockIdx.x, n_cta), u1 = share(U, blockIdx.x + 1, n_cta);
+    int nu = units_of(len);
+    const long long at = u0 - start_before * HG;     // unit inside the row's (tile, unit) range
+    int tile = (int)divide(at, nu), unit = (int)(at - (long long)tile * nu);
     int kvh = tile / a.tiles_per_head, sub = tile % a.tiles_per_head;
     const int32_t *pages = a.table + (long long)trow * a.table_stride;
     auto fetch = [&](int base) -> int { return base + lane < a.table_width ? __ldg(pages + base + lane) : -1; };
@@ -358,7 +441,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           int kind = OUT_WHOLE;
           if (last && unit + 1 < nu) kind = item >= u0 ? OUT_TAIL : OUT_HEAD;   // the item goes on in the next CTA
           else if (last && item < u0) kind = OUT_HEAD;                          // its last piece
-          info.flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (int)(pieces << 4) | (kind << 12);
+          info.flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (left == 1 ? STAGE_FINAL : 0) | (int)(pieces << 4) | (kind << 12);
           s_info[s] = info;
           mb_arrive_tx(full, (uint32_t)__popc(pieces) * 2u * kPiece * C::kRow + (first ? (uint32_t)nh * DH * QBytes<X>::v : 0u));
         }
@@ -384,8 +467,12 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         if (++sub == a.tiles_per_head) { sub = 0; ++kvh; }
         if (tile == HG) {
           tile = kvh = 0;
-          do { ++row; trow = row < a.n_rows ? row_of(row, dummy) : 0; } while (trow < 0);
-          len = length_of(row, dummy);
+          do {
+            ++row;
+            if (++at_entry == per) { at_entry = 0; ++at_lane; }
+            trow = row >= a.n_rows ? 0 : few ? kept(r_) : row_of(row, dummy);
+          } while (trow < 0);
+          len = row >= a.n_rows ? 0 : few ? kept(c_) : length_of(row, dummy);
           nu = units_of(len);
           pages = a.table + (long long)trow * a.table_stride;
         }
@@ -396,7 +483,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       int4 join = make_int4(0, 0, 0, 0);
       if (ok && unit < nu && item >= u0) {   // (unit counts the units passed)
         const long long end = item + nu;     // CTAs up to the one that holds unit end - 1
-        join = make_int4((int)((end * n_cta + U - 1) / U) - (int)blockIdx.x, row, tile, 0);
+        const long long x = end * n_cta + U - 1;
+        join = make_int4((int)(U < (1ll << 31) ? divide(x, (int)U) : x / U) - (int)blockIdx.x, row, tile, 0);
       }
       a.join[blockIdx.x] = join;
     }
@@ -421,7 +509,9 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const int me = warp - C::kWarps;
     for (uint32_t parity = 0;; parity ^= 1u) {
       if (!__all_sync(0xffffffffu, mb_wait(smem_u32(&s_sums_full), parity, &s_abort, a.wait_ns))) break;
+      if (parity == 0u) pdl_wait();   // returns at once: the producers' has
       const ItemInfo item = s_item;
+      if (item.kind == OUT_NONE) break;
       const int kvh = item.tile / a.tiles_per_head, g0 = (item.tile % a.tiles_per_head) * a.heads_per_tile;
       const int nh = min(a.heads_per_tile, a.group - g0);
       for (int h = me; h < nh; h += C::kEpilogue) {
@@ -499,16 +589,17 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   }
   int piece_turn = 0;       // pieces of the CTA so far, mod kWarps: whose turn it is
   int items = 0;
-  const int n_units = (int)(u1 - u0);
   bool ok = true;
   int s = 0;
   uint32_t parity = 0;
-  for (int k = 0; k < n_units; ++k) {
+  for (bool more = true; more;) {
     if (!mb_wait(smem_u32(&s_full[s]), parity, &s_abort, a.wait_ns)) ok = false;
     ok = __all_sync(0xffffffffu, ok);
     if (!ok) break;
     const StageInfo info = s_info[s];
+    more = !(info.flags & STAGE_FINAL);
     if (info.flags & STAGE_FIRST) {
+      if (items == 0) pdl_wait();   // returns at once: the producers' has
       // ---- this thread's fragments of Q, and what a raw score is multiplied by
       const int kvh = info.tile / a.tiles_per_head, g0 = (info.tile % a.tiles_per_head) * a.heads_per_tile;
       const int nh = min(a.heads_per_tile, a.group - g0);
@@ -583,32 +674,39 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       const int valid = info.n - p * kPiece;   // positions of the piece (>= 1)
       // 16-byte chunk c (even) past the lane's own: an XOR inside the 128-byte line, the next column behind it
       auto chunk = [&](uint32_t base, int c) -> uint32_t { return (base ^ ((c % kPerRow) << 4)) + (c / kPerRow) * (kUnit * C::kBox); };
-      float sc[KT][4];
+      // all fragments of K are asked for before the first product, those of V before the softmax
+      constexpr int NF = CACHE == D3_E4M3 ? KK / 2 : KK;   // ldmatrix per operand
+      uint32_t kf[NF][4], vf[NF][4];
 #pragma unroll
-      for (int i = 0; i < KT; ++i) sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
-      if constexpr (CACHE != D3_E4M3) {
+      for (int n = 0; n < NF; ++n) ldsm4(kf[n], chunk(kbase, 2 * n));
+      float sc[KT][4];
+      {
+        float part[KT][2][4];   // two chains of products each
+#pragma unroll
+        for (int i = 0; i < KT; ++i)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) part[i][c][0] = part[i][c][1] = part[i][c][2] = part[i][c][3] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
           uint32_t f[4];
-          ldsm4(f, chunk(kbase, 2 * kk));
+          if constexpr (CACHE != D3_E4M3) {
+            f[0] = kf[kk][0]; f[1] = kf[kk][1]; f[2] = kf[kk][2]; f[3] = kf[kk][3];
+          } else {   // chunk kk of positions 0-7 and of 8-15: four dims 4t.. of position g
+            const uint32_t x = kf[kk / 2][2 * (kk & 1)], y = kf[kk / 2][2 * (kk & 1) + 1];
+            f[0] = widen(x); f[1] = widen(y); f[2] = widen(x >> 16); f[3] = widen(y >> 16);
+          }
 #pragma unroll
           for (int i = 0; i < KT; ++i)
 #pragma unroll
-            for (int q = TQ - 1; q >= 0; --q) mma<F16>(sc[i], f, qb[i][q][kk][0], qb[i][q][kk][1]);
+            for (int q = TQ - 1; q >= 0; --q) mma<F16>(part[i][kk & 1], f, qb[i][q][kk][0], qb[i][q][kk][1]);
         }
-      } else {
 #pragma unroll
-        for (int kk = 0; kk < KK; kk += 2) {
-          uint32_t b[4];   // chunk kk of positions 0-7, of 8-15, then chunk kk + 1: four dims 4t.. of position g
-          ldsm4(b, chunk(kbase, kk));
+        for (int i = 0; i < KT; ++i)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const uint32_t f[4] = {widen(b[2 * q]), widen(b[2 * q + 1]), widen(b[2 * q] >> 16), widen(b[2 * q + 1] >> 16)};
-#pragma unroll
-            for (int i = 0; i < KT; ++i) mma<F16>(sc[i], f, qb[i][0][kk + q][0], qb[i][0][kk + q][1]);
-          }
-        }
+          for (int e = 0; e < 4; ++e) sc[i][e] = part[i][0][e] + part[i][1][e];
       }
+#pragma unroll
+      for (int n = 0; n < NF; ++n) ldsm4t(vf[n], chunk(vbase, 2 * n));
       // ---- softmax of the piece: [0] head 2t, [1] head 2t + 1 of position g; [2], [3] of position g + 8
       const bool partial = valid < kPiece;
       uint32_t pb[KT][TP][2];
@@ -664,34 +762,22 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         keep0 = (2 * t < valid ? 0xffffu : 0u) | (2 * t + 1 < valid ? 0xffff0000u : 0u);
         keep1 = (2 * t + 8 < valid ? 0xffffu : 0u) | (2 * t + 9 < valid ? 0xffff0000u : 0u);
       }
-      auto add = [&](int n, uint32_t (&f)[4]) {
+#pragma unroll
+      for (int n = 0; n < KK; ++n) {
+        uint32_t f[4];
+        if constexpr (CACHE != D3_E4M3) {   // dims 16n.. / +8 of positions 0-7, then of 8-15
+          f[0] = vf[n][0]; f[1] = vf[n][1]; f[2] = vf[n][2]; f[3] = vf[n][3];
+        } else {
+          // chunk n of positions 0-7 and of 8-15: positions 2t, 2t + 1 of dims 2g, 2g + 1.  Even dims make rows
+          // 0-7 of the product, odd ones rows 8-15
+          const uint32_t lo = __byte_perm(vf[n / 2][2 * (n & 1)], 0, 0x3120), hi = __byte_perm(vf[n / 2][2 * (n & 1) + 1], 0, 0x3120);
+          f[0] = widen(lo); f[1] = widen(lo >> 16); f[2] = widen(hi); f[3] = widen(hi >> 16);
+        }
         if (partial) { f[0] &= keep0; f[1] &= keep0; f[2] &= keep1; f[3] &= keep1; }
 #pragma unroll
         for (int i = 0; i < KT; ++i)
 #pragma unroll
           for (int q = TP - 1; q >= 0; --q) mma<F16>(o[i][n], f, pb[i][q][0], pb[i][q][1]);
-      };
-      if constexpr (CACHE != D3_E4M3) {
-#pragma unroll
-        for (int n = 0; n < KK; ++n) {
-          uint32_t f[4];   // dims 16n.. / +8 of positions 0-7, then of 8-15
-          ldsm4t(f, chunk(vbase, 2 * n));
-          add(n, f);
-        }
-      } else {
-#pragma unroll
-        for (int n = 0; n < KK; n += 2) {
-          // chunk n of positions 0-7, of 8-15, then chunk n + 1: positions 2t, 2t + 1 of dims 2g, 2g + 1.  Even
-          // dims make rows 0-7 of the product, odd ones rows 8-15
-          uint32_t b[4];
-          ldsm4t(b, chunk(vbase, n));
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const uint32_t lo = __byte_perm(b[2 * q], 0, 0x3120), hi = __byte_perm(b[2 * q + 1], 0, 0x3120);
-            uint32_t f[4] = {widen(lo), widen(lo >> 16), widen(hi), widen(hi >> 16)};
-            add(n + q, f);
-          }
-        }
       }
     }
     __syncwarp();
@@ -731,7 +817,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
         for (int n = 0; n < KK; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
       }
-      if (warp == 0 && lane == 0) s_item = ItemInfo{info.row, info.tile, (info.flags >> 12) & 3, k + 1 == n_units};
+      if (warp == 0 && lane == 0) s_item = ItemInfo{info.row, info.tile, (info.flags >> 12) & 3, !more};
       __syncwarp();
       if (lane == 0) mb_arrive(smem_u32(&s_sums_full));
       ++items;
