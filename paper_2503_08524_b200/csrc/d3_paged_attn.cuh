@@ -1,6 +1,6 @@
 // Attention of one new token per row over a paged cache: the kernel, compiled per head dimension.
 //
-// Mathematics.  For a tile of up to 8 query heads of one kv head (16 with two score tiles) and a piece of 16
+// Mathematics.  For up to 8 query heads of one kv head (16 with two products) and a tile of 16
 // positions: S^T = K Q^T, the running maximum m and sum l of exp2(S scale log2 e - m), O^T = O^T exp2(m_old - m) +
 // V^T P^T.  O, m and l are additive over any cut of the positions once brought to a common maximum, which is all that
 // the split over the length needs.
@@ -39,7 +39,7 @@
 namespace d3 {
 namespace paged_attn {
 
-constexpr int kPiece = 16;            // positions of a warp's trip, and of the smallest TMA box
+constexpr int kTile = 16;             // positions of a product's rows, and of the smallest TMA box
 constexpr int kProducers = 2;         // warps that issue copies, stage by stage in turn
 constexpr int kFewRows = 128;         // rows that a producer warp sums up by itself
 constexpr int kMaxStages = 12;
@@ -175,7 +175,7 @@ enum { OUT_WHOLE = 0, OUT_HEAD = 1, OUT_TAIL = 2, OUT_NONE = 3 };
 struct StageInfo {
   int row, tile;        // tile = kv head * tiles_per_head + tile of its query heads
   int n;                // positions in the stage (0 .. kUnit)
-  int flags;            // STAGE_* | pieces that hold positions << 4 | OUT_* << 12
+  int flags;            // STAGE_* | tiles that hold positions << 4 | OUT_* << 12
 };
 
 template <int DH, int CACHE, int X, int MT>
@@ -186,13 +186,14 @@ struct Cfg {
   static constexpr int kBoxes = kRow / kBox;                 // boxes per piece of K (or V)
   static constexpr int kHeads = X == D3_FP32 ? 8 : 8 * MT;   // query heads of a tile
   static constexpr int kUnit = kRow > 128 ? 64 : 128;        // positions of a stage (of up to 32 KB)
+  static constexpr int kPT = kRow > 128 ? 1 : 2;             // tiles of a piece, i.e. of a warp's trip (32 fragment registers)
   static constexpr int kHalfBytes = kUnit * kRow;            // K (or V) of a stage
   static constexpr int kQBytes = kHeads * DH * QBytes<X>::v;
   static constexpr int kStageBytes = 2 * kHalfBytes;
   // Registers are dealt out to four warps at a time: 16 warps of 128 (which 32 accumulator and 16 query registers fit
   // into), or 12 of 168 for 16 heads or three-term queries.
-  static constexpr int kWarps = MT == 1 ? 10 : 8;            // consumers
-  static constexpr int kEpilogue = MT == 1 ? 4 : 2;
+  static constexpr int kWarps = MT == 1 ? 12 : 8;            // consumers
+  static constexpr int kEpilogue = 2;
   static constexpr int kThreads = 32 * (kWarps + kProducers + kEpilogue);
   static constexpr int kHeadFloats = DH + 4;                 // of a head's sums in shared memory (padded: no bank conflicts)
   static constexpr bool kF16 = CACHE != D3_BF16;
@@ -207,7 +208,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                   const __grid_constant__ PagedAttnArgs a) {
   using C = Cfg<DH, CACHE, X, MT>;
   constexpr int kUnit = C::kUnit;
-  constexpr int KK = DH / 16, KT = C::kTiles, TQ = C::kQTerms, TP = C::kPTerms;
+  constexpr int KK = DH / 16, KT = C::kTiles, TQ = C::kQTerms, TP = C::kPTerms, PT = C::kPT;
   constexpr bool F16 = C::kF16;
   extern __shared__ unsigned char s_dyn[];
   __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sums_full, s_sums_free;
@@ -417,13 +418,13 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             win0 += 32; win = win_next; win_next = fetch(win0 + 32);
           }
         }
-        // which pieces are there: lane p looks at piece p
-        const int id_p = __shfl_sync(0xffffffffu, win, ((p0 + lane * kPiece) >> a.page_shift) & 31);
-        const bool inside = lane * kPiece < n, good = id_p >= 0 && id_p < a.n_pages;
-        const unsigned pieces = __ballot_sync(0xffffffffu, inside && good);
+        // which tiles are there: lane p looks at tile p
+        const int id_p = __shfl_sync(0xffffffffu, win, ((p0 + lane * kTile) >> a.page_shift) & 31);
+        const bool inside = lane * kTile < n, good = id_p >= 0 && id_p < a.n_pages;
+        const unsigned tiles = __ballot_sync(0xffffffffu, inside && good);
         if (inside && !good && a.status) *a.status = D3_EINVAL;
         // this lane's copy: box of positions, K or V, 128-byte column.  Whole units go in boxes of up to a page, the
-        // last unit of a row in boxes of 16 positions (nothing is fetched behind the piece the row ends in).
+        // last unit of a row in boxes of 16 positions (nothing is fetched behind the tile the row ends in).
         const bool whole = n == kUnit;
         const int bs = whole ? full_shift : (kUnit == 64 ? 2 : 3);
         const int box = lane & ((1 << bs) - 1), is_v = (lane >> bs) & 1, col = lane >> (bs + 1);
@@ -441,9 +442,9 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           int kind = OUT_WHOLE;
           if (last && unit + 1 < nu) kind = item >= u0 ? OUT_TAIL : OUT_HEAD;   // the item goes on in the next CTA
           else if (last && item < u0) kind = OUT_HEAD;                          // its last piece
-          info.flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (left == 1 ? STAGE_FINAL : 0) | (int)(pieces << 4) | (kind << 12);
+          info.flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (left == 1 ? STAGE_FINAL : 0) | (int)(tiles << 4) | (kind << 12);
           s_info[s] = info;
-          mb_arrive_tx(full, (uint32_t)__popc(pieces) * 2u * kPiece * C::kRow + (first ? (uint32_t)nh * DH * QBytes<X>::v : 0u));
+          mb_arrive_tx(full, (uint32_t)__popc(tiles) * 2u * kTile * C::kRow + (first ? (uint32_t)nh * DH * QBytes<X>::v : 0u));
         }
         __syncwarp();
         if (want) {
@@ -661,65 +662,76 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         mul[i][1] = __shfl_sync(0xffffffffu, factor, 8 * t + 4);
       }
     }
-    const int n_pieces = (info.n + kPiece - 1) / kPiece;
+    const int n_pieces = (info.n + PT * kTile - 1) / (PT * kTile);
     // pieces go round the warps
     int p = warp - piece_turn;
     if (p < 0) p += C::kWarps;
     piece_turn += n_pieces;
-    while (piece_turn >= C::kWarps) piece_turn -= C::kWarps;
-    for (; p < n_pieces; p += C::kWarps) {
-      if (!((info.flags >> (4 + p)) & 1)) continue;   // its page id was out of range
-      const uint32_t kbase = ring + s * C::kStageBytes + p * (kPiece * C::kBox) + k_lane;
-      const uint32_t vbase = ring + s * C::kStageBytes + C::kHalfBytes + p * (kPiece * C::kBox) + v_lane;
-      const int valid = info.n - p * kPiece;   // positions of the piece (>= 1)
-      // 16-byte chunk c (even) past the lane's own: an XOR inside the 128-byte line, the next column behind it
-      auto chunk = [&](uint32_t base, int c) -> uint32_t { return (base ^ ((c % kPerRow) << 4)) + (c / kPerRow) * (kUnit * C::kBox); };
-      // all fragments of K are asked for before the first product, those of V before the softmax
-      constexpr int NF = CACHE == D3_E4M3 ? KK / 2 : KK;   // ldmatrix per operand
-      uint32_t kf[NF][4], vf[NF][4];
+    if (piece_turn >= C::kWarps) piece_turn -= C::kWarps;
+    if (p < n_pieces) {   // (a stage has 4 pieces at most)
+      // positions of each tile of the piece; none where its page id was out of range
+      int valid[PT];
 #pragma unroll
-      for (int n = 0; n < NF; ++n) ldsm4(kf[n], chunk(kbase, 2 * n));
-      float sc[KT][4];
-      {
-        float part[KT][2][4];   // two chains of products each
+      for (int j = 0; j < PT; ++j)
+        valid[j] = (info.flags >> (4 + p * PT + j)) & 1 ? min(kTile, info.n - (p * PT + j) * kTile) : 0;
+      const bool partial = PT == 1 ? valid[0] < kTile : valid[0] + valid[PT - 1] < PT * kTile;
+      const uint32_t kbase = ring + s * C::kStageBytes + p * (PT * kTile * C::kBox) + k_lane;
+      const uint32_t vbase = ring + s * C::kStageBytes + C::kHalfBytes + p * (PT * kTile * C::kBox) + v_lane;
+      // 16-byte chunk c (even) of tile j past the lane's own: an XOR inside the 128-byte line, the next column behind it
+      auto chunk = [&](uint32_t base, int j, int c) -> uint32_t {
+        return (base ^ ((c % kPerRow) << 4)) + (c / kPerRow) * (kUnit * C::kBox) + j * (kTile * C::kBox);
+      };
+      // all fragments of K are asked for before the first product, those of V before the softmax
+      constexpr int NF = CACHE == D3_E4M3 ? KK / 2 : KK;   // ldmatrix per tile and operand
+      uint32_t kf[PT][NF][4], vf[PT][NF][4];
+#pragma unroll
+      for (int j = 0; j < PT; ++j)
+#pragma unroll
+        for (int n = 0; n < NF; ++n) ldsm4(kf[j][n], chunk(kbase, j, 2 * n));
+      constexpr int NC = PT * KT == 1 ? 2 : 1;   // chains of products that a score is summed in
+      float sc[PT][KT][NC][4];
+#pragma unroll
+      for (int j = 0; j < PT; ++j)
 #pragma unroll
         for (int i = 0; i < KT; ++i)
 #pragma unroll
-          for (int c = 0; c < 2; ++c) part[i][c][0] = part[i][c][1] = part[i][c][2] = part[i][c][3] = 0.f;
+          for (int c = 0; c < NC; ++c) sc[j][i][c][0] = sc[j][i][c][1] = sc[j][i][c][2] = sc[j][i][c][3] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int j = 0; j < PT; ++j) {
           uint32_t f[4];
           if constexpr (CACHE != D3_E4M3) {
-            f[0] = kf[kk][0]; f[1] = kf[kk][1]; f[2] = kf[kk][2]; f[3] = kf[kk][3];
+            f[0] = kf[j][kk][0]; f[1] = kf[j][kk][1]; f[2] = kf[j][kk][2]; f[3] = kf[j][kk][3];
           } else {   // chunk kk of positions 0-7 and of 8-15: four dims 4t.. of position g
-            const uint32_t x = kf[kk / 2][2 * (kk & 1)], y = kf[kk / 2][2 * (kk & 1) + 1];
+            const uint32_t x = kf[j][kk / 2][2 * (kk & 1)], y = kf[j][kk / 2][2 * (kk & 1) + 1];
             f[0] = widen(x); f[1] = widen(y); f[2] = widen(x >> 16); f[3] = widen(y >> 16);
           }
 #pragma unroll
           for (int i = 0; i < KT; ++i)
 #pragma unroll
-            for (int q = TQ - 1; q >= 0; --q) mma<F16>(part[i][kk & 1], f, qb[i][q][kk][0], qb[i][q][kk][1]);
+            for (int q = TQ - 1; q >= 0; --q) mma<F16>(sc[j][i][kk % NC], f, qb[i][q][kk][0], qb[i][q][kk][1]);
         }
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
+      for (int j = 0; j < PT; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[i][e] = part[i][0][e] + part[i][1][e];
-      }
-#pragma unroll
-      for (int n = 0; n < NF; ++n) ldsm4t(vf[n], chunk(vbase, 2 * n));
-      // ---- softmax of the piece: [0] head 2t, [1] head 2t + 1 of position g; [2], [3] of position g + 8
-      const bool partial = valid < kPiece;
-      uint32_t pb[KT][TP][2];
+        for (int n = 0; n < NF; ++n) ldsm4t(vf[j][n], chunk(vbase, j, 2 * n));
+      // ---- softmax of the piece: [0] head 2t, [1] head 2t + 1 of position g; [2], [3] of position g + 8 (of each tile)
+      uint32_t pb[PT][KT][TP][2];
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
-        float v[4];
+        float v[PT][4], cm[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = sc[i][e] * mul[i][e & 1];
-        if (partial) {
-          if (g >= valid) v[0] = v[1] = -INFINITY;
-          if (g + 8 >= valid) v[2] = v[3] = -INFINITY;
+        for (int j = 0; j < PT; ++j) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[j][e] = (NC == 2 ? sc[j][i][0][e] + sc[j][i][NC - 1][e] : sc[j][i][0][e]) * mul[i][e & 1];
+          if (partial) {
+            if (g >= valid[j]) v[j][0] = v[j][1] = -INFINITY;
+            if (g + 8 >= valid[j]) v[j][2] = v[j][3] = -INFINITY;
+          }
+          cm[0] = fmaxf(cm[0], fmaxf(v[j][0], v[j][2]));
+          cm[1] = fmaxf(cm[1], fmaxf(v[j][1], v[j][3]));
         }
-        float cm[2] = {fmaxf(v[0], v[2]), fmaxf(v[1], v[3])};
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
           cm[0] = fmaxf(cm[0], __shfl_xor_sync(0xffffffffu, cm[0], d));
@@ -733,51 +745,59 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
           for (int n = 0; n < KK; ++n) { o[i][n][0] *= c0; o[i][n][1] *= c1; o[i][n][2] *= c0; o[i][n][3] *= c1; }
         }
-        float pr[4];
+        float ref[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float m = mx[i][e & 1], ref = m == -INFINITY ? 0.f : (F16 ? m - 15.f : m);
-          pr[e] = exp2_fast(v[e] - ref);
-          sum[i][e & 1] += pr[e];
-        }
-        // P^T fragments: positions 2t, 2t + 1 (+ 8) of head g, the transpose of what this thread holds
+        for (int e = 0; e < 2; ++e) ref[e] = mx[i][e] == -INFINITY ? 0.f : (F16 ? mx[i][e] - 15.f : mx[i][e]);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float x = pr[2 * j], y = pr[2 * j + 1];
-          if constexpr (TP == 3) {
+        for (int j = 0; j < PT; ++j) {
+          float pr[4];
 #pragma unroll
-            for (int q = 0; q < 3; ++q) pb[i][q][j] = transpose8(cut(x, y));
-          } else {
-            const uint32_t hi = pack<F16>(x, y);
-            float hx, hy;
-            unpack<F16>(hi, hx, hy);
-            pb[i][0][j] = transpose8(hi);
-            pb[i][1][j] = transpose8(pack<F16>(x - hx, y - hy));
+          for (int e = 0; e < 4; ++e) {
+            pr[e] = exp2_fast(v[j][e] - ref[e & 1]);
+            sum[i][e & 1] += pr[e];
+          }
+          // P^T fragments: positions 2t, 2t + 1 (+ 8) of head g, the transpose of what this thread holds
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float x = pr[2 * r], y = pr[2 * r + 1];
+            if constexpr (TP == 3) {
+#pragma unroll
+              for (int q = 0; q < 3; ++q) pb[j][i][q][r] = transpose8(cut(x, y));
+            } else {
+              const uint32_t hi = pack<F16>(x, y);
+              float hx, hy;
+              unpack<F16>(hi, hx, hy);
+              pb[j][i][0][r] = transpose8(hi);
+              pb[j][i][1][r] = transpose8(pack<F16>(x - hx, y - hy));
+            }
           }
         }
       }
       // ---- O^T += V^T P^T.  What the page holds behind the row's end must not reach a product (0 x NaN is NaN).
-      uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
-      if (partial) {
-        keep0 = (2 * t < valid ? 0xffffu : 0u) | (2 * t + 1 < valid ? 0xffff0000u : 0u);
-        keep1 = (2 * t + 8 < valid ? 0xffffu : 0u) | (2 * t + 9 < valid ? 0xffff0000u : 0u);
-      }
 #pragma unroll
-      for (int n = 0; n < KK; ++n) {
-        uint32_t f[4];
-        if constexpr (CACHE != D3_E4M3) {   // dims 16n.. / +8 of positions 0-7, then of 8-15
-          f[0] = vf[n][0]; f[1] = vf[n][1]; f[2] = vf[n][2]; f[3] = vf[n][3];
-        } else {
-          // chunk n of positions 0-7 and of 8-15: positions 2t, 2t + 1 of dims 2g, 2g + 1.  Even dims make rows
-          // 0-7 of the product, odd ones rows 8-15
-          const uint32_t lo = __byte_perm(vf[n / 2][2 * (n & 1)], 0, 0x3120), hi = __byte_perm(vf[n / 2][2 * (n & 1) + 1], 0, 0x3120);
-          f[0] = widen(lo); f[1] = widen(lo >> 16); f[2] = widen(hi); f[3] = widen(hi >> 16);
+      for (int j = 0; j < PT; ++j) {
+        uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
+        if (partial) {
+          keep0 = (2 * t < valid[j] ? 0xffffu : 0u) | (2 * t + 1 < valid[j] ? 0xffff0000u : 0u);
+          keep1 = (2 * t + 8 < valid[j] ? 0xffffu : 0u) | (2 * t + 9 < valid[j] ? 0xffff0000u : 0u);
         }
-        if (partial) { f[0] &= keep0; f[1] &= keep0; f[2] &= keep1; f[3] &= keep1; }
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
+        for (int n = 0; n < KK; ++n) {
+          uint32_t f[4];
+          if constexpr (CACHE != D3_E4M3) {   // dims 16n.. / +8 of positions 0-7, then of 8-15
+            f[0] = vf[j][n][0]; f[1] = vf[j][n][1]; f[2] = vf[j][n][2]; f[3] = vf[j][n][3];
+          } else {
+            // chunk n of positions 0-7 and of 8-15: positions 2t, 2t + 1 of dims 2g, 2g + 1.  Even dims make rows
+            // 0-7 of the product, odd ones rows 8-15
+            const uint32_t lo = __byte_perm(vf[j][n / 2][2 * (n & 1)], 0, 0x3120), hi = __byte_perm(vf[j][n / 2][2 * (n & 1) + 1], 0, 0x3120);
+            f[0] = widen(lo); f[1] = widen(lo >> 16); f[2] = widen(hi); f[3] = widen(hi >> 16);
+          }
+          if (partial) { f[0] &= keep0; f[1] &= keep0; f[2] &= keep1; f[3] &= keep1; }
 #pragma unroll
-          for (int q = TP - 1; q >= 0; --q) mma<F16>(o[i][n], f, pb[i][q][0], pb[i][q][1]);
+          for (int i = 0; i < KT; ++i)
+#pragma unroll
+            for (int q = TP - 1; q >= 0; --q) mma<F16>(o[i][n], f, pb[j][i][q][0], pb[j][i][q][1]);
+        }
       }
     }
     __syncwarp();
@@ -922,7 +942,7 @@ int launch(const d3_paged_kv &kv, PagedAttnArgs a, cudaStream_t st) {
   TMap k, v, k16, v16;
   const int rows = kv.page_size < C::kUnit ? kv.page_size : C::kUnit;
   if (!encode_pool_map(&k, kv, kv.k_dev, rows) || !encode_pool_map(&v, kv, kv.v_dev, rows) ||
-      !encode_pool_map(&k16, kv, kv.k_dev, kPiece) || !encode_pool_map(&v16, kv, kv.v_dev, kPiece))
+      !encode_pool_map(&k16, kv, kv.k_dev, kTile) || !encode_pool_map(&v16, kv, kv.v_dev, kTile))
     return -1;
   const int merge = C::kWarps * a.heads_per_tile * C::kHeadFloats * (int)sizeof(float);
   int stages = (kSmemMost - 1024 - merge) / (C::kStageBytes + C::kQBytes);
