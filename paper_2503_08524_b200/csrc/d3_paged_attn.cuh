@@ -33,6 +33,7 @@
 #include <cuda_fp16.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "d3_paged.cuh"
 
@@ -156,26 +157,46 @@ __device__ __forceinline__ uint32_t cut(float &x, float &y) {
   return (a >> 16) | b;
 }
 
-// What the consumers tell the epilogue warps about an item.
-struct ItemInfo {
-  int row, tile, kind, final;
-};
-
-// x / y and the start of CTA i's share of U units among n, without a 64-bit division where 32 bits do
+// x / y, without a 64-bit division where 32 bits do
 __device__ __forceinline__ long long divide(long long x, int y) {
   return x < (1ll << 32) ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
 }
-__device__ __forceinline__ long long share(long long U, int i, int n) { return divide(U * i, n); }
+// How `total` cost is dealt out to n CTAs: the first `more` of them get each + 1, the others each.
+struct Shares {
+  long long each, more;
+  __device__ __forceinline__ Shares(long long total, int n) {
+    each = divide(total, n);
+    more = total - each * n;
+  }
+  __device__ __forceinline__ long long start(int i) const { return each * i + (i < more ? i : more); }
+  __device__ __forceinline__ int holder(long long x) const {   // the CTA that x belongs to
+    const long long edge = (each + 1) * more;
+    if (x < edge) return (int)(x / (each + 1));
+    return (int)(more + (x - edge) / each);
+  }
+};
+// Cost of an item (the pass over a row's positions for one tile of heads): kUnitCost per unit and kItemCost for its query
+// fragments and its sums.  The unit i of an item that starts at cost S belongs to the CTA that holds S + kItemCost +
+// kUnitCost * i.  With few units per CTA only units count, so that no CTA is left without one.
+constexpr int kUnitCost = 4, kItemCost = 3;
+struct Cost {
+  int unit, item;
+  __device__ __forceinline__ long long of(int units) const { return (long long)unit * units + item; }
+};
 
 enum { STAGE_FIRST = 1, STAGE_LAST = 2, STAGE_FINAL = 4 };   // of the item within this CTA; of the CTA
 // an item lies in this CTA / started before it / starts in it and goes on; no item at all
 enum { OUT_WHOLE = 0, OUT_HEAD = 1, OUT_TAIL = 2, OUT_NONE = 3 };
 
-// What the producer tells the consumers about a stage.
-struct StageInfo {
-  int row, tile;        // tile = kv head * tiles_per_head + tile of its query heads
-  int n;                // positions in the stage (0 .. kUnit)
-  int flags;            // STAGE_* | tiles that hold positions << 4 | OUT_* << 12
+// What the producers tell the consumers about a stage (one 16-byte load).
+struct __align__(16) StageInfo {
+  int row, head, kvh;   // head: the tile's first query head
+  uint32_t bits;        // positions in the stage (0 .. 128) | STAGE_* << 8 | OUT_* << 11 | heads of the tile << 13 | tiles that hold positions << 18
+};
+// What the consumers tell the epilogue warps about an item.
+struct __align__(16) ItemInfo {
+  int row, head, kvh;
+  uint32_t bits;        // OUT_* | last of the CTA << 2 | heads << 3 | first warp with a piece of it << 8 | such warps << 16
 };
 
 template <int DH, int CACHE, int X, int MT>
@@ -188,7 +209,8 @@ struct Cfg {
   static constexpr int kUnit = kRow > 128 ? 64 : 128;        // positions of a stage (of up to 32 KB)
   static constexpr int kPT = kRow > 128 ? 1 : 2;             // tiles of a piece, i.e. of a warp's trip (32 fragment registers)
   static constexpr int kHalfBytes = kUnit * kRow;            // K (or V) of a stage
-  static constexpr int kQBytes = kHeads * DH * QBytes<X>::v;
+  static constexpr int kQRow = DH * QBytes<X>::v + 16;       // a query head in shared memory (padded: no bank conflicts)
+  static constexpr int kQBytes = kHeads * kQRow;
   static constexpr int kStageBytes = 2 * kHalfBytes;
   // Registers are dealt out to four warps at a time: 16 warps of 128 (which 32 accumulator and 16 query registers fit
   // into), or 12 of 168 for 16 heads or three-term queries.
@@ -258,26 +280,31 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   };
   auto units_of = [&](int len) -> int { return len > 0 ? (len + kUnit - 1) / kUnit : 1; };   // a row without context still gets its zeros
   const bool few = a.n_rows <= kFewRows;
-  long long total = 0;
+  long long units = 0;   // of all rows, for one tile of heads
+  int live_rows = 0;
+  auto cost_of = [&](long long n) -> Cost {
+    return n * HG >= 4ll * gridDim.x ? Cost{kUnitCost, kItemCost} : Cost{1, 0};
+  };
   if (!few) {
     pdl_wait();
     pdl_trigger();
     const int per = (a.n_rows + C::kThreads - 1) / C::kThreads;
     long long mine = 0;
     bool bad = false;
+    int mine_rows = 0;
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
       if (b < a.n_rows) {
-        const int len = length_of(b, bad);   // (padding may hold anything)
-        bool strange = false;
-        if (row_of(b, strange) >= 0) mine += units_of(len);
-        else bad = false;
+        bool strange = false, unused = false;
+        if (row_of(b, strange) >= 0) { mine += units_of(length_of(b, strange)); ++mine_rows; }
+        else length_of(b, unused);   // (padding may hold anything)
         bad = bad || strange;
-        if (bad && blockIdx.x == 0 && a.status) *a.status = D3_EINVAL;
-        bad = false;
       }
     }
-    long long inc = mine;
+    if (bad && blockIdx.x == 0 && a.status) *a.status = D3_EINVAL;
+    // units in the upper, rows in the lower bits of one sum
+    long long inc = (mine << 17) | mine_rows;
+    const long long own_sum = inc;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const long long u = __shfl_up_sync(0xffffffffu, inc, d);
@@ -285,24 +312,27 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     }
     if (lane == 31) s_sum[warp] = inc;
     __syncthreads();
-    long long before = inc - mine;
+    long long before = inc - own_sum, all = 0;
     for (int w = 0; w < C::kThreads / 32; ++w) {
       const long long v = s_sum[w];
       if (w < warp) before += v;
-      total += v;
+      all += v;
     }
-    const long long U = total * HG;
-    const int n_cta = (int)(U < (long long)gridDim.x ? U : (long long)gridDim.x);
+    units = all >> 17;
+    live_rows = (int)(all & 0x1ffff);
+    const Cost cost = cost_of(units);
+    const int n_cta = (int)min(units * HG, (long long)gridDim.x);
     if ((int)blockIdx.x < n_cta) {
-      const long long t0 = divide(share(U, blockIdx.x, n_cta), HG);   // the first row is the one whose range of the sums holds t0
-      if (t0 >= before && t0 < before + mine) {
-        long long p = before;
-        for (int i = 0; i < per; ++i) {
+      const Shares sh((units * cost.unit + (long long)live_rows * cost.item) * HG, n_cta);
+      const long long x0 = sh.start(blockIdx.x);
+      long long p = ((before >> 17) * cost.unit + (before & 0x1ffff) * cost.item) * HG;
+      if (x0 >= p && x0 < p + (mine * cost.unit + (long long)mine_rows * cost.item) * HG) {
+        for (int i = 0; i < per; ++i) {   // the first row is the one whose range of the costs holds x0
           const int b = tid * per + i;
           bool dummy = false;
           if (b < a.n_rows && row_of(b, dummy) >= 0) {
-            const int n = units_of(length_of(b, dummy));
-            if (t0 < p + n) { s_start_row = b; s_start_before = p; break; }
+            const long long n = cost.of(units_of(length_of(b, dummy))) * HG;
+            if (x0 < p + n) { s_start_row = b; s_start_before = p; break; }
             p += n;
           }
         }
@@ -316,7 +346,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const int me = warp - C::kWarps - C::kEpilogue;
     bool dummy = false;
     int row, trow, len;
-    long long start_before;
+    long long start_before = 0;   // cost of the rows before the first one
     // few rows: their table rows and lengths stay in registers, row lane * per + i in entry i
     constexpr int kPer = kFewRows / 32;
     const int per = (a.n_rows + 31) / 32;
@@ -327,10 +357,10 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       for (int i = 1; i < kPer; ++i) x = at_entry == i ? v[i] : x;
       return __shfl_sync(0xffffffffu, x, at_lane);
     };
+    long long mine = 0, inc = 0;
     if (few) {
       pdl_wait();
       pdl_trigger();
-      long long mine = 0;
       bool bad = false;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
@@ -340,59 +370,70 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           bool strange = false;
           c_[i] = length_of(b, strange);
           r_[i] = row_of(b, bad);
-          if (r_[i] >= 0) { mine += units_of(c_[i]); bad = bad || strange; }
+          if (r_[i] >= 0) { mine += ((long long)units_of(c_[i]) << 17) | 1; bad = bad || strange; }
         }
       }
       if (bad && blockIdx.x == 0 && a.status) *a.status = D3_EINVAL;
-      long long inc = mine;
+      inc = mine;   // units in the upper, rows in the lower bits
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
         const long long u = __shfl_up_sync(0xffffffffu, inc, d);
         if (lane >= d) inc += u;
       }
-      total = __shfl_sync(0xffffffffu, inc, 31);
-      const long long U = total * HG;
-      const int n_cta = (int)(U < (long long)gridDim.x ? U : (long long)gridDim.x);
-      if ((int)blockIdx.x < n_cta) {
-        const long long t0 = divide(share(U, blockIdx.x, n_cta), HG);
-        long long p = inc - mine;
-        at_lane = __ffs(__ballot_sync(0xffffffffu, t0 >= p && t0 < inc)) - 1;
-        int entry = 0;
-        bool found = false;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const int n = r_[i] >= 0 ? units_of(c_[i]) : 0;
-          if (!found) {
-            if (t0 < p + n) { entry = i; found = true; }
-            else p += n;
-          }
-        }
-        at_entry = __shfl_sync(0xffffffffu, entry, at_lane);
-        start_before = __shfl_sync(0xffffffffu, p, at_lane);
-        row = at_lane * per + at_entry;
-        trow = kept(r_);
-        len = kept(c_);
-      }
-    } else {
-      row = s_start_row;
-      start_before = s_start_before;
-      if (row < a.n_rows) { trow = row_of(row, dummy); len = length_of(row, dummy); }
+      const long long all = __shfl_sync(0xffffffffu, inc, 31);
+      units = all >> 17;
+      live_rows = (int)(all & 0x1ffff);
     }
-    const long long U = total * HG;
-    const int n_cta = (int)(U < (long long)gridDim.x ? U : (long long)gridDim.x);   // every one of them has work
+    const int n_cta = (int)min(units * HG, (long long)gridDim.x);   // every one of them has work
     if ((int)blockIdx.x >= n_cta) {
       if (me == 0 && lane == 0) {
         a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
-        s_info[0] = StageInfo{0, 0, 0, STAGE_LAST | STAGE_FINAL | (OUT_NONE << 12)};
+        s_info[0] = StageInfo{0, 0, 0, (uint32_t)((STAGE_LAST | STAGE_FINAL) << 8 | OUT_NONE << 11)};
         mb_arrive(smem_u32(&s_full[0]));
       }
       return;
     }
-    const long long u0 = share(U, blockIdx.x, n_cta), u1 = share(U, blockIdx.x + 1, n_cta);
-    int nu = units_of(len);
-    const long long at = u0 - start_before * HG;     // unit inside the row's (tile, unit) range
-    int tile = (int)divide(at, nu), unit = (int)(at - (long long)tile * nu);
-    int kvh = tile / a.tiles_per_head, sub = tile % a.tiles_per_head;
+    const Cost cost = cost_of(units);
+    const Shares sh((units * cost.unit + (long long)live_rows * cost.item) * HG, n_cta);
+    const long long x0 = sh.start(blockIdx.x), x1 = sh.start(blockIdx.x + 1);
+    if (few) {
+      auto cost_sum = [&](long long v) -> long long { return ((v >> 17) * cost.unit + (v & 0x1ffff) * cost.item) * HG; };
+      long long p = cost_sum(inc - mine);
+      at_lane = __ffs(__ballot_sync(0xffffffffu, x0 >= p && x0 < cost_sum(inc))) - 1;
+      int entry = 0;
+      bool found = false;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const long long n = r_[i] >= 0 ? cost.of(units_of(c_[i])) * HG : 0;
+        if (!found) {
+          if (x0 < p + n) { entry = i; found = true; }
+          else p += n;
+        }
+      }
+      at_entry = __shfl_sync(0xffffffffu, entry, at_lane);
+      start_before = __shfl_sync(0xffffffffu, p, at_lane);
+      row = at_lane * per + at_entry;
+      trow = kept(r_);
+      len = kept(c_);
+    } else {
+      row = s_start_row;
+      start_before = s_start_before;
+      trow = row_of(row, dummy);
+      len = length_of(row, dummy);
+    }
+    int nu = units_of(len), tile, unit;
+    long long item;        // cost at which the item starts
+    bool behind;           // no unit of that item is this CTA's: begin with the next one
+    {
+      const long long at = x0 - start_before, one = cost.of(nu);
+      tile = one < (1ll << 31) ? (int)divide(at, (int)one) : (int)(at / one);
+      item = start_before + tile * one;
+      const long long in = x0 - item - cost.item;
+      unit = in <= 0 ? 0 : (int)((in + cost.unit - 1) / cost.unit);
+      behind = unit >= nu;
+    }
+    int kvh = tile, sub = 0;
+    if (a.tiles_per_head > 1) { kvh = tile / a.tiles_per_head; sub = tile % a.tiles_per_head; }
     const int32_t *pages = a.table + (long long)trow * a.table_stride;
     auto fetch = [&](int base) -> int { return base + lane < a.table_width ? __ldg(pages + base + lane) : -1; };
     // page ids of the row, one per lane: 32 aligned pages in `win`, the next 32 in `win_next`.  A unit is at most 8
@@ -403,11 +444,39 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     int s = 0, issued = 0;
     uint32_t parity = 1;
     bool first = true, ok = true;
-    const int n_units = (int)(u1 - u0);
-    int left = n_units;
-    long long item = u0 - unit;        // where the item's units start
-    for (int k = 0; k < n_units; ++k, --left) {
-      const bool last = left == 1 || unit + 1 == nu;
+    auto next_item = [&]() {   // next tile of the row, or next row
+      unit = 0;
+      item += cost.of(nu);
+      if (win0 > 0) win0 = -1;   // (a row's first window serves its next tile too)
+      ++tile;
+      if (++sub == a.tiles_per_head) { sub = 0; ++kvh; }
+      if (tile == HG) {
+        tile = kvh = 0;
+        win0 = -1;
+        do {
+          ++row;
+          if (++at_entry == per) { at_entry = 0; ++at_lane; }
+          trow = row >= a.n_rows ? 0 : few ? kept(r_) : row_of(row, dummy);
+        } while (trow < 0);
+        len = row >= a.n_rows ? 0 : few ? kept(c_) : length_of(row, dummy);
+        nu = units_of(len);
+        pages = a.table + (long long)trow * a.table_stride;
+      }
+    };
+    if (behind) next_item();
+    long long at = item + cost.item + (long long)cost.unit * unit;   // of the unit
+    int cut_row = -1, cut_head = 0, cut_kvh = 0, cut_nh = 0;         // the item that goes on in the next CTA, if it starts here
+    long long cut_last = 0;
+    for (int k = 0; at < x1; ++k) {
+      const bool ends = unit + 1 == nu;
+      const long long next = ends ? at + cost.unit + cost.item : at + cost.unit;
+      const bool last = ends || next >= x1, final = next >= x1;
+      const int nh = min(a.heads_per_tile, a.group - sub * a.heads_per_tile), head = kvh * a.group + sub * a.heads_per_tile;
+      const bool whole_start = item + cost.item >= x0;      // its unit 0 is this CTA's
+      if (last && !ends && whole_start) {
+        cut_row = row; cut_head = head; cut_kvh = kvh; cut_nh = nh;
+        cut_last = item + cost.item + (long long)cost.unit * (nu - 1);
+      }
       if ((k & (kProducers - 1)) == me) {
         const int p0 = unit * kUnit, n = max(0, min(kUnit, len - p0));   // n = 0 only for a row without context
         const int pg0 = p0 >> a.page_shift;
@@ -435,16 +504,11 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         const uint32_t full = smem_u32(&s_full[s]);
-        const int nh = min(a.heads_per_tile, a.group - sub * a.heads_per_tile);
         if (lane == 0) {
-          StageInfo info;
-          info.row = row; info.tile = tile; info.n = n;
-          int kind = OUT_WHOLE;
-          if (last && unit + 1 < nu) kind = item >= u0 ? OUT_TAIL : OUT_HEAD;   // the item goes on in the next CTA
-          else if (last && item < u0) kind = OUT_HEAD;                          // its last piece
-          info.flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (left == 1 ? STAGE_FINAL : 0) | (int)(tiles << 4) | (kind << 12);
-          s_info[s] = info;
-          mb_arrive_tx(full, (uint32_t)__popc(tiles) * 2u * kTile * C::kRow + (first ? (uint32_t)nh * DH * QBytes<X>::v : 0u));
+          const int kind = !last || (ends && whole_start) ? OUT_WHOLE : !ends && whole_start ? OUT_TAIL : OUT_HEAD;
+          const int flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (final ? STAGE_FINAL : 0);
+          s_info[s] = StageInfo{row, head, kvh, (uint32_t)n | (uint32_t)flags << 8 | (uint32_t)kind << 11 | (uint32_t)nh << 13 | tiles << 18};
+          mb_arrive_tx(full, (uint32_t)__popc(tiles) * 2u * kTile * C::kRow + (first ? (uint32_t)(nh * DH * QBytes<X>::v) : 0u));
         }
         __syncwarp();
         if (want) {
@@ -453,40 +517,22 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           tma_box(dst, map, col * (C::kBox / C::kEs), pos & page_mask, kvh, id, full);
         }
         if (first && lane < nh) {
-          const long long h = (long long)kvh * a.group + sub * a.heads_per_tile + lane;
-          bulk_copy(smem_u32(q_slots) + s * C::kQBytes + lane * DH * QBytes<X>::v,
-                    static_cast<const char *>(a.q) + (row * a.q_row_stride + h * a.q_head_stride) * QBytes<X>::v, DH * QBytes<X>::v, full);
+          bulk_copy(smem_u32(q_slots) + s * C::kQBytes + lane * C::kQRow,
+                    static_cast<const char *>(a.q) + (row * a.q_row_stride + (head + lane) * a.q_head_stride) * QBytes<X>::v,
+                    DH * QBytes<X>::v, full);
         }
       }
       issued = k + 1;
       first = last;
       if (++s == S) { s = 0; parity ^= 1u; }
-      if (++unit == nu && left > 1) {   // next tile of the row, or next row
-        unit = 0; win0 = -1;
-        item += nu;
-        ++tile;
-        if (++sub == a.tiles_per_head) { sub = 0; ++kvh; }
-        if (tile == HG) {
-          tile = kvh = 0;
-          do {
-            ++row;
-            if (++at_entry == per) { at_entry = 0; ++at_lane; }
-            trow = row >= a.n_rows ? 0 : few ? kept(r_) : row_of(row, dummy);
-          } while (trow < 0);
-          len = row >= a.n_rows ? 0 : few ? kept(c_) : length_of(row, dummy);
-          nu = units_of(len);
-          pages = a.table + (long long)trow * a.table_stride;
-        }
-      }
+      ++unit;
+      if (ends && !final) next_item();
+      at = next;
     }
     if (me == 0 && lane == 0) {
-      // the last item, if it starts here and goes on: what the joining kernel adds up
+      // an item that starts here and goes on: what the joining kernel adds up
       int4 join = make_int4(0, 0, 0, 0);
-      if (ok && unit < nu && item >= u0) {   // (unit counts the units passed)
-        const long long end = item + nu;     // CTAs up to the one that holds unit end - 1
-        const long long x = end * n_cta + U - 1;
-        join = make_int4((int)(U < (1ll << 31) ? divide(x, (int)U) : x / U) - (int)blockIdx.x, row, tile, 0);
-      }
+      if (ok && cut_row >= 0) join = make_int4(sh.holder(cut_last) - (int)blockIdx.x + 1, cut_row, cut_head, cut_kvh | cut_nh << 16);
       a.join[blockIdx.x] = join;
     }
     if (!ok) {   // copies in flight end by themselves: wait for them before the shared memory goes
@@ -512,56 +558,82 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       if (!__all_sync(0xffffffffu, mb_wait(smem_u32(&s_sums_full), parity, &s_abort, a.wait_ns))) break;
       if (parity == 0u) pdl_wait();   // returns at once: the producers' has
       const ItemInfo item = s_item;
-      if (item.kind == OUT_NONE) break;
-      const int kvh = item.tile / a.tiles_per_head, g0 = (item.tile % a.tiles_per_head) * a.heads_per_tile;
-      const int nh = min(a.heads_per_tile, a.group - g0);
-      for (int h = me; h < nh; h += C::kEpilogue) {
-        const float l = lane < C::kWarps ? s_l[lane][h] : 0.f;
-        const float m = lane < C::kWarps ? s_m[lane][h] : -INFINITY;
-        float M = m;
+      const int kind = item.bits & 3, nh = (item.bits >> 3) & 31, first_warp = (item.bits >> 8) & 255, warps = item.bits >> 16;
+      if (kind == OUT_NONE) break;
+      int from = first_warp + min(lane, warps - 1);   // lane k: the k-th warp that had a piece of the item
+      if (from >= C::kWarps) from -= C::kWarps;
+      const float vs = a.v_scale ? __ldg(a.v_scale + item.kvh) : 1.f;
+      // HB heads at a time, in independent chains: this is all latency
+      auto heads = [&](auto hb, int h0) {
+        constexpr int HB = decltype(hb)::value;
+        float M[HB], L[HB], c[HB], o[HB][V];
 #pragma unroll
-        for (int d = 8; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-        M = __shfl_sync(0xffffffffu, M, 0);
-        // a warp that had no position of the item counts with factor 0, whatever lies in its sums
-        const float c = l != 0.f ? exp2_fast(m - (M == -INFINITY ? 0.f : M)) : 0.f;
-        float L = l != 0.f ? l * c : 0.f;
-#pragma unroll
-        for (int d = 8; d; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
-        L = __shfl_sync(0xffffffffu, L, 0);
-        const unsigned took_part = __ballot_sync(0xffffffffu, l != 0.f);
-        float o[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = 0.f;
-#pragma unroll
-        for (int w = 0; w < C::kWarps; ++w) {
-          const float cw = __shfl_sync(0xffffffffu, c, w);
-          const float *src = s_o + (w * a.heads_per_tile + h) * C::kHeadFloats + lane * V;
-          const uint32_t there = 0u - (took_part >> w & 1u);   // a mask: sums that were not written may be anything
-          uint32_t x[V];
-          if constexpr (V == 4) { const uint4 v = *reinterpret_cast<const uint4 *>(src); x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
-          else if constexpr (V == 2) { const uint2 v = *reinterpret_cast<const uint2 *>(src); x[0] = v.x; x[1] = v.y; }
-          else x[0] = *reinterpret_cast<const uint32_t *>(src);
-#pragma unroll
-          for (int e = 0; e < V; ++e) o[e] += cw * __uint_as_float(x[e] & there);
+        for (int i = 0; i < HB; ++i) {
+          const int h = min(h0 + i * C::kEpilogue, nh - 1);
+          L[i] = lane < warps ? s_l[from][h] : 0.f;
+          c[i] = lane < warps ? s_m[from][h] : -INFINITY;
+          M[i] = c[i];
         }
-        const long long head = (long long)kvh * a.group + g0 + h;
-        if (item.kind == OUT_WHOLE) {
-          const float f = L == 0.f ? 0.f : (a.v_scale ? __ldg(a.v_scale + kvh) : 1.f) / L;
-          const long long at = item.row * a.out_row_stride + head * a.out_head_stride + lane * V;
 #pragma unroll
-          for (int e = 0; e < V; ++e) write_out(at + e, o[e] * f);
-          if (lane == 0 && a.lse)
-            a.lse[(long long)item.row * a.hq + head] = L == 0.f ? -INFINITY : (M + (log2f(L) - (F16 ? 15.f : 0.f))) * kLn2;
-        } else {
-          const size_t part = (size_t)(2 * blockIdx.x + (item.kind == OUT_TAIL ? 1 : 0)) * 16 + h;
+        for (int d = 8; d; d >>= 1)
 #pragma unroll
-          for (int e = 0; e < V; ++e) a.part_o[part * DH + lane * V + e] = o[e];
-          if (lane == 0) { a.part_ml[2 * part] = M; a.part_ml[2 * part + 1] = L; }
+          for (int i = 0; i < HB; ++i) M[i] = fmaxf(M[i], __shfl_xor_sync(0xffffffffu, M[i], d));
+#pragma unroll
+        for (int i = 0; i < HB; ++i) {
+          c[i] = exp2_fast(c[i] - (M[i] == -INFINITY ? 0.f : M[i]));   // 0 beyond the warps that had pieces
+          L[i] *= c[i];
+#pragma unroll
+          for (int e = 0; e < V; ++e) o[i][e] = 0.f;
         }
-      }
+#pragma unroll
+        for (int d = 8; d; d >>= 1)
+#pragma unroll
+          for (int i = 0; i < HB; ++i) L[i] += __shfl_xor_sync(0xffffffffu, L[i], d);
+        // groups of the warps; what is past the last one counts as that one with factor 0
+        constexpr int GR = HB == 1 ? 4 : 2;
+        for (int k = 0; k < warps; k += GR) {
+#pragma unroll
+          for (int j = 0; j < GR; ++j) {
+            const int w = __shfl_sync(0xffffffffu, from, k + j);
+#pragma unroll
+            for (int i = 0; i < HB; ++i) {
+              const int h = min(h0 + i * C::kEpilogue, nh - 1);
+              const float cw = __shfl_sync(0xffffffffu, c[i], k + j);
+              const float *src = s_o + (w * a.heads_per_tile + h) * C::kHeadFloats + lane * V;
+              float x[V];
+              if constexpr (V == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+              else if constexpr (V == 2) { const float2 v = *reinterpret_cast<const float2 *>(src); x[0] = v.x; x[1] = v.y; }
+              else x[0] = *src;
+#pragma unroll
+              for (int e = 0; e < V; ++e) o[i][e] += cw * x[e];
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < HB; ++i) {
+          const int h = h0 + i * C::kEpilogue;
+          if (h >= nh) break;
+          const float l = __shfl_sync(0xffffffffu, L[i], 0), m = __shfl_sync(0xffffffffu, M[i], 0);
+          if (kind == OUT_WHOLE) {
+            const float f = l == 0.f ? 0.f : vs / l;
+            const long long at = item.row * a.out_row_stride + (long long)(item.head + h) * a.out_head_stride + lane * V;
+#pragma unroll
+            for (int e = 0; e < V; ++e) write_out(at + e, o[i][e] * f);
+            if (lane == 0 && a.lse)
+              a.lse[(long long)item.row * a.hq + item.head + h] = l == 0.f ? -INFINITY : (m + (log2f(l) - (F16 ? 15.f : 0.f))) * kLn2;
+          } else {
+            const size_t part = (size_t)(2 * blockIdx.x + (kind == OUT_TAIL ? 1 : 0)) * 16 + h;
+#pragma unroll
+            for (int e = 0; e < V; ++e) a.part_o[part * DH + lane * V + e] = o[i][e];
+            if (lane == 0) { a.part_ml[2 * part] = m; a.part_ml[2 * part + 1] = l; }
+          }
+        }
+      };
+      if (nh <= C::kEpilogue) { if (me < nh) heads(std::integral_constant<int, 1>(), me); }
+      else for (int h0 = me; h0 < nh; h0 += 4 * C::kEpilogue) heads(std::integral_constant<int, 4>(), h0);
       __syncwarp();
       if (lane == 0) mb_arrive(smem_u32(&s_sums_free));
-      if (item.final) break;
+      if (item.bits & 4) break;
     }
     return;
   }
@@ -591,6 +663,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   int piece_turn = 0;       // pieces of the CTA so far, mod kWarps: whose turn it is
   int items = 0;
   bool ok = true;
+  int first_warp = 0, item_pieces = 0;   // of the running item: whose its first piece was, and how many there were
   int s = 0;
   uint32_t parity = 0;
   for (bool more = true; more;) {
@@ -598,18 +671,20 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     ok = __all_sync(0xffffffffu, ok);
     if (!ok) break;
     const StageInfo info = s_info[s];
-    more = !(info.flags & STAGE_FINAL);
-    if (info.flags & STAGE_FIRST) {
+    const uint32_t flags = info.bits >> 8;
+    const int n = info.bits & 255;
+    more = !(flags & STAGE_FINAL);
+    if (flags & STAGE_FIRST) {
       if (items == 0) pdl_wait();   // returns at once: the producers' has
       // ---- this thread's fragments of Q, and what a raw score is multiplied by
-      const int kvh = info.tile / a.tiles_per_head, g0 = (info.tile % a.tiles_per_head) * a.heads_per_tile;
-      const int nh = min(a.heads_per_tile, a.group - g0);
-      const float ks = a.k_scale ? __ldg(a.k_scale + kvh) : 1.f;
+      const int nh = (info.bits >> 13) & 31;
+      first_warp = piece_turn; item_pieces = 0;
+      const float ks = a.k_scale ? __ldg(a.k_scale + info.kvh) : 1.f;
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
         const int h = g + 8 * i;
         const bool live = h < nh;
-        const unsigned char *qp = q_slots + (size_t)s * C::kQBytes + (size_t)(live ? h : 0) * DH * QBytes<X>::v;
+        const unsigned char *qp = q_slots + s * C::kQBytes + (live ? h : 0) * C::kQRow;
         float factor = a.scale * kLog2e * ks;
         if constexpr (X == D3_FP32) {
 #pragma unroll
@@ -662,7 +737,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         mul[i][1] = __shfl_sync(0xffffffffu, factor, 8 * t + 4);
       }
     }
-    const int n_pieces = (info.n + PT * kTile - 1) / (PT * kTile);
+    const int n_pieces = (n + PT * kTile - 1) / (PT * kTile);
+    item_pieces += n_pieces;
     // pieces go round the warps
     int p = warp - piece_turn;
     if (p < 0) p += C::kWarps;
@@ -673,7 +749,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       int valid[PT];
 #pragma unroll
       for (int j = 0; j < PT; ++j)
-        valid[j] = (info.flags >> (4 + p * PT + j)) & 1 ? min(kTile, info.n - (p * PT + j) * kTile) : 0;
+        valid[j] = (info.bits >> (18 + p * PT + j)) & 1 ? min(kTile, n - (p * PT + j) * kTile) : 0;
       const bool partial = PT == 1 ? valid[0] < kTile : valid[0] + valid[PT - 1] < PT * kTile;
       const uint32_t kbase = ring + s * C::kStageBytes + p * (PT * kTile * C::kBox) + k_lane;
       const uint32_t vbase = ring + s * C::kStageBytes + C::kHalfBytes + p * (PT * kTile * C::kBox) + v_lane;
@@ -687,7 +763,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
       for (int j = 0; j < PT; ++j)
 #pragma unroll
-        for (int n = 0; n < NF; ++n) ldsm4(kf[j][n], chunk(kbase, j, 2 * n));
+        for (int c = 0; c < NF; ++c) ldsm4(kf[j][c], chunk(kbase, j, 2 * c));
       constexpr int NC = PT * KT == 1 ? 2 : 1;   // chains of products that a score is summed in
       float sc[PT][KT][NC][4];
 #pragma unroll
@@ -715,7 +791,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
       for (int j = 0; j < PT; ++j)
 #pragma unroll
-        for (int n = 0; n < NF; ++n) ldsm4t(vf[j][n], chunk(vbase, j, 2 * n));
+        for (int c = 0; c < NF; ++c) ldsm4t(vf[j][c], chunk(vbase, j, 2 * c));
       // ---- softmax of the piece: [0] head 2t, [1] head 2t + 1 of position g; [2], [3] of position g + 8 (of each tile)
       uint32_t pb[PT][KT][TP][2];
 #pragma unroll
@@ -804,22 +880,23 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (lane == 0) mb_arrive(smem_u32(&s_empty[s]));
     if (++s == S) { s = 0; parity ^= 1u; }
 
-    if (info.flags & STAGE_LAST) {
+    if (flags & STAGE_LAST) {
       // ---- the item's end in this CTA: this warp's sums to shared memory, for the epilogue warps to add up
       if (items > 0 && !mb_wait(smem_u32(&s_sums_free), (uint32_t)((items - 1) & 1), &s_abort, a.wait_ns)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
+      const int warps = min(item_pieces, C::kWarps), turn = warp - first_warp + (warp < first_warp ? C::kWarps : 0);
+      if (turn < warps) {
 #pragma unroll
-      for (int i = 0; i < KT; ++i) {
+        for (int i = 0; i < KT; ++i) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int h = 2 * t + e + 8 * i;
-          float l = sum[i][e];
+          for (int e = 0; e < 2; ++e) {
+            const int h = 2 * t + e + 8 * i;
+            float l = sum[i][e];
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-          if (h < a.heads_per_tile) {
-            float *dst = s_o + (warp * a.heads_per_tile + h) * C::kHeadFloats;
-            if (l != 0.f) {
+            for (int d = 4; d < 32; d <<= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+            if (h < a.heads_per_tile) {
+              float *dst = s_o + (warp * a.heads_per_tile + h) * C::kHeadFloats;
 #pragma unroll
               for (int n = 0; n < KK; ++n) {
                 if constexpr (CACHE == D3_E4M3) {
@@ -829,15 +906,17 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                   dst[16 * n + 8 + g] = o[i][n][2 + e];
                 }
               }
+              if (g == 0) { s_m[warp][h] = mx[i][e]; s_l[warp][h] = l; }
             }
-            if (g == 0) { s_m[warp][h] = mx[i][e]; s_l[warp][h] = l; }
+            mx[i][e] = -INFINITY; sum[i][e] = 0.f;
           }
-          mx[i][e] = -INFINITY; sum[i][e] = 0.f;
-        }
 #pragma unroll
-        for (int n = 0; n < KK; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+          for (int n = 0; n < KK; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+        }
       }
-      if (warp == 0 && lane == 0) s_item = ItemInfo{info.row, info.tile, (info.flags >> 12) & 3, !more};
+      if (warp == 0 && lane == 0)
+        s_item = ItemInfo{info.row, info.head, info.kvh,
+                          ((flags >> 3) & 3) | (more ? 0u : 4u) | ((info.bits >> 13) & 31) << 3 | (uint32_t)first_warp << 8 | (uint32_t)warps << 16};
       __syncwarp();
       if (lane == 0) mb_arrive(smem_u32(&s_sums_full));
       ++items;
@@ -858,9 +937,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_join(const __grid_con
   pdl_trigger();
   const int4 job = a.join[blockIdx.x];
   if (job.x == 0) return;
-  const int parts = job.x, row = job.y, tile = job.z;
-  const int kvh = tile / a.tiles_per_head, g0 = (tile % a.tiles_per_head) * a.heads_per_tile;
-  const int nh = min(a.heads_per_tile, a.group - g0);
+  const int parts = job.x, row = job.y, kvh = job.w & 0xffff, nh = job.w >> 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int share_of = kJoinWarps / nh, h = warp / share_of, first = warp % share_of;   // warps from nh * share_of on are idle
   const bool busy = h < nh;
@@ -923,7 +1000,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_join(const __grid_con
     for (int e = 0; e < V; ++e) o[e] += s_o[warp + w][lane * V + e] * c;
   }
   const float f = L == 0.f ? 0.f : (a.v_scale ? __ldg(a.v_scale + kvh) : 1.f) / L;
-  const long long head = (long long)kvh * a.group + g0 + h;
+  const long long head = job.z + h;
   const long long at = row * a.out_row_stride + head * a.out_head_stride + lane * V;
 #pragma unroll
   for (int e = 0; e < V; ++e) {
