@@ -29,7 +29,7 @@ EXPORTS = ("d3_depth", "d3_schedule", "d3_workspace_bytes", "d3_load", "d3_prefi
            "d3_decode_step_noalloc", "d3_noalloc_status", "d3_set_policy", "d3_set_wait_ns",
            "d3_stall_next_step", "d3_slot_pos",
            "d3_kv_pages_used", "d3_reset_slot", "d3_sync", "d3_free", "d3_strerror",
-           "d3_page_plan", "d3_paged_append", "d3_rope_table", "d3_paged_attention",
+           "d3_paged_maps", "d3_page_plan", "d3_paged_append", "d3_rope_table", "d3_paged_attention",
            "d3_paged_attention_workspace", "d3_paged_view")
 
 
@@ -101,6 +101,7 @@ def _load() -> C.CDLL:
     lib.d3_strerror.argtypes = [I32]
     lib.d3_strerror.restype = C.c_char_p
     # paged key-value operators: the argument structs are in paged.py
+    lib.d3_paged_maps.argtypes = [P, P]
     lib.d3_page_plan.argtypes = [P, P]
     lib.d3_paged_append.argtypes = [P, P, P]
     lib.d3_rope_table.argtypes = [I32, I32, C.c_float, P, P]

@@ -454,21 +454,31 @@ AttnWorkspace attn_workspace(int dh) {
 
 }  // namespace
 
-bool encode_pool_map(TMap *out, const d3_paged_kv &kv, void *base, int box_rows) {
+bool encode_pool_maps(PoolMaps *out, const d3_paged_kv &kv) {
   EncodeTiledFn fn = pool_encoder();
   if (!fn) return false;
   const int es = bytes_of(kv.dtype), row = kv.head_dim * es, box_bytes = row < 128 ? row : 128;
+  const int unit = unit_positions(kv.head_dim, es), rows = kv.page_size < unit ? kv.page_size : unit;
   cuuint64_t dims[4] = {(cuuint64_t)kv.head_dim, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};
   cuuint64_t strides[3] = {(cuuint64_t)(kv.token_stride * es), (cuuint64_t)(kv.head_stride * es),
                            (cuuint64_t)(kv.page_stride * es)};
-  cuuint32_t box[4] = {(cuuint32_t)(box_bytes / es), (cuuint32_t)box_rows, 1, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
   const CUtensorMapDataType type = kv.dtype == D3_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                    : kv.dtype == D3_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
   const CUtensorMapSwizzle sw = box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B
                                 : box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
-  return fn(reinterpret_cast<CUtensorMap *>(out), type, 4, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  auto encode = [&](TMap *m, void *base, int box_rows) {
+    cuuint32_t box[4] = {(cuuint32_t)(box_bytes / es), (cuuint32_t)box_rows, 1, 1};
+    return fn(reinterpret_cast<CUtensorMap *>(m), type, 4, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  if (!encode(&out->k, kv.k_dev, rows) || !encode(&out->v, kv.v_dev, rows)) return false;
+  if (rows == 16) { out->k16 = out->k; out->v16 = out->v; }
+  else if (!encode(&out->k16, kv.k_dev, 16) || !encode(&out->v16, kv.v_dev, 16)) return false;
+  out->of = kv;
+  out->of.maps = nullptr;
+  out->of.k_scale_dev = out->of.v_scale_dev = nullptr;
+  return true;
 }
 
 }  // namespace d3
@@ -476,6 +486,11 @@ bool encode_pool_map(TMap *out, const d3_paged_kv &kv, void *base, int box_rows)
 using namespace d3;
 
 extern "C" {
+
+int32_t d3_paged_maps(const d3_paged_kv *kv, void *maps) {
+  if (!kv_ok(kv, true) || !maps || ((uintptr_t)maps & 63)) return D3_EINVAL;
+  return encode_pool_maps(static_cast<PoolMaps *>(maps), *kv) ? D3_OK : D3_ECUDA;
+}
 
 int32_t d3_page_plan(const d3_page_plan_args *a, void *cuda_stream) {
   if (!a || a->struct_size != sizeof(d3_page_plan_args)) return D3_EINVAL;
@@ -611,7 +626,21 @@ int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args 
     return D3_EINVAL;
   const AttnWorkspace w = attn_workspace(dh);
   if (!a->workspace_dev || ((uintptr_t)a->workspace_dev & 255) || a->workspace_bytes < w.total) return D3_EINVAL;
+  const PoolMaps *maps = static_cast<const PoolMaps *>(kv->maps);
+  if (maps) {   // made for this pool?
+    const d3_paged_kv &o = maps->of;
+    if (((uintptr_t)maps & 63) || o.struct_size != kv->struct_size || o.dtype != kv->dtype || o.n_pages != kv->n_pages ||
+        o.page_size != kv->page_size || o.n_kv_heads != kv->n_kv_heads || o.head_dim != kv->head_dim ||
+        o.page_stride != kv->page_stride || o.head_stride != kv->head_stride || o.token_stride != kv->token_stride ||
+        o.k_dev != kv->k_dev || o.v_dev != kv->v_dev)
+      return D3_EINVAL;
+  }
   if (a->n_rows == 0) return D3_OK;
+  PoolMaps fresh;
+  if (!maps) {
+    if (!encode_pool_maps(&fresh, *kv)) return D3_ECUDA;
+    maps = &fresh;
+  }
   PagedAttnArgs p;
   memset(&p, 0, sizeof(p));
   p.n_rows = a->n_rows; p.hq = a->n_q_heads; p.hkv = kv->n_kv_heads; p.group = a->n_q_heads / kv->n_kv_heads;
@@ -632,9 +661,9 @@ int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args 
   p.status = a->status_dev;
   p.wait_ns = 2000000000ull;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int rc = dh == 128 ? launch_paged_attention_128(*kv, p, a->dtype, st)
-                 : dh == 64 ? launch_paged_attention_64(*kv, p, a->dtype, st)
-                            : launch_paged_attention_32(*kv, p, a->dtype, st);
+  const int rc = dh == 128 ? launch_paged_attention_128(*maps, p, a->dtype, st)
+                 : dh == 64 ? launch_paged_attention_64(*maps, p, a->dtype, st)
+                            : launch_paged_attention_32(*maps, p, a->dtype, st);
   return rc == 0 && cudaGetLastError() == cudaSuccess ? D3_OK : D3_ECUDA;
 }
 

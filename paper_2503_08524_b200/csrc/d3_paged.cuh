@@ -52,9 +52,16 @@ inline KvPool pool_of(const d3_paged_kv &kv) {
   return p;
 }
 
-// tensor map of a pool's K or V (encoded by the driver; false when it refuses or is absent):
-// (dim, position, kv head, page), boxes of box_rows positions x min(128 bytes, a row)
-bool encode_pool_map(TMap *out, const d3_paged_kv &kv, void *base, int box_rows);
+// Positions of a unit, the attention kernel's stage: up to 32 KB of K and V.
+__host__ __device__ constexpr int unit_positions(int head_dim, int elem_bytes) { return head_dim * elem_bytes > 128 ? 64 : 128; }
+// Tensor maps of a pool: (dim, position, kv head, page), boxes of min(128 bytes, a row) x up to a page's or a unit's
+// positions (k, v) and x 16 positions (k16, v16); `of` is the pool they were made for.
+struct PoolMaps {
+  TMap k, v, k16, v16;
+  d3_paged_kv of;
+};
+static_assert(sizeof(PoolMaps) <= D3_PAGED_MAPS_BYTES, "room for the maps");
+bool encode_pool_maps(PoolMaps *out, const d3_paged_kv &kv);   // false when the driver refuses or has no encoder
 
 // What the attention launch gets (device pointers; strides in elements).
 struct PagedAttnArgs {
@@ -75,8 +82,8 @@ struct PagedAttnArgs {
   unsigned long long wait_ns;
 };
 // one translation unit per head dimension (each compiles every type pair)
-int launch_paged_attention_32(const d3_paged_kv &kv, const PagedAttnArgs &a, int x, cudaStream_t st);
-int launch_paged_attention_64(const d3_paged_kv &kv, const PagedAttnArgs &a, int x, cudaStream_t st);
-int launch_paged_attention_128(const d3_paged_kv &kv, const PagedAttnArgs &a, int x, cudaStream_t st);
+int launch_paged_attention_32(const PoolMaps &m, const PagedAttnArgs &a, int x, cudaStream_t st);
+int launch_paged_attention_64(const PoolMaps &m, const PagedAttnArgs &a, int x, cudaStream_t st);
+int launch_paged_attention_128(const PoolMaps &m, const PagedAttnArgs &a, int x, cudaStream_t st);
 
 }  // namespace d3

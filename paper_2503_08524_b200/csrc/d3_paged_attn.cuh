@@ -206,7 +206,7 @@ struct Cfg {
   static constexpr int kBox = kRow < 128 ? kRow : 128;       // bytes of a box row = swizzle width
   static constexpr int kBoxes = kRow / kBox;                 // boxes per piece of K (or V)
   static constexpr int kHeads = X == D3_FP32 ? 8 : 8 * MT;   // query heads of a tile
-  static constexpr int kUnit = kRow > 128 ? 64 : 128;        // positions of a stage (of up to 32 KB)
+  static constexpr int kUnit = unit_positions(DH, kEs);      // positions of a stage (of up to 32 KB)
   static constexpr int kPT = kRow > 128 ? 1 : 2;             // tiles of a piece, i.e. of a warp's trip (32 fragment registers)
   static constexpr int kHalfBytes = kUnit * kRow;            // K (or V) of a stage
   static constexpr int kQRow = DH * QBytes<X>::v + 16;       // a query head in shared memory (padded: no bank conflicts)
@@ -935,22 +935,26 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_join(const __grid_con
   __shared__ float s_o[kJoinWarps][DH], s_l[kJoinWarps], s_m[kJoinWarps];
   pdl_wait();
   pdl_trigger();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int share_of = kJoinWarps / a.heads_per_tile, h = warp / share_of, first = warp % share_of;
+  auto part = [&](int k) -> size_t { return (size_t)(k == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + k)) * 16 + h; };
+  // the first 32 (m, l) are asked for together with the job; what of them is not a part of it is not used
+  float2 next_ml = make_float2(-INFINITY, 0.f);
+  const int mine0 = first + lane * share_of;
+  if (h < a.heads_per_tile && blockIdx.x + mine0 < gridDim.x) next_ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * part(mine0));
   const int4 job = a.join[blockIdx.x];
   if (job.x == 0) return;
   const int parts = job.x, row = job.y, kvh = job.w & 0xffff, nh = job.w >> 16;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int share_of = kJoinWarps / nh, h = warp / share_of, first = warp % share_of;   // warps from nh * share_of on are idle
   const bool busy = h < nh;
-  auto part = [&](int k) -> size_t { return (size_t)(k == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + k)) * 16 + h; };
   float M = -INFINITY, L = 0.f, o[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) o[e] = 0.f;
   if (busy) {
-    // 32 parts at a time: their (m, l) by one load, then their sums, 8 loads in flight
+    // 32 parts at a time: their (m, l), then their sums, 8 loads in flight
     for (int k0 = first; k0 < parts; k0 += 32 * share_of) {
       const int mine = k0 + lane * share_of;
       float2 ml = make_float2(-INFINITY, 0.f);
-      if (mine < parts) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * part(mine));
+      if (mine < parts) ml = k0 == first ? next_ml : *reinterpret_cast<const float2 *>(a.part_ml + 2 * part(mine));
       float m = ml.x;
 #pragma unroll
       for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
@@ -1014,13 +1018,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_join(const __grid_con
 
 // ---------------------------------------------------------------- launch
 template <int DH, int CACHE, int X, int MT>
-int launch(const d3_paged_kv &kv, PagedAttnArgs a, cudaStream_t st) {
+int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
   using C = Cfg<DH, CACHE, X, MT>;
-  TMap k, v, k16, v16;
-  const int rows = kv.page_size < C::kUnit ? kv.page_size : C::kUnit;
-  if (!encode_pool_map(&k, kv, kv.k_dev, rows) || !encode_pool_map(&v, kv, kv.v_dev, rows) ||
-      !encode_pool_map(&k16, kv, kv.k_dev, kTile) || !encode_pool_map(&v16, kv, kv.v_dev, kTile))
-    return -1;
   const int merge = C::kWarps * a.heads_per_tile * C::kHeadFloats * (int)sizeof(float);
   int stages = (kSmemMost - 1024 - merge) / (C::kStageBytes + C::kQBytes);
   if (stages > kMaxStages) stages = kMaxStages;
@@ -1039,7 +1038,7 @@ int launch(const d3_paged_kv &kv, PagedAttnArgs a, cudaStream_t st) {
     ready[dev].store(n, std::memory_order_release);
   }
   auto map = [](const TMap &m) -> const CUtensorMap & { return *reinterpret_cast<const CUtensorMap *>(&m); };
-  if (launch_pdl(k_paged_attention<DH, CACHE, X, MT>, dim3(n), dim3(C::kThreads), smem, st, map(k), map(v), map(k16), map(v16), a) !=
+  if (launch_pdl(k_paged_attention<DH, CACHE, X, MT>, dim3(n), dim3(C::kThreads), smem, st, map(m.k), map(m.v), map(m.k16), map(m.v16), a) !=
       cudaSuccess)
     return -1;
   // a table of at most one unit's positions cannot be cut
@@ -1049,14 +1048,14 @@ int launch(const d3_paged_kv &kv, PagedAttnArgs a, cudaStream_t st) {
 }
 
 template <int DH>
-int launch_types(const d3_paged_kv &kv, const PagedAttnArgs &a, int x, cudaStream_t st) {
-  const int cache = kv.dtype;
+int launch_types(const PoolMaps &m, const PagedAttnArgs &a, int x, cudaStream_t st) {
+  const int cache = m.of.dtype;
   const bool wide = a.heads_per_tile > 8;
-  if (cache == D3_BF16 && x == D3_FP32) return launch<DH, D3_BF16, D3_FP32, 2>(kv, a, st);
-  if (cache == D3_BF16) return wide ? launch<DH, D3_BF16, D3_BF16, 2>(kv, a, st) : launch<DH, D3_BF16, D3_BF16, 1>(kv, a, st);
-  if (cache == D3_FP16) return wide ? launch<DH, D3_FP16, D3_FP16, 2>(kv, a, st) : launch<DH, D3_FP16, D3_FP16, 1>(kv, a, st);
-  if (x == D3_BF16) return wide ? launch<DH, D3_E4M3, D3_BF16, 2>(kv, a, st) : launch<DH, D3_E4M3, D3_BF16, 1>(kv, a, st);
-  return wide ? launch<DH, D3_E4M3, D3_FP16, 2>(kv, a, st) : launch<DH, D3_E4M3, D3_FP16, 1>(kv, a, st);
+  if (cache == D3_BF16 && x == D3_FP32) return launch<DH, D3_BF16, D3_FP32, 2>(m, a, st);
+  if (cache == D3_BF16) return wide ? launch<DH, D3_BF16, D3_BF16, 2>(m, a, st) : launch<DH, D3_BF16, D3_BF16, 1>(m, a, st);
+  if (cache == D3_FP16) return wide ? launch<DH, D3_FP16, D3_FP16, 2>(m, a, st) : launch<DH, D3_FP16, D3_FP16, 1>(m, a, st);
+  if (x == D3_BF16) return wide ? launch<DH, D3_E4M3, D3_BF16, 2>(m, a, st) : launch<DH, D3_E4M3, D3_BF16, 1>(m, a, st);
+  return wide ? launch<DH, D3_E4M3, D3_FP16, 2>(m, a, st) : launch<DH, D3_E4M3, D3_FP16, 1>(m, a, st);
 }
 
 }  // namespace paged_attn

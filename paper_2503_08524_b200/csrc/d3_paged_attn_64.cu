@@ -3,8 +3,8 @@
 
 namespace d3 {
 
-int launch_paged_attention_64(const d3_paged_kv &kv, const PagedAttnArgs &a, int x, cudaStream_t st) {
-  return paged_attn::launch_types<64>(kv, a, x, st);
+int launch_paged_attention_64(const PoolMaps &m, const PagedAttnArgs &a, int x, cudaStream_t st) {
+  return paged_attn::launch_types<64>(m, a, x, st);
 }
 
 }  // namespace d3

@@ -22,7 +22,7 @@ import torch
 from .binding import EINVAL, LIB, OK, D3Error
 
 BF16, FP16, FP32, E4M3 = 0, 1, 2, 3
-MAX_REQUESTS = 4096
+MAX_REQUESTS, MAPS_BYTES = 4096, 640
 _TYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32, torch.float8_e4m3fn: E4M3}
 
 _I32T, _I64T, _F32 = torch.int32, torch.int64, torch.float32
@@ -33,7 +33,7 @@ class PagedKVArgs(C.Structure):
     _fields_ = [("struct_size", _U32)] + \
         [(n, _I32) for n in ("dtype", "n_pages", "page_size", "n_kv_heads", "head_dim")] + \
         [(n, _I64) for n in ("page_stride", "head_stride", "token_stride")] + \
-        [(n, _P) for n in ("k_dev", "v_dev", "k_scale_dev", "v_scale_dev")]
+        [(n, _P) for n in ("k_dev", "v_dev", "k_scale_dev", "v_scale_dev", "maps")]
 
 
 class PagePlanArgs(C.Structure):
@@ -135,11 +135,18 @@ class PagedKV:
             _refuse("PagedKV: scales belong to an 8-bit pool")
         st = _strides(k)
         self.args = PagedKVArgs(C.sizeof(PagedKVArgs), _TYPES[k.dtype], self.n_pages, self.page_size, self.n_kv_heads,
-                                self.head_dim, st[0], st[1], st[2], k.data_ptr(), v.data_ptr(), sc[0], sc[1])
+                                self.head_dim, st[0], st[1], st[2], k.data_ptr(), v.data_ptr(), sc[0], sc[1], None)
         self._ref = C.byref(self.args)
         n = C.c_size_t()   # the sizes this library serves
         if LIB.d3_paged_attention_workspace(self._ref, self.n_kv_heads, C.byref(n)) != OK:
             _refuse("PagedKV: page_size a power of two in 16..1024, head_dim 32, 64 or 128")
+        if self.index >= 0:   # the pool's tensor maps, encoded once
+            self._maps = C.create_string_buffer(MAPS_BYTES + 64)
+            maps = (C.addressof(self._maps) + 63) & ~63
+            rc = LIB.d3_paged_maps(self._ref, maps)
+            if rc != OK:
+                raise D3Error(rc, "PagedKV")
+            self.args.maps = maps
 
 
 def model_view(model, layer: int):
@@ -303,15 +310,17 @@ def d3_paged_attention(cache: PagedKV, q: torch.Tensor, table: torch.Tensor, con
     if rows_n < 1 or width < 1 or (inner != 1 and width > 1):
         _refuse(f"{what}: table must have entries and contiguous rows")
     if out is None:
-        out = q.new_empty((n, hq, dh))
-    op, ot, oh = _heads(out, n, hq, dh, dtype, dev, what, "out")
+        out = torch.empty_like(q) if q.is_contiguous() else q.new_empty((n, hq, dh))
+        op, ot, oh = out.data_ptr(), hq * dh, dh
+    else:
+        op, ot, oh = _heads(out, n, hq, dh, dtype, dev, what, "out")
     if scale is None:
         scale = dh ** -0.5
     elif not -3e38 < scale < 3e38:
         _refuse(f"{what}: scale must be finite")
     if lse is None:
         if with_lse:
-            lse = q.new_empty((n, hq), dtype=_F32)
+            lse = torch.empty_strided((n, hq), (hq, 1), dtype=_F32, device=q.device)
     elif lse.shape != (n, hq) or lse.dtype is not _F32 or lse.get_device() != dev or not lse.is_contiguous():
         _refuse(f"{what}: lse must be contiguous fp32 [{n}][{hq}] on device {dev}")
     if workspace is None:

@@ -273,6 +273,16 @@ def test_attention_equal_inputs_give_equal_bits_and_ignore_the_workspace(paged):
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
 
 
+def test_attention_with_and_without_the_pools_maps(paged):
+    cache, table, q, ctx = make(paged, [300, 5], 8, 2, 64, 32, BF16, BF16, seed=13)
+    want = paged.d3_paged_attention(cache, q, table, ctx)
+    maps, cache.args.maps = cache.args.maps, None
+    assert torch.equal(paged.d3_paged_attention(cache, q, table, ctx), want)
+    cache.args.maps, cache.args.n_pages = maps, cache.n_pages - 1
+    with pytest.raises(paged.D3Error):
+        paged.d3_paged_attention(cache, q, table, ctx)
+
+
 def test_attention_entries_beyond_32_bit_offsets(paged):
     """A pool of more than 2^32 bytes and 2^31 elements per tensor; the row's pages sit at its two ends."""
     hkv, page, dh = 8, 64, 128

@@ -12,7 +12,7 @@ FAKE = 1 << 20        # an aligned address that no refused call may touch
 
 
 def kv_args(**kw):
-    a = P.PagedKVArgs(C.sizeof(P.PagedKVArgs), P.BF16, 10, 16, 2, 64, 2 * 16 * 64, 16 * 64, 64, FAKE, FAKE, None, None)
+    a = P.PagedKVArgs(C.sizeof(P.PagedKVArgs), P.BF16, 10, 16, 2, 64, 2 * 16 * 64, 16 * 64, 64, FAKE, FAKE, None, None, None)
     for k, v in kw.items():
         setattr(a, k, v)
     return a
@@ -96,10 +96,18 @@ def test_null_arguments():
     assert B.LIB.d3_paged_attention_workspace(None, 4, C.byref(n)) == B.EINVAL
     assert B.LIB.d3_paged_attention_workspace(C.byref(kv_args()), 4, None) == B.EINVAL
     assert B.LIB.d3_paged_attention_workspace(C.byref(kv_args()), 3, C.byref(n)) == B.EINVAL
+    assert B.LIB.d3_paged_maps(None, FAKE) == B.EINVAL and B.LIB.d3_paged_maps(C.byref(kv_args()), None) == B.EINVAL
+    assert B.LIB.d3_paged_maps(C.byref(kv_args()), FAKE + 32) == B.EINVAL
     assert B.LIB.d3_paged_view(None, 0, None, None, None, None) == B.EINVAL
     for bad in ((0, 64, 1e4, FAKE), (5, 48, 1e4, FAKE), (5, 64, 0.0, FAKE), (5, 64, float("nan"), FAKE), (5, 64, 1e4, None),
                 (5, 64, 1e4, FAKE + 8), (2 ** 31 - 1, 128, 1e4, FAKE)):
         assert B.LIB.d3_rope_table(*bad, None) == B.EINVAL
+
+
+def test_tensor_maps_of_another_pool_are_refused():
+    kv, room = kv_args(), C.create_string_buffer(P.MAPS_BYTES + 64)
+    kv.maps = (C.addressof(room) + 63) & ~63       # zeros: made for no pool
+    assert B.LIB.d3_paged_attention(C.byref(kv), C.byref(attention_args(n_rows=0)), None) == B.EINVAL
 
 
 def test_calls_without_work_return_at_once():
@@ -115,7 +123,7 @@ def test_workspace_holds_two_pieces_per_multiprocessor():
 
 
 def test_struct_sizes_match_the_header():
-    assert [C.sizeof(t) for t in (P.PagedKVArgs, P.PagePlanArgs, P.PagedAppendArgs, P.PagedAttentionArgs)] == [80, 128, 152, 144]
+    assert [C.sizeof(t) for t in (P.PagedKVArgs, P.PagePlanArgs, P.PagedAppendArgs, P.PagedAttentionArgs)] == [88, 128, 152, 144]
 
 
 def pool(**kw):
