@@ -163,12 +163,14 @@ __device__ __forceinline__ long long divide(long long x, int y) {
 }
 // How `total` cost is dealt out to n CTAs: the first `more` of them get each + 1, the others each.
 struct Shares {
-  long long each, more;
+  long long each;
+  int more;
+  __device__ __forceinline__ Shares() {}
   __device__ __forceinline__ Shares(long long total, int n) {
     each = divide(total, n);
-    more = total - each * n;
+    more = (int)(total - each * n);
   }
-  __device__ __forceinline__ long long start(int i) const { return each * i + (i < more ? i : more); }
+  __device__ __forceinline__ long long start(int i) const { return each * i + min(i, more); }
   __device__ __forceinline__ int holder(long long x) const {   // the CTA that x belongs to
     const long long edge = (each + 1) * more;
     if (x < edge) return (int)(x / (each + 1));
@@ -178,7 +180,7 @@ struct Shares {
 // Cost of an item (the pass over a row's positions for one tile of heads): kUnitCost per unit and kItemCost for its query
 // fragments and its sums.  The unit i of an item that starts at cost S belongs to the CTA that holds S + kItemCost +
 // kUnitCost * i.  With few units per CTA only units count, so that no CTA is left without one.
-constexpr int kUnitCost = 4, kItemCost = 3;
+constexpr int kUnitShift = 2, kUnitCost = 1 << kUnitShift, kItemCost = 3;
 struct Cost {
   int unit, item;
   __device__ __forceinline__ long long of(int units) const { return (long long)unit * units + item; }
@@ -279,7 +281,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     return c;
   };
   auto units_of = [&](int len) -> int { return len > 0 ? (len + kUnit - 1) / kUnit : 1; };   // a row without context still gets its zeros
-  const bool few = a.n_rows <= kFewRows;
+  const bool few = a.few;
   long long units = 0;   // of all rows, for one tile of heads
   int live_rows = 0;
   auto cost_of = [&](long long n) -> Cost {
@@ -346,7 +348,6 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const int me = warp - C::kWarps - C::kEpilogue;
     bool dummy = false;
     int row, trow, len;
-    long long start_before = 0;   // cost of the rows before the first one
     // few rows: their table rows and lengths stay in registers, row lane * per + i in entry i
     constexpr int kPer = kFewRows / 32;
     const int per = (a.n_rows + 31) / 32;
@@ -357,7 +358,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       for (int i = 1; i < kPer; ++i) x = at_entry == i ? v[i] : x;
       return __shfl_sync(0xffffffffu, x, at_lane);
     };
-    long long mine = 0, inc = 0;
+    int few_units = 0, few_rows = 0;   // of this lane
     if (few) {
       pdl_wait();
       pdl_trigger();
@@ -370,19 +371,12 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           bool strange = false;
           c_[i] = length_of(b, strange);
           r_[i] = row_of(b, bad);
-          if (r_[i] >= 0) { mine += ((long long)units_of(c_[i]) << 17) | 1; bad = bad || strange; }
+          if (r_[i] >= 0) { few_units += units_of(c_[i]); ++few_rows; bad = bad || strange; }
         }
       }
       if (bad && blockIdx.x == 0 && a.status) *a.status = D3_EINVAL;
-      inc = mine;   // units in the upper, rows in the lower bits
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const long long u = __shfl_up_sync(0xffffffffu, inc, d);
-        if (lane >= d) inc += u;
-      }
-      const long long all = __shfl_sync(0xffffffffu, inc, 31);
-      units = all >> 17;
-      live_rows = (int)(all & 0x1ffff);
+      units = __reduce_add_sync(0xffffffffu, few_units);
+      live_rows = __reduce_add_sync(0xffffffffu, few_rows);
     }
     const int n_cta = (int)min(units * HG, (long long)gridDim.x);   // every one of them has work
     if ((int)blockIdx.x >= n_cta) {
@@ -394,44 +388,55 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       return;
     }
     const Cost cost = cost_of(units);
-    const Shares sh((units * cost.unit + (long long)live_rows * cost.item) * HG, n_cta);
-    const long long x0 = sh.start(blockIdx.x), x1 = sh.start(blockIdx.x + 1);
-    if (few) {
-      auto cost_sum = [&](long long v) -> long long { return ((v >> 17) * cost.unit + (v & 0x1ffff) * cost.item) * HG; };
-      long long p = cost_sum(inc - mine);
-      at_lane = __ffs(__ballot_sync(0xffffffffu, x0 >= p && x0 < cost_sum(inc))) - 1;
-      int entry = 0;
-      bool found = false;
+    Shares sh;
+    long long x0, x1, item;   // this CTA's costs; where its first item starts
+    int nu, tile, unit;
+    if (few) {   // all of it in 32 bits
+      const int total = ((int)units * cost.unit + live_rows * cost.item) * HG, each = (int)((unsigned)total / (unsigned)n_cta);
+      sh.each = each; sh.more = total - each * n_cta;
+      const int x = each * (int)blockIdx.x + min((int)blockIdx.x, sh.more);
+      x0 = x;
+      x1 = x + each + ((int)blockIdx.x < sh.more ? 1 : 0);
+      const int mine = (few_units * cost.unit + few_rows * cost.item) * HG;
+      int inc = mine;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const long long n = r_[i] >= 0 ? cost.of(units_of(c_[i])) * HG : 0;
-        if (!found) {
-          if (x0 < p + n) { entry = i; found = true; }
-          else p += n;
-        }
+      for (int d = 1; d < 32; d <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, inc, d);
+        if (lane >= d) inc += u;
+      }
+      int p = inc - mine, entry = 0;
+      at_lane = __ffs(__ballot_sync(0xffffffffu, x >= p && x < inc)) - 1;
+#pragma unroll
+      for (int i = 0; i + 1 < kPer; ++i) {
+        const int n = r_[i] >= 0 ? (cost.unit * units_of(c_[i]) + cost.item) * HG : 0;
+        if (entry == i && x >= p + n) { p += n; entry = i + 1; }
       }
       at_entry = __shfl_sync(0xffffffffu, entry, at_lane);
-      start_before = __shfl_sync(0xffffffffu, p, at_lane);
+      const int start_before = __shfl_sync(0xffffffffu, p, at_lane);
       row = at_lane * per + at_entry;
       trow = kept(r_);
       len = kept(c_);
+      nu = units_of(len);
+      const int one = cost.unit * nu + cost.item, at = x - start_before;
+      tile = (int)((unsigned)at / (unsigned)one);
+      const int in = at - tile * one - cost.item;
+      item = start_before + tile * one;
+      unit = in <= 0 ? 0 : (in + cost.unit - 1) >> (cost.unit == 1 ? 0 : kUnitShift);
     } else {
+      sh = Shares((units * cost.unit + (long long)live_rows * cost.item) * HG, n_cta);
+      x0 = sh.start(blockIdx.x);
+      x1 = sh.start(blockIdx.x + 1);
       row = s_start_row;
-      start_before = s_start_before;
       trow = row_of(row, dummy);
       len = length_of(row, dummy);
-    }
-    int nu = units_of(len), tile, unit;
-    long long item;        // cost at which the item starts
-    bool behind;           // no unit of that item is this CTA's: begin with the next one
-    {
-      const long long at = x0 - start_before, one = cost.of(nu);
+      nu = units_of(len);
+      const long long at = x0 - s_start_before, one = cost.of(nu);   // s_start_before: cost of the rows before
       tile = one < (1ll << 31) ? (int)divide(at, (int)one) : (int)(at / one);
-      item = start_before + tile * one;
+      item = s_start_before + tile * one;
       const long long in = x0 - item - cost.item;
-      unit = in <= 0 ? 0 : (int)((in + cost.unit - 1) / cost.unit);
-      behind = unit >= nu;
+      unit = in <= 0 ? 0 : (int)((in + cost.unit - 1) >> (cost.unit == 1 ? 0 : kUnitShift));
     }
+    const bool behind = unit >= nu;   // no unit of that item is this CTA's: begin with the next one
     int kvh = tile, sub = 0;
     if (a.tiles_per_head > 1) { kvh = tile / a.tiles_per_head; sub = tile % a.tiles_per_head; }
     const int32_t *pages = a.table + (long long)trow * a.table_stride;
@@ -1025,6 +1030,9 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
   if (stages > kMaxStages) stages = kMaxStages;
   if (stages < 2) return -1;
   a.n_stages = stages;
+  // few enough rows for a warp, and all costs within 32 bits whatever the lengths are
+  const double capacity = ((double)a.table_width * (1 << a.page_shift) / C::kUnit + 1) * kUnitCost + kItemCost;
+  a.few = a.n_rows <= kFewRows && a.n_rows * capacity * a.hkv * a.tiles_per_head < 1.0e9 ? 1 : 0;
   const size_t smem = 1024 + (size_t)stages * (C::kStageBytes + C::kQBytes) + merge;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
