@@ -943,10 +943,23 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_join(const __grid_con
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int share_of = kJoinWarps / a.heads_per_tile, h = warp / share_of, first = warp % share_of;
   auto part = [&](int k) -> size_t { return (size_t)(k == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + k)) * 16 + h; };
-  // the first 32 (m, l) are asked for together with the job; what of them is not a part of it is not used
+  auto sums_of = [&](int k, float (&x)[V]) {
+    const float *src = a.part_o + part(k) * DH + lane * V;
+    if constexpr (V == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+    else if constexpr (V == 2) { const float2 v = *reinterpret_cast<const float2 *>(src); x[0] = v.x; x[1] = v.y; }
+    else x[0] = *src;
+  };
+  // one round trip: the first 32 (m, l) and the sums of the first two parts are asked for together with the job; what
+  // of them is not a part of it is not used
   float2 next_ml = make_float2(-INFINITY, 0.f);
-  const int mine0 = first + lane * share_of;
-  if (h < a.heads_per_tile && blockIdx.x + mine0 < gridDim.x) next_ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * part(mine0));
+  float early[2][V];
+  if (h < a.heads_per_tile) {
+    const int mine0 = first + lane * share_of;
+    if (blockIdx.x + mine0 < gridDim.x) next_ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * part(mine0));
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (blockIdx.x + first + i * share_of < gridDim.x) sums_of(first + i * share_of, early[i]);
+  }
   const int4 job = a.join[blockIdx.x];
   if (job.x == 0) return;
   const int parts = job.x, row = job.y, kvh = job.w & 0xffff, nh = job.w >> 16;
@@ -976,16 +989,22 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_join(const __grid_con
       for (int e = 0; e < V; ++e) o[e] *= keep;
       const unsigned there = __ballot_sync(0xffffffffu, ml.y != 0.f);
       const int n = min(32, (parts - k0 + share_of - 1) / share_of);
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) {
+      auto take = [&](int i, const float (&x)[V]) {
         const float ci = __shfl_sync(0xffffffffu, c, i);
-        const float *src = a.part_o + part(k0 + i * share_of) * DH + lane * V;
-        float x[V];
-        if constexpr (V == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
-        else if constexpr (V == 2) { const float2 v = *reinterpret_cast<const float2 *>(src); x[0] = v.x; x[1] = v.y; }
-        else x[0] = *src;
 #pragma unroll
         for (int e = 0; e < V; ++e) o[e] += (there >> i & 1) ? ci * x[e] : 0.f;
+      };
+      int i = 0;
+      if (k0 == first) {
+        take(0, early[0]);
+        if (n > 1) take(1, early[1]);
+        i = 2;
+      }
+#pragma unroll 8
+      for (; i < n; ++i) {
+        float x[V];
+        sums_of(k0 + i * share_of, x);
+        take(i, x);
       }
     }
   }
