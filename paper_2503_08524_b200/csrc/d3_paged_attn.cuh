@@ -178,12 +178,16 @@ struct Shares {
   }
 };
 // Cost of an item (the pass over a row's positions for one tile of heads): kUnitCost per unit and kItemCost for its query
-// fragments and its sums.  The unit i of an item that starts at cost S belongs to the CTA that holds S + kItemCost +
-// kUnitCost * i.  With few units per CTA only units count, so that no CTA is left without one.
+// fragments and its sums.  The unit i of an item that starts at cost S belongs to the CTA that holds S + lead +
+// step * i.  With few units per CTA only units count, so that no CTA is left without one.  Where items stay whole
+// (no join) step and lead are 0, and with no more items than CTAs only items count.
 constexpr int kUnitShift = 2, kUnitCost = 1 << kUnitShift, kItemCost = 3;
 struct Cost {
-  int unit, item;
+  int unit, item, lead, step;
   __device__ __forceinline__ long long of(int units) const { return (long long)unit * units + item; }
+  __device__ __forceinline__ long long first_unit(long long past) const {   // the first one at or behind S + lead + past
+    return past <= 0 ? 0 : step == 0 ? 0x7fffffff : step == 1 ? past : (past + kUnitCost - 1) >> kUnitShift;
+  }
 };
 
 enum { STAGE_FIRST = 1, STAGE_LAST = 2, STAGE_FINAL = 4 };   // of the item within this CTA; of the CTA
@@ -284,8 +288,10 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   const bool few = a.few;
   long long units = 0;   // of all rows, for one tile of heads
   int live_rows = 0;
+  bool whole = a.whole;   // no item is cut between CTAs
   auto cost_of = [&](long long n) -> Cost {
-    return n * HG >= 4ll * gridDim.x ? Cost{kUnitCost, kItemCost} : Cost{1, 0};
+    if (whole) return (long long)live_rows * HG <= gridDim.x ? Cost{0, 1, 0, 0} : Cost{kUnitCost, kItemCost, 0, 0};
+    return n * HG >= 4ll * gridDim.x ? Cost{kUnitCost, kItemCost, kItemCost, kUnitCost} : Cost{1, 0, 0, 1};
   };
   if (!few) {
     pdl_wait();
@@ -323,7 +329,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     units = all >> 17;
     live_rows = (int)(all & 0x1ffff);
     const Cost cost = cost_of(units);
-    const int n_cta = (int)min(units * HG, (long long)gridDim.x);
+    const int n_cta = (int)min((whole ? live_rows : units) * HG, (long long)gridDim.x);
     if ((int)blockIdx.x < n_cta) {
       const Shares sh((units * cost.unit + (long long)live_rows * cost.item) * HG, n_cta);
       const long long x0 = sh.start(blockIdx.x);
@@ -358,7 +364,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       for (int i = 1; i < kPer; ++i) x = at_entry == i ? v[i] : x;
       return __shfl_sync(0xffffffffu, x, at_lane);
     };
-    int few_units = 0, few_rows = 0;   // of this lane
+    int few_units = 0, few_rows = 0, few_longest = 0;   // of this lane
     if (few) {
       pdl_wait();
       pdl_trigger();
@@ -371,22 +377,27 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           bool strange = false;
           c_[i] = length_of(b, strange);
           r_[i] = row_of(b, bad);
-          if (r_[i] >= 0) { few_units += units_of(c_[i]); ++few_rows; bad = bad || strange; }
+          if (r_[i] >= 0) { few_units += units_of(c_[i]); few_longest = max(few_longest, units_of(c_[i])); ++few_rows; bad = bad || strange; }
         }
       }
       if (bad && blockIdx.x == 0 && a.status) *a.status = D3_EINVAL;
       units = __reduce_add_sync(0xffffffffu, few_units);
       live_rows = __reduce_add_sync(0xffffffffu, few_rows);
+      // Items stay whole where that makes the busiest CTA at most 8 units longer than an even share: a unit takes 0.5 us, the
+      // sums of a cut item and their join about 4 (4 rows of 2048 positions, 32 heads: 25.4 us whole, 30.0 cut).
+      const long long items = (long long)live_rows * HG, even = units * HG;
+      const int longest = __reduce_max_sync(0xffffffffu, few_longest);
+      whole = whole || (items <= gridDim.x ? longest * (long long)gridDim.x <= even + 8ll * gridDim.x : longest <= 8);
     }
-    const int n_cta = (int)min(units * HG, (long long)gridDim.x);   // every one of them has work
-    if ((int)blockIdx.x >= n_cta) {
+    const int n_cta = (int)min((whole ? live_rows : units) * HG, (long long)gridDim.x);   // every one of them has work
+    auto idle = [&]() {   // a stage that sends the other warps home
       if (me == 0 && lane == 0) {
-        a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (!a.whole) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
         s_info[0] = StageInfo{0, 0, 0, (uint32_t)((STAGE_LAST | STAGE_FINAL) << 8 | OUT_NONE << 11)};
         mb_arrive(smem_u32(&s_full[0]));
       }
-      return;
-    }
+    };
+    if ((int)blockIdx.x >= n_cta) { idle(); return; }
     const Cost cost = cost_of(units);
     Shares sh;
     long long x0, x1, item;   // this CTA's costs; where its first item starts
@@ -419,9 +430,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       nu = units_of(len);
       const int one = cost.unit * nu + cost.item, at = x - start_before;
       tile = (int)((unsigned)at / (unsigned)one);
-      const int in = at - tile * one - cost.item;
       item = start_before + tile * one;
-      unit = in <= 0 ? 0 : (in + cost.unit - 1) >> (cost.unit == 1 ? 0 : kUnitShift);
+      unit = (int)cost.first_unit(at - tile * one - cost.lead);
     } else {
       sh = Shares((units * cost.unit + (long long)live_rows * cost.item) * HG, n_cta);
       x0 = sh.start(blockIdx.x);
@@ -433,8 +443,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       const long long at = x0 - s_start_before, one = cost.of(nu);   // s_start_before: cost of the rows before
       tile = one < (1ll << 31) ? (int)divide(at, (int)one) : (int)(at / one);
       item = s_start_before + tile * one;
-      const long long in = x0 - item - cost.item;
-      unit = in <= 0 ? 0 : (int)((in + cost.unit - 1) >> (cost.unit == 1 ? 0 : kUnitShift));
+      unit = (int)min(cost.first_unit(x0 - item - cost.lead), 0x7fffffffll);
     }
     const bool behind = unit >= nu;   // no unit of that item is this CTA's: begin with the next one
     int kvh = tile, sub = 0;
@@ -469,18 +478,19 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       }
     };
     if (behind) next_item();
-    long long at = item + cost.item + (long long)cost.unit * unit;   // of the unit
+    long long at = item + cost.lead + (long long)cost.step * unit;   // of the unit
+    if (at >= x1) { idle(); return; }   // whole items: none starts in this CTA's share
     int cut_row = -1, cut_head = 0, cut_kvh = 0, cut_nh = 0;         // the item that goes on in the next CTA, if it starts here
     long long cut_last = 0;
     for (int k = 0; at < x1; ++k) {
       const bool ends = unit + 1 == nu;
-      const long long next = ends ? at + cost.unit + cost.item : at + cost.unit;
+      const long long next = ends ? item + cost.of(nu) + cost.lead : at + cost.step;
       const bool last = ends || next >= x1, final = next >= x1;
       const int nh = min(a.heads_per_tile, a.group - sub * a.heads_per_tile), head = kvh * a.group + sub * a.heads_per_tile;
-      const bool whole_start = item + cost.item >= x0;      // its unit 0 is this CTA's
+      const bool whole_start = item + cost.lead >= x0;      // its unit 0 is this CTA's
       if (last && !ends && whole_start) {
         cut_row = row; cut_head = head; cut_kvh = kvh; cut_nh = nh;
-        cut_last = item + cost.item + (long long)cost.unit * (nu - 1);
+        cut_last = item + cost.lead + (long long)cost.step * (nu - 1);
       }
       if ((k & (kProducers - 1)) == me) {
         const int p0 = unit * kUnit, n = max(0, min(kUnit, len - p0));   // n = 0 only for a row without context
@@ -538,7 +548,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       // an item that starts here and goes on: what the joining kernel adds up
       int4 join = make_int4(0, 0, 0, 0);
       if (ok && cut_row >= 0) join = make_int4(sh.holder(cut_last) - (int)blockIdx.x + 1, cut_row, cut_head, cut_kvh | cut_nh << 16);
-      a.join[blockIdx.x] = join;
+      if (!a.whole) a.join[blockIdx.x] = join;
     }
     if (!ok) {   // copies in flight end by themselves: wait for them before the shared memory goes
       const unsigned long long drain = a.wait_ns > kDrainFloorNs ? a.wait_ns : kDrainFloorNs;
@@ -1049,9 +1059,6 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
   if (stages > kMaxStages) stages = kMaxStages;
   if (stages < 2) return -1;
   a.n_stages = stages;
-  // few enough rows for a warp, and all costs within 32 bits whatever the lengths are
-  const double capacity = ((double)a.table_width * (1 << a.page_shift) / C::kUnit + 1) * kUnitCost + kItemCost;
-  a.few = a.n_rows <= kFewRows && a.n_rows * capacity * a.hkv * a.tiles_per_head < 1.0e9 ? 1 : 0;
   const size_t smem = 1024 + (size_t)stages * (C::kStageBytes + C::kQBytes) + merge;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
@@ -1064,12 +1071,19 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
     if (n > kFusedMaxCtas) n = kFusedMaxCtas;
     ready[dev].store(n, std::memory_order_release);
   }
+  // Items stay whole whatever the lengths, and no join is launched, where the table has room for 10 units a row at most: the
+  // busiest CTA is at most one row longer than an even share (bf16, 32 kv heads, whole / cut: 1 row of 512
+  // positions 8.1 / 9.3 us, of 1024 11.9 / 10.3; 4 rows of 512 10.1 / 14.1).
+  const long long most = (((long long)a.table_width << a.page_shift) + C::kUnit - 1) / C::kUnit;
+  a.whole = most <= 10;
+  // few enough rows for a warp, and all costs within 32 bits whatever the lengths are
+  const double capacity = ((double)a.table_width * (1 << a.page_shift) / C::kUnit + 1) * kUnitCost + kItemCost;
+  a.few = a.n_rows <= kFewRows && a.n_rows * capacity * a.hkv * a.tiles_per_head < 1.0e9 ? 1 : 0;
   auto map = [](const TMap &m) -> const CUtensorMap & { return *reinterpret_cast<const CUtensorMap *>(&m); };
   if (launch_pdl(k_paged_attention<DH, CACHE, X, MT>, dim3(n), dim3(C::kThreads), smem, st, map(m.k), map(m.v), map(m.k16), map(m.v16), a) !=
       cudaSuccess)
     return -1;
-  // a table of at most one unit's positions cannot be cut
-  if (((long long)a.table_width << a.page_shift) > C::kUnit)
+  if (!a.whole)
     if (launch_pdl(k_paged_join<DH, X, C::kF16>, dim3(n), dim3(32 * kJoinWarps), 0, st, a) != cudaSuccess) return -1;
   return 0;
 }
