@@ -436,7 +436,7 @@ typedef struct d3_paged_append_args {
   uint32_t struct_size;
   int32_t dtype;
   int32_t n_tokens;          /* >= 0                                                     */
-  int32_t n_q_heads;         /* with q_dev; n_q_heads + 2 n_kv_heads <= 65535            */
+  int32_t n_q_heads;         /* with q_dev; (tokens x heads) below 2^31                  */
   int32_t rope_len;
   const void *k_dev, *v_dev;
   int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;

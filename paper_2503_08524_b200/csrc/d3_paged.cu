@@ -5,6 +5,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "d3_paged.cuh"
 
@@ -226,16 +227,22 @@ __global__ void __launch_bounds__(kPlanMaxThreads) k_page_plan(const __grid_cons
 // ------------------------------------------------------------------ append
 // Bandwidth: every number once in and once out.  A thread takes the pairs (8 numbers of a head's lower
 // half, the 8 that they are paired with), so the rotation needs no exchange and all traffic is in
-// 16-byte pieces (8 for the 8-bit cache); it does that for H heads of one token, whose (cos, sin) it loads
-// once.  A CTA's threads are tokens x heads x pieces, powers of two, so that no index needs a division; all loads are
-// in flight before the slot is looked at.
+// 16-byte pieces (8 for the 8-bit cache); it does that for H neighbouring heads of one token, whose (cos, sin) it loads
+// once.  q, K and V have blocks of their own, so that what a block does and where its numbers lie is uniform;
+// inside, (token, group of H heads) is one index.  All loads are in flight before the slot is looked at.
+struct AppendPart {
+  const void *src;
+  void *dst;
+  long long st, sh, dt, dh;     // strides of tokens (q_out alone) and heads
+  const float *scale;
+  int heads, groups;            // groups of H heads
+  unsigned first_block;         // its blocks start here
+  unsigned magic, shift;        // index / groups = index * magic >> shift
+  int rotate;
+};
 struct AppendArgs {
-  long long n_tokens;
-  int hq, rope_len;
-  int head_shift;               // log2 of the heads (of a token) that a CTA's threads stand for
-  const void *k, *v, *q;
-  void *q_out;
-  long long kt, kh, vt, vh, qt, qh, ot, oh;   // token and head strides
+  AppendPart part[3];           // q, K, V
+  int n_tokens, rope_len;
   const long long *slots;
   const int32_t *context;
   const float *rope;
@@ -273,14 +280,32 @@ __device__ __forceinline__ void widen8(const Raw8<__half> &r, float *f) {
     f[2 * i] = v.x; f[2 * i + 1] = v.y;
   }
 }
-// x / d rounded once, for a d whose correctly rounded reciprocal r is known (2^-60 <= |d| <= 2^60): the remainder of the first
-// quotient is exact in one FMA, and adding it times r rounds like the division (Markstein 1990).  Quotients
-// beyond 10^4, infinities and NaN stay as the product has them: the 8-bit type saturates at 448.
+// the largest |x| of eight numbers, NaN counting as infinite: at least their true one
+__device__ __forceinline__ float reach(const Raw8<float> &r) {
+  const uint32_t w[8] = {r.u.x, r.u.y, r.u.z, r.u.w, r.w.x, r.w.y, r.w.z, r.w.w};
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
+  return m > 0x7f800000u ? INFINITY : __uint_as_float(m);
+}
+__device__ __forceinline__ float reach(const Raw8<bf16> &r) {
+  const uint32_t m = __vmaxu2(__vmaxu2(r.u.x & 0x7fff7fffu, r.u.y & 0x7fff7fffu), __vmaxu2(r.u.z & 0x7fff7fffu, r.u.w & 0x7fff7fffu));
+  const uint32_t v = max(m & 0xffffu, m >> 16);
+  return v > 0x7f80u ? INFINITY : __uint_as_float(v << 16);
+}
+__device__ __forceinline__ float reach(const Raw8<__half> &r) {
+  const uint32_t m = __vmaxu2(__vmaxu2(r.u.x & 0x7fff7fffu, r.u.y & 0x7fff7fffu), __vmaxu2(r.u.z & 0x7fff7fffu, r.u.w & 0x7fff7fffu));
+  const uint32_t v = max(m & 0xffffu, m >> 16);
+  return v >= 0x7c00u ? INFINITY : 65504.f;
+}
+// the plain division, out of line: it is rarely taken, and 64 copies of it would crowd the instruction cache
+__device__ __noinline__ float plain_division(float x, float d) { return __fdiv_rn(x, d); }
+// x / d rounded once, for |x| <= 2^40 and a d in 2^-60 .. 2^60 whose correctly rounded reciprocal r is known: the remainder
+// of the first quotient is exact in one FMA, and taking it times r off rounds like the division (Markstein 1990).
+// In these signs a zero keeps its own.
 __device__ __forceinline__ float divide(float x, float d, float r) {
   const float q = __fmul_rn(x, r);
-  const float better = __fmaf_rn(__fmaf_rn(-q, d, x), r, q);
-  const float v = fabsf(q) < 1.0e4f ? better : q;
-  return __uint_as_float(__float_as_uint(v) | (__float_as_uint(q) & 0x80000000u));   // -0 stays -0
+  return __fmaf_rn(__fmaf_rn(q, d, -x), -r, q);
 }
 __device__ __forceinline__ void store8(float *p, const float *f) {
   reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
@@ -315,51 +340,50 @@ __device__ __forceinline__ void store8(__nv_fp8_e4m3 *p, const float *f) {
   *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
 }
 
+// 8-bit stores compute more per byte (a division and a conversion): four blocks an SM, 64 registers, two heads a thread
+// hide that (4097 tokens, 40 + 80 heads of 128: 40.2 us; three blocks 45.5, five, which spill, 55.6; 16-bit: 40.3).
 template <typename X, typename C, int DH, int H>
-__global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ AppendArgs a) {
-  constexpr int HALF = DH / 2, PIECES = HALF / 8, LANES = 256 / PIECES;   // (token, head) pairs of a CTA
+__global__ void __launch_bounds__(256, sizeof(C) == 1 ? 4 : 1) k_paged_append(const __grid_constant__ AppendArgs a) {
+  constexpr int HALF = DH / 2, PIECES = HALF / 8, LANES = 256 / PIECES;   // (token, group) pairs of a block
   pdl_wait();
   pdl_trigger();
-  const int j = threadIdx.x % PIECES, u = threadIdx.x / PIECES, step = 1 << a.head_shift;
-  const long long t = (long long)blockIdx.x * (LANES >> a.head_shift) + (u >> a.head_shift);
+  const int which = (blockIdx.x >= a.part[1].first_block ? 1 : 0) + (blockIdx.x >= a.part[2].first_block ? 1 : 0);
+  const AppendPart &p = a.part[which];
+  const int j = threadIdx.x % PIECES;
+  const unsigned index = (blockIdx.x - p.first_block) * LANES + threadIdx.x / PIECES;
+  const int t = (int)(((unsigned long long)index * p.magic) >> p.shift), h0 = (int)(index - (unsigned)t * p.groups) * H;
   if (t >= a.n_tokens) return;
-  const int heads = a.hq + 2 * a.kv.n_kv_heads, h0 = blockIdx.y * (step * H) + (u & (step - 1));
   const long long slot = a.slots[t];
   const int pos = a.rope ? a.context[t] - 1 : 0;
 
   Raw8<X> raw[H][2];
+  const X *src = static_cast<const X *>(p.src) + t * p.st + h0 * p.sh + 8 * j;
 #pragma unroll
-  for (int i = 0; i < H; ++i) {
-    const int h = h0 + i * step;
-    if (h < heads) {
-      const X *p = h < a.hq ? static_cast<const X *>(a.q) + t * a.qt + (long long)h * a.qh
-                   : h < a.hq + a.kv.n_kv_heads ? static_cast<const X *>(a.k) + t * a.kt + (long long)(h - a.hq) * a.kh
-                   : static_cast<const X *>(a.v) + t * a.vt + (long long)(h - a.hq - a.kv.n_kv_heads) * a.vh;
-      fetch(raw[i][0], p + 8 * j);
-      fetch(raw[i][1], p + HALF + 8 * j);
+  for (int i = 0; i < H; ++i)
+    if (h0 + i < p.heads) {
+      fetch(raw[i][0], src + i * p.sh);
+      fetch(raw[i][1], src + i * p.sh + HALF);
     }
-  }
   if (slot < 0) return;
   if (slot >= ((long long)a.kv.n_pages << a.kv.page_shift) || (a.rope && (pos < 0 || pos >= a.rope_len))) {
     if (a.status) *a.status = D3_EINVAL;
     return;
   }
-  const long long in_page = slot & ((1 << a.kv.page_shift) - 1);
-  const long long entry = (slot >> a.kv.page_shift) * a.kv.page_stride + in_page * a.kv.token_stride;
   float4 cs[4];   // (cos, sin) of the eight pairs
-  if (a.rope && h0 < a.hq + a.kv.n_kv_heads) {
+  if (p.rotate) {
     const float4 *r = reinterpret_cast<const float4 *>(a.rope + ((long long)pos * HALF + 8 * j) * 2);
 #pragma unroll
     for (int i = 0; i < 4; ++i) cs[i] = __ldg(r + i);
   }
+  const long long in_page = slot & ((1 << a.kv.page_shift) - 1);
+  const long long entry = which == 0 ? t * p.dt : (slot >> a.kv.page_shift) * a.kv.page_stride + in_page * a.kv.token_stride;
 #pragma unroll
   for (int i = 0; i < H; ++i) {
-    const int h = h0 + i * step;
-    if (h >= heads) continue;
+    if (h0 + i >= p.heads) break;
     float lo[8], hi[8];
     widen8(raw[i][0], lo);
     widen8(raw[i][1], hi);
-    if (a.rope && h < a.hq + a.kv.n_kv_heads) {
+    if (p.rotate) {
       // products and sums rounded one by one: no contraction, so every store rounds the same number
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -368,55 +392,63 @@ __global__ void __launch_bounds__(256) k_paged_append(const __grid_constant__ Ap
         hi[e] = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
       }
     }
-    if (h < a.hq) {
-      X *p = static_cast<X *>(a.q_out) + t * a.ot + (long long)h * a.oh;
-      store8(p + 8 * j, lo);
-      store8(p + HALF + 8 * j, hi);
+    const long long at = entry + (h0 + i) * p.dh + 8 * j;
+    if (std::is_same<X, C>::value || which == 0) {
+      X *dst = static_cast<X *>(p.dst) + at;
+      store8(dst, lo);
+      store8(dst + HALF, hi);
     } else {
-      const bool is_v = h >= a.hq + a.kv.n_kv_heads;
-      const int kh = h - a.hq - (is_v ? a.kv.n_kv_heads : 0);
-      C *p = static_cast<C *>(is_v ? a.kv.v : a.kv.k) + entry + (long long)kh * a.kv.head_stride;
-      if (sizeof(C) == 1) {
-        const float *sc = is_v ? a.kv.v_scale : a.kv.k_scale;
-        if (sc) {
-          const float d = __ldg(sc + kh);
-          if (fabsf(d) >= 0x1p-60f && fabsf(d) <= 0x1p60f) {
-            const float r = __frcp_rn(d);
+      if (sizeof(C) == 1 && p.scale) {
+        const float d = __ldg(p.scale + h0 + i);
+        // (a rotated number is at most twice the largest of its head)
+        if (d >= 0x1p-60f && d <= 0x1p60f && fmaxf(reach(raw[i][0]), reach(raw[i][1])) <= 0x1p38f) {
+          const float r = __frcp_rn(d);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { lo[e] = divide(lo[e], d, r); hi[e] = divide(hi[e], d, r); }
-          } else {
+          for (int e = 0; e < 8; ++e) { lo[e] = divide(lo[e], d, r); hi[e] = divide(hi[e], d, r); }
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { lo[e] = __fdiv_rn(lo[e], d); hi[e] = __fdiv_rn(hi[e], d); }
-          }
+          for (int e = 0; e < 8; ++e) { lo[e] = plain_division(lo[e], d); hi[e] = plain_division(hi[e], d); }
         }
       }
-      store8(p + 8 * j, lo);
-      store8(p + HALF + 8 * j, hi);
+      C *dst = static_cast<C *>(p.dst) + at;
+      store8(dst, lo);
+      store8(dst + HALF, hi);
     }
   }
 }
 
+template <typename X, typename C, int DH, int H>
+bool launch_append_heads(AppendArgs &a, cudaStream_t st) {
+  constexpr unsigned LANES = 256 / (DH / 16);
+  unsigned long long blocks = 0;
+  for (int i = 0; i < 3; ++i) {
+    AppendPart &p = a.part[i];
+    p.groups = (p.heads + H - 1) / H;
+    p.first_block = (unsigned)blocks;
+    const unsigned long long pairs = (unsigned long long)a.n_tokens * p.groups;
+    if (pairs >= (1ull << 31) - LANES) return false;
+    blocks += (pairs + LANES - 1) / LANES;
+    // exact for indexes below 2^31: magic = ceil(2^(31 + s) / groups), s = ceil(log2(groups))
+    unsigned s = 0;
+    while ((1u << s) < (unsigned)p.groups) ++s;
+    p.shift = 31 + s;
+    p.magic = p.groups ? (unsigned)(((1ull << p.shift) + p.groups - 1) / p.groups) : 0;
+  }
+  if (blocks >= 1ull << 31) return false;
+  launch_pdl(k_paged_append<X, C, DH, H>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+  return true;
+}
 template <typename X, typename C, int DH>
-void launch_append_dh(AppendArgs &a, cudaStream_t st) {
-  constexpr int LANES = 256 / (DH / 16);
-  const int heads = a.hq + 2 * a.kv.n_kv_heads;
-  a.head_shift = 0;
-  while ((1 << a.head_shift) < heads && (1 << a.head_shift) < LANES) ++a.head_shift;
-  const int step = 1 << a.head_shift, tokens = LANES >> a.head_shift, rounds = (heads + step - 1) / step;
-  const long long groups = (a.n_tokens + tokens - 1) / tokens;
+bool launch_append_dh(AppendArgs &a, cudaStream_t st) {
   // Several heads per thread read (cos, sin) once for all of them; with few tokens one head per thread spreads the call
   // over more SMs.
-  const int ny = groups * rounds <= 4 * 148 ? rounds : (rounds + 2) / 3, H = (rounds + ny - 1) / ny;
-  const dim3 grid((unsigned)groups, (unsigned)ny);
-  if (H == 1) launch_pdl(k_paged_append<X, C, DH, 1>, grid, dim3(256), 0, st, a);
-  else if (H == 2) launch_pdl(k_paged_append<X, C, DH, 2>, grid, dim3(256), 0, st, a);
-  else launch_pdl(k_paged_append<X, C, DH, 3>, grid, dim3(256), 0, st, a);
+  const long long heads = a.part[0].heads + 2ll * a.kv.n_kv_heads;
+  if (a.n_tokens * heads * (DH / 16) <= 4ll * 148 * 256) return launch_append_heads<X, C, DH, 1>(a, st);
+  return launch_append_heads<X, C, DH, sizeof(C) == 1 ? 2 : 4>(a, st);
 }
 template <typename X, typename C>
-void launch_append(AppendArgs &a, int dh, cudaStream_t st) {
-  if (dh == 128) launch_append_dh<X, C, 128>(a, st);
-  else if (dh == 64) launch_append_dh<X, C, 64>(a, st);
-  else launch_append_dh<X, C, 32>(a, st);
+bool launch_append(AppendArgs &a, int dh, cudaStream_t st) {
+  return dh == 128 ? launch_append_dh<X, C, 128>(a, st) : dh == 64 ? launch_append_dh<X, C, 64>(a, st) : launch_append_dh<X, C, 32>(a, st);
 }
 
 bool int_span_ok(const void *p, unsigned align) { return p && ((uintptr_t)p & (align - 1)) == 0; }
@@ -571,23 +603,32 @@ int32_t d3_paged_append(const d3_paged_kv *kv, const d3_paged_append_args *a, vo
   if (a->n_tokens == 0) return D3_OK;
   AppendArgs p;
   memset(&p, 0, sizeof(p));
-  p.n_tokens = a->n_tokens; p.hq = a->q_dev ? a->n_q_heads : 0; p.rope_len = a->rope_len;
-  p.k = a->k_dev; p.v = a->v_dev; p.q = a->q_dev; p.q_out = a->q_out_dev;
-  p.kt = a->k_token_stride; p.kh = a->k_head_stride; p.vt = a->v_token_stride; p.vh = a->v_head_stride;
-  p.qt = a->q_token_stride; p.qh = a->q_head_stride; p.ot = a->q_out_token_stride; p.oh = a->q_out_head_stride;
+  p.n_tokens = a->n_tokens; p.rope_len = a->rope_len;
   p.slots = reinterpret_cast<const long long *>(a->slots_dev); p.context = a->context_dev; p.rope = a->rope_dev; p.status = a->status_dev;
   p.kv = pool_of(*kv);
-  if (p.hq + 2ll * kv->n_kv_heads > 65535) return D3_EINVAL;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (kv->dtype == D3_BF16) {
-    if (a->dtype == D3_BF16) launch_append<bf16, bf16>(p, dh, st);
-    else launch_append<float, bf16>(p, dh, st);
-  } else if (kv->dtype == D3_FP16) {
-    launch_append<__half, __half>(p, dh, st);
-  } else {
-    if (a->dtype == D3_BF16) launch_append<bf16, __nv_fp8_e4m3>(p, dh, st);
-    else launch_append<__half, __nv_fp8_e4m3>(p, dh, st);
+  const int rotate = a->rope_dev ? 1 : 0;
+  if (a->q_dev) {
+    AppendPart &q = p.part[0];
+    q.src = a->q_dev; q.dst = a->q_out_dev; q.heads = a->n_q_heads; q.rotate = rotate;
+    q.st = a->q_token_stride; q.sh = a->q_head_stride; q.dt = a->q_out_token_stride; q.dh = a->q_out_head_stride;
   }
+  for (int i = 1; i < 3; ++i) {
+    AppendPart &x = p.part[i];
+    x.src = i == 1 ? a->k_dev : a->v_dev; x.dst = i == 1 ? kv->k_dev : kv->v_dev;
+    x.st = i == 1 ? a->k_token_stride : a->v_token_stride; x.sh = i == 1 ? a->k_head_stride : a->v_head_stride;
+    x.dh = kv->head_stride; x.scale = i == 1 ? kv->k_scale_dev : kv->v_scale_dev;
+    x.heads = kv->n_kv_heads; x.rotate = i == 1 ? rotate : 0;
+  }
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  bool fits;
+  if (kv->dtype == D3_BF16) {
+    fits = a->dtype == D3_BF16 ? launch_append<bf16, bf16>(p, dh, st) : launch_append<float, bf16>(p, dh, st);
+  } else if (kv->dtype == D3_FP16) {
+    fits = launch_append<__half, __half>(p, dh, st);
+  } else {
+    fits = a->dtype == D3_BF16 ? launch_append<bf16, __nv_fp8_e4m3>(p, dh, st) : launch_append<__half, __nv_fp8_e4m3>(p, dh, st);
+  }
+  if (!fits) return D3_EINVAL;
   return cudaGetLastError() == cudaSuccess ? D3_OK : D3_ECUDA;
 }
 

@@ -71,7 +71,7 @@ def test_plans_that_are_refused(bad):
     dict(k_head_stride=65), dict(v_token_stride=130), dict(v_head_stride=1 << 40), dict(rope_len=0), dict(rope_dev=FAKE + 8),
     dict(context_dev=None), dict(rope_dev=None), dict(n_q_heads=0), dict(q_out_dev=None), dict(q_dev=FAKE + 2), dict(q_out_dev=FAKE + 2),
     dict(q_token_stride=257), dict(q_out_token_stride=32), dict(q_out_head_stride=0), dict(status_dev=FAKE + 1),
-    dict(n_q_heads=65532)], ids=str)
+    dict(n_q_heads=65536), dict(n_tokens=2 ** 31 - 1)], ids=str)
 def test_appends_that_are_refused(bad):
     assert B.LIB.d3_paged_append(C.byref(kv_args()), C.byref(append_args(**bad)), None) == B.EINVAL
 
