@@ -226,7 +226,8 @@ struct Cfg {
   static constexpr int kHeadFloats = DH + 4;                 // of a head's sums in shared memory (padded: no bank conflicts)
   static constexpr bool kF16 = CACHE != D3_BF16;
   static constexpr int kTiles = X == D3_FP32 ? 1 : MT;       // 8-head tiles
-  static constexpr int kQTerms = X == D3_FP32 ? 3 : 1, kPTerms = X == D3_FP32 ? 3 : 2;
+  // terms of P: one fp16 number (2^-11 of it) is enough under a bf16 result, whose own rounding is up to 2^-8
+  static constexpr int kQTerms = X == D3_FP32 ? 3 : 1, kPTerms = X == D3_FP32 ? 3 : CACHE == D3_E4M3 && X == D3_BF16 ? 1 : 2;
 };
 
 template <int DH, int CACHE, int X, int MT>
@@ -779,7 +780,10 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       for (int j = 0; j < PT; ++j)
 #pragma unroll
         for (int c = 0; c < NF; ++c) ldsm4(kf[j][c], chunk(kbase, j, 2 * c));
-      constexpr int NC = PT * KT == 1 ? 2 : 1;   // chains of products that a score is summed in
+      // Chains of products that a score is summed in: two where a warp has only one at a time to work on; with three terms the
+      // largest has two and the others have their own, because the tensor cores' sums lose a little with every product of
+      // a chain (error of fp32 outputs against 64 bits at 5000 positions 1.2e-6 with one chain).
+      constexpr int NC = TQ == 3 ? 3 : PT * KT == 1 ? 2 : 1;
       float sc[PT][KT][NC][4];
 #pragma unroll
       for (int j = 0; j < PT; ++j)
@@ -801,7 +805,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
           for (int i = 0; i < KT; ++i)
 #pragma unroll
-            for (int q = TQ - 1; q >= 0; --q) mma<F16>(sc[j][i][kk % NC], f, qb[i][q][kk][0], qb[i][q][kk][1]);
+            for (int q = TQ - 1; q >= 0; --q)
+              mma<F16>(sc[j][i][NC == 3 ? (q == 0 ? kk & 1 : 2) : kk % NC], f, qb[i][q][kk][0], qb[i][q][kk][1]);
         }
 #pragma unroll
       for (int j = 0; j < PT; ++j)
@@ -815,7 +820,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
         for (int j = 0; j < PT; ++j) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[j][e] = (NC == 2 ? sc[j][i][0][e] + sc[j][i][NC - 1][e] : sc[j][i][0][e]) * mul[i][e & 1];
+          for (int e = 0; e < 4; ++e) v[j][e] = (NC == 3 ? sc[j][i][2 % NC][e] + (sc[j][i][0][e] + sc[j][i][1 % NC][e])
+                                                               : NC == 2 ? sc[j][i][0][e] + sc[j][i][NC - 1][e] : sc[j][i][0][e]) * mul[i][e & 1];
           if (partial) {
             if (g >= valid[j]) v[j][0] = v[j][1] = -INFINITY;
             if (g + 8 >= valid[j]) v[j][2] = v[j][3] = -INFINITY;
@@ -856,10 +862,12 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
               for (int q = 0; q < 3; ++q) pb[j][i][q][r] = transpose8(cut(x, y));
             } else {
               const uint32_t hi = pack<F16>(x, y);
-              float hx, hy;
-              unpack<F16>(hi, hx, hy);
               pb[j][i][0][r] = transpose8(hi);
-              pb[j][i][1][r] = transpose8(pack<F16>(x - hx, y - hy));
+              if constexpr (TP == 2) {
+                float hx, hy;
+                unpack<F16>(hi, hx, hy);
+                pb[j][i][TP - 1][r] = transpose8(pack<F16>(x - hx, y - hy));
+              }
             }
           }
         }
@@ -885,9 +893,18 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           }
           if (partial) { f[0] &= keep0; f[1] &= keep0; f[2] &= keep1; f[3] &= keep1; }
 #pragma unroll
-          for (int i = 0; i < KT; ++i)
+          for (int i = 0; i < KT; ++i) {
+            if constexpr (TP == 3) {   // fp32 results: every piece's products in a chain of their own
+              float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int q = TP - 1; q >= 0; --q) mma<F16>(o[i][n], f, pb[j][i][q][0], pb[j][i][q][1]);
+              for (int q = TP - 1; q >= 0; --q) mma<F16>(d, f, pb[j][i][q][0], pb[j][i][q][1]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][n][e] += d[e];
+            } else {
+#pragma unroll
+              for (int q = TP - 1; q >= 0; --q) mma<F16>(o[i][n], f, pb[j][i][q][0], pb[j][i][q][1]);
+            }
+          }
         }
       }
     }

@@ -5,8 +5,9 @@ that rounding the attention kernel works in fp32, so with A = sum_t p_t |v_t| / 
 off by at most E * A, where E adds up
   2 d     d = the largest error of a score: (dh + 8) fp32 roundings of at most scale * sum |q_d k_d|
           (a weight is off by a factor e^d, numerator and denominator both)
-  2^-16   what is left of a weight after its two 16-bit terms (2^-8 of it after the first, rounded to 2^-9 of that
-          again; 2^-22 with three terms or fp16), twice 2^-17 for good measure
+  2^-16   what is left of a weight after its two bf16 terms (2^-8 of it after the first, 2^-8 of that after the second);
+          2^-21 with two fp16 or three bf16 ones (2^-22, 2^-24); 2^-10 with one fp16 term (8-bit cache, bf16 result:
+          2^-11 of it, and as much again for sums that use the unrounded weights)
   c 2^-23 c = sums of length/16 tensor-core steps and the joining of warps and CTAs
   2^-20   two exponentials of 2^-22 each (the weight, the rescaling) in numerator and denominator
 The rotary products and sums of append are rounded one by one, so its results are compared bit for bit
@@ -78,7 +79,7 @@ def check(out, lse, q, cache, table, contexts, scale=None, rows=None):
     scale = dh ** -0.5 if scale is None else scale
     half = torch.finfo(out.dtype).eps / 2
     t = table.cpu().tolist()
-    terms = 2.0 ** -16 if k.dtype == BF16 and q.dtype == BF16 else 2.0 ** -21
+    terms = 2.0 ** -16 if k.dtype == BF16 and q.dtype == BF16 else 2.0 ** -10 if k.dtype == E4M3 and q.dtype == BF16 else 2.0 ** -21
     for b, n in enumerate(contexts):
         r = b if rows is None else rows[b]
         if r < 0:
