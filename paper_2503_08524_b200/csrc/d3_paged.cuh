@@ -53,7 +53,9 @@ inline KvPool pool_of(const d3_paged_kv &kv) {
 }
 
 // Positions of a unit, the attention kernel's stage: up to 32 KB of K and V.
-__host__ __device__ constexpr int unit_positions(int head_dim, int elem_bytes) { return head_dim * elem_bytes > 128 ? 64 : 128; }
+__host__ __device__ constexpr int unit_positions(int head_dim, int elem_bytes) {
+  return head_dim * elem_bytes > 128 ? 64 : head_dim * elem_bytes > 64 ? 128 : 256;
+}
 // Tensor maps of a pool: (dim, position, kv head, page), boxes of min(128 bytes, a row) x up to a page's or a unit's
 // positions (k, v) and x 16 positions (k16, v16); `of` is the pool they were made for.
 struct PoolMaps {

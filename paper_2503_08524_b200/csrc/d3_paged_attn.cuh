@@ -196,12 +196,15 @@ enum { OUT_WHOLE = 0, OUT_HEAD = 1, OUT_TAIL = 2, OUT_NONE = 3 };
 
 // What the producers tell the consumers about a stage (one 16-byte load).
 struct __align__(16) StageInfo {
-  int row, head, kvh;   // head: the tile's first query head
-  uint32_t bits;        // positions in the stage (0 .. 128) | STAGE_* << 8 | OUT_* << 11 | heads of the tile << 13 | tiles that hold positions << 18
+  int row;
+  uint32_t heads;       // the tile's first query head | kv head << 16
+  uint32_t bits;        // positions in the stage (0 .. 256) | STAGE_* << 9 | OUT_* << 12 | heads of the tile << 14
+  uint32_t tiles;       // which tiles hold positions
 };
 // What the consumers tell the epilogue warps about an item.
 struct __align__(16) ItemInfo {
-  int row, head, kvh;
+  int row;
+  uint32_t heads;       // as above
   uint32_t bits;        // OUT_* | last of the CTA << 2 | heads << 3 | first warp with a piece of it << 8 | such warps << 16
 };
 
@@ -213,7 +216,7 @@ struct Cfg {
   static constexpr int kBoxes = kRow / kBox;                 // boxes per piece of K (or V)
   static constexpr int kHeads = X == D3_FP32 ? 8 : 8 * MT;   // query heads of a tile
   static constexpr int kUnit = unit_positions(DH, kEs);      // positions of a stage (of up to 32 KB)
-  static constexpr int kPT = kRow > 128 ? 1 : 2;             // tiles of a piece, i.e. of a warp's trip (32 fragment registers)
+  static constexpr int kPT = kRow > 128 ? 1 : kRow > 64 ? 2 : 4;   // tiles of a piece, i.e. of a warp's trip (32 fragment registers)
   static constexpr int kHalfBytes = kUnit * kRow;            // K (or V) of a stage
   static constexpr int kQRow = DH * QBytes<X>::v + 16;       // a query head in shared memory (padded: no bank conflicts)
   static constexpr int kQBytes = kHeads * kQRow;
@@ -394,7 +397,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     auto idle = [&]() {   // a stage that sends the other warps home
       if (me == 0 && lane == 0) {
         if (!a.whole) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
-        s_info[0] = StageInfo{0, 0, 0, (uint32_t)((STAGE_LAST | STAGE_FINAL) << 8 | OUT_NONE << 11)};
+        s_info[0] = StageInfo{0, 0u, (uint32_t)((STAGE_LAST | STAGE_FINAL) << 9 | OUT_NONE << 12), 0u};
         mb_arrive(smem_u32(&s_full[0]));
       }
     };
@@ -451,7 +454,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (a.tiles_per_head > 1) { kvh = tile / a.tiles_per_head; sub = tile % a.tiles_per_head; }
     const int32_t *pages = a.table + (long long)trow * a.table_stride;
     auto fetch = [&](int base) -> int { return base + lane < a.table_width ? __ldg(pages + base + lane) : -1; };
-    // page ids of the row, one per lane: 32 aligned pages in `win`, the next 32 in `win_next`.  A unit is at most 8
+    // page ids of the row, one per lane: 32 aligned pages in `win`, the next 32 in `win_next`.  A unit is at most 16
     // aligned pages and never straddles a window.
     int win0 = -1, win = 0, win_next = 0;
     const int box_rows = min(1 << a.page_shift, kUnit), page_mask = (1 << a.page_shift) - 1;
@@ -499,7 +502,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         if (n > 0) {
           if (win0 < 0) { win0 = pg0 & ~31; win = fetch(win0); win_next = fetch(win0 + 32); }
           else if (pg0 >= win0 + 32) {
-            // the other producers' units may have moved past the whole next window only if a unit had more than 16 pages
+            // (a unit is 16 pages at most, and the other producer takes every second one: never past the next window)
             win0 += 32; win = win_next; win_next = fetch(win0 + 32);
           }
         }
@@ -511,7 +514,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         // this lane's copy: box of positions, K or V, 128-byte column.  Whole units go in boxes of up to a page, the
         // last unit of a row in boxes of 16 positions (nothing is fetched behind the tile the row ends in).
         const bool whole = n == kUnit;
-        const int bs = whole ? full_shift : (kUnit == 64 ? 2 : 3);
+        const int bs = whole ? full_shift : (kUnit == 64 ? 2 : kUnit == 128 ? 3 : 4);
         const int box = lane & ((1 << bs) - 1), is_v = (lane >> bs) & 1, col = lane >> (bs + 1);
         const int off = box * (kUnit >> bs), pos = p0 + off;
         const int id = __shfl_sync(0xffffffffu, win, (pos >> a.page_shift) & 31);
@@ -523,7 +526,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         if (lane == 0) {
           const int kind = !last || (ends && whole_start) ? OUT_WHOLE : !ends && whole_start ? OUT_TAIL : OUT_HEAD;
           const int flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (final ? STAGE_FINAL : 0);
-          s_info[s] = StageInfo{row, head, kvh, (uint32_t)n | (uint32_t)flags << 8 | (uint32_t)kind << 11 | (uint32_t)nh << 13 | tiles << 18};
+          s_info[s] = StageInfo{row, (uint32_t)head | (uint32_t)kvh << 16,
+                                (uint32_t)n | (uint32_t)flags << 9 | (uint32_t)kind << 12 | (uint32_t)nh << 14, tiles};
           mb_arrive_tx(full, (uint32_t)__popc(tiles) * 2u * kTile * C::kRow + (first ? (uint32_t)(nh * DH * QBytes<X>::v) : 0u));
         }
         __syncwarp();
@@ -578,7 +582,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       if (kind == OUT_NONE) break;
       int from = first_warp + min(lane, warps - 1);   // lane k: the k-th warp that had a piece of the item
       if (from >= C::kWarps) from -= C::kWarps;
-      const float vs = a.v_scale ? __ldg(a.v_scale + item.kvh) : 1.f;
+      const float vs = a.v_scale ? __ldg(a.v_scale + (item.heads >> 16)) : 1.f;
       // HB heads at a time, in independent chains: this is all latency
       auto heads = [&](auto hb, int h0) {
         constexpr int HB = decltype(hb)::value;
@@ -632,11 +636,11 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           const float l = __shfl_sync(0xffffffffu, L[i], 0), m = __shfl_sync(0xffffffffu, M[i], 0);
           if (kind == OUT_WHOLE) {
             const float f = l == 0.f ? 0.f : vs / l;
-            const long long at = item.row * a.out_row_stride + (long long)(item.head + h) * a.out_head_stride + lane * V;
+            const long long at = item.row * a.out_row_stride + (long long)((item.heads & 0xffffu) + h) * a.out_head_stride + lane * V;
 #pragma unroll
             for (int e = 0; e < V; ++e) write_out(at + e, o[i][e] * f);
             if (lane == 0 && a.lse)
-              a.lse[(long long)item.row * a.hq + item.head + h] = l == 0.f ? -INFINITY : (m + (log2f(l) - (F16 ? 15.f : 0.f))) * kLn2;
+              a.lse[(long long)item.row * a.hq + (item.heads & 0xffffu) + h] = l == 0.f ? -INFINITY : (m + (log2f(l) - (F16 ? 15.f : 0.f))) * kLn2;
           } else {
             const size_t part = (size_t)(2 * blockIdx.x + (kind == OUT_TAIL ? 1 : 0)) * 16 + h;
 #pragma unroll
@@ -687,15 +691,15 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     ok = __all_sync(0xffffffffu, ok);
     if (!ok) break;
     const StageInfo info = s_info[s];
-    const uint32_t flags = info.bits >> 8;
-    const int n = info.bits & 255;
+    const uint32_t flags = info.bits >> 9;
+    const int n = info.bits & 511;
     more = !(flags & STAGE_FINAL);
     if (flags & STAGE_FIRST) {
       if (items == 0) pdl_wait();   // returns at once: the producers' has
       // ---- this thread's fragments of Q, and what a raw score is multiplied by
-      const int nh = (info.bits >> 13) & 31;
+      const int nh = (info.bits >> 14) & 31;
       first_warp = piece_turn; item_pieces = 0;
-      const float ks = a.k_scale ? __ldg(a.k_scale + info.kvh) : 1.f;
+      const float ks = a.k_scale ? __ldg(a.k_scale + (info.heads >> 16)) : 1.f;
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
         const int h = g + 8 * i;
@@ -765,8 +769,11 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       int valid[PT];
 #pragma unroll
       for (int j = 0; j < PT; ++j)
-        valid[j] = (info.bits >> (18 + p * PT + j)) & 1 ? min(kTile, n - (p * PT + j) * kTile) : 0;
-      const bool partial = PT == 1 ? valid[0] < kTile : valid[0] + valid[PT - 1] < PT * kTile;
+        valid[j] = (info.tiles >> (p * PT + j)) & 1 ? min(kTile, n - (p * PT + j) * kTile) : 0;
+      int there = 0;
+#pragma unroll
+      for (int j = 0; j < PT; ++j) there += valid[j];
+      const bool partial = there < PT * kTile;
       const uint32_t kbase = ring + s * C::kStageBytes + p * (PT * kTile * C::kBox) + k_lane;
       const uint32_t vbase = ring + s * C::kStageBytes + C::kHalfBytes + p * (PT * kTile * C::kBox) + v_lane;
       // 16-byte chunk c (even) of tile j past the lane's own: an XOR inside the 128-byte line, the next column behind it
@@ -947,8 +954,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
       }
       if (warp == 0 && lane == 0)
-        s_item = ItemInfo{info.row, info.head, info.kvh,
-                          ((flags >> 3) & 3) | (more ? 0u : 4u) | ((info.bits >> 13) & 31) << 3 | (uint32_t)first_warp << 8 | (uint32_t)warps << 16};
+        s_item = ItemInfo{info.row, info.heads,
+                          ((flags >> 3) & 3) | (more ? 0u : 4u) | ((info.bits >> 14) & 31) << 3 | (uint32_t)first_warp << 8 | (uint32_t)warps << 16};
       __syncwarp();
       if (lane == 0) mb_arrive(smem_u32(&s_sums_full));
       ++items;
