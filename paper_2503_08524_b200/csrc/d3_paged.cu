@@ -18,8 +18,9 @@ namespace {
 // (tokens, pages needed, pages given back) of all requests in shared memory; after that the CTAs share page and token
 // entries between them and need nothing of one another: a page that is taken is looked up by its rank in
 // (old stack ++ pages given back), so nothing waits for the stack or the table to be written, and what is written is
-// never what another CTA reads.  Only where the new lengths replace the old ones in place do the CTAs have to have read
-// them all first: then they are one cluster with a barrier, of up to eight.
+// never what another CTA reads.  Only where the new lengths replace the old ones in place must no CTA read them any
+// more when they are written: with several CTAs a second launch, of one CTA, then writes the lengths
+// (192 prompts in place: 8.4 us; as one cluster of eight CTAs with a barrier 20.8).
 constexpr int kPlanMaxThreads = 1024;
 constexpr int kPlanMaxPer = D3_MAX_REQUESTS / kPlanMaxThreads;   // requests of one thread
 
@@ -32,12 +33,8 @@ struct PlanArgs {
   int32_t *cached_out, *n_free_out, *first;
   long long *slots;
   int32_t *row, *context, *status;
-  int cluster;   // the grid is one cluster that has to meet before the first store
+  int maps, lengths;   // what this launch writes: pages, maps and `first`; cached_out and n_free_out
 };
-
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-}
 
 // the request whose half-open range [sum[b], sum[b + 1]) holds x  (sum[0] = 0 <= x < sum[R])
 __device__ __forceinline__ int owner(const int *sum, int R, int x) {
@@ -135,9 +132,7 @@ __global__ void __launch_bounds__(kPlanMaxThreads) k_page_plan(const __grid_cons
     }
     if (tid == 0) { s_first[a.R] = (int)total[0]; s_need[a.R] = (int)total[1]; s_back[a.R] = (int)total[2]; }
   }
-  // in place: all CTAs have read the lengths and the stack's height, they may be overwritten from here on
-  if (a.cluster) cluster_barrier();
-  __syncthreads();
+  __syncthreads();   // (one CTA may write in place: all its threads have read the lengths and the stack's height)
 
   const int gid = blockIdx.x * threads + tid, step = gridDim.x * threads;
   if (blockIdx.x == 0) {
@@ -145,22 +140,23 @@ __global__ void __launch_bounds__(kPlanMaxThreads) k_page_plan(const __grid_cons
     for (int i = 0; i < kPlanMaxPer; ++i) {
       const int b = tid * per + i;
       if (i < per && b < a.R) {
-        if (!bad) {
-          a.cached_out[b] = back_[i] ? 0 : c_[i] + add_[i];
-          a.first[b] = s_first[b];
-        } else {
-          if (a.cached_out != a.cached) a.cached_out[b] = a.cached[b];
-          a.first[b] = 0;
+        if (a.lengths) {
+          if (!bad) a.cached_out[b] = back_[i] ? 0 : c_[i] + add_[i];
+          else if (a.cached_out != a.cached) a.cached_out[b] = a.cached[b];
         }
+        if (a.maps) a.first[b] = bad ? 0 : s_first[b];
       }
     }
     if (tid == 0) {
-      a.first[a.R] = bad ? 0 : (int)total[0];
-      if (!bad) *a.n_free_out = (int)(n_free + total[2] - total[1]);
-      else if (a.n_free_out != a.n_free) *a.n_free_out = n_free;
+      if (a.maps) a.first[a.R] = bad ? 0 : (int)total[0];
+      if (a.lengths) {
+        if (!bad) *a.n_free_out = (int)(n_free + total[2] - total[1]);
+        else if (a.n_free_out != a.n_free) *a.n_free_out = n_free;
+      }
       if (bad && a.status) *a.status = (bad & 2) ? D3_EINVAL : D3_ECAPACITY;
     }
   }
+  if (!a.maps) return;
   const int n_tok = bad ? 0 : (int)total[0], n_need = bad ? 0 : (int)total[1], n_back = bad ? 0 : (int)total[2];
   const int top = n_free + n_back;
   // entry i of (old stack ++ pages given back)
@@ -280,24 +276,6 @@ __device__ __forceinline__ void widen8(const Raw8<__half> &r, float *f) {
     f[2 * i] = v.x; f[2 * i + 1] = v.y;
   }
 }
-// the largest |x| of eight numbers, NaN counting as infinite: at least their true one
-__device__ __forceinline__ float reach(const Raw8<float> &r) {
-  const uint32_t w[8] = {r.u.x, r.u.y, r.u.z, r.u.w, r.w.x, r.w.y, r.w.z, r.w.w};
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
-  return m > 0x7f800000u ? INFINITY : __uint_as_float(m);
-}
-__device__ __forceinline__ float reach(const Raw8<bf16> &r) {
-  const uint32_t m = __vmaxu2(__vmaxu2(r.u.x & 0x7fff7fffu, r.u.y & 0x7fff7fffu), __vmaxu2(r.u.z & 0x7fff7fffu, r.u.w & 0x7fff7fffu));
-  const uint32_t v = max(m & 0xffffu, m >> 16);
-  return v > 0x7f80u ? INFINITY : __uint_as_float(v << 16);
-}
-__device__ __forceinline__ float reach(const Raw8<__half> &r) {
-  const uint32_t m = __vmaxu2(__vmaxu2(r.u.x & 0x7fff7fffu, r.u.y & 0x7fff7fffu), __vmaxu2(r.u.z & 0x7fff7fffu, r.u.w & 0x7fff7fffu));
-  const uint32_t v = max(m & 0xffffu, m >> 16);
-  return v >= 0x7c00u ? INFINITY : 65504.f;
-}
 // the plain division, out of line: it is rarely taken, and 64 copies of it would crowd the instruction cache
 __device__ __noinline__ float plain_division(float x, float d) { return __fdiv_rn(x, d); }
 // x / d rounded once, for |x| <= 2^40 and a d in 2^-60 .. 2^60 whose correctly rounded reciprocal r is known: the remainder
@@ -400,8 +378,10 @@ __global__ void __launch_bounds__(256, sizeof(C) == 1 ? 4 : 1) k_paged_append(co
     } else {
       if (sizeof(C) == 1 && p.scale) {
         const float d = __ldg(p.scale + h0 + i);
-        // (a rotated number is at most twice the largest of its head)
-        if (d >= 0x1p-60f && d <= 0x1p60f && fmaxf(reach(raw[i][0]), reach(raw[i][1])) <= 0x1p38f) {
+        float top = 0.f;   // (NaN is passed over here, and through the division)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(fabsf(lo[e]), fabsf(hi[e])));
+        if (d >= 0x1p-60f && d <= 0x1p60f && top <= 0x1p40f) {
           const float r = __frcp_rn(d);
 #pragma unroll
           for (int e = 0; e < 8; ++e) { lo[e] = divide(lo[e], d, r); hi[e] = divide(hi[e], d, r); }
@@ -543,18 +523,18 @@ int32_t d3_page_plan(const d3_page_plan_args *a, void *cuda_stream) {
   p.n_free = a->n_free_dev; p.cached_out = a->cached_out_dev; p.n_free_out = a->n_free_out_dev; p.first = a->first_dev;
   p.slots = reinterpret_cast<long long *>(a->slots_dev); p.row = a->row_dev; p.context = a->context_dev; p.status = a->status_dev;
   const size_t smem = ((size_t)4 * a->n_requests + 3) * sizeof(int);
-  // In place: one CTA while its threads take at most one group of four tokens each, then a cluster of eight.  Elsewhere as many
-  // CTAs as there are groups of four tokens for, up to one per SM (192 prompts of 129..2048 tokens, 209,000
-  // in all: 21.3 us as a cluster of eight, PLAN_GRID_US as 52 CTAs).
+  // As many CTAs as there are entries for, up to one per SM (192 prompts of 129..2048 tokens, 209,000 in all: 21.3 us as
+  // eight CTAs, 6.1 as 148); few tokens are one small CTA's.
   const bool in_place = a->cached_out_dev == a->cached_dev || a->n_free_out_dev == a->n_free_dev;
-  const int threads = a->n_requests <= 128 && a->max_tokens <= 512 ? 128 : in_place || a->n_requests > 1024 ? 1024 : 256;
+  const int threads = a->n_requests <= 128 && a->max_tokens <= 512 ? 128 : a->n_requests > 1024 ? 1024 : 256;
   const long long entries = ((long long)a->max_tokens + 3) / 4 + (a->max_tokens > 512 ? a->n_pages / 4 : 0);
   long long ctas = (entries + threads - 1) / threads;
   if (ctas > 148) ctas = 148;
-  if (in_place && ctas > 1) ctas = 8;
-  p.cluster = in_place && ctas > 1 ? 1 : 0;
-  // sums of at most 4096 entries of at most 2^19 stay within 32 bits
-  const bool narrow = a->max_tokens <= (1 << 19) && a->n_pages <= (1 << 19) && a->table_width <= (1 << 19);
+  const bool twice = in_place && ctas > 1;
+  p.maps = 1;
+  p.lengths = twice ? 0 : 1;
+  // sums of at most 4096 entries of at most 2^18 stay within 32 bits
+  const bool narrow = a->max_tokens <= (1 << 18) && a->n_pages <= (1 << 18) && a->table_width <= (1 << 18);
   void (*kernel)(PlanArgs) = narrow ? k_page_plan<int> : k_page_plan<long long>;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return D3_ECUDA;
@@ -565,20 +545,14 @@ int32_t d3_page_plan(const d3_page_plan_args *a, void *cuda_stream) {
       return D3_ECUDA;
     ready[narrow][dev].store(true, std::memory_order_release);
   }
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = static_cast<cudaStream_t>(cuda_stream);
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)ctas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = p.cluster ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? D3_OK : D3_ECUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (launch_pdl(kernel, dim3((unsigned)ctas), dim3((unsigned)threads), smem, st, p) != cudaSuccess) return D3_ECUDA;
+  if (twice) {
+    p.maps = 0;
+    p.lengths = 1;
+    if (launch_pdl(kernel, dim3(1), dim3((unsigned)threads), smem, st, p) != cudaSuccess) return D3_ECUDA;
+  }
+  return D3_OK;
 }
 
 int32_t d3_paged_append(const d3_paged_kv *kv, const d3_paged_append_args *a, void *cuda_stream) {

@@ -68,6 +68,8 @@ _APPEND = struct.Struct("=I4i4x2Q4q2Q4q4Q")
 _ATTENTION = struct.Struct("=I5iqf4xQ2qQ2q7Q")
 assert _APPEND.size == C.sizeof(PagedAppendArgs) and _ATTENTION.size == C.sizeof(PagedAttentionArgs)
 
+_APPEND_PACK, _APPEND_SIZE, _ATTENTION_PACK, _ATTENTION_SIZE = _APPEND.pack, _APPEND.size, _ATTENTION.pack, _ATTENTION.size
+
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _device_now = torch._C._cuda_getDevice
 
@@ -110,7 +112,7 @@ def _on_stream(call, index: int, stream, what: str):
 
 def _vector(t: torch.Tensor, dtype, n: int, index: int, what: str, name: str) -> int:
     """Data pointer of a contiguous 1-D tensor of `n` entries (-1: any number)."""
-    if t.dtype is not dtype or t.dim() != 1 or (t.shape[0] != n and n != -1) or t.get_device() != index or not t.is_contiguous():
+    if t.dtype is not dtype or t.get_device() != index or t.dim() != 1 or (t.shape[0] != n and n != -1) or not t.is_contiguous():
         _refuse(f"{what}: {name} must be a contiguous {dtype} vector" + ("" if n < 0 else f" of {n}") + f" on device {index}")
     return t.data_ptr()
 
@@ -271,7 +273,7 @@ def d3_paged_append(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, slots: tor
         op, ot, oh = _heads(q_out, n, hq, dh, dtype, dev, what, "q_out")
     elif q_out is not None:
         _refuse(f"{what}: q_out without q")
-    a = _APPEND.pack(_APPEND.size, _TYPES[dtype], n, hq, rope_len, kp, vp, kt, kh, vt, vh, qp, op, qt, qh, ot, oh,
+    a = _APPEND_PACK(_APPEND_SIZE, _TYPES[dtype], n, hq, rope_len, kp, vp, kt, kh, vt, vh, qp, op, qt, qh, ot, oh,
                      _vector(slots, _I64T, n, dev, what, "slots"), context_p, rope_p, 0 if status is None else _vector(status, _I32T, 1, dev, what, "status"))
     if n > 0:
         _call(LIB.d3_paged_append, what, dev, cache._ref, a)
@@ -299,10 +301,17 @@ def d3_paged_attention(cache: PagedKV, q: torch.Tensor, table: torch.Tensor, con
     if stream is not None:
         return _on_stream(lambda: d3_paged_attention(cache, q, table, context, rows=rows, scale=scale, out=out, lse=lse,
                                                      with_lse=with_lse, workspace=workspace, status=status), dev, stream, what)
-    if q.dim() != 3 or dtype not in _TYPES:
+    code = _TYPES.get(dtype)
+    if q.dim() != 3 or code is None:
         _refuse(f"{what}: q must be [n][n_q_heads][head_dim]")
     n, hq, dh = q.shape
-    qp, qt, qh = _heads(q, n, hq, cache.head_dim, dtype, dev, what, "q")
+    qt, qh, q1 = q.stride()
+    if dh != cache.head_dim or q1 != 1 or q.get_device() != dev:
+        _refuse(f"{what}: q must be [n][n_q_heads][{cache.head_dim}] on device {dev}, last dimension contiguous")
+    if hq == 1:
+        qh = dh
+    if n <= 1:
+        qt = hq * qh
     if table.dtype is not _I32T or table.dim() != 2 or table.get_device() != dev:
         _refuse(f"{what}: table must be int32 [rows][width] on device {dev}")
     rows_n, width = table.shape
@@ -310,7 +319,7 @@ def d3_paged_attention(cache: PagedKV, q: torch.Tensor, table: torch.Tensor, con
     if rows_n < 1 or width < 1 or (inner != 1 and width > 1):
         _refuse(f"{what}: table must have entries and contiguous rows")
     if out is None:
-        out = torch.empty_like(q) if q.is_contiguous() else q.new_empty((n, hq, dh))
+        out = torch.empty_like(q) if qt == hq * dh and qh == dh else q.new_empty((n, hq, dh))
         op, ot, oh = out.data_ptr(), hq * dh, dh
     else:
         op, ot, oh = _heads(out, n, hq, dh, dtype, dev, what, "out")
@@ -325,13 +334,13 @@ def d3_paged_attention(cache: PagedKV, q: torch.Tensor, table: torch.Tensor, con
         _refuse(f"{what}: lse must be contiguous fp32 [{n}][{hq}] on device {dev}")
     if workspace is None:
         workspace = attention_workspace(cache, hq)
-    elif workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
-        _refuse(f"{what}: workspace must be contiguous uint8 on device {dev}")
-    a = _ATTENTION.pack(_ATTENTION.size, _TYPES[dtype], n, hq, rows_n, width, stride if rows_n > 1 else width,
-                        scale, qp, qt, qh, op, ot, oh, 0 if lse is None else lse.data_ptr(),
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse(f"{what}: workspace must be contiguous, on device {dev}")
+    a = _ATTENTION_PACK(_ATTENTION_SIZE, code, n, hq, rows_n, width, stride if rows_n > 1 else width,
+                        scale, q.data_ptr(), qt, qh, op, ot, oh, 0 if lse is None else lse.data_ptr(),
                         table.data_ptr(), _vector(context, _I32T, n, dev, what, "context"),
                         0 if rows is None else _vector(rows, _I32T, n, dev, what, "rows"),
-                        workspace.data_ptr(), workspace.numel(), 0 if status is None else _vector(status, _I32T, 1, dev, what, "status"))
+                        workspace.data_ptr(), workspace.nbytes, 0 if status is None else _vector(status, _I32T, 1, dev, what, "status"))
     if n > 0:
         _call(LIB.d3_paged_attention, what, dev, cache._ref, a)
     return out if lse is None else (out, lse)

@@ -156,12 +156,24 @@ def test_attention_page_sizes_and_long_rows(paged, page, layout):
     check(out, lse, q, cache, table, contexts)
 
 
-@pytest.mark.parametrize("n,hq,hkv", [(1, 8, 1), (1, 32, 32), (3, 64, 8), (700, 4, 4), (1100, 2, 1)])
+@pytest.mark.parametrize("n,hq,hkv", [(1, 8, 1), (1, 32, 32), (3, 64, 8), (700, 4, 4), (1100, 2, 1), (128, 3, 3), (129, 3, 3)])
 def test_attention_row_counts(paged, n, hq, hkv):
     """One row cut over all SMs; more rows than threads of a CTA."""
     contexts = [40000] if n == 1 and hkv == 1 else [777, 1500, 2048][:n] if n <= 3 else [(37 * i) % 130 for i in range(n)]
     cache, table, q, ctx = make(paged, contexts, hq, hkv, 64, 32, FP16, FP16, seed=n)
     out, lse = paged.d3_paged_attention(cache, q, table, ctx, with_lse=True)
+    check(out, lse, q, cache, table, contexts)
+
+
+@pytest.mark.parametrize("contexts", [[2000] * 4, [1100] * 9, [700, 640, 0, 655], [3000, 1, 1, 1, 1, 1], [500] * 40], ids=str)
+def test_attention_whole_and_cut_rows(paged, contexts):
+    """Rows of like lengths stay whole in one CTA, others are cut: the results do not tell."""
+    cache, table, q, ctx = make(paged, contexts, 32, 32, 128, 64, BF16, BF16, seed=len(contexts))
+    out, lse = paged.d3_paged_attention(cache, q, table, ctx, with_lse=True)
+    check(out, lse, q, cache, table, contexts)
+    wide = torch.full((len(contexts), 4000), -1, dtype=torch.int32, device=DEV)      # room for more than any row has
+    wide[:, :table.shape[1]] = table
+    out, lse = paged.d3_paged_attention(cache, q, wide, ctx, with_lse=True)
     check(out, lse, q, cache, table, contexts)
 
 
@@ -377,6 +389,35 @@ def test_append_without_rotation_saturates_and_keeps_nan(paged):
     a, b = k[1, 0, 1].float(), v[2, 0, 8].float()
     assert a[:4].tolist() == [448.0, -448.0, 448.0, -448.0] and a[4].isnan() and float(a[5]) == 2.0 ** -9 * round(0.001 * 512)
     assert b[:4].tolist() == [448.0, 448.0, 16.0, 20.0]
+
+
+@pytest.mark.parametrize("scale", [1.0, 3e-3, 1e-25, 1e25, 2.0 ** -130, float("inf"), -0.7])
+def test_append_division_by_any_scale(paged, scale):
+    """What is stored is x / scale, rounded once to fp32 and then to 8 bits, for ordinary and for extreme numbers."""
+    g = torch.Generator(DEV).manual_seed(4)
+    n, dh = 4096, 64
+    x = torch.empty((n, 1, dh), dtype=BF16, device=DEV).normal_(generator=g)
+    x = (x.float() * 10.0 ** torch.empty((n, 1, 1), device=DEV).uniform_(-30, 30, generator=g)).to(BF16)
+    x[0, 0, :8] = torch.tensor([0.0, -0.0, math.inf, -math.inf, 1e38, -1e38, 1e-38, 3e-39])
+    k, v = pool(n // 16, 1, 16, dh, E4M3)
+    sc = torch.full((1,), scale, device=DEV)
+    paged.d3_paged_append(paged.PagedKV(k, v, sc, sc), x, x, torch.arange(n, device=DEV))
+    want = (x.float() / sc).clamp(-448.0, 448.0).to(E4M3).float().reshape(n, dh)
+    for t in (k, v):
+        got = t.float().permute(0, 2, 1, 3).reshape(n, dh)
+        assert torch.equal(got.nan_to_num(9e9), want.nan_to_num(9e9))
+
+
+def test_append_a_rotary_table_beyond_the_unit_circle(paged):
+    """Tables that also scale (or hold anything else) are taken as they are."""
+    x = torch.full((16, 1, 64), 3e4, dtype=FP16, device=DEV)
+    k, v = pool(1, 1, 16, 64, E4M3)
+    one = torch.ones(1, device=DEV)
+    rope = torch.tensor([[1e35, -1e35], [2.0, 0.5], [1e-3, 1e-3]], device=DEV)[:, None, :].expand(3, 32, 2).contiguous()
+    ctx = torch.tensor([1 + i % 3 for i in range(16)], dtype=torch.int32, device=DEV)
+    paged.d3_paged_append(paged.PagedKV(k, v, one, one), x, x, torch.arange(16, device=DEV), rope=rope, context=ctx)
+    want = rotated(x, rope, ctx).clamp(-448.0, 448.0).to(E4M3).float()      # (inf - inf among it)
+    assert torch.equal(k.float().permute(0, 2, 1, 3).reshape(16, 1, 64).nan_to_num(9e9), want.nan_to_num(9e9))
 
 
 def test_append_bad_slots_and_positions_are_skipped_and_reported(paged):

@@ -160,7 +160,7 @@ def test_binding_refusals():
     refused(P.d3_paged_attention, cache, q, table, ctx, rows=ctx[:2])
     refused(P.d3_paged_attention, cache, q, table, ctx, out=q[:2])
     refused(P.d3_paged_attention, cache, q, table, ctx, lse=torch.zeros(3, 5))
-    refused(P.d3_paged_attention, cache, q, table, ctx, workspace=torch.zeros(5))
+    refused(P.d3_paged_attention, cache, q, table, ctx, workspace=torch.zeros(5, 2)[:, 0])
     x, slots = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64)
     rope = torch.zeros(7, 32, 2)
     refused(P.d3_paged_append, cache, x, x, slots)                             # not on a CUDA device
