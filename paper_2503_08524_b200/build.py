@@ -1,5 +1,6 @@
 """Builds libd3.so (the CUDA library behind the C ABI of include/d3.h) in-tree
-with nvcc for sm_100a.  No GPU is needed to build."""
+with nvcc for sm_100a, and _paged_call.so (the Python side of the paged operators'
+calls, csrc/paged_call.cpp) with g++.  No GPU is needed to build."""
 from __future__ import annotations
 
 import glob
@@ -11,6 +12,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libd3.so")
+CALL = os.path.join(PKG, "_paged_call.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
@@ -63,5 +65,27 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def build_call(force: bool = False) -> str:
+    """Compile and link the extension module that makes the paged operators' calls; returns its path."""
+    src, header = os.path.join(CSRC, "paged_call.cpp"), os.path.join(ROOT, "include", "d3.h")
+    if not force and os.path.exists(CALL) and os.path.getmtime(CALL) > max(os.path.getmtime(src), os.path.getmtime(header)):
+        return CALL
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(NVCC))
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(base, "include"),
+           "-I", os.path.join(base, "include", "torch", "csrc", "api", "include"), "-I", os.path.join(cuda, "include"), src, "-o", CALL + ".new",
+           "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed on " + src + ":\n" + res.stdout + res.stderr)
+    os.replace(CALL + ".new", CALL)
+    return CALL
+
+
 if __name__ == "__main__":
     print(build(force=True, verbose="-v" in sys.argv))
+    print(build_call(force=True))

@@ -2,7 +2,8 @@
 lengths, append with rotary positions, attention of one new token per row.
 
 Marshalling only, like `binding`: tensors in, one C call, no host synchronisation; the calls can be
-captured into a CUDA graph.  They run on the current stream of the tensors' device unless `stream`
+captured into a CUDA graph.  The checks of each call are in csrc/paged_call.cpp (a small decode step is
+bound by the host side of its calls).  They run on the current stream of the tensors' device unless `stream`
 is given.  A refused call raises D3Error (EINVAL) before anything is enqueued; what only the device
 can see (a page id out of range, too few free pages) goes to the `status` tensor.
 
@@ -14,18 +15,23 @@ can see (a page id out of range, too few free pages) goes to the `status` tensor
 from __future__ import annotations
 
 import ctypes as C
-import struct
 from typing import Optional
 
 import torch
 
+from . import build as _build
 from .binding import EINVAL, LIB, OK, D3Error
+
+_build.build_call()
+from . import _paged_call  # noqa: E402
+
+_paged_call.bind(*[C.cast(f, C.c_void_p).value for f in (LIB.d3_page_plan, LIB.d3_paged_append, LIB.d3_paged_attention,
+                                                         LIB.d3_paged_attention_workspace)], D3Error)
 
 BF16, FP16, FP32, E4M3 = 0, 1, 2, 3
 MAX_REQUESTS, MAPS_BYTES = 4096, 640
 _TYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32, torch.float8_e4m3fn: E4M3}
 
-_I32T, _I64T, _F32 = torch.int32, torch.int64, torch.float32
 _I32, _I64, _U32, _P = C.c_int32, C.c_int64, C.c_uint32, C.c_void_p
 
 
@@ -62,18 +68,6 @@ class PagedAttentionArgs(C.Structure):
          ("status_dev", _P)]
 
 
-# The two structs that are filled on every call, as one packing each (the fields above, in order; a null pointer is
-# 0): a small decode step is bound by the host side of its calls.
-_APPEND = struct.Struct("=I4i4x2Q4q2Q4q4Q")
-_ATTENTION = struct.Struct("=I5iqf4xQ2qQ2q7Q")
-assert _APPEND.size == C.sizeof(PagedAppendArgs) and _ATTENTION.size == C.sizeof(PagedAttentionArgs)
-
-_APPEND_PACK, _APPEND_SIZE, _ATTENTION_PACK, _ATTENTION_SIZE = _APPEND.pack, _APPEND.size, _ATTENTION.pack, _ATTENTION.size
-
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_device_now = torch._C._cuda_getDevice
-
-
 def _refuse(what: str):
     raise D3Error(EINVAL, what)
 
@@ -87,19 +81,6 @@ def _strides(t: torch.Tensor):
             st[d] = inner
         inner = max(inner, st[d] * t.shape[d])
     return st[:-1]
-
-
-def _call(fn, what: str, index: int, *args) -> None:
-    """One C call on the current stream of device `index`, with that device current."""
-    if index < 0:
-        _refuse(what + ": tensors must be on a CUDA device")
-    if _device_now() == index:
-        rc = fn(*args, _raw_stream(index))
-    else:
-        with torch.cuda.device(index):
-            rc = fn(*args, _raw_stream(index))
-    if rc != OK:
-        raise D3Error(rc, what)
 
 
 def _on_stream(call, index: int, stream, what: str):
@@ -138,7 +119,7 @@ class PagedKV:
         st = _strides(k)
         self.args = PagedKVArgs(C.sizeof(PagedKVArgs), _TYPES[k.dtype], self.n_pages, self.page_size, self.n_kv_heads,
                                 self.head_dim, st[0], st[1], st[2], k.data_ptr(), v.data_ptr(), sc[0], sc[1], None)
-        self._ref = C.byref(self.args)
+        self._ref, self._at = C.byref(self.args), C.addressof(self.args)
         n = C.c_size_t()   # the sizes this library serves
         if LIB.d3_paged_attention_workspace(self._ref, self.n_kv_heads, C.byref(n)) != OK:
             _refuse("PagedKV: page_size a power of two in 16..1024, head_dim 32, 64 or 128")
@@ -200,26 +181,13 @@ class PagePlan:
             _vector(n_free, i32, 1, index, what, "n_free"), _vector(self.cached_out, i32, R, index, what, "cached_out"),
             _vector(self.n_free_out, i32, 1, index, what, "n_free_out"), self.first.data_ptr(), self.slots.data_ptr(),
             self.row.data_ptr(), self.context.data_ptr(), _vector(self.status, i32, 1, index, what, "status"))
-        self._ref = C.byref(self.args)
+        self._at = C.addressof(self.args)
 
     def d3_page_plan(self, stream=None) -> "PagePlan":
         if stream is not None:
             return _on_stream(self.d3_page_plan, self.index, stream, "d3_page_plan")
-        _call(LIB.d3_page_plan, "d3_page_plan", self.index, self._ref)
+        _paged_call.plan(self._at, self.index)
         return self
-
-
-def _heads(t: torch.Tensor, n: int, heads: int, dh: int, dtype, index: int, what: str, name: str):
-    """(data pointer, stride of dimension 0, of dimension 1) of [n][heads][dh] with dh contiguous.  The stride of a
-    dimension of one entry, which torch leaves arbitrary, is taken as if the tensor were contiguous there."""
-    if t.shape != (n, heads, dh) or t.dtype is not dtype or t.get_device() != index:
-        _refuse(f"{what}: {name} must be {dtype} [{n}][{heads}][{dh}] on device {index}")
-    s0, s1, s2 = t.stride()
-    if s2 != 1:
-        _refuse(f"{what}: the last dimension of {name} must be contiguous")
-    if heads == 1:
-        s1 = dh
-    return t.data_ptr(), s0 if n > 1 else heads * s1, s1
 
 
 def d3_rope_table(n_positions: int, head_dim: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
@@ -233,7 +201,12 @@ def d3_rope_table(n_positions: int, head_dim: int, base: float = 10000.0, device
         return _on_stream(lambda: d3_rope_table(n_positions, head_dim, base, dev), -1 if dev.type != "cuda" else dev.index, stream,
                           "d3_rope_table")
     t = torch.empty((n_positions, head_dim // 2, 2), dtype=torch.float32, device=dev)
-    _call(LIB.d3_rope_table, "d3_rope_table", t.get_device(), n_positions, head_dim, float(base), t.data_ptr())
+    if dev.type != "cuda":
+        _refuse("d3_rope_table: a CUDA device")
+    with torch.cuda.device(dev):
+        rc = LIB.d3_rope_table(n_positions, head_dim, float(base), t.data_ptr(), torch.cuda.current_stream(dev).cuda_stream)
+    if rc != OK:
+        raise D3Error(rc, "d3_rope_table")
     return t
 
 
@@ -244,40 +217,10 @@ def d3_paged_append(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, slots: tor
     """k, v [n][n_kv_heads][head_dim] to the slots (int64 [n], negative = padding); with `rope`, k is
     rotated by position context - 1 and q [n][n_q_heads][head_dim] goes rotated to q_out (default: a
     new tensor whose padding rows are undefined; q itself is allowed).  Returns q_out."""
-    what, dev = "d3_paged_append", cache.index
     if stream is not None:
         return _on_stream(lambda: d3_paged_append(cache, k, v, slots, q=q, q_out=q_out, rope=rope, context=context, status=status),
-                          dev, stream, what)
-    n, hkv, dh, dtype = slots.shape[0] if slots.dim() == 1 else -1, cache.n_kv_heads, cache.head_dim, k.dtype
-    if dtype not in _TYPES:
-        _refuse(f"{what}: unsupported type {dtype}")
-    kp, kt, kh = _heads(k, n, hkv, dh, dtype, dev, what, "k")
-    vp, vt, vh = _heads(v, n, hkv, dh, dtype, dev, what, "v")
-    rope_p = rope_len = context_p = 0
-    if rope is not None:
-        if rope.dtype is not _F32 or rope.dim() != 3 or rope.shape[1] != dh // 2 or rope.shape[2] != 2 or rope.get_device() != dev or \
-                not rope.is_contiguous():
-            _refuse(f"{what}: rope must be contiguous fp32 [positions][{dh // 2}][2] on device {dev}")
-        if context is None:
-            _refuse(f"{what}: rope needs context")
-        rope_p, rope_len = rope.data_ptr(), rope.shape[0]
-        context_p = _vector(context, _I32T, n, dev, what, "context")
-    hq = qp = qt = qh = op = ot = oh = 0
-    if q is not None:
-        if rope is None:
-            _refuse(f"{what}: q is only rotated, and there is no rope")
-        hq = q.shape[1] if q.dim() == 3 else -1
-        qp, qt, qh = _heads(q, n, hq, dh, dtype, dev, what, "q")
-        if q_out is None:
-            q_out = q.new_empty((n, hq, dh))
-        op, ot, oh = _heads(q_out, n, hq, dh, dtype, dev, what, "q_out")
-    elif q_out is not None:
-        _refuse(f"{what}: q_out without q")
-    a = _APPEND_PACK(_APPEND_SIZE, _TYPES[dtype], n, hq, rope_len, kp, vp, kt, kh, vt, vh, qp, op, qt, qh, ot, oh,
-                     _vector(slots, _I64T, n, dev, what, "slots"), context_p, rope_p, 0 if status is None else _vector(status, _I32T, 1, dev, what, "status"))
-    if n > 0:
-        _call(LIB.d3_paged_append, what, dev, cache._ref, a)
-    return q_out
+                          cache.index, stream, "d3_paged_append")
+    return _paged_call.append(cache._at, cache.index, k, v, slots, q, q_out, rope, context, status)
 
 
 def attention_workspace(cache: PagedKV, n_q_heads: int) -> torch.Tensor:
@@ -297,50 +240,8 @@ def d3_paged_attention(cache: PagedKV, q: torch.Tensor, table: torch.Tensor, con
     table[rows[b] or b] names (see include/d3.h).  scale: default head_dim^-0.5.  Returns out, or
     (out, lse) with `with_lse` or an `lse` tensor (fp32 [n][n_q_heads]).  Without `workspace` one is allocated for the
     call."""
-    what, dev, dtype = "d3_paged_attention", cache.index, q.dtype
     if stream is not None:
         return _on_stream(lambda: d3_paged_attention(cache, q, table, context, rows=rows, scale=scale, out=out, lse=lse,
-                                                     with_lse=with_lse, workspace=workspace, status=status), dev, stream, what)
-    code = _TYPES.get(dtype)
-    if q.dim() != 3 or code is None:
-        _refuse(f"{what}: q must be [n][n_q_heads][head_dim]")
-    n, hq, dh = q.shape
-    qt, qh, q1 = q.stride()
-    if dh != cache.head_dim or q1 != 1 or q.get_device() != dev:
-        _refuse(f"{what}: q must be [n][n_q_heads][{cache.head_dim}] on device {dev}, last dimension contiguous")
-    if hq == 1:
-        qh = dh
-    if n <= 1:
-        qt = hq * qh
-    if table.dtype is not _I32T or table.dim() != 2 or table.get_device() != dev:
-        _refuse(f"{what}: table must be int32 [rows][width] on device {dev}")
-    rows_n, width = table.shape
-    stride, inner = table.stride()
-    if rows_n < 1 or width < 1 or (inner != 1 and width > 1):
-        _refuse(f"{what}: table must have entries and contiguous rows")
-    if out is None:
-        out = torch.empty_like(q) if qt == hq * dh and qh == dh else q.new_empty((n, hq, dh))
-        op, ot, oh = out.data_ptr(), hq * dh, dh
-    else:
-        op, ot, oh = _heads(out, n, hq, dh, dtype, dev, what, "out")
-    if scale is None:
-        scale = dh ** -0.5
-    elif not -3e38 < scale < 3e38:
-        _refuse(f"{what}: scale must be finite")
-    if lse is None:
-        if with_lse:
-            lse = torch.empty_strided((n, hq), (hq, 1), dtype=_F32, device=q.device)
-    elif lse.shape != (n, hq) or lse.dtype is not _F32 or lse.get_device() != dev or not lse.is_contiguous():
-        _refuse(f"{what}: lse must be contiguous fp32 [{n}][{hq}] on device {dev}")
-    if workspace is None:
-        workspace = attention_workspace(cache, hq)
-    elif workspace.get_device() != dev or not workspace.is_contiguous():
-        _refuse(f"{what}: workspace must be contiguous, on device {dev}")
-    a = _ATTENTION_PACK(_ATTENTION_SIZE, code, n, hq, rows_n, width, stride if rows_n > 1 else width,
-                        scale, q.data_ptr(), qt, qh, op, ot, oh, 0 if lse is None else lse.data_ptr(),
-                        table.data_ptr(), _vector(context, _I32T, n, dev, what, "context"),
-                        0 if rows is None else _vector(rows, _I32T, n, dev, what, "rows"),
-                        workspace.data_ptr(), workspace.nbytes, 0 if status is None else _vector(status, _I32T, 1, dev, what, "status"))
-    if n > 0:
-        _call(LIB.d3_paged_attention, what, dev, cache._ref, a)
-    return out if lse is None else (out, lse)
+                                                     with_lse=with_lse, workspace=workspace, status=status),
+                          cache.index, stream, "d3_paged_attention")
+    return _paged_call.attention(cache._at, cache.index, q, table, context, rows, scale, out, lse, with_lse, workspace, status)
