@@ -81,6 +81,7 @@ struct PagedAttnArgs {
   int4 *join;                          // per CTA: what the joining kernel has to do
   int32_t *status;
   int n_stages;
+  int cluster;                         // CTAs that share an item, as a cluster (0: none)
   int whole;                           // no row is cut between CTAs: no join
   int few;                             // the rows are summed up by the producer warps alone, in 32 bits
   unsigned long long wait_ns;

@@ -73,12 +73,14 @@ __device__ __forceinline__ bool mb_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 // Bounded wait; false once it, or another wait of the CTA, has run out.
+__device__ __forceinline__ bool mb_try_cluster(uint32_t bar, uint32_t parity);
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mb_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, unsigned long long wait_ns,
                                         bool check_abort = true) {
-  if (mb_try(bar, parity)) return true;
+  if (CLUSTER ? mb_try_cluster(bar, parity) : mb_try(bar, parity)) return true;
   const uint64_t t0 = now_ns();
   for (uint32_t it = 1;; ++it) {
-    if (mb_try(bar, parity)) return true;
+    if (CLUSTER ? mb_try_cluster(bar, parity) : mb_try(bar, parity)) return true;
     if ((it & 31u) == 0u) {
       if (check_abort && *abort_flag) return false;
       if (now_ns() - t0 > wait_ns) break;
@@ -86,6 +88,30 @@ __device__ __forceinline__ bool mb_wait(uint32_t bar, uint32_t parity, volatile 
   }
   *abort_flag = 1;
   return false;
+}
+// ---- thread-block clusters: an address of another CTA's shared memory, stores and arrivals there
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+template <int V>
+__device__ __forceinline__ void store_there(uint32_t addr, const float (&v)[V]) {
+  if constexpr (V == 4) asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
+  else if constexpr (V == 2) asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(addr), "f"(v[0]), "f"(v[1]) : "memory");
+  else asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v[0]) : "memory");
+}
+__device__ __forceinline__ void arrive_there(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ bool mb_try_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
 }
 __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap *map, int dim, int pos, int head, int page, uint32_t bar) {
   asm volatile(
@@ -198,14 +224,14 @@ enum { OUT_WHOLE = 0, OUT_HEAD = 1, OUT_TAIL = 2, OUT_NONE = 3 };
 struct __align__(16) StageInfo {
   int row;
   uint32_t heads;       // the tile's first query head | kv head << 16
-  uint32_t bits;        // positions in the stage (0 .. 256) | STAGE_* << 9 | OUT_* << 12 | heads of the tile << 14
+  uint32_t bits;        // positions in the stage (0 .. 256) | STAGE_* << 9 | OUT_* << 12 | heads of the tile << 14 | (cluster) CTAs it lies in << 19
   uint32_t tiles;       // which tiles hold positions
 };
 // What the consumers tell the epilogue warps about an item.
 struct __align__(16) ItemInfo {
   int row;
   uint32_t heads;       // as above
-  uint32_t bits;        // OUT_* | last of the CTA << 2 | heads << 3 | first warp with a piece of it << 8 | such warps << 16
+  uint32_t bits;        // OUT_* | last of the CTA << 2 | heads << 3 | first warp with a piece of it << 8 | such warps << 16 | (cluster) CTAs << 24
 };
 
 template <int DH, int CACHE, int X, int MT>
@@ -243,7 +269,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   constexpr int KK = DH / 16, KT = C::kTiles, TQ = C::kQTerms, TP = C::kPTerms, PT = C::kPT;
   constexpr bool F16 = C::kF16;
   extern __shared__ unsigned char s_dyn[];
-  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sums_full, s_sums_free;
+  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sums_full, s_sums_free, s_joined[C::kEpilogue];
   __shared__ StageInfo s_info[kMaxStages];
   __shared__ float s_m[C::kWarps][C::kHeads], s_l[C::kWarps][C::kHeads];
   __shared__ ItemInfo s_item;
@@ -256,7 +282,9 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   unsigned char *ring_p = s_dyn + (ring - smem_u32(s_dyn));
   unsigned char *q_slots = ring_p + (size_t)S * C::kStageBytes;
   float *s_o = reinterpret_cast<float *>(q_slots + (size_t)S * C::kQBytes);   // [warp][head][kHeadFloats]
+  float *s_j = s_o + (size_t)C::kWarps * a.heads_per_tile * C::kHeadFloats;   // cluster: [CTA][head][kHeadFloats], (m, l) behind the sums
   const int HG = a.hkv * a.tiles_per_head;
+  const int CL = a.cluster, rank = CL ? (int)blockIdx.x % CL : 0;   // CTAs of a cluster (0: none), which share an item
 
   if (tid == 0) {
     for (int i = 0; i < S; ++i) {
@@ -265,6 +293,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     }
     mb_init(smem_u32(&s_sums_full), C::kWarps);
     mb_init(smem_u32(&s_sums_free), C::kEpilogue);
+    for (int i = 0; i < C::kEpilogue; ++i) mb_init(smem_u32(&s_joined[i]), CL > 1 ? CL - 1 : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s_abort = 0;
     s_start_row = a.n_rows;
@@ -297,7 +326,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (whole) return (long long)live_rows * HG <= gridDim.x ? Cost{0, 1, 0, 0} : Cost{kUnitCost, kItemCost, 0, 0};
     return n * HG >= 4ll * gridDim.x ? Cost{kUnitCost, kItemCost, kItemCost, kUnitCost} : Cost{1, 0, 0, 1};
   };
-  if (!few) {
+  if (!few && !CL) {
     pdl_wait();
     pdl_trigger();
     const int per = (a.n_rows + C::kThreads - 1) / C::kThreads;
@@ -352,8 +381,9 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     }
   }
   __syncthreads();   // the barriers, and the first row where it was looked for
+  if (CL) cluster_arrive();
 
-  if (warp >= C::kWarps + C::kEpilogue) {
+  auto produce = [&]() {
     // ------------------------------------------------------------ producers
     const int me = warp - C::kWarps - C::kEpilogue;
     bool dummy = false;
@@ -369,7 +399,10 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       return __shfl_sync(0xffffffffu, x, at_lane);
     };
     int few_units = 0, few_rows = 0, few_longest = 0;   // of this lane
-    if (few) {
+    if (CL) {
+      pdl_wait();
+      pdl_trigger();
+    } else if (few) {
       pdl_wait();
       pdl_trigger();
       bool bad = false;
@@ -396,17 +429,33 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const int n_cta = (int)min((whole ? live_rows : units) * HG, (long long)gridDim.x);   // every one of them has work
     auto idle = [&]() {   // a stage that sends the other warps home
       if (me == 0 && lane == 0) {
-        if (!a.whole) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (!a.whole && !CL) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
         s_info[0] = StageInfo{0, 0u, (uint32_t)((STAGE_LAST | STAGE_FINAL) << 9 | OUT_NONE << 12), 0u};
         mb_arrive(smem_u32(&s_full[0]));
       }
     };
-    if ((int)blockIdx.x >= n_cta) { idle(); return; }
-    const Cost cost = cost_of(units);
+    if (!CL && (int)blockIdx.x >= n_cta) { idle(); return; }
+    const Cost cost = CL ? Cost{1, 0, 0, 1} : cost_of(units);
     Shares sh;
     long long x0, x1, item;   // this CTA's costs; where its first item starts
-    int nu, tile, unit;
-    if (few) {   // all of it in 32 bits
+    int nu, tile, unit, lies_in = 1;
+    if (CL) {   // a cluster per item, its CTAs take equal runs of the units
+      const int index = (int)blockIdx.x / CL;
+      bool bad = false;
+      row = index / HG;
+      tile = index - row * HG;
+      trow = row_of(row, bad);
+      len = trow >= 0 ? length_of(row, bad) : 0;
+      if (bad && rank == 0 && tile == 0 && a.status) *a.status = D3_EINVAL;
+      nu = units_of(len);
+      lies_in = min(nu, CL);
+      const int each = nu / CL, more = nu - each * CL;
+      x0 = each * rank + min(rank, more);
+      x1 = x0 + each + (rank < more ? 1 : 0);
+      if (trow < 0 || x0 == x1) { idle(); return; }
+      item = 0;
+      unit = (int)x0;
+    } else if (few) {   // all of it in 32 bits
       const int total = ((int)units * cost.unit + live_rows * cost.item) * HG, each = (int)((unsigned)total / (unsigned)n_cta);
       sh.each = each; sh.more = total - each * n_cta;
       const int x = each * (int)blockIdx.x + min((int)blockIdx.x, sh.more);
@@ -527,7 +576,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           const int kind = !last || (ends && whole_start) ? OUT_WHOLE : !ends && whole_start ? OUT_TAIL : OUT_HEAD;
           const int flags = (first ? STAGE_FIRST : 0) | (last ? STAGE_LAST : 0) | (final ? STAGE_FINAL : 0);
           s_info[s] = StageInfo{row, (uint32_t)head | (uint32_t)kvh << 16,
-                                (uint32_t)n | (uint32_t)flags << 9 | (uint32_t)kind << 12 | (uint32_t)nh << 14, tiles};
+                                (uint32_t)n | (uint32_t)flags << 9 | (uint32_t)kind << 12 | (uint32_t)nh << 14 | (uint32_t)lies_in << 19, tiles};
           mb_arrive_tx(full, (uint32_t)__popc(tiles) * 2u * kTile * C::kRow + (first ? (uint32_t)(nh * DH * QBytes<X>::v) : 0u));
         }
         __syncwarp();
@@ -552,8 +601,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (me == 0 && lane == 0) {
       // an item that starts here and goes on: what the joining kernel adds up
       int4 join = make_int4(0, 0, 0, 0);
-      if (ok && cut_row >= 0) join = make_int4(sh.holder(cut_last) - (int)blockIdx.x + 1, cut_row, cut_head, cut_kvh | cut_nh << 16);
-      if (!a.whole) a.join[blockIdx.x] = join;
+      if (ok && cut_row >= 0 && !CL) join = make_int4(sh.holder(cut_last) - (int)blockIdx.x + 1, cut_row, cut_head, cut_kvh | cut_nh << 16);
+      if (!a.whole && !CL) a.join[blockIdx.x] = join;
     }
     if (!ok) {   // copies in flight end by themselves: wait for them before the shared memory goes
       const unsigned long long drain = a.wait_ns > kDrainFloorNs ? a.wait_ns : kDrainFloorNs;
@@ -561,8 +610,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         if ((k & (kProducers - 1)) == me) mb_wait(smem_u32(&s_full[k % S]), (uint32_t)((k / S) & 1), &s_abort, drain, false);
       if (lane == 0 && a.status) *a.status = D3_ETIMEOUT;
     }
-    return;
-  }
+  };
 
   auto write_out = [&](long long at, float val) {
     if (X == D3_FP32) static_cast<float *>(a.out)[at] = val;
@@ -570,7 +618,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     else static_cast<__half *>(a.out)[at] = __float2half_rn(val);
   };
 
-  if (warp >= C::kWarps) {
+  bool met = false;   // this thread has seen the whole cluster started
+  auto epilogue = [&]() {
     // ------------------------------------------------------------ epilogue: a head per warp, DH / 32 dims per lane
     constexpr int V = DH / 32;
     const int me = warp - C::kWarps;
@@ -578,11 +627,23 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       if (!__all_sync(0xffffffffu, mb_wait(smem_u32(&s_sums_full), parity, &s_abort, a.wait_ns))) break;
       if (parity == 0u) pdl_wait();   // returns at once: the producers' has
       const ItemInfo item = s_item;
-      const int kind = item.bits & 3, nh = (item.bits >> 3) & 31, first_warp = (item.bits >> 8) & 255, warps = item.bits >> 16;
-      if (kind == OUT_NONE) break;
+      const int kind = item.bits & 3, nh = (item.bits >> 3) & 31, first_warp = (item.bits >> 8) & 255, warps = (item.bits >> 16) & 255;
+      if (CL && kind != OUT_WHOLE && rank > 0) { cluster_wait(); met = true; }   // the first CTA's barriers are there
+      if (kind == OUT_NONE) {
+        if (CL && rank > 0 && lane == 0) arrive_there(in_cta(smem_u32(&s_joined[me]), 0));
+        break;
+      }
       int from = first_warp + min(lane, warps - 1);   // lane k: the k-th warp that had a piece of the item
       if (from >= C::kWarps) from -= C::kWarps;
       const float vs = a.v_scale ? __ldg(a.v_scale + (item.heads >> 16)) : 1.f;
+      auto finish = [&](int h, const float (&o)[V], float m, float l) {
+        const float f = l == 0.f ? 0.f : vs / l;
+        const long long at = item.row * a.out_row_stride + (long long)((item.heads & 0xffffu) + h) * a.out_head_stride + lane * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) write_out(at + e, o[e] * f);
+        if (lane == 0 && a.lse)
+          a.lse[(long long)item.row * a.hq + (item.heads & 0xffffu) + h] = l == 0.f ? -INFINITY : (m + (log2f(l) - (F16 ? 15.f : 0.f))) * kLn2;
+      };
       // HB heads at a time, in independent chains: this is all latency
       auto heads = [&](auto hb, int h0) {
         constexpr int HB = decltype(hb)::value;
@@ -635,12 +696,15 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           if (h >= nh) break;
           const float l = __shfl_sync(0xffffffffu, L[i], 0), m = __shfl_sync(0xffffffffu, M[i], 0);
           if (kind == OUT_WHOLE) {
-            const float f = l == 0.f ? 0.f : vs / l;
-            const long long at = item.row * a.out_row_stride + (long long)((item.heads & 0xffffu) + h) * a.out_head_stride + lane * V;
-#pragma unroll
-            for (int e = 0; e < V; ++e) write_out(at + e, o[i][e] * f);
-            if (lane == 0 && a.lse)
-              a.lse[(long long)item.row * a.hq + (item.heads & 0xffffu) + h] = l == 0.f ? -INFINITY : (m + (log2f(l) - (F16 ? 15.f : 0.f))) * kLn2;
+            finish(h, o[i], m, l);
+          } else if (CL) {   // to the cluster's first CTA
+            float *dst = s_j + ((size_t)rank * a.heads_per_tile + h) * C::kHeadFloats;
+            const uint32_t there = in_cta(smem_u32(dst), 0);
+            store_there<V>(there + 4 * lane * V, o[i]);
+            if (lane == 0) {
+              const float ml[2] = {m, l};
+              store_there<2>(there + 4 * DH, ml);
+            }
           } else {
             const size_t part = (size_t)(2 * blockIdx.x + (kind == OUT_TAIL ? 1 : 0)) * 16 + h;
 #pragma unroll
@@ -653,12 +717,70 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       else for (int h0 = me; h0 < nh; h0 += 4 * C::kEpilogue) heads(std::integral_constant<int, 4>(), h0);
       __syncwarp();
       if (lane == 0) mb_arrive(smem_u32(&s_sums_free));
+      if (CL && kind != OUT_WHOLE) {
+        if (rank > 0) {
+          if (lane == 0) arrive_there(in_cta(smem_u32(&s_joined[me]), 0));
+        } else {
+          // ---- the item's first CTA: the pieces of all, in their order
+          const int pieces = item.bits >> 24;
+          if (!__all_sync(0xffffffffu, mb_wait<true>(smem_u32(&s_joined[me]), 0, &s_abort, a.wait_ns))) break;
+          const int stride = a.heads_per_tile * C::kHeadFloats;
+          auto join = [&](auto hb, int h0) {
+            constexpr int HB = decltype(hb)::value;
+            float M[HB], L[HB], c[HB], o[HB][V];
+            const float *all[HB];
+#pragma unroll
+            for (int i = 0; i < HB; ++i) {
+              all[i] = s_j + min(h0 + i * C::kEpilogue, nh - 1) * C::kHeadFloats;
+              const float2 ml = *reinterpret_cast<const float2 *>(all[i] + min(lane, pieces - 1) * stride + DH);
+              c[i] = M[i] = lane < pieces ? ml.x : -INFINITY;
+              L[i] = ml.y;
+#pragma unroll
+              for (int e = 0; e < V; ++e) o[i][e] = 0.f;
+            }
+#pragma unroll
+            for (int d = 8; d; d >>= 1)
+#pragma unroll
+              for (int i = 0; i < HB; ++i) M[i] = fmaxf(M[i], __shfl_xor_sync(0xffffffffu, M[i], d));
+#pragma unroll
+            for (int i = 0; i < HB; ++i) {
+              c[i] = exp2_fast(c[i] - (M[i] == -INFINITY ? 0.f : M[i]));   // 0 beyond the pieces
+              L[i] = lane < pieces ? L[i] * c[i] : 0.f;
+            }
+#pragma unroll
+            for (int d = 8; d; d >>= 1)
+#pragma unroll
+              for (int i = 0; i < HB; ++i) L[i] += __shfl_xor_sync(0xffffffffu, L[i], d);
+            for (int k = 0; k < pieces; k += 2) {
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < HB; ++i) {
+                  const float ck = __shfl_sync(0xffffffffu, c[i], k + j);
+                  const float *src = all[i] + min(k + j, pieces - 1) * stride + lane * V;
+                  float x[V];
+                  if constexpr (V == 4) { const float4 v = *reinterpret_cast<const float4 *>(src); x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+                  else if constexpr (V == 2) { const float2 v = *reinterpret_cast<const float2 *>(src); x[0] = v.x; x[1] = v.y; }
+                  else x[0] = *src;
+#pragma unroll
+                  for (int e = 0; e < V; ++e) o[i][e] += ck * x[e];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < HB; ++i)
+              if (h0 + i * C::kEpilogue < nh)
+                finish(h0 + i * C::kEpilogue, o[i], __shfl_sync(0xffffffffu, M[i], 0), __shfl_sync(0xffffffffu, L[i], 0));
+          };
+          if (nh <= C::kEpilogue) { if (me < nh) join(std::integral_constant<int, 1>(), me); }
+          else for (int h0 = me; h0 < nh; h0 += 4 * C::kEpilogue) join(std::integral_constant<int, 4>(), h0);
+        }
+      }
       if (item.bits & 4) break;
     }
-    return;
-  }
+  };
 
   // -------------------------------------------------------------- consumers
+  auto consume = [&]() {
   // Fragments (g = lane / 4, t = lane % 4).  Scores: A = K (rows = positions), B = Q^T (column g = head), result: positions
   // g, g + 8 of heads 2t, 2t + 1.  Sums: A = V^T (rows = dims), B = P^T, result: dims g, g + 8 of heads 2t, 2t + 1.
   const int g = lane >> 2, t = lane & 3, mat = lane >> 3;
@@ -955,13 +1077,24 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       }
       if (warp == 0 && lane == 0)
         s_item = ItemInfo{info.row, info.heads,
-                          ((flags >> 3) & 3) | (more ? 0u : 4u) | ((info.bits >> 14) & 31) << 3 | (uint32_t)first_warp << 8 | (uint32_t)warps << 16};
+                          ((flags >> 3) & 3) | (more ? 0u : 4u) | ((info.bits >> 14) & 31) << 3 | (uint32_t)first_warp << 8 | (uint32_t)warps << 16 |
+                              ((info.bits >> 19) & 31) << 24};
       __syncwarp();
       if (lane == 0) mb_arrive(smem_u32(&s_sums_full));
       ++items;
     }
   }
   if (!ok && lane == 0 && a.status) *a.status = D3_ETIMEOUT;
+  };
+
+  if (warp >= C::kWarps + C::kEpilogue) produce();
+  else if (warp >= C::kWarps) epilogue();
+  else consume();
+  if (CL) {   // no CTA of the cluster leaves while another may still write to it (every wait before this one is bounded)
+    if (!met) cluster_wait();
+    cluster_arrive();
+    cluster_wait();
+  }
 }
 
 // Joins the pieces of the item that starts in CTA blockIdx.x and goes on behind it.  Parts: this CTA's second slot, then the
@@ -1075,38 +1208,96 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_join(const __grid_con
 }
 
 // ---------------------------------------------------------------- launch
+// What is known of a kernel on a device: the SMs (0: not asked yet) and how many clusters of 2 .. 16 CTAs run at once.
+struct Device {
+  std::atomic<int> sms;
+  int clusters[17];
+};
+
 template <int DH, int CACHE, int X, int MT>
 int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
   using C = Cfg<DH, CACHE, X, MT>;
-  const int merge = C::kWarps * a.heads_per_tile * C::kHeadFloats * (int)sizeof(float);
-  int stages = (kSmemMost - 1024 - merge) / (C::kStageBytes + C::kQBytes);
-  if (stages > kMaxStages) stages = kMaxStages;
-  if (stages < 2) return -1;
-  a.n_stages = stages;
-  const size_t smem = 1024 + (size_t)stages * (C::kStageBytes + C::kQBytes) + merge;
+  auto kernel = k_paged_attention<DH, CACHE, X, MT>;
+  const int head_bytes = a.heads_per_tile * C::kHeadFloats * (int)sizeof(float);   // a set of sums
+  auto stages_beside = [&](int sets) {
+    const int n = (kSmemMost - 1024 - sets * head_bytes) / (C::kStageBytes + C::kQBytes);
+    return n < kMaxStages ? n : kMaxStages;
+  };
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
-  static std::atomic<int> ready[64];   // per device: its SM count once the kernel's attribute is set there
-  int n = ready[dev].load(std::memory_order_acquire);
+  static Device devices[64];
+  Device &d = devices[dev];
+  int n = d.sms.load(std::memory_order_acquire);
   if (n == 0) {
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return -1;
-    if (cudaFuncSetAttribute(k_paged_attention<DH, CACHE, X, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost) != cudaSuccess)
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost) != cudaSuccess ||
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
       return -1;
+    for (int cl = 2; cl <= 16; ++cl) {
+      cudaLaunchConfig_t cfg;
+      memset(&cfg, 0, sizeof(cfg));
+      cfg.gridDim = dim3(cl);
+      cfg.blockDim = dim3(C::kThreads);
+      cfg.dynamicSmemBytes = kSmemMost;
+      cudaLaunchAttribute attr;
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = cl; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
+      int most = 0;
+      if (cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); most = 0; }
+      d.clusters[cl] = most;   // (the same numbers, if two threads are here)
+    }
     if (n > kFusedMaxCtas) n = kFusedMaxCtas;
-    ready[dev].store(n, std::memory_order_release);
+    d.sms.store(n, std::memory_order_release);
   }
-  // Items stay whole whatever the lengths, and no join is launched, where the table has room for 10 units a row at most: the
-  // busiest CTA is at most one row longer than an even share (bf16, 32 kv heads, whole / cut: 1 row of 512
-  // positions 8.1 / 9.3 us, of 1024 11.9 / 10.3; 4 rows of 512 10.1 / 14.1).
-  const long long most = (((long long)a.table_width << a.page_shift) + C::kUnit - 1) / C::kUnit;
-  a.whole = most <= 10;
+  const long long most = (((long long)a.table_width << a.page_shift) + C::kUnit - 1) / C::kUnit;   // units a row can have
+  const long long items = (long long)a.n_rows * a.hkv * a.tiles_per_head;
+  // Few items: a cluster of CTAs for each, as many as run at once, whose first CTA gets the others' sums through
+  // distributed shared memory; no sums over all rows at the start, no join (which costs 4.5 us).  A unit takes a CTA 0.5 us, and
+  // all of them no less than HBM needs; rows of very different lengths would leave clusters idle, so several rows
+  // may take 24 units a CTA at most (whatever the table has room for counts).  Under 5 units a row stays whole (1 row,
+  // 32 kv heads of 128, bf16, whole or cut / cluster: 128 positions 5.3 / 5.7 us, 512 8.1 / 7.0, 2048 13.8 / 10.3;
+  // 1 row, 8 kv heads: 512 8.8 / 7.0, 2048 10.8 / 9.2).
+  a.cluster = 0;
+  if (most >= 5) {
+    int cl = (int)(most < 16 ? most : 16);
+    while (cl >= 2 && (items > d.clusters[cl] || stages_beside(C::kWarps + cl) < 3)) --cl;
+    if (cl >= 2) {
+      const long long longest = (most + cl - 1) / cl;
+      const double hbm_us = (double)(items * most) * C::kStageBytes / 7.0e6, in_cluster = 0.5 * longest, cut = 0.5 * items * most / n;
+      if ((a.n_rows == 1 || longest <= 24) && (in_cluster > hbm_us ? in_cluster : hbm_us) <= (cut > hbm_us ? cut : hbm_us) + 4.5) a.cluster = cl;
+    }
+  }
+  // Otherwise items stay whole whatever the lengths, and no join is launched, where the table has room for 10 units a row at
+  // most: the busiest CTA is at most one row longer than an even share (40 kv heads, 8 rows of 512 positions: 20.9 us whole,
+  // 22.7 cut).
+  a.whole = !a.cluster && most <= 10;
+  const int sets = C::kWarps + a.cluster;
+  a.n_stages = stages_beside(sets);
+  if (a.n_stages < 2) return -1;
+  const size_t smem = 1024 + (size_t)a.n_stages * (C::kStageBytes + C::kQBytes) + (size_t)sets * head_bytes;
   // few enough rows for a warp, and all costs within 32 bits whatever the lengths are
   const double capacity = ((double)a.table_width * (1 << a.page_shift) / C::kUnit + 1) * kUnitCost + kItemCost;
   a.few = a.n_rows <= kFewRows && a.n_rows * capacity * a.hkv * a.tiles_per_head < 1.0e9 ? 1 : 0;
-  auto map = [](const TMap &m) -> const CUtensorMap & { return *reinterpret_cast<const CUtensorMap *>(&m); };
-  if (launch_pdl(k_paged_attention<DH, CACHE, X, MT>, dim3(n), dim3(C::kThreads), smem, st, map(m.k), map(m.v), map(m.k16), map(m.v16), a) !=
-      cudaSuccess)
-    return -1;
+  auto map = [](const TMap &t) -> const CUtensorMap & { return *reinterpret_cast<const CUtensorMap *>(&t); };
+  if (a.cluster) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)(items * a.cluster));
+    cfg.blockDim = dim3(C::kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = a.cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, map(m.k), map(m.v), map(m.k16), map(m.v16), a) == cudaSuccess ? 0 : -1;
+  }
+  if (launch_pdl(kernel, dim3(n), dim3(C::kThreads), smem, st, map(m.k), map(m.v), map(m.k16), map(m.v16), a) != cudaSuccess) return -1;
   if (!a.whole)
     if (launch_pdl(k_paged_join<DH, X, C::kF16>, dim3(n), dim3(32 * kJoinWarps), 0, st, a) != cudaSuccess) return -1;
   return 0;
