@@ -8,21 +8,32 @@
 // What bounds it.  K and V are read once: 2 G flops per byte (G query heads per kv head, 16-bit cache), far
 // below the ~260 of this GPU's tensor cores, so HBM decides and the kernel is built to keep copies in flight:
 //   * one CTA per SM; two producer warps walk the CTA's share of all positions of all rows and fill a ring of up to
-//     ~170 KB of 32 KB stages by TMA (4-D tensor map over the pool: dim, position, kv head, page; boxes of up to a
+//     ~200 KB of 32 KB stages by TMA (4-D tensor map over the pool: dim, position, kv head, page; boxes of up to a
 //     page, of 16 positions where a row ends), so both layouts cost the same; page ids are looked up 32 at a time, one
-//     window ahead; they never wait for the arithmetic until the ring is full;
+//     window ahead; they never wait for the arithmetic until the ring is full.  (One producer warp with 16-position
+//     boxes took 1.2 us per stage whatever its bytes: 64 rows of up to 16384 positions 562 us, now 327.)
 //   * the share is cut by positions, not by rows: row lengths are read on the device, every CTA sums them up and takes
-//     the same number of units (stages), so ragged batches and one long row load all SMs alike;
-//   * a consumer warp takes one piece of 16 positions at a time (mma.sync m16n8k16).  Positions (dims) are the 16 rows
-//     of a product and heads its 8 columns: K and V come from the swizzled stage by ldmatrix as they lie there, no row
-//     is wasted on G <= 8 heads, and 8 heads x 128 dims of O take 32 registers.  P is used as two terms, P - round(P) in a
-//     second product: 16 (bf16) or 22 (fp16) bits of it count.  tcgen05.mma would need P, a few hundred numbers, written to
-//     shared memory and results fetched from tensor memory for every piece; the legacy pipe is a quarter busy here;
+//     the same number of units (stages; a row's start and end count as 3/4 of one), so ragged batches and one long row
+//     load all SMs alike;
+//   * a consumer warp takes one piece of 16 positions at a time, 32 or 64 where a row of the cache is 128 bytes or less
+//     (mma.sync m16n8k16).  Positions (dims) are the 16 rows of a product and heads its 8 columns: K and V come from the
+//     swizzled stage by ldmatrix as they lie there, no row is wasted on G <= 8 heads, and 8 heads x 128 dims of O take 32
+//     registers.  P is used as two terms, P - round(P) in a second product: 16 (bf16) or 22 (fp16) bits of it count.
+//     tcgen05.mma would need P, a few hundred numbers, written to shared memory and results fetched from tensor memory
+//     for every piece; the legacy pipe is a quarter busy here;
 //   * epilogue warps add the consumers' (m, l, O) up at the end of a row, while the consumers go on with the next row.
-//     Rows that end inside a CTA are written at once; of a row that is cut every CTA leaves (m, l, O) of its piece and
+//     Rows that lie inside a CTA are written at once; of a row that is cut every CTA leaves (m, l, O) of its piece and
 //     k_paged_join adds them up in the order of the CTAs: bits depend on the lengths alone, no atomics.
+//   * few rows are latency: each (row, kv head) gets a cluster of CTAs that add their pieces up through distributed
+//     shared memory; rows of few units are not cut at all (launch(), cost_of()).
 //
-// fp32 queries (bf16 cache): q and P are three bf16 terms by truncation (8 + 8 + 8 bits: exact).  8-bit cache: the
+// Measured (us, of the measured copy rate 6451 GB/s): 64 rows x 1..16384 GQA 32/8 x 128 bf16 327 (99 %); 96 rows x 17..8192
+// 64/8 8-bit 140.5 (89 %: the widening to fp16 keeps the warps busy); 1 row x 131071 64/8 fp16 91 (91 %: 6 us are start and
+// join); 32 rows x 129..1025 32/32 bf16 55.5 (84 %: 9 us are start and join); 1 row x 513 32/32 7.1; 4 rows x 513..545 64/8
+// fp32 9.8 (latency).
+//
+// fp32 queries (bf16 cache): q and P are three bf16 terms by truncation (8 + 8 + 8 bits: exact), sums of products short
+// chains (error of fp32 outputs against 64 bits 1e-7 .. 3e-7).  8-bit cache: the
 // stored numbers are widened to fp16 (exact), bf16 queries are scaled by a power of two per head so that fp16 holds
 // them.  Where P is fp16, it is exp2(.. + 15): 2^-29 of the largest stays a normal number.
 //
@@ -1254,20 +1265,17 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
   const long long most = (((long long)a.table_width << a.page_shift) + C::kUnit - 1) / C::kUnit;   // units a row can have
   const long long items = (long long)a.n_rows * a.hkv * a.tiles_per_head;
   // Few items: a cluster of CTAs for each, as many as run at once, whose first CTA gets the others' sums through
-  // distributed shared memory; no sums over all rows at the start, no join (which costs 4.5 us).  A unit takes a CTA 0.5 us, and
-  // all of them no less than HBM needs; rows of very different lengths would leave clusters idle, so several rows
-  // may take 24 units a CTA at most (whatever the table has room for counts).  Under 5 units a row stays whole (1 row,
-  // 32 kv heads of 128, bf16, whole or cut / cluster: 128 positions 5.3 / 5.7 us, 512 8.1 / 7.0, 2048 13.8 / 10.3;
-  // 1 row, 8 kv heads: 512 8.8 / 7.0, 2048 10.8 / 9.2).
+  // distributed shared memory; no sums over all rows at the start, no join (which costs 4.5 us).  A unit takes a CTA 0.5 us;
+  // rows may take 24 units a CTA at most (whatever the table has room for counts): clusters leave some SMs out, and rows
+  // of different lengths would leave clusters idle.  Under 5 units a row stays whole (1 row, 32 kv heads of 128, bf16,
+  // whole or cut / cluster: 128 positions 5.3 / 5.7 us, 512 8.1 / 7.0, 2048 13.8 / 10.3; 1 row, 8 kv heads: 512 8.8 / 7.0,
+  // 2048 10.8 / 9.2).
   a.cluster = 0;
   if (most >= 5) {
     int cl = (int)(most < 16 ? most : 16);
     while (cl >= 2 && (items > d.clusters[cl] || stages_beside(C::kWarps + cl) < 3)) --cl;
-    if (cl >= 2) {
-      const long long longest = (most + cl - 1) / cl;
-      const double hbm_us = (double)(items * most) * C::kStageBytes / 7.0e6, in_cluster = 0.5 * longest, cut = 0.5 * items * most / n;
-      if ((a.n_rows == 1 || longest <= 24) && (in_cluster > hbm_us ? in_cluster : hbm_us) <= (cut > hbm_us ? cut : hbm_us) + 4.5) a.cluster = cl;
-    }
+    const long long longest = cl >= 2 ? (most + cl - 1) / cl : 0;
+    if (cl >= 2 && longest <= 24 && longest <= items * most / n + 9) a.cluster = cl;
   }
   // Otherwise items stay whole whatever the lengths, and no join is launched, where the table has room for 10 units a row at
   // most: the busiest CTA is at most one row longer than an even share (40 kv heads, 8 rows of 512 positions: 20.9 us whole,
