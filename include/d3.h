@@ -359,7 +359,9 @@ const char *d3_strerror(int32_t code);
  * Device data is checked where it is used, against the bounds the host gave: a value out of range is
  * never used as an index; the call skips what it stands for, as said below, and stores D3_EINVAL to
  * `status_dev` (int32, never cleared by these calls; nullable except where noted).  One workspace
- * serves one call at a time: calls that may overlap need a workspace each. */
+ * serves one call at a time: calls that may overlap need a workspace each.  Rows of one output (and of a
+ * pool that is appended to) must not overlap: D3_EINVAL, so is a stride that does not reach over what
+ * the smaller strides span.  Nothing here is differentiable. */
 #define D3_BF16 0
 #define D3_FP16 1
 #define D3_FP32 2
@@ -459,11 +461,13 @@ int32_t d3_rope_table(int32_t n_positions, int32_t head_dim, float rope_base, fl
  * the pages that table row rows[b] names (rows_dev NULL: row b itself), kv head h / (Hq / Hkv):
  *   out = sum_t softmax_t(scale q . k_t) v_t,   lse = log sum_t exp(scale q . k_t)  (nullable)
  * Scores, softmax and sums are fp32; out is rounded once to dtype.  Types as in d3_paged_append (q
- * and out / cache).  The length is cut into equal shares over the SMs, whichever rows they fall in,
- * and a second kernel joins the rows that were cut; the order of the sums is fixed by the lengths, so
- * equal inputs give equal bits.
+ * and out / cache).  Many rows: the lengths are cut into equal shares over the SMs, whichever rows they
+ * fall in, and a second kernel joins the rows that were cut.  Few rows: a cluster of CTAs for each row
+ * and kv head.  The order of the sums is fixed by the lengths, n_rows, the width of the table and the
+ * GPU, so the same call gives the same bits; a row's bits may depend on the rows beside it.
  * context 0: out = 0, lse = -inf.  rows[b] = -1: padding, the row's outputs stay as they are.  What
- * the pages hold behind the context is never used, NaN included.  Out-of-range data stores D3_EINVAL:
+ * the pages hold behind the context is never used, NaN included.  Non-finite numbers inside it make the
+ * results of their heads non-finite, an infinity possibly a NaN.  Out-of-range data stores D3_EINVAL:
  * a context beyond table_width pages (or negative) counts as 0, another bad rows[b] as padding, and
  * the positions of a bad page id are left out.  status_dev also gets D3_ETIMEOUT when a bounded wait ran out (out and
  * lse are then undefined).  workspace_dev: d3_paged_attention_workspace bytes, 256-byte aligned,

@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kPlanMaxThreads) k_page_plan(const __grid_cons
   }
   bad = s_bad;
   if ((long long)n_free + total[2] > a.n_pages) bad |= 2;      // more pages than there are came back
-  if (total[0] > a.T || total[1] > n_free + total[2]) bad |= 1;
+  if (total[0] > a.T || total[1] > (long long)n_free + total[2]) bad |= 1;
   if (!bad) {
 #pragma unroll
     for (int i = 0; i < kPlanMaxPer; ++i) {
@@ -319,7 +319,7 @@ __device__ __forceinline__ void store8(__nv_fp8_e4m3 *p, const float *f) {
 }
 
 // 8-bit stores compute more per byte (a division and a conversion): four blocks an SM, 64 registers, two heads a thread
-// hide that (4097 tokens, 40 + 80 heads of 128: 40.2 us; three blocks 45.5, five, which spill, 55.6; 16-bit: 40.3).
+// hide that (4097 tokens, 40 + 80 heads of 128: 39.7 us; three blocks 45.5, five, which spill, 55.6).
 template <typename X, typename C, int DH, int H>
 __global__ void __launch_bounds__(256, sizeof(C) == 1 ? 4 : 1) k_paged_append(const __grid_constant__ AppendArgs a) {
   constexpr int HALF = DH / 2, PIECES = HALF / 8, LANES = 256 / PIECES;   // (token, group) pairs of a block
@@ -565,13 +565,15 @@ int32_t d3_paged_append(const d3_paged_kv *kv, const d3_paged_append_args *a, vo
   if (!stride_ok(a->k_token_stride, xs, 0) || !stride_ok(a->k_head_stride, xs, 0) || !stride_ok(a->v_token_stride, xs, 0) ||
       !stride_ok(a->v_head_stride, xs, 0))
     return D3_EINVAL;
+  if (!rows_apart(dh, kv->n_pages, kv->page_stride, kv->n_kv_heads, kv->head_stride, kv->page_size, kv->token_stride)) return D3_EINVAL;
   if (a->rope_dev) {
     if (!aligned16(a->rope_dev) || a->rope_len < 1 || !a->context_dev || ((uintptr_t)a->context_dev & 3)) return D3_EINVAL;
   }
   if (a->q_dev) {
     if (!a->rope_dev || a->n_q_heads < 1 || a->n_q_heads > 65535 || !a->q_out_dev || !aligned16(a->q_dev) || !aligned16(a->q_out_dev) ||
         !stride_ok(a->q_token_stride, xs, 0) || !stride_ok(a->q_head_stride, xs, 0) ||
-        !stride_ok(a->q_out_token_stride, xs, dh) || !stride_ok(a->q_out_head_stride, xs, dh))
+        !stride_ok(a->q_out_token_stride, xs, dh) || !stride_ok(a->q_out_head_stride, xs, dh) ||
+        !rows_apart(dh, a->n_tokens, a->q_out_token_stride, a->n_q_heads, a->q_out_head_stride))
       return D3_EINVAL;
   }
   if (a->n_tokens == 0) return D3_OK;
@@ -637,7 +639,8 @@ int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args 
       ((uintptr_t)a->rows_dev & 3) || ((uintptr_t)a->status_dev & 3))
     return D3_EINVAL;
   if (!stride_ok(a->q_row_stride, xs, 0) || !stride_ok(a->q_head_stride, xs, 0)) return D3_EINVAL;
-  if (a->out_row_stride < dh || a->out_head_stride < dh || a->out_row_stride > ((int64_t)1 << 38) || a->out_head_stride > ((int64_t)1 << 38))
+  if (a->out_row_stride < dh || a->out_head_stride < dh || a->out_row_stride > ((int64_t)1 << 38) || a->out_head_stride > ((int64_t)1 << 38) ||
+      !rows_apart(dh, a->n_rows, a->out_row_stride, a->n_q_heads, a->out_head_stride))
     return D3_EINVAL;
   const AttnWorkspace w = attn_workspace(dh);
   if (!a->workspace_dev || ((uintptr_t)a->workspace_dev & 255) || a->workspace_bytes < w.total) return D3_EINVAL;
@@ -679,7 +682,8 @@ int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args 
   const int rc = dh == 128 ? launch_paged_attention_128(*maps, p, a->dtype, st)
                  : dh == 64 ? launch_paged_attention_64(*maps, p, a->dtype, st)
                             : launch_paged_attention_32(*maps, p, a->dtype, st);
-  return rc == 0 && cudaGetLastError() == cudaSuccess ? D3_OK : D3_ECUDA;
+  const cudaError_t err = cudaGetLastError();   // (asked for whatever the launch said: no error is left for the next call)
+  return rc == 0 && err == cudaSuccess ? D3_OK : D3_ECUDA;
 }
 
 }  // extern "C"

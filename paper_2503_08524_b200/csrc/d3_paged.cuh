@@ -25,6 +25,22 @@ inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 inline bool stride_ok(int64_t s, int elem_bytes, int64_t at_least) {
   return s >= at_least && s <= ((int64_t)1 << 38) && (s * elem_bytes) % 16 == 0;
 }
+// Rows of `dh` numbers at all combinations of three indexes (count, stride) do not overlap: every stride reaches over what
+// the smaller ones span.  (Written memory: two rows at one address would be a race.)
+inline bool rows_apart(int dh, int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2 = 1, int64_t s2 = 0) {
+  int64_t n[3] = {n0, n1, n2}, s[3] = {s0, s1, s2};
+  double span = dh;   // (exact as far as any memory reaches)
+  for (int done = 0; done < 3; ++done) {
+    int at = -1;
+    for (int i = 0; i < 3; ++i)
+      if (n[i] > 1 && (at < 0 || s[i] < s[at])) at = i;
+    if (at < 0) return true;
+    if ((double)s[at] < span) return false;
+    span += (double)(n[at] - 1) * (double)s[at];
+    n[at] = 1;
+  }
+  return true;
+}
 // (type of q, k, v as given, type of the cache) pairs that the operators serve
 inline bool types_ok(int x, int cache) {
   return (cache == D3_BF16 && (x == D3_BF16 || x == D3_FP32)) || (cache == D3_FP16 && x == D3_FP16) ||

@@ -37,7 +37,8 @@
 // stored numbers are widened to fp16 (exact), bf16 queries are scaled by a power of two per head so that fp16 holds
 // them.  Where P is fp16, it is exp2(.. + 15): 2^-29 of the largest stays a normal number.
 //
-// Every wait is bounded; when one runs out the CTA stores D3_ETIMEOUT, stops issuing, lets its copies land and ends.
+// Every wait is bounded; when one runs out the CTA stores D3_ETIMEOUT, stops issuing, lets its copies land and ends.  (A
+// cluster's hardware barriers are met by every thread on every path, so they end when those waits have.)
 #pragma once
 
 #include <cuda.h>
@@ -634,8 +635,9 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     // ------------------------------------------------------------ epilogue: a head per warp, DH / 32 dims per lane
     constexpr int V = DH / 32;
     const int me = warp - C::kWarps;
+    auto gave_up = [&]() { if (lane == 0 && a.status) *a.status = D3_ETIMEOUT; };
     for (uint32_t parity = 0;; parity ^= 1u) {
-      if (!__all_sync(0xffffffffu, mb_wait(smem_u32(&s_sums_full), parity, &s_abort, a.wait_ns))) break;
+      if (!__all_sync(0xffffffffu, mb_wait(smem_u32(&s_sums_full), parity, &s_abort, a.wait_ns))) { gave_up(); break; }
       if (parity == 0u) pdl_wait();   // returns at once: the producers' has
       const ItemInfo item = s_item;
       const int kind = item.bits & 3, nh = (item.bits >> 3) & 31, first_warp = (item.bits >> 8) & 255, warps = (item.bits >> 16) & 255;
@@ -734,7 +736,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         } else {
           // ---- the item's first CTA: the pieces of all, in their order
           const int pieces = item.bits >> 24;
-          if (!__all_sync(0xffffffffu, mb_wait<true>(smem_u32(&s_joined[me]), 0, &s_abort, a.wait_ns))) break;
+          if (!__all_sync(0xffffffffu, mb_wait<true>(smem_u32(&s_joined[me]), 0, &s_abort, a.wait_ns))) { gave_up(); break; }
           const int stride = a.heads_per_tile * C::kHeadFloats;
           auto join = [&](auto hb, int h0) {
             constexpr int HB = decltype(hb)::value;
@@ -1221,8 +1223,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_join(const __grid_con
 // ---------------------------------------------------------------- launch
 // What is known of a kernel on a device: the SMs (0: not asked yet) and how many clusters of 2 .. 16 CTAs run at once.
 struct Device {
-  std::atomic<int> sms;
-  int clusters[17];
+  std::atomic<int> sms, clusters[17];
 };
 
 template <int DH, int CACHE, int X, int MT>
@@ -1257,7 +1258,7 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
       cfg.numAttrs = 1;
       int most = 0;
       if (cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); most = 0; }
-      d.clusters[cl] = most;   // (the same numbers, if two threads are here)
+      d.clusters[cl].store(most, std::memory_order_relaxed);   // (the same numbers, if two threads are here)
     }
     if (n > kFusedMaxCtas) n = kFusedMaxCtas;
     d.sms.store(n, std::memory_order_release);
@@ -1273,7 +1274,7 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
   a.cluster = 0;
   if (most >= 5) {
     int cl = (int)(most < 16 ? most : 16);
-    while (cl >= 2 && (items > d.clusters[cl] || stages_beside(C::kWarps + cl) < 3)) --cl;
+    while (cl >= 2 && (items > d.clusters[cl].load(std::memory_order_relaxed) || stages_beside(C::kWarps + cl) < 3)) --cl;
     const long long longest = cl >= 2 ? (most + cl - 1) / cl : 0;
     if (cl >= 2 && longest <= 24 && longest <= items * most / n + 9) a.cluster = cl;
   }

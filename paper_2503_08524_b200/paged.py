@@ -4,7 +4,7 @@ lengths, append with rotary positions, attention of one new token per row.
 Marshalling only, like `binding`: tensors in, one C call, no host synchronisation; the calls can be
 captured into a CUDA graph.  The checks of each call are in csrc/paged_call.cpp (a small decode step is
 bound by the host side of its calls).  They run on the current stream of the tensors' device unless `stream`
-is given.  A refused call raises D3Error (EINVAL) before anything is enqueued; what only the device
+is given.  Results carry no gradient.  A refused call raises D3Error (EINVAL) before anything is enqueued; what only the device
 can see (a page id out of range, too few free pages) goes to the `status` tensor.
 
     plan = PagePlan(cached=..., new_tokens=..., table=..., free=..., n_free=..., page_size=..., max_tokens=...)

@@ -177,6 +177,117 @@ def test_attention_whole_and_cut_rows(paged, contexts):
     check(out, lse, q, cache, table, contexts)
 
 
+@pytest.mark.parametrize("kv,x", [(BF16, BF16), (BF16, FP32), (FP16, FP16), (E4M3, BF16), (E4M3, FP16)],
+                         ids=["bf16", "bf16-fp32", "fp16", "e4m3-bf16", "e4m3-fp16"])
+@pytest.mark.parametrize("dh,page", [(32, 256), (64, 16), (128, 64)])
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (5, 1), (12, 1), (19, 1)])
+def test_attention_few_rows_of_wide_tables(paged, kv, x, dh, page, hq, hkv):
+    """Clusters of CTAs share a row: more pieces than units, fewer, none; padding rows; a row that ends in a unit's first tile."""
+    contexts = [1700, 1, 0, 65, 257, 1024]
+    cache, table, q, ctx = make(paged, contexts, hq, hkv, dh, page, kv, x, seed=hq + dh)
+    poison_behind(cache, table, contexts)
+    rows = [0, 1, 2, 3, -1, 5]
+    out, lse = torch.full_like(q, 7.0), torch.full((6, hq), 5.0, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for _ in range(3):
+        paged.d3_paged_attention(cache, q, table, ctx, rows=torch.tensor(rows, dtype=torch.int32, device=DEV), out=out, lse=lse,
+                                 status=status)
+    assert int(status) == 0 and (out[4] == 7.0).all() and (lse[4] == 5.0).all()
+    check(out, lse, q, cache, table, contexts, rows=rows)
+
+
+def test_attention_few_rows_of_wide_tables_with_bad_device_data(paged):
+    contexts = [1000, 700, 90]
+    cache, table, q, ctx = make(paged, contexts, 8, 2, 128, 16, BF16, BF16, seed=26)
+    ids = table[0].tolist()[:63]
+    for bad in (-1, cache.n_pages, 2 ** 31 - 1, -2 ** 31):
+        t = table.clone()
+        t[0, 3], t[0, 62], t[0, 20:40] = bad, bad, bad       # a page, the last one, whole units of several CTAs
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        out, lse = paged.d3_paged_attention(cache, q, t, ctx, with_lse=True, status=status)
+        assert int(status) == -1
+        kd, vd = dense(cache.k, ids, 1000), dense(cache.v, ids, 1000)
+        keep = [i for i in range(992) if i // 16 != 3 and not 20 <= i // 16 < 40]
+        want, want_lse, tol, tol_lse = reference(q[0].double(), kd[:, keep], vd[:, keep], 128 ** -0.5, 2.0 ** -16)
+        assert ((out[0].double() - want).abs() <= 2.0 ** -8 * (want.abs() + tol) + tol).all()
+        assert ((lse[0].double() - want_lse).abs() <= tol_lse).all()
+        check(out[1:], lse[1:], q[1:], cache, table[1:], contexts[1:])
+    t = torch.full_like(table, -5)                             # no page at all
+    out, lse = paged.d3_paged_attention(cache, q, t, ctx, with_lse=True, status=status)
+    assert (out == 0).all() and (lse == -math.inf).all()
+    for bad in (-1, 16 * table.shape[1] + 1, 2 ** 31 - 1):
+        status.zero_()
+        c = ctx.clone()
+        c[1] = bad
+        out, lse = paged.d3_paged_attention(cache, q, table, c, with_lse=True, status=status)
+        assert int(status) == -1
+        check(out, lse, q, cache, table, [1000, 0, 90])
+    status.zero_()
+    out = torch.full_like(q, 3.0)
+    rows = torch.tensor([0, 3, -7], dtype=torch.int32, device=DEV)
+    paged.d3_paged_attention(cache, q, table, ctx, rows=rows, out=out, status=status)
+    assert int(status) == -1 and (out[1:] == 3.0).all() and not (out[0] == 3.0).all()
+
+
+def test_attention_few_rows_captured_and_replayed_with_other_lengths(paged):
+    contexts = [1500, 1500, 1500]
+    cache, table, q, ctx = make(paged, contexts, 8, 2, 128, 16, BF16, BF16, seed=31)
+    ws, out, lse = paged.attention_workspace(cache, 8), torch.zeros_like(q), torch.zeros((3, 8), device=DEV)
+    call = lambda: paged.d3_paged_attention(cache, q, table, ctx, out=out, lse=lse, workspace=ws)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+        call()
+    for lengths in ([1500, 1, 0], [64, 65, 1499], [0, 0, 0], [1, 1, 1], [1024, 1500, 700]):
+        ctx.copy_(torch.tensor(lengths, dtype=torch.int32))
+        graph.replay()
+        check(out, lse, q, cache, table, lengths)
+        bits = out.clone()
+        call()
+        assert torch.equal(out, bits)
+
+
+FIRST_CALL = """
+import torch
+from paper_2503_08524_b200 import paged as P
+dev = "cuda:0"
+k, v = (torch.randn(40, 2, 16, 64, device=dev).bfloat16() for _ in range(2))
+cache = P.PagedKV(k, v)
+q, new = torch.randn(2, 8, 64, device=dev).bfloat16(), torch.randn(2, 2, 64, device=dev).bfloat16()
+i32 = dict(dtype=torch.int32, device=dev)
+table = torch.arange(40, **i32).view(2, 20)
+n_free = torch.zeros(1, **i32)
+plan = P.PagePlan(cached=torch.tensor([99, 300], **i32), new_tokens=torch.tensor([1, 1], **i32), table=table, free=torch.zeros(40, **i32),
+                  n_free=n_free, page_size=16, max_tokens=2, cached_out=torch.zeros(2, **i32), n_free_out=torch.zeros(1, **i32))
+rope = P.d3_rope_table(400, 64)
+q_out, out, ws = torch.zeros_like(q), torch.zeros_like(q), P.attention_workspace(cache, 8)
+def step():
+    plan.d3_page_plan()
+    P.d3_paged_append(cache, new, new, plan.slots, q=q, q_out=q_out, rope=rope, context=plan.context)
+    P.d3_paged_attention(cache, q_out, table, plan.context, rows=plan.row, out=out, workspace=ws)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    step()
+assert not out.any()
+graph.replay()
+got = out.clone()
+step()
+assert int(plan.status) == 0 and got.any() and torch.equal(out, got), (got, out)
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST_CALL], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
+
+
 def test_attention_peaked_scores_and_far_tails(paged):
     """One position outweighs the rest by e^16, in every type: the tail still counts (fp16 weights of 2^-24 and below)."""
     for kv, x in ((BF16, BF16), (FP16, FP16), (E4M3, FP16), (BF16, FP32)):

@@ -88,6 +88,23 @@ def test_attentions_that_are_refused(bad):
     assert B.LIB.d3_paged_attention(C.byref(kv_args()), C.byref(attention_args(**bad)), None) == B.EINVAL
 
 
+def test_outputs_that_overlap_are_refused():
+    for bad in (dict(q_out_token_stride=64), dict(q_out_head_stride=128), dict(q_out_token_stride=248)):
+        assert B.LIB.d3_paged_append(C.byref(kv_args()), C.byref(append_args(**bad)), None) == B.EINVAL, bad
+    for bad in (dict(head_stride=64), dict(page_stride=16 * 64), dict(page_stride=64), dict(token_stride=128)):
+        kv = kv_args(**bad)
+        assert B.LIB.d3_paged_append(C.byref(kv), C.byref(append_args()), None) == B.EINVAL, bad
+        assert B.LIB.d3_paged_attention(C.byref(kv), C.byref(attention_args(n_rows=0)), None) == B.OK, bad    # reads alone
+    for bad in (dict(out_row_stride=64), dict(out_head_stride=72), dict(out_row_stride=255)):
+        assert B.LIB.d3_paged_attention(C.byref(kv_args()), C.byref(attention_args(**bad)), None) == B.EINVAL, bad
+    nothing = dict(n_tokens=0)
+    for kv in (kv_args(), kv_args(token_stride=128, head_stride=64, page_stride=2048), kv_args(page_stride=64, head_stride=640, token_stride=1280),
+               kv_args(n_pages=1, page_stride=64)):
+        assert B.LIB.d3_paged_append(C.byref(kv), C.byref(append_args(**nothing)), None) == B.OK
+    for good in (dict(q_out_token_stride=64, q_out_head_stride=320), dict(q_out_token_stride=512, q_out_head_stride=128)):
+        assert B.LIB.d3_paged_append(C.byref(kv_args()), C.byref(append_args(n_tokens=0, **good)), None) == B.OK
+
+
 def test_null_arguments():
     n = C.c_size_t()
     assert B.LIB.d3_page_plan(None, None) == B.EINVAL
