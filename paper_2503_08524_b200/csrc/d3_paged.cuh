@@ -88,6 +88,7 @@ struct PagedAttnArgs {
   int table_rows, table_width, page_shift, n_pages;
   long long table_stride, q_row_stride, q_head_stride, out_row_stride, out_head_stride;
   float scale;
+  int out_wide;                        // results may be written DH / 32 numbers at a time
   const void *q;
   void *out;
   float *lse;

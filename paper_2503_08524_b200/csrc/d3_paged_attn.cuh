@@ -232,6 +232,27 @@ enum { STAGE_FIRST = 1, STAGE_LAST = 2, STAGE_FINAL = 4 };   // of the item with
 // an item lies in this CTA / started before it / starts in it and goes on; no item at all
 enum { OUT_WHOLE = 0, OUT_HEAD = 1, OUT_TAIL = 2, OUT_NONE = 3 };
 
+// V neighbouring dims of a result, times f, rounded once
+template <int X, int V>
+__device__ __forceinline__ void write_out(const PagedAttnArgs &a, long long at, const float (&o)[V], float f) {
+  if constexpr (X == D3_FP32) {
+    float *p = static_cast<float *>(a.out) + at;
+    if (V == 4 && a.out_wide) { *reinterpret_cast<float4 *>(p) = make_float4(o[0] * f, o[1 % V] * f, o[2 % V] * f, o[3 % V] * f); return; }
+    if (V == 2 && a.out_wide) { *reinterpret_cast<float2 *>(p) = make_float2(o[0] * f, o[1 % V] * f); return; }
+#pragma unroll
+    for (int e = 0; e < V; ++e) p[e] = o[e] * f;
+  } else {
+    uint16_t *p = static_cast<uint16_t *>(a.out) + at;
+    uint32_t w[(V + 1) / 2];
+#pragma unroll
+    for (int e = 0; e < V; e += 2) w[e / 2] = pack<X == D3_FP16>(o[e] * f, V > 1 ? o[(e + 1) % V] * f : 0.f);
+    if (V == 4 && a.out_wide) { *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[V / 2 - 1 < 0 ? 0 : V / 2 - 1]); return; }
+    if (V == 2 && a.out_wide) { *reinterpret_cast<uint32_t *>(p) = w[0]; return; }
+#pragma unroll
+    for (int e = 0; e < V; ++e) p[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+  }
+}
+
 // What the producers tell the consumers about a stage (one 16-byte load).
 struct __align__(16) StageInfo {
   int row;
@@ -281,7 +302,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   constexpr int KK = DH / 16, KT = C::kTiles, TQ = C::kQTerms, TP = C::kPTerms, PT = C::kPT;
   constexpr bool F16 = C::kF16;
   extern __shared__ unsigned char s_dyn[];
-  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sums_full, s_sums_free, s_joined[C::kEpilogue];
+  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sums_full, s_sums_free, s_joined[C::kWarps + C::kEpilogue];
   __shared__ StageInfo s_info[kMaxStages];
   __shared__ float s_m[C::kWarps][C::kHeads], s_l[C::kWarps][C::kHeads];
   __shared__ ItemInfo s_item;
@@ -298,17 +319,20 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   const int HG = a.hkv * a.tiles_per_head;
   const int CL = a.cluster, rank = CL ? (int)blockIdx.x % CL : 0;   // CTAs of a cluster (0: none), which share an item
 
-  if (tid == 0) {
-    for (int i = 0; i < S; ++i) {
-      mb_init(smem_u32(&s_full[i]), 1);
-      mb_init(smem_u32(&s_empty[i]), C::kWarps);
+  if (warp == 0) {
+    if (lane < S) {
+      mb_init(smem_u32(&s_full[lane]), 1);
+      mb_init(smem_u32(&s_empty[lane]), C::kWarps);
     }
-    mb_init(smem_u32(&s_sums_full), C::kWarps);
-    mb_init(smem_u32(&s_sums_free), C::kEpilogue);
-    for (int i = 0; i < C::kEpilogue; ++i) mb_init(smem_u32(&s_joined[i]), CL > 1 ? CL - 1 : 1);
+    if (lane < C::kWarps + C::kEpilogue) mb_init(smem_u32(&s_joined[lane]), CL > 1 ? CL - 1 : 1);
+    if (lane == 31) {
+      mb_init(smem_u32(&s_sums_full), C::kWarps);
+      mb_init(smem_u32(&s_sums_free), C::kEpilogue);
+      s_abort = 0;
+      s_start_row = a.n_rows;
+      s_start_before = 0;
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    s_abort = 0;
-    s_start_row = a.n_rows;
   }
   if (warp == C::kWarps + C::kEpilogue && lane < 4) {
     const CUtensorMap *m = lane == 0 ? &map_k : lane == 1 ? &map_v : lane == 2 ? &map_k16 : &map_v16;
@@ -317,18 +341,17 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
   // ---- the rows' unit counts, summed over all rows by every CTA: up to 128 rows by each producer warp for itself, more of
   // them by all threads
-  auto row_of = [&](int b, bool &bad) -> int {   // table row, -1 = padding
-    if (!a.rows) return b;
-    const int r = a.rows[b];
+  auto as_row = [&](int r, bool &bad) -> int {   // table row, -1 = padding
     if (r >= 0 && r < a.table_rows) return r;
     if (r != -1) bad = true;
     return -1;
   };
-  auto length_of = [&](int b, bool &bad) -> int {
-    const int c = a.context[b];
+  auto as_length = [&](int c, bool &bad) -> int {
     if (c < 0 || c > ((long long)a.table_width << a.page_shift)) { bad = true; return 0; }
     return c;
   };
+  auto row_of = [&](int b, bool &bad) -> int { return a.rows ? as_row(a.rows[b], bad) : b; };
+  auto length_of = [&](int b, bool &bad) -> int { return as_length(a.context[b], bad); };
   auto units_of = [&](int len) -> int { return len > 0 ? (len + kUnit - 1) / kUnit : 1; };   // a row without context still gets its zeros
   const bool few = a.few;
   long long units = 0;   // of all rows, for one tile of heads
@@ -419,13 +442,18 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       pdl_trigger();
       bool bad = false;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
+      for (int i = 0; i < kPer; ++i) {   // (all loads before the first use)
         const int b = lane * per + i;
-        r_[i] = -1; c_[i] = 0;
-        if (i < per && b < a.n_rows) {
+        const bool there = i < per && b < a.n_rows;
+        c_[i] = there ? a.context[b] : 0;
+        r_[i] = !there ? -1 : a.rows ? a.rows[b] : b;
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (i < per && lane * per + i < a.n_rows) {
           bool strange = false;
-          c_[i] = length_of(b, strange);
-          r_[i] = row_of(b, bad);
+          c_[i] = as_length(c_[i], strange);
+          r_[i] = as_row(r_[i], bad);
           if (r_[i] >= 0) { few_units += units_of(c_[i]); few_longest = max(few_longest, units_of(c_[i])); ++few_rows; bad = bad || strange; }
         }
       }
@@ -451,13 +479,23 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     Shares sh;
     long long x0, x1, item;   // this CTA's costs; where its first item starts
     int nu, tile, unit, lies_in = 1;
+    const int32_t *pages = a.table;
+    auto fetch = [&](int base) -> int { return base + lane < a.table_width ? __ldg(pages + base + lane) : -1; };
+    // page ids of the row, one per lane: 32 aligned pages in `win`, the next 32 in `win_next`.  A unit is at most 16
+    // aligned pages and never straddles a window.
+    int win0 = -1, win = 0, win_next = 0;
     if (CL) {   // a cluster per item, its CTAs take equal runs of the units
       const int index = (int)blockIdx.x / CL;
       bool bad = false;
       row = index / HG;
       tile = index - row * HG;
+      // the length and the first page ids are asked for together
+      const int c = a.context[row];
       trow = row_of(row, bad);
-      len = trow >= 0 ? length_of(row, bad) : 0;
+      pages = a.table + (long long)max(trow, 0) * a.table_stride;
+      win = fetch(0);
+      win_next = fetch(32);
+      len = trow >= 0 ? as_length(c, bad) : 0;
       if (bad && rank == 0 && tile == 0 && a.status) *a.status = D3_EINVAL;
       nu = units_of(len);
       lies_in = min(nu, CL);
@@ -467,6 +505,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       if (trow < 0 || x0 == x1) { idle(); return; }
       item = 0;
       unit = (int)x0;
+      if ((unit * kUnit) >> a.page_shift < 32) win0 = 0;
     } else if (few) {   // all of it in 32 bits
       const int total = ((int)units * cost.unit + live_rows * cost.item) * HG, each = (int)((unsigned)total / (unsigned)n_cta);
       sh.each = each; sh.more = total - each * n_cta;
@@ -501,23 +540,19 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       sh = Shares((units * cost.unit + (long long)live_rows * cost.item) * HG, n_cta);
       x0 = sh.start(blockIdx.x);
       x1 = sh.start(blockIdx.x + 1);
-      row = s_start_row;
-      trow = row_of(row, dummy);
+      row = min(s_start_row, a.n_rows - 1);   // (these bounds matter when somebody else changes the lengths during the call)
+      trow = max(row_of(row, dummy), 0);
       len = length_of(row, dummy);
       nu = units_of(len);
       const long long at = x0 - s_start_before, one = cost.of(nu);   // s_start_before: cost of the rows before
-      tile = one < (1ll << 31) ? (int)divide(at, (int)one) : (int)(at / one);
+      tile = (int)min(max(one < (1ll << 31) ? divide(at, (int)one) : at / one, 0ll), (long long)HG - 1);
       item = s_start_before + tile * one;
       unit = (int)min(cost.first_unit(x0 - item - cost.lead), 0x7fffffffll);
     }
     const bool behind = unit >= nu;   // no unit of that item is this CTA's: begin with the next one
     int kvh = tile, sub = 0;
     if (a.tiles_per_head > 1) { kvh = tile / a.tiles_per_head; sub = tile % a.tiles_per_head; }
-    const int32_t *pages = a.table + (long long)trow * a.table_stride;
-    auto fetch = [&](int base) -> int { return base + lane < a.table_width ? __ldg(pages + base + lane) : -1; };
-    // page ids of the row, one per lane: 32 aligned pages in `win`, the next 32 in `win_next`.  A unit is at most 16
-    // aligned pages and never straddles a window.
-    int win0 = -1, win = 0, win_next = 0;
+    if (!CL) pages = a.table + (long long)trow * a.table_stride;
     const int box_rows = min(1 << a.page_shift, kUnit), page_mask = (1 << a.page_shift) - 1;
     const int full_boxes = kUnit / box_rows, full_shift = 31 - __clz(full_boxes);
     int s = 0, issued = 0;
@@ -538,6 +573,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           trow = row >= a.n_rows ? 0 : few ? kept(r_) : row_of(row, dummy);
         } while (trow < 0);
         len = row >= a.n_rows ? 0 : few ? kept(c_) : length_of(row, dummy);
+        row = min(row, a.n_rows - 1);   // (behind the last row only when somebody else changes the lengths during the call)
         nu = units_of(len);
         pages = a.table + (long long)trow * a.table_stride;
       }
@@ -613,34 +649,31 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (me == 0 && lane == 0) {
       // an item that starts here and goes on: what the joining kernel adds up
       int4 join = make_int4(0, 0, 0, 0);
-      if (ok && cut_row >= 0 && !CL) join = make_int4(sh.holder(cut_last) - (int)blockIdx.x + 1, cut_row, cut_head, cut_kvh | cut_nh << 16);
+      if (ok && cut_row >= 0 && !CL) join = make_int4(min(sh.holder(cut_last), n_cta - 1) - (int)blockIdx.x + 1, cut_row, cut_head, cut_kvh | cut_nh << 16);
       if (!a.whole && !CL) a.join[blockIdx.x] = join;
     }
-    if (!ok) {   // copies in flight end by themselves: wait for them before the shared memory goes
-      const unsigned long long drain = a.wait_ns > kDrainFloorNs ? a.wait_ns : kDrainFloorNs;
-      for (int k = max(0, issued - S); k < issued; ++k)
-        if ((k & (kProducers - 1)) == me) mb_wait(smem_u32(&s_full[k % S]), (uint32_t)((k / S) & 1), &s_abort, drain, false);
-      if (lane == 0 && a.status) *a.status = D3_ETIMEOUT;
-    }
-  };
-
-  auto write_out = [&](long long at, float val) {
-    if (X == D3_FP32) static_cast<float *>(a.out)[at] = val;
-    else if (X == D3_BF16) static_cast<bf16 *>(a.out)[at] = __float2bfloat16_rn(val);
-    else static_cast<__half *>(a.out)[at] = __float2half_rn(val);
+    // Copies in flight end by themselves: wait for them before the shared memory goes, also where the consumers are already gone
+    // (a wait ran out; or somebody else changed the lengths during the call and the two producers saw different ones).
+    const unsigned long long drain = a.wait_ns > kDrainFloorNs ? a.wait_ns : kDrainFloorNs;
+    for (int k = max(0, issued - S); k < issued; ++k)
+      if ((k & (kProducers - 1)) == me && !mb_wait(smem_u32(&s_full[k % S]), (uint32_t)((k / S) & 1), &s_abort, drain, false)) ok = false;
+    if (!ok && lane == 0 && a.status) *a.status = D3_ETIMEOUT;
   };
 
   bool met = false;   // this thread has seen the whole cluster started
-  auto epilogue = [&]() {
-    // ------------------------------------------------------------ epilogue: a head per warp, DH / 32 dims per lane
+  auto epilogue = [&](uint32_t parity) {
+    // ------------------------------------------------------------ epilogue: a head per warp, DH / 32 dims per lane.  The
+    // consumers have nothing left to do at a CTA's last item and help there (4 rows x 545, 8 heads a tile: 9.7 -> 8.4 us).
     constexpr int V = DH / 32;
-    const int me = warp - C::kWarps;
+    const bool helps = warp < C::kWarps;
+    const int me = helps ? warp + C::kEpilogue : warp - C::kWarps;
     auto gave_up = [&]() { if (lane == 0 && a.status) *a.status = D3_ETIMEOUT; };
-    for (uint32_t parity = 0;; parity ^= 1u) {
+    for (bool first = true;; first = false, parity ^= 1u) {
       if (!__all_sync(0xffffffffu, mb_wait(smem_u32(&s_sums_full), parity, &s_abort, a.wait_ns))) { gave_up(); break; }
-      if (parity == 0u) pdl_wait();   // returns at once: the producers' has
+      if (first) pdl_wait();   // returns at once: the producers' has
       const ItemInfo item = s_item;
       const int kind = item.bits & 3, nh = (item.bits >> 3) & 31, first_warp = (item.bits >> 8) & 255, warps = (item.bits >> 16) & 255;
+      const int workers = item.bits & 4 ? C::kWarps + C::kEpilogue : C::kEpilogue;
       if (CL && kind != OUT_WHOLE && rank > 0) { cluster_wait(); met = true; }   // the first CTA's barriers are there
       if (kind == OUT_NONE) {
         if (CL && rank > 0 && lane == 0) arrive_there(in_cta(smem_u32(&s_joined[me]), 0));
@@ -651,9 +684,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
       const float vs = a.v_scale ? __ldg(a.v_scale + (item.heads >> 16)) : 1.f;
       auto finish = [&](int h, const float (&o)[V], float m, float l) {
         const float f = l == 0.f ? 0.f : vs / l;
-        const long long at = item.row * a.out_row_stride + (long long)((item.heads & 0xffffu) + h) * a.out_head_stride + lane * V;
-#pragma unroll
-        for (int e = 0; e < V; ++e) write_out(at + e, o[e] * f);
+        write_out<X, V>(a, item.row * a.out_row_stride + (long long)((item.heads & 0xffffu) + h) * a.out_head_stride + lane * V, o, f);
         if (lane == 0 && a.lse)
           a.lse[(long long)item.row * a.hq + (item.heads & 0xffffu) + h] = l == 0.f ? -INFINITY : (m + (log2f(l) - (F16 ? 15.f : 0.f))) * kLn2;
       };
@@ -663,7 +694,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         float M[HB], L[HB], c[HB], o[HB][V];
 #pragma unroll
         for (int i = 0; i < HB; ++i) {
-          const int h = min(h0 + i * C::kEpilogue, nh - 1);
+          const int h = min(h0 + i * workers, nh - 1);
           L[i] = lane < warps ? s_l[from][h] : 0.f;
           c[i] = lane < warps ? s_m[from][h] : -INFINITY;
           M[i] = c[i];
@@ -691,7 +722,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const int w = __shfl_sync(0xffffffffu, from, k + j);
 #pragma unroll
             for (int i = 0; i < HB; ++i) {
-              const int h = min(h0 + i * C::kEpilogue, nh - 1);
+              const int h = min(h0 + i * workers, nh - 1);
               const float cw = __shfl_sync(0xffffffffu, c[i], k + j);
               const float *src = s_o + (w * a.heads_per_tile + h) * C::kHeadFloats + lane * V;
               float x[V];
@@ -705,7 +736,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
 #pragma unroll
         for (int i = 0; i < HB; ++i) {
-          const int h = h0 + i * C::kEpilogue;
+          const int h = h0 + i * workers;
           if (h >= nh) break;
           const float l = __shfl_sync(0xffffffffu, L[i], 0), m = __shfl_sync(0xffffffffu, M[i], 0);
           if (kind == OUT_WHOLE) {
@@ -726,10 +757,10 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
           }
         }
       };
-      if (nh <= C::kEpilogue) { if (me < nh) heads(std::integral_constant<int, 1>(), me); }
-      else for (int h0 = me; h0 < nh; h0 += 4 * C::kEpilogue) heads(std::integral_constant<int, 4>(), h0);
+      if (nh <= workers) { if (me < nh) heads(std::integral_constant<int, 1>(), me); }
+      else for (int h0 = me; h0 < nh; h0 += 4 * workers) heads(std::integral_constant<int, 4>(), h0);
       __syncwarp();
-      if (lane == 0) mb_arrive(smem_u32(&s_sums_free));
+      if (lane == 0 && !helps) mb_arrive(smem_u32(&s_sums_free));
       if (CL && kind != OUT_WHOLE) {
         if (rank > 0) {
           if (lane == 0) arrive_there(in_cta(smem_u32(&s_joined[me]), 0));
@@ -744,7 +775,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const float *all[HB];
 #pragma unroll
             for (int i = 0; i < HB; ++i) {
-              all[i] = s_j + min(h0 + i * C::kEpilogue, nh - 1) * C::kHeadFloats;
+              all[i] = s_j + min(h0 + i * workers, nh - 1) * C::kHeadFloats;
               const float2 ml = *reinterpret_cast<const float2 *>(all[i] + min(lane, pieces - 1) * stride + DH);
               c[i] = M[i] = lane < pieces ? ml.x : -INFINITY;
               L[i] = ml.y;
@@ -781,11 +812,11 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
 #pragma unroll
             for (int i = 0; i < HB; ++i)
-              if (h0 + i * C::kEpilogue < nh)
-                finish(h0 + i * C::kEpilogue, o[i], __shfl_sync(0xffffffffu, M[i], 0), __shfl_sync(0xffffffffu, L[i], 0));
+              if (h0 + i * workers < nh)
+                finish(h0 + i * workers, o[i], __shfl_sync(0xffffffffu, M[i], 0), __shfl_sync(0xffffffffu, L[i], 0));
           };
-          if (nh <= C::kEpilogue) { if (me < nh) join(std::integral_constant<int, 1>(), me); }
-          else for (int h0 = me; h0 < nh; h0 += 4 * C::kEpilogue) join(std::integral_constant<int, 4>(), h0);
+          if (nh <= workers) { if (me < nh) join(std::integral_constant<int, 1>(), me); }
+          else for (int h0 = me; h0 < nh; h0 += 4 * workers) join(std::integral_constant<int, 4>(), h0);
         }
       }
       if (item.bits & 4) break;
@@ -793,7 +824,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   };
 
   // -------------------------------------------------------------- consumers
-  auto consume = [&]() {
+  auto consume = [&]() -> int {   // how many items ended here; 0 when a wait ran out
   // Fragments (g = lane / 4, t = lane % 4).  Scores: A = K (rows = positions), B = Q^T (column g = head), result: positions
   // g, g + 8 of heads 2t, 2t + 1.  Sums: A = V^T (rows = dims), B = P^T, result: dims g, g + 8 of heads 2t, 2t + 1.
   const int g = lane >> 2, t = lane & 3, mat = lane >> 3;
@@ -1098,11 +1129,15 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     }
   }
   if (!ok && lane == 0 && a.status) *a.status = D3_ETIMEOUT;
+  return ok ? items : 0;
   };
 
-  if (warp >= C::kWarps + C::kEpilogue) produce();
-  else if (warp >= C::kWarps) epilogue();
-  else consume();
+  if (warp >= C::kWarps + C::kEpilogue) {
+    produce();
+  } else {
+    const int items = warp < C::kWarps ? consume() : 1;
+    if (items > 0) epilogue((uint32_t)(items - 1) & 1u);
+  }
   if (CL) {   // no CTA of the cluster leaves while another may still write to it (every wait before this one is bounded)
     if (!met) cluster_wait();
     cluster_arrive();
@@ -1209,14 +1244,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_paged_join(const __grid_con
   }
   const float f = L == 0.f ? 0.f : (a.v_scale ? __ldg(a.v_scale + kvh) : 1.f) / L;
   const long long head = job.z + h;
-  const long long at = row * a.out_row_stride + head * a.out_head_stride + lane * V;
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const float val = o[e] * f;
-    if (X == D3_FP32) static_cast<float *>(a.out)[at + e] = val;
-    else if (X == D3_BF16) static_cast<bf16 *>(a.out)[at + e] = __float2bfloat16_rn(val);
-    else static_cast<__half *>(a.out)[at + e] = __float2half_rn(val);
-  }
+  write_out<X, V>(a, row * a.out_row_stride + head * a.out_head_stride + lane * V, o, f);
   if (lane == 0 && a.lse) a.lse[(long long)row * a.hq + head] = L == 0.f ? -INFINITY : (top + (log2f(L) - (F16 ? 15.f : 0.f))) * kLn2;
 }
 
@@ -1271,6 +1299,8 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
   // of different lengths would leave clusters idle.  Under 5 units a row stays whole (1 row, 32 kv heads of 128, bf16,
   // whole or cut / cluster: 128 positions 5.3 / 5.7 us, 512 8.1 / 7.0, 2048 13.8 / 10.3; 1 row, 8 kv heads: 512 8.8 / 7.0,
   // 2048 10.8 / 9.2).
+  constexpr int kWide = DH / 32 * QBytes<X>::v;   // bytes of the dims a lane writes
+  a.out_wide = (uintptr_t)a.out % kWide == 0 && a.out_row_stride * QBytes<X>::v % kWide == 0 && a.out_head_stride * QBytes<X>::v % kWide == 0;
   a.cluster = 0;
   if (most >= 5) {
     int cl = (int)(most < 16 ? most : 16);
