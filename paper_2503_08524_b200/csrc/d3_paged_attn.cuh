@@ -11,7 +11,7 @@
 //     ~200 KB of 32 KB stages by TMA (4-D tensor map over the pool: dim, position, kv head, page; boxes of up to a
 //     page, of 16 positions where a row ends), so both layouts cost the same; page ids are looked up 32 at a time, one
 //     window ahead; they never wait for the arithmetic until the ring is full.  (One producer warp with 16-position
-//     boxes took 1.2 us per stage whatever its bytes: 64 rows of up to 16384 positions 562 us, now 327.)
+//     boxes took 1.2 us per stage whatever its bytes: 64 rows of up to 16384 positions 562 us, now 322.)
 //   * the share is cut by positions, not by rows: row lengths are read on the device, every CTA sums them up and takes
 //     the same number of units (stages; a row's start and end count as 3/4 of one), so ragged batches and one long row
 //     load all SMs alike;
@@ -21,16 +21,18 @@
 //     registers.  P is used as two terms, P - round(P) in a second product: 16 (bf16) or 22 (fp16) bits of it count.
 //     tcgen05.mma would need P, a few hundred numbers, written to shared memory and results fetched from tensor memory
 //     for every piece; the legacy pipe is a quarter busy here;
-//   * epilogue warps add the consumers' (m, l, O) up at the end of a row, while the consumers go on with the next row.
+//   * epilogue warps add the consumers' (m, l, O) up at the end of a row, while the consumers go on with the next row.  They are
+//     latency-bound, so 16-bit caches have four of them beside ten consumers (two beside twelve: 512 rows x 100, 32/8
+//     heads 72 us, now 57; 64 rows x 16384 329, now 322); the widening of 8-bit caches wants the twelve.
 //     Rows that lie inside a CTA are written at once; of a row that is cut every CTA leaves (m, l, O) of its piece and
 //     k_paged_join adds them up in the order of the CTAs: bits depend on the lengths alone, no atomics.
 //   * few rows are latency: each (row, kv head) gets a cluster of CTAs that add their pieces up through distributed
 //     shared memory; rows of few units are not cut at all (launch(), cost_of()).
 //
-// Measured (us, of the measured copy rate 6451 GB/s): 64 rows x 1..16384 GQA 32/8 x 128 bf16 327 (99 %); 96 rows x 17..8192
+// Measured (us, of the measured copy rate 6451 GB/s): 64 rows x 1..16384 GQA 32/8 x 128 bf16 322 (100 %); 96 rows x 17..8192
 // 64/8 8-bit 140.5 (89 %: the widening to fp16 keeps the warps busy); 1 row x 131071 64/8 fp16 91 (91 %: 6 us are start and
-// join); 32 rows x 129..1025 32/32 bf16 55.5 (84 %: 9 us are start and join); 1 row x 513 32/32 7.1; 4 rows x 513..545 64/8
-// fp32 9.8 (latency).
+// join); 32 rows x 129..1025 32/32 bf16 56 (84 %: 9 us are start and join); 1 row x 513 32/32 7.2; 4 rows x 513..545 64/8
+// fp32 8.6 (latency).  Short rows pay about 1 us per row and kv head for their ends: 128 rows x 200, 64/8 28.5 (59 %).
 //
 // fp32 queries (bf16 cache): q and P are three bf16 terms by truncation (8 + 8 + 8 bits: exact), sums of products short
 // chains (error of fp32 outputs against 64 bits 1e-7 .. 3e-7).  8-bit cache: the
@@ -56,6 +58,7 @@ constexpr int kTile = 16;             // positions of a product's rows, and of t
 constexpr int kProducers = 2;         // warps that issue copies, stage by stage in turn
 constexpr int kFewRows = 128;         // rows that a producer warp sums up by itself
 constexpr int kMaxStages = 12;
+constexpr int kItems = 4;              // items between the consumers and the epilogue at most
 constexpr int kSmemMost = 224 * 1024; // of 227 KB
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -282,8 +285,9 @@ struct Cfg {
   static constexpr int kStageBytes = 2 * kHalfBytes;
   // Registers are dealt out to four warps at a time: 16 warps of 128 (which 32 accumulator and 16 query registers fit
   // into), or 12 of 168 for 16 heads or three-term queries.
-  static constexpr int kWarps = MT == 1 ? 12 : 8;            // consumers
-  static constexpr int kEpilogue = 2;
+  static constexpr int kEpilogue = MT == 1 && CACHE != D3_E4M3 ? 4 : 2;
+  static constexpr int kWarps = MT == 1 ? 14 - kEpilogue : 8;      // consumers
+  static constexpr int kClusterWarps = MT == 1 ? 12 : 8;           // consumers of a cluster's CTA (three units are one turn)
   static constexpr int kThreads = 32 * (kWarps + kProducers + kEpilogue);
   static constexpr int kHeadFloats = DH + 4;                 // of a head's sums in shared memory (padded: no bank conflicts)
   static constexpr bool kF16 = CACHE != D3_BF16;
@@ -302,32 +306,37 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   constexpr int KK = DH / 16, KT = C::kTiles, TQ = C::kQTerms, TP = C::kPTerms, PT = C::kPT;
   constexpr bool F16 = C::kF16;
   extern __shared__ unsigned char s_dyn[];
-  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sums_full, s_sums_free, s_joined[C::kWarps + C::kEpilogue];
+  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sums_full[kItems], s_sums_free[kItems], s_own[C::kWarps],
+      s_joined[C::kWarps + C::kEpilogue];
   __shared__ StageInfo s_info[kMaxStages];
-  __shared__ float s_m[C::kWarps][C::kHeads], s_l[C::kWarps][C::kHeads];
-  __shared__ ItemInfo s_item;
+  __shared__ float s_m[C::kWarps + C::kEpilogue][C::kHeads], s_l[C::kWarps + C::kEpilogue][C::kHeads];
+  __shared__ ItemInfo s_item[kItems];
   __shared__ long long s_sum[32];
   __shared__ int s_abort, s_start_row;   // (start: the first row's, where all threads look for it)
   __shared__ long long s_start_before;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int HG = a.hkv * a.tiles_per_head;
+  const int CL = a.cluster, rank = CL ? (int)blockIdx.x % CL : 0;   // CTAs of a cluster (0: none), which share an item
+  const int NW = CL ? C::kClusterWarps : C::kWarps;   // consumers: a cluster's CTA has one item, and no epilogue beside it
   const int S = a.n_stages;
   const uint32_t ring = (smem_u32(s_dyn) + 1023u) & ~1023u;
   unsigned char *ring_p = s_dyn + (ring - smem_u32(s_dyn));
   unsigned char *q_slots = ring_p + (size_t)S * C::kStageBytes;
   float *s_o = reinterpret_cast<float *>(q_slots + (size_t)S * C::kQBytes);   // [warp][head][kHeadFloats]
-  float *s_j = s_o + (size_t)C::kWarps * a.heads_per_tile * C::kHeadFloats;   // cluster: [CTA][head][kHeadFloats], (m, l) behind the sums
-  const int HG = a.hkv * a.tiles_per_head;
-  const int CL = a.cluster, rank = CL ? (int)blockIdx.x % CL : 0;   // CTAs of a cluster (0: none), which share an item
+  float *s_j = s_o + (size_t)NW * a.heads_per_tile * C::kHeadFloats;   // cluster: [CTA][head][kHeadFloats], (m, l) behind the sums
 
   if (warp == 0) {
     if (lane < S) {
       mb_init(smem_u32(&s_full[lane]), 1);
-      mb_init(smem_u32(&s_empty[lane]), C::kWarps);
+      mb_init(smem_u32(&s_empty[lane]), NW);
     }
-    if (lane < C::kWarps + C::kEpilogue) mb_init(smem_u32(&s_joined[lane]), CL > 1 ? CL - 1 : 1);
+    if (lane < C::kWarps + C::kEpilogue && CL) mb_init(smem_u32(&s_joined[lane]), CL - 1);
+    if (lane < C::kWarps && !CL) mb_init(smem_u32(&s_own[lane]), C::kEpilogue);
+    if (lane >= 32 - kItems) {
+      mb_init(smem_u32(&s_sums_full[lane & (kItems - 1)]), NW);
+      mb_init(smem_u32(&s_sums_free[lane & (kItems - 1)]), C::kEpilogue);
+    }
     if (lane == 31) {
-      mb_init(smem_u32(&s_sums_full), C::kWarps);
-      mb_init(smem_u32(&s_sums_free), C::kEpilogue);
       s_abort = 0;
       s_start_row = a.n_rows;
       s_start_before = 0;
@@ -661,17 +670,18 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   };
 
   bool met = false;   // this thread has seen the whole cluster started
-  auto epilogue = [&](uint32_t parity) {
+  auto epilogue = [&](int i0) {
     // ------------------------------------------------------------ epilogue: a head per warp, DH / 32 dims per lane.  The
-    // consumers have nothing left to do at a CTA's last item and help there (4 rows x 545, 8 heads a tile: 9.7 -> 8.4 us).
+    // consumers have nothing left to do at a CTA's last item and help there (4 rows x 545, 8 heads a tile: 9.7 us without, 8.6 with).
     constexpr int V = DH / 32;
-    const bool helps = warp < C::kWarps;
-    const int me = helps ? warp + C::kEpilogue : warp - C::kWarps;
+    constexpr int kMany = C::kEpilogue == 4 ? 2 : 4;   // heads of a warp at a time
+    const bool helps = CL || warp < NW;
     auto gave_up = [&]() { if (lane == 0 && a.status) *a.status = D3_ETIMEOUT; };
-    for (bool first = true;; first = false, parity ^= 1u) {
-      if (!__all_sync(0xffffffffu, mb_wait(smem_u32(&s_sums_full), parity, &s_abort, a.wait_ns))) { gave_up(); break; }
-      if (first) pdl_wait();   // returns at once: the producers' has
-      const ItemInfo item = s_item;
+    for (int it = i0;; ++it) {
+      const int at = it & (kItems - 1), me = CL ? warp : helps ? warp + C::kEpilogue : (warp - C::kWarps + it) & (C::kEpilogue - 1);   // (single heads in turn)
+      if (!__all_sync(0xffffffffu, mb_wait(smem_u32(&s_sums_full[at]), (uint32_t)(it / kItems) & 1u, &s_abort, a.wait_ns))) { gave_up(); break; }
+      if (it == i0) pdl_wait();   // returns at once: the producers' has
+      const ItemInfo item = s_item[at];
       const int kind = item.bits & 3, nh = (item.bits >> 3) & 31, first_warp = (item.bits >> 8) & 255, warps = (item.bits >> 16) & 255;
       const int workers = item.bits & 4 ? C::kWarps + C::kEpilogue : C::kEpilogue;
       if (CL && kind != OUT_WHOLE && rank > 0) { cluster_wait(); met = true; }   // the first CTA's barriers are there
@@ -680,7 +690,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         break;
       }
       int from = first_warp + min(lane, warps - 1);   // lane k: the k-th warp that had a piece of the item
-      if (from >= C::kWarps) from -= C::kWarps;
+      if (from >= NW) from -= NW;
       const float vs = a.v_scale ? __ldg(a.v_scale + (item.heads >> 16)) : 1.f;
       auto finish = [&](int h, const float (&o)[V], float m, float l) {
         const float f = l == 0.f ? 0.f : vs / l;
@@ -758,9 +768,12 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
       };
       if (nh <= workers) { if (me < nh) heads(std::integral_constant<int, 1>(), me); }
-      else for (int h0 = me; h0 < nh; h0 += 4 * workers) heads(std::integral_constant<int, 4>(), h0);
+      else for (int h0 = me; h0 < nh; h0 += kMany * workers) heads(std::integral_constant<int, kMany>(), h0);
       __syncwarp();
-      if (lane == 0 && !helps) mb_arrive(smem_u32(&s_sums_free));
+      if (!helps) {
+        if (lane == 0) mb_arrive(smem_u32(&s_sums_free[at]));
+        if (lane < warps) mb_arrive(smem_u32(&s_own[from]));
+      }
       if (CL && kind != OUT_WHOLE) {
         if (rank > 0) {
           if (lane == 0) arrive_there(in_cta(smem_u32(&s_joined[me]), 0));
@@ -816,7 +829,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 finish(h0 + i * workers, o[i], __shfl_sync(0xffffffffu, M[i], 0), __shfl_sync(0xffffffffu, L[i], 0));
           };
           if (nh <= workers) { if (me < nh) join(std::integral_constant<int, 1>(), me); }
-          else for (int h0 = me; h0 < nh; h0 += 4 * workers) join(std::integral_constant<int, 4>(), h0);
+          else for (int h0 = me; h0 < nh; h0 += kMany * workers) join(std::integral_constant<int, kMany>(), h0);
         }
       }
       if (item.bits & 4) break;
@@ -846,8 +859,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
     for (int n = 0; n < KK; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
   }
-  int piece_turn = 0;       // pieces of the CTA so far, mod kWarps: whose turn it is
-  int items = 0;
+  int piece_turn = 0;       // pieces of the CTA so far, mod NW: whose turn it is
+  int items = 0, uses = 0;   // that ended; that this warp had a part of
   bool ok = true;
   int first_warp = 0, item_pieces = 0;   // of the running item: whose its first piece was, and how many there were
   int s = 0;
@@ -927,9 +940,9 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     item_pieces += n_pieces;
     // pieces go round the warps
     int p = warp - piece_turn;
-    if (p < 0) p += C::kWarps;
+    if (p < 0) p += NW;
     piece_turn += n_pieces;
-    if (piece_turn >= C::kWarps) piece_turn -= C::kWarps;
+    if (piece_turn >= NW) piece_turn -= NW;
     if (p < n_pieces) {   // (a stage has 4 pieces at most)
       // positions of each tile of the piece; none where its page id was out of range
       int valid[PT];
@@ -1087,11 +1100,17 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
     if (flags & STAGE_LAST) {
       // ---- the item's end in this CTA: this warp's sums to shared memory, for the epilogue warps to add up
-      if (items > 0 && !mb_wait(smem_u32(&s_sums_free), (uint32_t)((items - 1) & 1), &s_abort, a.wait_ns)) ok = false;
+      const int warps = min(item_pieces, NW), turn = warp - first_warp + (warp < first_warp ? NW : 0);
+      // Room in the ring of items, and this warp's sums of the last item that it had a part of are taken: short items lie in
+      // different warps, and none waits for the one before it (128 rows of 64 positions, 64 / 8 heads: 20.2 us with one set for
+      // all, 18.3 so, 14.8 with four epilogue warps as well).
+      const int slot = items & (kItems - 1);
+      if (items >= kItems && !mb_wait(smem_u32(&s_sums_free[slot]), (uint32_t)(items / kItems - 1) & 1u, &s_abort, a.wait_ns)) ok = false;
+      if (turn < warps && uses > 0 && !mb_wait(smem_u32(&s_own[warp]), (uint32_t)(uses - 1) & 1u, &s_abort, a.wait_ns)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      const int warps = min(item_pieces, C::kWarps), turn = warp - first_warp + (warp < first_warp ? C::kWarps : 0);
       if (turn < warps) {
+        ++uses;
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
 #pragma unroll
@@ -1120,11 +1139,11 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
       }
       if (warp == 0 && lane == 0)
-        s_item = ItemInfo{info.row, info.heads,
+        s_item[slot] = ItemInfo{info.row, info.heads,
                           ((flags >> 3) & 3) | (more ? 0u : 4u) | ((info.bits >> 14) & 31) << 3 | (uint32_t)first_warp << 8 | (uint32_t)warps << 16 |
                               ((info.bits >> 19) & 31) << 24};
       __syncwarp();
-      if (lane == 0) mb_arrive(smem_u32(&s_sums_full));
+      if (lane == 0) mb_arrive(smem_u32(&s_sums_full[slot]));
       ++items;
     }
   }
@@ -1135,8 +1154,8 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   if (warp >= C::kWarps + C::kEpilogue) {
     produce();
   } else {
-    const int items = warp < C::kWarps ? consume() : 1;
-    if (items > 0) epilogue((uint32_t)(items - 1) & 1u);
+    const int items = warp < NW ? consume() : 1;
+    if (items > 0) epilogue(items - 1);
   }
   if (CL) {   // no CTA of the cluster leaves while another may still write to it (every wait before this one is bounded)
     if (!met) cluster_wait();
@@ -1304,7 +1323,7 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
   a.cluster = 0;
   if (most >= 5) {
     int cl = (int)(most < 16 ? most : 16);
-    while (cl >= 2 && (items > d.clusters[cl].load(std::memory_order_relaxed) || stages_beside(C::kWarps + cl) < 3)) --cl;
+    while (cl >= 2 && (items > d.clusters[cl].load(std::memory_order_relaxed) || stages_beside(C::kClusterWarps + cl) < 3)) --cl;
     const long long longest = cl >= 2 ? (most + cl - 1) / cl : 0;
     if (cl >= 2 && longest <= 24 && longest <= items * most / n + 9) a.cluster = cl;
   }
@@ -1312,7 +1331,7 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
   // most: the busiest CTA is at most one row longer than an even share (40 kv heads, 8 rows of 512 positions: 20.9 us whole,
   // 22.7 cut).
   a.whole = !a.cluster && most <= 10;
-  const int sets = C::kWarps + a.cluster;
+  const int sets = a.cluster ? C::kClusterWarps + a.cluster : C::kWarps;
   a.n_stages = stages_beside(sets);
   if (a.n_stages < 2) return -1;
   const size_t smem = 1024 + (size_t)a.n_stages * (C::kStageBytes + C::kQBytes) + (size_t)sets * head_bytes;
