@@ -22,15 +22,15 @@
 //     tcgen05.mma would need P, a few hundred numbers, written to shared memory and results fetched from tensor memory
 //     for every piece; the legacy pipe is a quarter busy here;
 //   * epilogue warps add the consumers' (m, l, O) up at the end of a row, while the consumers go on with the next row.  They are
-//     latency-bound, so 16-bit caches have four of them beside ten consumers (two beside twelve: 512 rows x 100, 32/8
-//     heads 72 us, now 57; 64 rows x 16384 329, now 322); the widening of 8-bit caches wants the twelve.
+//     latency-bound: four of them beside ten consumers (two beside twelve: 512 rows x 100, 32/8 heads 72 us, now 57; 64 rows
+//     x 16384 329, now 322; 8-bit 64 x 4096, 32/8 102, now 99, but 96 x 8192, 64/8 140.5, now 141.4).
 //     Rows that lie inside a CTA are written at once; of a row that is cut every CTA leaves (m, l, O) of its piece and
 //     k_paged_join adds them up in the order of the CTAs: bits depend on the lengths alone, no atomics.
 //   * few rows are latency: each (row, kv head) gets a cluster of CTAs that add their pieces up through distributed
 //     shared memory; rows of few units are not cut at all (launch(), cost_of()).
 //
 // Measured (us, of the measured copy rate 6451 GB/s): 64 rows x 1..16384 GQA 32/8 x 128 bf16 322 (100 %); 96 rows x 17..8192
-// 64/8 8-bit 140.5 (89 %: the widening to fp16 keeps the warps busy); 1 row x 131071 64/8 fp16 91 (91 %: 6 us are start and
+// 64/8 8-bit 141 (89 %: the widening to fp16 keeps the warps busy); 1 row x 131071 64/8 fp16 91 (91 %: 6 us are start and
 // join); 32 rows x 129..1025 32/32 bf16 56 (84 %: 9 us are start and join); 1 row x 513 32/32 7.2; 4 rows x 513..545 64/8
 // fp32 8.6 (latency).  Short rows pay about 1 us per row and kv head for their ends: 128 rows x 200, 64/8 28.5 (59 %).
 //
@@ -285,7 +285,7 @@ struct Cfg {
   static constexpr int kStageBytes = 2 * kHalfBytes;
   // Registers are dealt out to four warps at a time: 16 warps of 128 (which 32 accumulator and 16 query registers fit
   // into), or 12 of 168 for 16 heads or three-term queries.
-  static constexpr int kEpilogue = MT == 1 && CACHE != D3_E4M3 ? 4 : 2;
+  static constexpr int kEpilogue = MT == 1 ? 4 : 2;
   static constexpr int kWarps = MT == 1 ? 14 - kEpilogue : 8;      // consumers
   static constexpr int kClusterWarps = MT == 1 ? 12 : 8;           // consumers of a cluster's CTA (three units are one turn)
   static constexpr int kThreads = 32 * (kWarps + kProducers + kEpilogue);
@@ -1329,8 +1329,8 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
   }
   // Otherwise items stay whole whatever the lengths, and no join is launched, where the table has room for 10 units a row at
   // most: the busiest CTA is at most one row longer than an even share (40 kv heads, 8 rows of 512 positions: 20.9 us whole,
-  // 22.7 cut).
-  a.whole = !a.cluster && most <= 10;
+  // 22.7 cut); 16 units where every item has a CTA for itself (32 kv heads, 4 rows of 768: 13.1 us without the join, 15.9 with it).
+  a.whole = !a.cluster && most <= (items <= n ? 16 : 10);
   const int sets = a.cluster ? C::kClusterWarps + a.cluster : C::kWarps;
   a.n_stages = stages_beside(sets);
   if (a.n_stages < 2) return -1;
