@@ -359,7 +359,9 @@ const char *d3_strerror(int32_t code);
  * Device data is checked where it is used, against the bounds the host gave: a value out of range is
  * never used as an index; the call skips what it stands for, as said below, and stores D3_EINVAL to
  * `status_dev` (int32, never cleared by these calls; nullable except where noted).  One workspace
- * serves one call at a time: calls that may overlap need a workspace each.  Rows of one output (and of a
+ * serves one call at a time: calls that may overlap need a workspace each.  What a call reads must hold
+ * still until it ends (order it behind what writes its tensors, on another stream too); its results
+ * are undefined otherwise.  Rows of one output (and of a
  * pool that is appended to) must not overlap: D3_EINVAL, so is a stride that does not reach over what
  * the smaller strides span.  Nothing here is differentiable. */
 #define D3_BF16 0

@@ -288,6 +288,26 @@ def test_the_first_calls_of_a_process_may_be_captured():
     assert done.returncode == 0, done.stderr[-2000:]
 
 
+@pytest.mark.parametrize("kv,x", [(BF16, BF16), (BF16, FP32), (E4M3, BF16)], ids=["bf16", "bf16-fp32", "e4m3-bf16"])
+@pytest.mark.parametrize("dh,hq,hkv", [(128, 16, 2), (64, 6, 2), (32, 32, 2), (128, 3, 3)])
+@pytest.mark.parametrize("long", [0, 3000])
+def test_attention_many_short_rows(paged, kv, x, dh, hq, hkv, long):
+    """Many row ends close together, lengths 0 to 300, alone (no row is cut) and beside a long row (rows are cut); equal bits each time."""
+    g = torch.Generator().manual_seed(dh + hq + long)
+    contexts = torch.randint(0, 301, (260,), generator=g).tolist()
+    contexts[7:40] = [n % 17 for n in contexts[7:40]]
+    if long:
+        contexts[100] = long
+    cache, table, q, ctx = make(paged, contexts, hq, hkv, dh, 16, kv, x, seed=41)
+    first = None
+    for _ in range(4):
+        out, lse = paged.d3_paged_attention(cache, q, table, ctx, with_lse=True)
+        if first is None:
+            first = (out, lse)
+            check(out, lse, q, cache, table, contexts)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+
+
 def test_attention_peaked_scores_and_far_tails(paged):
     """One position outweighs the rest by e^16, in every type: the tail still counts (fp16 weights of 2^-24 and below)."""
     for kv, x in ((BF16, BF16), (FP16, FP16), (E4M3, FP16), (BF16, FP32)):
