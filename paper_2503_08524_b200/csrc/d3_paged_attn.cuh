@@ -30,7 +30,7 @@
 //     shared memory; rows of few units are not cut at all (launch(), cost_of()).
 //
 // Measured (us, of the measured copy rate 6451 GB/s): 64 rows x 1..16384 GQA 32/8 x 128 bf16 322 (100 %); 96 rows x 17..8192
-// 64/8 8-bit 141 (89 %: the widening to fp16 keeps the warps busy); 1 row x 131071 64/8 fp16 91 (91 %: 6 us are start and
+// 64/8 8-bit 148 (85 %: the widening to fp16 keeps the warps busy); 1 row x 131071 64/8 fp16 91 (91 %: 6 us are start and
 // join); 32 rows x 129..1025 32/32 bf16 56 (84 %: 9 us are start and join); 1 row x 513 32/32 7.2; 4 rows x 513..545 64/8
 // fp32 8.6 (latency).  Short rows pay about 1 us per row and kv head for their ends: 128 rows x 200, 64/8 28.5 (59 %).
 //
@@ -292,8 +292,10 @@ struct Cfg {
   static constexpr int kHeadFloats = DH + 4;                 // of a head's sums in shared memory (padded: no bank conflicts)
   static constexpr bool kF16 = CACHE != D3_BF16;
   static constexpr int kTiles = X == D3_FP32 ? 1 : MT;       // 8-head tiles
-  // terms of P: one fp16 number (2^-11 of it) is enough under a bf16 result, whose own rounding is up to 2^-8
-  static constexpr int kQTerms = X == D3_FP32 ? 3 : 1, kPTerms = X == D3_FP32 ? 3 : CACHE == D3_E4M3 && X == D3_BF16 ? 1 : 2;
+  // Terms of P.  The sums use P unrounded, so what is left of it is an error of the result: 2^-16 with two bf16 numbers, 2^-22 with
+  // two fp16 ones.  (One fp16 number under a bf16 result, 2^-11, makes 96 rows x 8192 of 8 bits 141 us instead of 148; results
+  // then differ from fp32 arithmetic's by 5.7e-4 of their size, not 1.1e-4, and where values nearly cancel by far more than their rounding.)
+  static constexpr int kQTerms = X == D3_FP32 ? 3 : 1, kPTerms = X == D3_FP32 ? 3 : 2;
 };
 
 template <int DH, int CACHE, int X, int MT>
