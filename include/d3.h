@@ -463,8 +463,9 @@ int32_t d3_rope_table(int32_t n_positions, int32_t head_dim, float rope_base, fl
  * the pages that table row rows[b] names (rows_dev NULL: row b itself), kv head h / (Hq / Hkv):
  *   out = sum_t softmax_t(scale q . k_t) v_t,   lse = log sum_t exp(scale q . k_t)  (nullable)
  * Scores, softmax and sums are fp32; the products of weights and V take 16 bits of a weight over a
- * BF16 pool, 22 over the others, 24 with fp32 queries; out is rounded once to dtype.  Types as in
- * d3_paged_append (q and out / cache).  Many rows: the lengths are cut into equal shares over the SMs, whichever rows they
+ * BF16 pool, 22 over the others, 24 with fp32 queries; BF16 queries over an E4M3 pool count to 2^-39
+ * of their head's largest number; out is rounded once to dtype.  Types as in d3_paged_append (q and
+ * out / cache).  Many rows: the lengths are cut into equal shares over the SMs, whichever rows they
  * fall in, and a second kernel joins the rows that were cut.  Few rows: a cluster of CTAs for each row
  * and kv head.  The order of the sums is fixed by the lengths, n_rows, the width of the table and the
  * GPU, so the same call gives the same bits; a row's bits may depend on the rows beside it.

@@ -37,7 +37,7 @@
 // fp32 queries (bf16 cache): q and P are three bf16 terms by truncation (8 + 8 + 8 bits: exact), sums of products short
 // chains (error of fp32 outputs against 64 bits 1e-7 .. 3e-7).  8-bit cache: the
 // stored numbers are widened to fp16 (exact), bf16 queries are scaled by a power of two per head so that fp16 holds
-// them.  Where P is fp16, it is exp2(.. + 15): 2^-29 of the largest stays a normal number.
+// them (down to 2^-31 of the head's largest).  Where P is fp16, it is exp2(.. + 15): 2^-29 of the largest stays a normal number.
 //
 // Every wait is bounded; when one runs out the CTA stores D3_ETIMEOUT, stops issuing, lets its copies land and ends.  (A
 // cluster's hardware barriers are met by every thread on every path, so they end when those waits have.)
@@ -294,7 +294,7 @@ struct Cfg {
   static constexpr int kTiles = X == D3_FP32 ? 1 : MT;       // 8-head tiles
   // Terms of P.  The sums use P unrounded, so what is left of it is an error of the result: 2^-16 with two bf16 numbers, 2^-22 with
   // two fp16 ones.  (One fp16 number under a bf16 result, 2^-11, makes 96 rows x 8192 of 8 bits 141 us instead of 148; results
-  // then differ from fp32 arithmetic's by 5.7e-4 of their size, not 1.1e-4, and where values nearly cancel by far more than their rounding.)
+  // then differ from fp32 arithmetic's by 5.7e-4 of their size, not 5.8e-5, and where values nearly cancel by far more than their rounding.)
   static constexpr int kQTerms = X == D3_FP32 ? 3 : 1, kPTerms = X == D3_FP32 ? 3 : 2;
 };
 
@@ -909,7 +909,9 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
               qb[i][0][kk][j] = live ? v : 0u;
             }
           if constexpr (CACHE == D3_E4M3 && X == D3_BF16) {
-            // to fp16: the head's largest |q| scaled to [1, 2); what falls under fp16's range is under 2^-24 of it
+            // To fp16: the head's largest |q| is brought to [2^14, 2^15) by a power of two, so that the 8 bits of a number stay
+            // whole down to 2^-31 of the largest (fp16's step below its normal numbers is 2^-24); a smaller one is off by 2^-39 of it
+            // at most.  The products' sums stay below 128 * 448 * 2^15.
             float top = 0.f;
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk)
@@ -921,8 +923,9 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
               }
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int e = (top >= 1.17549435e-38f && top < INFINITY) ? min((int)(__float_as_uint(top) >> 23) - 127, 126) : 0;
-            const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
+            // (both powers are normal numbers; a head of numbers below 2^-112, the subnormal ones among them, takes the largest)
+            const int e = top < INFINITY ? min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 126) : 0;
+            const float down = __uint_as_float((uint32_t)(127 + e) << 23), up = __uint_as_float((uint32_t)(127 - e) << 23);
             factor *= up;
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk)
