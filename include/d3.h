@@ -496,6 +496,18 @@ typedef struct d3_paged_attention_args {
   int32_t *status_dev;
 } d3_paged_attention_args;
 int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args *a, void *cuda_stream);
+/* Failure detection, as d3_set_wait_ns for a model.  Every wait inside d3_paged_attention gives up after `ns`
+ * nanoseconds (default 2e9): the call stores D3_ETIMEOUT, stops issuing copies, lets the copies in flight land
+ * and ends; nothing traps, and the next call is not affected.  Process-wide, for calls made from now on (a
+ * captured call keeps the limit it was captured with).  ns >= 1. */
+int32_t d3_paged_set_wait_ns(uint64_t ns);
+/* Drill for the above: in the first CTA (of a row that a cluster shares: the second) of the next d3_paged_attention
+ * call with rows, the copies end after the first of several stages (D3_STALL_COPIES), or nobody takes what
+ * they bring (D3_STALL_SUMS), so the waits for it can only end by their limit.  0 takes a drill back.  That
+ * call's outputs are undefined.  A call whose first CTA has one stage alone passes D3_STALL_COPIES unharmed. */
+#define D3_STALL_COPIES 1
+#define D3_STALL_SUMS 2
+int32_t d3_paged_stall_next(int32_t what);
 /* Workspace bytes for any call over `kv` with n_q_heads query heads (k_dev, v_dev are not looked at). */
 int32_t d3_paged_attention_workspace(const d3_paged_kv *kv, int32_t n_q_heads, size_t *bytes);
 

@@ -30,7 +30,7 @@ EXPORTS = ("d3_depth", "d3_schedule", "d3_workspace_bytes", "d3_load", "d3_prefi
            "d3_stall_next_step", "d3_slot_pos",
            "d3_kv_pages_used", "d3_reset_slot", "d3_sync", "d3_free", "d3_strerror",
            "d3_paged_maps", "d3_page_plan", "d3_paged_append", "d3_rope_table", "d3_paged_attention",
-           "d3_paged_attention_workspace", "d3_paged_view")
+           "d3_paged_attention_workspace", "d3_paged_set_wait_ns", "d3_paged_stall_next", "d3_paged_view")
 
 
 class Config(C.Structure):
@@ -107,6 +107,8 @@ def _load() -> C.CDLL:
     lib.d3_rope_table.argtypes = [I32, I32, C.c_float, P, P]
     lib.d3_paged_attention.argtypes = [P, P, P]
     lib.d3_paged_attention_workspace.argtypes = [P, I32, C.POINTER(C.c_size_t)]
+    lib.d3_paged_set_wait_ns.argtypes = [C.c_uint64]
+    lib.d3_paged_stall_next.argtypes = [I32]
     lib.d3_paged_view.argtypes = [P, I32, P, C.POINTER(P), C.POINTER(I32), C.POINTER(I32)]
     return lib
 

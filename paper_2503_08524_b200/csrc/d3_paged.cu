@@ -442,6 +442,10 @@ bool launch_append(AppendArgs &a, int dh, cudaStream_t st) {
   return dh == 128 ? launch_append_dh<X, C, 128>(a, st) : dh == 64 ? launch_append_dh<X, C, 64>(a, st) : launch_append_dh<X, C, 32>(a, st);
 }
 
+// limit of the attention kernel's waits, and the drill of the next call
+std::atomic<unsigned long long> attention_wait_ns{2000000000ull};
+std::atomic<int> attention_stall_next{0};
+
 bool int_span_ok(const void *p, unsigned align) { return p && ((uintptr_t)p & (align - 1)) == 0; }
 
 // ------------------------------------------------------------------ tensor maps
@@ -633,6 +637,18 @@ int32_t d3_paged_attention_workspace(const d3_paged_kv *kv, int32_t n_q_heads, s
   return D3_OK;
 }
 
+int32_t d3_paged_set_wait_ns(uint64_t ns) {
+  if (ns == 0) return D3_EINVAL;
+  attention_wait_ns.store(ns, std::memory_order_relaxed);
+  return D3_OK;
+}
+
+int32_t d3_paged_stall_next(int32_t what) {
+  if (what != 0 && what != D3_STALL_COPIES && what != D3_STALL_SUMS) return D3_EINVAL;
+  attention_stall_next.store(what, std::memory_order_relaxed);
+  return D3_OK;
+}
+
 int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args *a, void *cuda_stream) {
   if (!kv_ok(kv, true) || !a || a->struct_size != sizeof(d3_paged_attention_args)) return D3_EINVAL;
   if (!types_ok(a->dtype, kv->dtype)) return D3_EINVAL;
@@ -688,7 +704,8 @@ int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args 
   p.part_o = reinterpret_cast<float *>(ws + w.part_o); p.part_ml = reinterpret_cast<float *>(ws + w.part_ml);
   p.join = reinterpret_cast<int4 *>(ws + w.join);
   p.status = a->status_dev;
-  p.wait_ns = 2000000000ull;
+  p.wait_ns = attention_wait_ns.load(std::memory_order_relaxed);
+  p.stall = attention_stall_next.load(std::memory_order_relaxed) ? attention_stall_next.exchange(0, std::memory_order_relaxed) : 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int rc = dh == 128 ? launch_paged_attention_128(*maps, p, a->dtype, st)
                  : dh == 64 ? launch_paged_attention_64(*maps, p, a->dtype, st)

@@ -102,6 +102,7 @@ struct PagedAttnArgs {
   int whole;                           // no row is cut between CTAs: no join
   int few;                             // the rows are summed up by the producer warps alone, in 32 bits
   unsigned long long wait_ns;
+  int stall;                           // drill: D3_STALL_*, 0 otherwise
 };
 // one translation unit per head dimension (each compiles every type pair)
 int launch_paged_attention_32(const PoolMaps &m, const PagedAttnArgs &a, int x, cudaStream_t st);

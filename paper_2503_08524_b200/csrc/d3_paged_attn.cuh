@@ -39,7 +39,7 @@
 // stored numbers are widened to fp16 (exact), bf16 queries are scaled by a power of two per head so that fp16 holds
 // them (down to 2^-31 of the head's largest).  Where P is fp16, it is exp2(.. + 15): 2^-29 of the largest stays a normal number.
 //
-// Every wait is bounded; when one runs out the CTA stores D3_ETIMEOUT, stops issuing, lets its copies land and ends.  (A
+// Every wait is bounded (d3_paged_set_wait_ns); when one runs out the CTA stores D3_ETIMEOUT, stops issuing, lets its copies land and ends.  (A
 // cluster's hardware barriers are met by every thread on every path, so they end when those waits have.)
 #pragma once
 
@@ -429,6 +429,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   __syncthreads();   // the barriers, and the first row where it was looked for
   if (CL) cluster_arrive();
 
+  auto stalled = [&](int what) { return a.stall == what && blockIdx.x == (CL ? 1u : 0u); };   // drill (d3_paged_stall_next)
   auto produce = [&]() {
     // ------------------------------------------------------------ producers
     const int me = warp - C::kWarps - C::kEpilogue;
@@ -595,6 +596,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     int cut_row = -1, cut_head = 0, cut_kvh = 0, cut_nh = 0;         // the item that goes on in the next CTA, if it starts here
     long long cut_last = 0;
     for (int k = 0; at < x1; ++k) {
+      if (k == 1 && stalled(D3_STALL_COPIES)) break;
       const bool ends = unit + 1 == nu;
       const long long next = ends ? item + cost.of(nu) + cost.lead : at + cost.step;
       const bool last = ends || next >= x1, final = next >= x1;
@@ -840,6 +842,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
   // -------------------------------------------------------------- consumers
   auto consume = [&]() -> int {   // how many items ended here; 0 when a wait ran out
+  if (stalled(D3_STALL_SUMS)) return 0;
   // Fragments (g = lane / 4, t = lane % 4).  Scores: A = K (rows = positions), B = Q^T (column g = head), result: positions
   // g, g + 8 of heads 2t, 2t + 1.  Sums: A = V^T (rows = dims), B = P^T, result: dims g, g + 8 of heads 2t, 2t + 1.
   const int g = lane >> 2, t = lane & 3, mat = lane >> 3;

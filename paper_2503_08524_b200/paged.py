@@ -29,6 +29,7 @@ _paged_call.bind(*[C.cast(f, C.c_void_p).value for f in (LIB.d3_page_plan, LIB.d
                                                          LIB.d3_paged_attention_workspace)], D3Error)
 
 BF16, FP16, FP32, E4M3 = 0, 1, 2, 3
+STALL_COPIES, STALL_SUMS = 1, 2
 MAX_REQUESTS, MAPS_BYTES = 4096, 640
 _TYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32, torch.float8_e4m3fn: E4M3}
 
@@ -230,6 +231,20 @@ def attention_workspace(cache: PagedKV, n_q_heads: int) -> torch.Tensor:
     if rc != OK:
         raise D3Error(rc, "d3_paged_attention_workspace")
     return torch.empty(n.value, dtype=torch.uint8, device=cache.device)
+
+
+def d3_paged_set_wait_ns(ns: int) -> None:
+    """Limit of every wait inside the d3_paged_attention calls of this process from now on (default 2e9)."""
+    rc = LIB.d3_paged_set_wait_ns(int(ns)) if int(ns) >= 0 else EINVAL
+    if rc != OK:
+        raise D3Error(rc, "d3_paged_set_wait_ns")
+
+
+def d3_paged_stall_next(what: int) -> None:
+    """Drill: a wait of the next d3_paged_attention call cannot be satisfied (STALL_COPIES, STALL_SUMS; 0: none)."""
+    rc = LIB.d3_paged_stall_next(int(what))
+    if rc != OK:
+        raise D3Error(rc, "d3_paged_stall_next")
 
 
 def d3_paged_attention(cache: PagedKV, q: torch.Tensor, table: torch.Tensor, context: torch.Tensor, *,
