@@ -684,7 +684,6 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     for (int it = i0;; ++it) {
       const int at = it & (kItems - 1), me = CL ? warp : helps ? warp + C::kEpilogue : (warp - C::kWarps + it) & (C::kEpilogue - 1);   // (single heads in turn)
       if (!__all_sync(0xffffffffu, mb_wait(smem_u32(&s_sums_full[at]), (uint32_t)(it / kItems) & 1u, &s_abort, a.wait_ns))) { gave_up(); break; }
-      if (it == i0) pdl_wait();   // returns at once: the producers' has
       const ItemInfo item = s_item[at];
       const int kind = item.bits & 3, nh = (item.bits >> 3) & 31, first_warp = (item.bits >> 8) & 255, warps = (item.bits >> 16) & 255;
       const int workers = item.bits & 4 ? C::kWarps + C::kEpilogue : C::kEpilogue;
@@ -879,7 +878,6 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const int n = info.bits & 511;
     more = !(flags & STAGE_FINAL);
     if (flags & STAGE_FIRST) {
-      if (items == 0) pdl_wait();   // returns at once: the producers' has
       // ---- this thread's fragments of Q, and what a raw score is multiplied by
       const int nh = (info.bits >> 14) & 31;
       first_warp = piece_turn; item_pieces = 0;
@@ -1162,6 +1160,7 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   if (warp >= C::kWarps + C::kEpilogue) {
     produce();
   } else {
+    pdl_wait();   // (before the first wait with a limit, which the kernel before this one must not use up)
     const int items = warp < NW ? consume() : 1;
     if (items > 0) epilogue(items - 1);
   }

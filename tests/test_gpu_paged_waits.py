@@ -53,3 +53,36 @@ def test_attention_waits_that_run_out_are_reported(paged, limit, dealt, what, kv
     paged.d3_paged_stall_next(0)                       # taken back
     again = call()
     assert int(status) == 0 and torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("dealt", ["cluster", "whole", "cut, few rows"])
+def test_attention_waits_do_not_count_the_call_before(paged, limit, dealt):
+    """The limit is that of the call's own waits: a call may start its CTAs while the one before it, some milliseconds long, runs."""
+    contexts, hq, hkv, width = DEALT[dealt]
+    cache, table, q, ctx = make(paged, contexts, hq, hkv, 128, 16, BF16, BF16, seed=19)
+    if width:
+        wide = torch.full((len(contexts), width), -1, dtype=torch.int32, device=DEV)
+        wide[:, :table.shape[1]] = table
+        table = wide
+    ws, status = paged.attention_workspace(cache, hq), torch.zeros(1, dtype=torch.int32, device=DEV)
+    call = lambda: paged.d3_paged_attention(cache, q, table, ctx, with_lse=True, workspace=ws, status=status)  # noqa: E731
+    out, lse = call()
+    # long and on one multiprocessor: a plan in which all of 100 long requests end
+    pages = 16384
+    i32 = dict(dtype=torch.int32, device=DEV)
+    plan = paged.PagePlan(cached=torch.full((100,), 16 * pages, **i32), new_tokens=torch.full((100,), -1, **i32),
+                          table=torch.arange(100 * pages, **i32).view(100, pages), free=torch.zeros(100 * pages, **i32),
+                          n_free=torch.zeros(1, **i32), page_size=16, max_tokens=8, cached_out=torch.zeros(100, **i32),
+                          n_free_out=torch.zeros(1, **i32))
+    plan.d3_page_plan()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    plan.d3_page_plan()
+    end.record()
+    torch.cuda.synchronize()
+    limit(500_000)
+    assert int(plan.status) == 0 and begin.elapsed_time(end) > 2.0      # much longer than the limit
+    plan.d3_page_plan()
+    again = call()
+    torch.cuda.synchronize()
+    assert int(status) == 0 and torch.equal(again[0], out) and torch.equal(again[1], lse)
