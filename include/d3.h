@@ -408,7 +408,9 @@ int32_t d3_paged_maps(const d3_paged_kv *kv, void *maps);
  * All or nothing: with too few free pages, a request longer than table_width pages, more tokens than
  * max_tokens (D3_ECAPACITY), or cached, n_free or the count of pages given back out of range
  * (D3_EINVAL), status_dev gets the code, table, stack and lengths stay, and every map entry is
- * padding.  A token whose page id is not in [0, n_pages) gets slot -1, and D3_EINVAL is stored. */
+ * padding.  A token whose page id is not in [0, n_pages) gets slot -1, and D3_EINVAL is stored; so it is
+ * when such an id comes back with an ended request's pages (it goes on the stack like the others, which
+ * keep their order, and the tokens of a request that gets it have no slots). */
 typedef struct d3_page_plan_args {
   uint32_t struct_size;
   int32_t n_requests;        /* 1..D3_MAX_REQUESTS                                       */

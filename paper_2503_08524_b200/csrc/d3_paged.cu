@@ -174,7 +174,9 @@ __global__ void __launch_bounds__(kPlanMaxThreads) k_page_plan(const __grid_cons
   for (long long at = gid; at < n_all; at += step) {
     if (at < n_back) {
       const int e = (int)at, b = owner(s_back, a.R, e);
-      a.free_pages[n_free + e] = a.table[b * a.table_stride + (e - s_back[b])];
+      const int id = a.table[b * a.table_stride + (e - s_back[b])];
+      if (id < 0 || id >= a.n_pages) strange = true;
+      a.free_pages[n_free + e] = id;
       continue;
     }
     if (at < (long long)n_back + n_need) {
