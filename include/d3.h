@@ -363,7 +363,10 @@ const char *d3_strerror(int32_t code);
  * still until it ends (order it behind what writes its tensors, on another stream too); its results
  * are undefined otherwise.  Rows of one output (and of a
  * pool that is appended to) must not overlap: D3_EINVAL, so is a stride that does not reach over what
- * the smaller strides span.  Nothing here is differentiable. */
+ * the smaller strides span.  What a call writes overlaps nothing else that it reads or writes, but for
+ * what is said to be allowed: D3_EINVAL for the buffers of a plan, the K and V of a pool that is appended
+ * to, and a q_out that meets a q of its own strides elsewhere than at the same numbers.  Nothing here is
+ * differentiable. */
 #define D3_BF16 0
 #define D3_FP16 1
 #define D3_FP32 2

@@ -450,6 +450,26 @@ std::atomic<int> attention_stall_next{0};
 
 bool int_span_ok(const void *p, unsigned align) { return p && ((uintptr_t)p & (align - 1)) == 0; }
 
+// What a plan reads and writes: the table's rows, `width` of every `stride` entries, and vectors.
+struct Span { uintptr_t at; size_t bytes; bool written; };
+// Nothing that is written overlaps anything else, the table's rows included: CTAs read and write side by side.  cached_out and
+// n_free_out may be what they replace, to the entry (in the vectors' order below: 0 and 1, 2 and 3).
+bool plan_apart(const Span (&v)[11], uintptr_t table, int rows, size_t width_bytes, size_t stride_bytes) {
+  for (int i = 0; i < 11; ++i) {
+    if (!v[i].at) continue;
+    for (int j = i + 1; j < 11; ++j) {
+      if (!v[j].at || (!v[i].written && !v[j].written)) continue;
+      if (v[i].at < v[j].at + v[j].bytes && v[j].at < v[i].at + v[i].bytes && !((i == 0 || i == 2) && j == i + 1 && v[i].at == v[j].at)) return false;
+    }
+    // the first row that ends behind the vector's start must start behind its end
+    if (v[i].at + v[i].bytes <= table) continue;
+    const size_t from = v[i].at > table ? v[i].at - table : 0;
+    const size_t row = from < width_bytes ? 0 : (from - width_bytes) / stride_bytes + 1;
+    if (row < (size_t)rows && table + row * stride_bytes < v[i].at + v[i].bytes) return false;
+  }
+  return true;
+}
+
 // ------------------------------------------------------------------ tensor maps
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
@@ -533,6 +553,13 @@ int32_t d3_page_plan(const d3_page_plan_args *a, void *cuda_stream) {
       !int_span_ok(a->n_free_out_dev, 4) || !int_span_ok(a->first_dev, 4) || !int_span_ok(a->slots_dev, 16) ||
       !int_span_ok(a->row_dev, 16) || !int_span_ok(a->context_dev, 16) || ((uintptr_t)a->status_dev & 3))
     return D3_EINVAL;
+  const size_t R4 = (size_t)a->n_requests * 4, T4 = (size_t)a->max_tokens * 4;
+  const Span spans[11] = {{(uintptr_t)a->cached_dev, R4, false}, {(uintptr_t)a->cached_out_dev, R4, true},
+                          {(uintptr_t)a->n_free_dev, 4, false}, {(uintptr_t)a->n_free_out_dev, 4, true},
+                          {(uintptr_t)a->new_tokens_dev, R4, false}, {(uintptr_t)a->free_dev, (size_t)a->n_pages * 4, true},
+                          {(uintptr_t)a->first_dev, R4 + 4, true}, {(uintptr_t)a->slots_dev, 2 * T4, true},
+                          {(uintptr_t)a->row_dev, T4, true}, {(uintptr_t)a->context_dev, T4, true}, {(uintptr_t)a->status_dev, 4, true}};
+  if (!plan_apart(spans, (uintptr_t)a->table_dev, a->n_requests, (size_t)a->table_width * 4, (size_t)a->table_stride * 4)) return D3_EINVAL;
   PlanArgs p;
   p.R = a->n_requests; p.page_shift = log2_of(a->page_size); p.n_pages = a->n_pages; p.width = a->table_width;
   p.T = a->max_tokens; p.table_stride = a->table_stride;
@@ -594,6 +621,15 @@ int32_t d3_paged_append(const d3_paged_kv *kv, const d3_paged_append_args *a, vo
       return D3_EINVAL;
   }
   if (a->n_tokens == 0) return D3_OK;
+  const int es = bytes_of(kv->dtype);
+  if (rows_meet(dh, ((intptr_t)kv->v_dev - (intptr_t)kv->k_dev) / es, kv->n_pages, kv->page_stride, kv->n_kv_heads, kv->head_stride, kv->page_size,
+                kv->token_stride))
+    return D3_EINVAL;
+  // q_out may be q itself, or lie beside it
+  if (a->q_dev && a->q_dev != a->q_out_dev && (a->n_tokens == 1 || a->q_token_stride == a->q_out_token_stride) &&
+      (a->n_q_heads == 1 || a->q_head_stride == a->q_out_head_stride) &&
+      rows_meet(dh, ((intptr_t)a->q_out_dev - (intptr_t)a->q_dev) / xs, a->n_tokens, a->q_out_token_stride, a->n_q_heads, a->q_out_head_stride))
+    return D3_EINVAL;
   AppendArgs p;
   memset(&p, 0, sizeof(p));
   p.n_tokens = a->n_tokens; p.rope_len = a->rope_len;

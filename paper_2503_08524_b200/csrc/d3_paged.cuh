@@ -41,6 +41,23 @@ inline bool rows_apart(int dh, int64_t n0, int64_t s0, int64_t n1, int64_t s1, i
   }
   return true;
 }
+// Two such sets of rows, with the same counts and strides (which keep the rows of either apart) and `delta` numbers between their
+// bases, have a number in common: delta is a sum of multiples of the strides, within the counts, and less than a row.  Each
+// stride reaches over what the smaller ones span, so only the two multiples next to what is left can be meant.
+inline bool rows_meet(int dh, int64_t delta, int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2 = 1, int64_t s2 = 0) {
+  int64_t n[3] = {n0, n1, n2}, s[3] = {s0, s1, s2};
+  int at = -1;
+  for (int i = 0; i < 3; ++i)
+    if (n[i] > 1 && (at < 0 || s[i] > s[at])) at = i;
+  if (at < 0) return delta > -dh && delta < dh;
+  const int64_t count = n[at], stride = s[at];
+  n[at] = 1;
+  int64_t q = delta / stride;
+  if (q * stride > delta) --q;
+  for (int i = 0; i < 2; ++i, ++q)
+    if (q > -count && q < count && rows_meet(dh, delta - q * stride, n[0], s[0], n[1], s[1], n[2], s[2])) return true;
+  return false;
+}
 // (type of q, k, v as given, type of the cache) pairs that the operators serve
 inline bool types_ok(int x, int cache) {
   return (cache == D3_BF16 && (x == D3_BF16 || x == D3_FP32)) || (cache == D3_FP16 && x == D3_FP16) ||
