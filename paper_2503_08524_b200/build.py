@@ -1,18 +1,19 @@
 """Builds libd3.so (the CUDA library behind the C ABI of include/d3.h) in-tree
-with nvcc for sm_100a, and _paged_call.so (the Python side of the paged operators'
+with nvcc for sm_100a, and _paged_call.*.so (the Python side of the paged operators'
 calls, csrc/paged_call.cpp) with g++.  No GPU is needed to build."""
 from __future__ import annotations
 
 import glob
 import os
+import re
 import subprocess
 import sys
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libd3.so")
-CALL = os.path.join(PKG, "_paged_call.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
@@ -65,25 +66,50 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def call_path() -> str:
+    """Where the extension module lies: it reads torch's objects, so its name says what it was built for."""
+    import torch
+    made_for = "-".join((sys.implementation.cache_tag, "torch" + torch.__version__, "cxx11abi%d" % torch._C._GLIBCXX_USE_CXX11_ABI))
+    return os.path.join(PKG, "_paged_call." + re.sub(r"[^0-9A-Za-z-]", "_", made_for) + ".so")
+
+
 def build_call(force: bool = False) -> str:
     """Compile and link the extension module that makes the paged operators' calls; returns its path."""
     src, header = os.path.join(CSRC, "paged_call.cpp"), os.path.join(ROOT, "include", "d3.h")
-    if not force and os.path.exists(CALL) and os.path.getmtime(CALL) > max(os.path.getmtime(src), os.path.getmtime(header)):
-        return CALL
+    out = call_path()
+    if not force and os.path.exists(out) and os.path.getmtime(out) > max(os.path.getmtime(src), os.path.getmtime(header)):
+        return out
     import sysconfig
 
     import torch
     base = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(NVCC))
+    # a file of this process's own until it is whole: ranks that import a fresh checkout build it side by side
+    handle, made = tempfile.mkstemp(dir=os.path.dirname(out), prefix="_paged_call.", suffix=".new")
+    os.close(handle)
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(base, "include"),
-           "-I", os.path.join(base, "include", "torch", "csrc", "api", "include"), "-I", os.path.join(cuda, "include"), src, "-o", CALL + ".new",
+           "-I", os.path.join(base, "include", "torch", "csrc", "api", "include"), "-I", os.path.join(cuda, "include"), src, "-o", made,
            "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("g++ failed on " + src + ":\n" + res.stdout + res.stderr)
-    os.replace(CALL + ".new", CALL)
-    return CALL
+    try:
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("g++ failed on " + src + ":\n" + res.stdout + res.stderr)
+        os.chmod(made, 0o755)      # (mkstemp's files are the owner's alone)
+        os.replace(made, out)
+    finally:
+        if os.path.exists(made):
+            os.remove(made)
+    return out
+
+
+def load_call():
+    """The extension module, built if need be."""
+    import importlib.util
+    spec = importlib.util.spec_from_file_location(__package__ + "._paged_call", build_call())
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
 
 
 if __name__ == "__main__":

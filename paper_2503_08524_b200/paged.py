@@ -22,9 +22,7 @@ import torch
 from . import build as _build
 from .binding import EINVAL, LIB, OK, D3Error
 
-_build.build_call()
-from . import _paged_call  # noqa: E402
-
+_paged_call = _build.load_call()
 _paged_call.bind(*[C.cast(f, C.c_void_p).value for f in (LIB.d3_page_plan, LIB.d3_paged_append, LIB.d3_paged_attention,
                                                          LIB.d3_paged_attention_workspace)], D3Error)
 
