@@ -73,38 +73,47 @@ std::string shape_text(const char *name, int64_t n, int64_t heads, int64_t dh) {
          "] of the call's type and device, last dimension contiguous";
 }
 
+// Counts a tensor that the call writes as changed in place: a graph that saved it refuses its backward pass instead of
+// computing with other numbers.  (Tensors of inference mode have no count.)
+void changed(const at::Tensor &t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 bool number(PyObject *o, long long &v) {
   v = PyLong_AsLongLong(o);
   return !(v == -1 && PyErr_Occurred());
 }
 
-// plan(address of the arguments, device)
+// plan(address of the arguments, device, tuple of the tensors written)
 PyObject *plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   long long at, device;
-  if (n != 2) return refuse("d3_page_plan", "2 arguments");
+  if (n != 3 || !PyTuple_Check(a[2])) return refuse("d3_page_plan", "3 arguments");
   if (!number(a[0], at) || !number(a[1], device)) return nullptr;
   if (device < 0) return refuse("d3_page_plan", "tensors must be on a CUDA device");
   const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
   const int rc = plan_call(reinterpret_cast<const d3_page_plan_args *>(at), c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream());
   if (rc != D3_OK) return fail(rc, "d3_page_plan");
+  for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[2]); ++i)
+    if (THPVariable_Check(PyTuple_GET_ITEM(a[2], i))) changed(THPVariable_Unpack(PyTuple_GET_ITEM(a[2], i)));
   Py_RETURN_NONE;
   END_HANDLE_TH_ERRORS
 }
 
-// append(pool, device, k, v, slots, q, q_out, rope, context, status) -> q_out
+// append(pool, device, k, v, slots, q, q_out, rope, context, status, the pool's K, its V) -> q_out
 PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t argc) {
   HANDLE_TH_ERRORS
   static const char *call = "d3_paged_append";
   long long pool, dev;
-  if (argc != 10) return refuse(call, "10 arguments");
+  if (argc != 12) return refuse(call, "12 arguments");
   if (!number(a[0], pool) || !number(a[1], dev)) return nullptr;
   const d3_paged_kv *kv = reinterpret_cast<const d3_paged_kv *>(pool);
   const int device = (int)dev;
   bool ok = true;
   const at::Tensor *k = tensor(a[2], ok), *v = tensor(a[3], ok), *slots = tensor(a[4], ok), *q = tensor(a[5], ok), *q_out = tensor(a[6], ok),
-                   *rope = tensor(a[7], ok), *context = tensor(a[8], ok), *status = tensor(a[9], ok);
-  if (!ok || !k || !v || !slots) return refuse(call, "k, v and slots must be tensors, the others tensors or None");
+                   *rope = tensor(a[7], ok), *context = tensor(a[8], ok), *status = tensor(a[9], ok), *pool_k = tensor(a[10], ok),
+                   *pool_v = tensor(a[11], ok);
+  if (!ok || !k || !v || !slots || !pool_k || !pool_v) return refuse(call, "k, v and slots must be tensors, the others tensors or None");
   const int code = code_of(k->scalar_type());
   if (code < 0) return refuse(call, "unsupported type");
   if (slots->dim() != 1 || !is_vector(*slots, at::kLong, slots->size(0), device)) return refuse(call, "slots must be a contiguous int64 vector");
@@ -155,6 +164,9 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t argc) {
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
     const int rc = append_call(kv, &args, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream());
     if (rc != D3_OK) return fail(rc, call);
+    changed(*pool_k);
+    changed(*pool_v);
+    if (q_out) changed(*q_out);
   }
   if (fresh.defined()) return THPVariable_Wrap(fresh);
   Py_INCREF(a[6]);
@@ -243,6 +255,8 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t argc) {
   if (n > 0) {
     const int rc = attention_call(kv, &args, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream());
     if (rc != D3_OK) return fail(rc, call);
+    if (out) changed(*out);
+    if (lse) changed(*lse);
   }
   PyObject *o = new_out.defined() ? THPVariable_Wrap(new_out) : a[7];
   if (!o) return nullptr;

@@ -4,7 +4,7 @@ lengths, append with rotary positions, attention of one new token per row.
 Marshalling only, like `binding`: tensors in, one C call, no host synchronisation; the calls can be
 captured into a CUDA graph.  The checks of each call are in csrc/paged_call.cpp (a small decode step is
 bound by the host side of its calls).  They run on the current stream of the tensors' device unless `stream`
-is given.  Results carry no gradient.  A refused call raises D3Error (EINVAL) before anything is enqueued; what only the device
+is given.  Results carry no gradient; what a call writes into counts as changed in place.  A refused call raises D3Error (EINVAL) before anything is enqueued; what only the device
 can see (a page id out of range, too few free pages) goes to the `status` tensor.
 
     plan = PagePlan(cached=..., new_tokens=..., table=..., free=..., n_free=..., page_size=..., max_tokens=...)
@@ -181,11 +181,12 @@ class PagePlan:
             _vector(self.n_free_out, i32, 1, index, what, "n_free_out"), self.first.data_ptr(), self.slots.data_ptr(),
             self.row.data_ptr(), self.context.data_ptr(), _vector(self.status, i32, 1, index, what, "status"))
         self._at = C.addressof(self.args)
+        self._written = (table, free, self.cached_out, self.n_free_out, self.slots, self.row, self.context, self.first)
 
     def d3_page_plan(self, stream=None) -> "PagePlan":
         if stream is not None:
             return _on_stream(self.d3_page_plan, self.index, stream, "d3_page_plan")
-        _paged_call.plan(self._at, self.index)
+        _paged_call.plan(self._at, self.index, self._written)
         return self
 
 
@@ -219,7 +220,7 @@ def d3_paged_append(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, slots: tor
     if stream is not None:
         return _on_stream(lambda: d3_paged_append(cache, k, v, slots, q=q, q_out=q_out, rope=rope, context=context, status=status),
                           cache.index, stream, "d3_paged_append")
-    return _paged_call.append(cache._at, cache.index, k, v, slots, q, q_out, rope, context, status)
+    return _paged_call.append(cache._at, cache.index, k, v, slots, q, q_out, rope, context, status, cache.k, cache.v)
 
 
 def attention_workspace(cache: PagedKV, n_q_heads: int) -> torch.Tensor:
