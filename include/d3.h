@@ -475,8 +475,10 @@ int32_t d3_rope_table(int32_t n_positions, int32_t head_dim, float rope_base, fl
  * and kv head.  The order of the sums is fixed by the lengths, n_rows, the width of the table and the
  * GPU, so the same call gives the same bits; a row's bits may depend on the rows beside it.
  * context 0: out = 0, lse = -inf.  rows[b] = -1: padding, the row's outputs stay as they are.  What
- * the pages hold behind the context is never used, NaN included.  Non-finite numbers inside it make the
- * results of their heads non-finite, an infinity possibly a NaN.  Out-of-range data stores D3_EINVAL:
+ * the pages hold behind the context is never used, NaN included.  Inside it, a score of NaN or +inf makes
+ * out and lse of its head NaN; a score of -inf has no weight, and a head that has no other scores is as
+ * one without context (with fp32 queries either head may be NaN); a NaN or infinity of V makes its dim
+ * NaN or infinite, whatever its weight, and no other.  Out-of-range data stores D3_EINVAL:
  * a context beyond table_width pages (or negative) counts as 0, another bad rows[b] as padding, and
  * the positions of a bad page id are left out.  status_dev also gets D3_ETIMEOUT when a bounded wait ran out (out and
  * lse are then undefined).  workspace_dev: d3_paged_attention_workspace bytes, 256-byte aligned,
