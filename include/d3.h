@@ -509,9 +509,10 @@ int32_t d3_paged_attention(const d3_paged_kv *kv, const d3_paged_attention_args 
  * captured call keeps the limit it was captured with).  ns >= 1. */
 int32_t d3_paged_set_wait_ns(uint64_t ns);
 /* Drill for the above: in the first CTA (of a row that a cluster shares: the second) of the next d3_paged_attention
- * call with rows, the copies end after the first of several stages (D3_STALL_COPIES), or nobody takes what
- * they bring (D3_STALL_SUMS), so the waits for it can only end by their limit.  0 takes a drill back.  That
- * call's outputs are undefined.  A call whose first CTA has one stage alone passes D3_STALL_COPIES unharmed. */
+ * call with rows, one arrival more is expected than comes for every stage of copies (D3_STALL_COPIES), or for
+ * every stage that is given back and every row's sums (D3_STALL_SUMS), so the waits for them can only end by
+ * their limit (set a short one first: the copies that landed are waited for too, one after another).  0 takes
+ * a drill back.  That call's outputs are undefined. */
 #define D3_STALL_COPIES 1
 #define D3_STALL_SUMS 2
 int32_t d3_paged_stall_next(int32_t what);

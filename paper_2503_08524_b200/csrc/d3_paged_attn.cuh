@@ -328,14 +328,17 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   float *s_j = s_o + (size_t)NW * a.heads_per_tile * C::kHeadFloats;   // cluster: [CTA][head][kHeadFloats], (m, l) behind the sums
 
   if (warp == 0) {
+    // Drills (d3_paged_stall_next) are in the barriers alone: they expect one arrival more than there will be, so none of them
+    // ends a phase.  (As tests in the loops of producers and consumers drills cost 64 rows x 16384 2.5 %.)
+    const int drill = blockIdx.x == (CL ? 1u : 0u) ? a.stall : 0, extra = drill == D3_STALL_SUMS ? 1 : 0;
     if (lane < S) {
-      mb_init(smem_u32(&s_full[lane]), 1);
-      mb_init(smem_u32(&s_empty[lane]), NW);
+      mb_init(smem_u32(&s_full[lane]), drill == D3_STALL_COPIES ? 2 : 1);
+      mb_init(smem_u32(&s_empty[lane]), NW + extra);
     }
     if (lane < C::kWarps + C::kEpilogue && CL) mb_init(smem_u32(&s_joined[lane]), CL - 1);
     if (lane < C::kWarps && !CL) mb_init(smem_u32(&s_own[lane]), C::kEpilogue);
     if (lane >= 32 - kItems) {
-      mb_init(smem_u32(&s_sums_full[lane & (kItems - 1)]), NW);
+      mb_init(smem_u32(&s_sums_full[lane & (kItems - 1)]), NW + extra);
       mb_init(smem_u32(&s_sums_free[lane & (kItems - 1)]), C::kEpilogue);
     }
     if (lane == 31) {
@@ -429,7 +432,6 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   __syncthreads();   // the barriers, and the first row where it was looked for
   if (CL) cluster_arrive();
 
-  auto stalled = [&](int what) { return a.stall == what && blockIdx.x == (CL ? 1u : 0u); };   // drill (d3_paged_stall_next)
   auto produce = [&]() {
     // ------------------------------------------------------------ producers
     const int me = warp - C::kWarps - C::kEpilogue;
@@ -596,7 +598,6 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     int cut_row = -1, cut_head = 0, cut_kvh = 0, cut_nh = 0;         // the item that goes on in the next CTA, if it starts here
     long long cut_last = 0;
     for (int k = 0; at < x1; ++k) {
-      if (k == 1 && stalled(D3_STALL_COPIES)) break;
       const bool ends = unit + 1 == nu;
       const long long next = ends ? item + cost.of(nu) + cost.lead : at + cost.step;
       const bool last = ends || next >= x1, final = next >= x1;
@@ -841,7 +842,6 @@ k_paged_attention(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
   // -------------------------------------------------------------- consumers
   auto consume = [&]() -> int {   // how many items ended here; 0 when a wait ran out
-  if (stalled(D3_STALL_SUMS)) return 0;
   // Fragments (g = lane / 4, t = lane % 4).  Scores: A = K (rows = positions), B = Q^T (column g = head), result: positions
   // g, g + 8 of heads 2t, 2t + 1.  Sums: A = V^T (rows = dims), B = P^T, result: dims g, g + 8 of heads 2t, 2t + 1.
   const int g = lane >> 2, t = lane & 3, mat = lane >> 3;
