@@ -20,19 +20,21 @@
 //     swizzled stage by ldmatrix as they lie there, no row is wasted on G <= 8 heads, and 8 heads x 128 dims of O take 32
 //     registers.  P is used as two terms, P - round(P) in a second product: 16 (bf16) or 22 (fp16) bits of it count.
 //     tcgen05.mma would need P, a few hundred numbers, written to shared memory and results fetched from tensor memory
-//     for every piece; the legacy pipe is a quarter busy here;
+//     for every piece; the legacy pipe is 14 to 25 % busy here;
 //   * epilogue warps add the consumers' (m, l, O) up at the end of a row, while the consumers go on with the next row.  They are
 //     latency-bound: four of them beside ten consumers (two beside twelve: 512 rows x 100, 32/8 heads 72 us, now 57; 64 rows
-//     x 16384 329, now 322; 8-bit 64 x 4096, 32/8 102, now 99, but 96 x 8192, 64/8 140.5, now 141.4).
+//     x 16384 329, now 322; with one term of an 8-bit weight, 64 x 4096, 32/8 102, then 99, but 96 x 8192, 64/8 140.5, then 141.4).
 //     Rows that lie inside a CTA are written at once; of a row that is cut every CTA leaves (m, l, O) of its piece and
 //     k_paged_join adds them up in the order of the CTAs: bits depend on the lengths alone, no atomics.
 //   * few rows are latency: each (row, kv head) gets a cluster of CTAs that add their pieces up through distributed
 //     shared memory; rows of few units are not cut at all (launch(), cost_of()).
 //
-// Measured (us, of the measured copy rate 6451 GB/s): 64 rows x 1..16384 GQA 32/8 x 128 bf16 322 (100 %); 96 rows x 17..8192
-// 64/8 8-bit 148 (85 %: the widening to fp16 keeps the warps busy); 1 row x 131071 64/8 fp16 91 (91 %: 6 us are start and
-// join); 32 rows x 129..1025 32/32 bf16 56 (84 %: 9 us are start and join); 1 row x 513 32/32 7.2; 4 rows x 513..545 64/8
-// fp32 8.6 (latency).  Short rows pay about 1 us per row and kv head for their ends: 128 rows x 200, 64/8 28.5 (59 %).
+// Measured (us in short replays, of the measured copy rate 6451 GB/s): 64 rows x 1..16384 GQA 32/8 x 128 bf16 321
+// (100 %); 96 rows x 17..8192 64/8 8-bit 148 (85 %: the widening to fp16 and two terms of a weight keep the warps busy); 1 row x 131071
+// 64/8 fp16 90 (92 %: 6 us are start and join); 32 rows x 129..1025 32/32 bf16 56 (84 %: 9 us are start and join); 1 row x 513 32/32 7.2;
+// 4 rows x 513..545 64/8 fp32 8.5 (latency).  In a loop of a second the GPU's power cap makes the first 331 to 359 and the second 157 to
+// 164.  Few rows over a table with room for 8192 positions or more are cut and joined instead of shared by clusters: 11.1 and 13.9.
+// Short rows pay about 1 us per row and kv head for their ends: 128 rows x 200, 64/8 27 (63 %), 128 x 64 15.9 (37 %; pages of 64).
 //
 // fp32 queries (bf16 cache): q and P are three bf16 terms by truncation (8 + 8 + 8 bits: exact), sums of products short
 // chains (error of fp32 outputs against 64 bits 1e-7 .. 3e-7).  8-bit cache: the
@@ -1334,6 +1336,7 @@ int launch(const PoolMaps &m, PagedAttnArgs a, cudaStream_t st) {
     const long long longest = cl >= 2 ? (most + cl - 1) / cl : 0;
     if (cl >= 2 && longest <= 24 && longest <= items * most / n + 9) a.cluster = cl;
   }
+  // (All of this is for tables no wider than the lengths need: the host knows no other bound of them.)
   // Otherwise items stay whole whatever the lengths, and no join is launched, where the table has room for 10 units a row at
   // most: the busiest CTA is at most one row longer than an even share (40 kv heads, 8 rows of 512 positions: 20.9 us whole,
   // 22.7 cut); 16 units where every item has a CTA for itself (32 kv heads, 4 rows of 768: 13.1 us without the join, 15.9 with it).

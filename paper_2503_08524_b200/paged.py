@@ -251,8 +251,8 @@ def d3_paged_attention(cache: PagedKV, q: torch.Tensor, table: torch.Tensor, con
                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, with_lse: bool = False,
                        workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
     """q [n][n_q_heads][head_dim] over the first context[b] positions of the pages that
-    table[rows[b] or b] names (see include/d3.h).  scale: default head_dim^-0.5.  Returns out, or
-    (out, lse) with `with_lse` or an `lse` tensor (fp32 [n][n_q_heads]).  Without `workspace` one is allocated for the
+    table[rows[b] or b] names (see include/d3.h).  scale: default head_dim^-0.5.  Returns out (default: a new
+    tensor whose padding rows are undefined), or (out, lse) with `with_lse` or an `lse` tensor (fp32 [n][n_q_heads]).  Without `workspace` one is allocated for the
     call."""
     if stream is not None:
         return _on_stream(lambda: d3_paged_attention(cache, q, table, context, rows=rows, scale=scale, out=out, lse=lse,
