@@ -512,7 +512,7 @@ int32_t d3_paged_set_wait_ns(uint64_t ns);
  * call with rows, one arrival more is expected than comes for every stage of copies (D3_STALL_COPIES), or for
  * every stage that is given back and every row's sums (D3_STALL_SUMS), so the waits for them can only end by
  * their limit (set a short one first: the copies that landed are waited for too, one after another).  0 takes
- * a drill back.  That call's outputs are undefined. */
+ * a drill back.  That call's outputs are undefined; if it is captured, every replay of it stalls. */
 #define D3_STALL_COPIES 1
 #define D3_STALL_SUMS 2
 int32_t d3_paged_stall_next(int32_t what);
