@@ -526,6 +526,112 @@ int32_t d3_paged_attention_workspace(const d3_paged_kv *kv, int32_t n_q_heads, s
 int32_t d3_paged_view(const d3_model *m, int32_t layer, d3_paged_kv *kv, const int32_t **table_dev,
                       int32_t *table_rows, int32_t *table_width);
 
+/* ---------------------------------------------------------------- 8-bit block operators
+ *
+ * The weight side of a decode or prompt step as operators of its own, for the caller that runs a block itself with the
+ * paged operators above, and what stands between its logits and a token:
+ *   d3_add_norm          residual sum, RMSNorm, the result in 8 bits with a scale per 128 numbers (or in a wider type)
+ *   d3_matmul8           rows in 8 bits times a weight matrix in 8 bits with a scale per block of 128 x 128
+ *   d3_gated_matmul8     silu(gate) * up of two such products, again in 8 bits with scales (or in a wider type)
+ *   d3_constrain_logits  penalties for repeated tokens, biases, a grammar's mask, and the best token that is left
+ *   d3_quantize_weight   a weight matrix to 8 bits, once
+ * The common rules of the paged operators hold (streams, host checks, status_dev, tensors that hold still, rows of an
+ * output apart, what is written overlaps nothing else but for what is said to be allowed).  No call needs a workspace,
+ * and all can be captured into a graph.  A row's result depends on that row and the weight alone, but its last bits also
+ * on n_rows (the order of the sums is fixed by the sizes and the GPU); the same call gives the same bits.
+ *
+ * Numbers in 8 bits: D3_E4M3 q[row][k] with fp32 scale[row][k / 128] (rows of activations) or
+ * scale[row / 128][k / 128] (weights); the value is q times its scale.  A scale that these calls write is
+ * max(largest absolute value of its block, 2^-100) / 448; NaN or infinite where the block holds a NaN or an infinity,
+ * which makes what is computed from that block NaN.  Rounding to 8 bits is to nearest even. */
+
+/* y[row] = s / sqrt(mean(s^2) + eps) * gain with s = x + add, fp32 throughout (s is not rounded in between);
+ * total = s in add's type.  gain_dev NULL: no norm, y = s.  Rows are `dim` contiguous numbers, strides in elements. */
+typedef struct d3_add_norm_args {
+  uint32_t struct_size;
+  int32_t n_rows;            /* >= 0                                                     */
+  int32_t dim;               /* a multiple of 8, 8..65536                                */
+  int32_t x_dtype;           /* D3_BF16, D3_FP16, D3_FP32                                */
+  int32_t add_dtype;         /* of add and total: the same or D3_FP32                    */
+  int32_t gain_dtype;        /* D3_BF16, D3_FP16, D3_FP32                                */
+  int32_t out_dtype;         /* D3_E4M3, D3_BF16, D3_FP16, D3_FP32                       */
+  float eps;                 /* >= 0, finite                                             */
+  const void *x_dev;         /* bases and strides in bytes: multiples of 16 (out in 8 bits: of 8) */
+  const void *add_dev;       /* nullable                                                 */
+  void *total_dev;           /* nullable; only with add_dev, which it may be; or x       */
+  const void *gain_dev;      /* nullable, [dim]                                          */
+  void *out_dev;             /* may be x, of the same type and stride                    */
+  float *scale_dev;          /* D3_E4M3: [n_rows][ceil(dim / 128)]                       */
+  int64_t x_stride, add_stride, total_stride, out_stride, scale_stride;
+} d3_add_norm_args;
+int32_t d3_add_norm(const d3_add_norm_args *a, void *cuda_stream);
+
+/* A weight matrix [n][k] in 8 bits (k contiguous: W of y = W x) with its scales. */
+typedef struct d3_weight8 {
+  uint32_t struct_size;
+  int32_t n, k;              /* k a multiple of 16                                       */
+  int64_t row_stride;        /* in bytes, a multiple of 16, >= k                         */
+  const void *q_dev;         /* 16-byte aligned                                          */
+  const float *scale_dev;    /* [ceil(n / 128)][ceil(k / 128)], contiguous               */
+  const void *map;           /* HOST, nullable: what d3_weight8_map wrote for this matrix; without it every product
+                                encodes its tensor map anew                              */
+} d3_weight8;
+/* Encodes the tensor map of a weight once, to D3_WEIGHT8_MAP_BYTES of caller-owned HOST memory (64-byte aligned); a call
+ * whose weight has other fields (scales aside) is refused.  D3_ECUDA when the driver has no encoder. */
+#define D3_WEIGHT8_MAP_BYTES 256
+int32_t d3_weight8_map(const d3_weight8 *w, void *map);
+
+/* w [n][k] (D3_BF16, D3_FP16, D3_FP32; row stride in elements) to w8's q and scales (which the call writes). */
+int32_t d3_quantize_weight(const void *w_dev, int32_t dtype, int64_t row_stride, const d3_weight8 *w8, void *cuda_stream);
+
+/* out[row][n] = sum_k a[row][k] w[n][k]: the products of a block of 128 k are summed by the tensor core in fp32, each
+ * block's sum is multiplied by the two scales and added in fp32; one rounding to out_dtype (D3_BF16, D3_FP16, D3_FP32).
+ * d3_gated_matmul8: g and u are such sums over `gate` and `up` (one shape), h = g / (1 + exp(-g)) * u in fp32, then
+ * rounded to out_dtype, or (D3_E4M3) to 8 bits with scales. */
+typedef struct d3_matmul8_args {
+  uint32_t struct_size;
+  int32_t n_rows;            /* >= 0                                                     */
+  int32_t out_dtype;
+  const void *a_dev;         /* D3_E4M3 [n_rows][k]; base and stride multiples of 16     */
+  const float *a_scale_dev;  /* [n_rows][ceil(k / 128)]                                  */
+  void *out_dev;             /* [n_rows][n]                                              */
+  float *scale_dev;          /* D3_E4M3 results: [n_rows][ceil(n / 128)]                 */
+  int64_t a_stride, a_scale_stride, out_stride, scale_stride;   /* in elements           */
+  int32_t *status_dev;       /* nullable; D3_ETIMEOUT when a bounded wait ran out (out is then undefined) */
+} d3_matmul8_args;
+int32_t d3_matmul8(const d3_weight8 *w, const d3_matmul8_args *a, void *cuda_stream);
+int32_t d3_gated_matmul8(const d3_weight8 *gate, const d3_weight8 *up, const d3_matmul8_args *a, void *cuda_stream);
+
+/* Row by row, z the row's logits in fp32, each step rounded once:
+ *   of a token among the first lengths[row] of history[row]:  z = z > 0 ? z / repetition : z * repetition
+ *   of one that occurs c > 0 times behind the first prompt[row] of them:  z -= frequency * c,  then z -= presence
+ *   of a token in bias_ids[row]:  z += bias (of an id that is there twice the later entry counts)
+ *   of a token whose bit in masks[mask_of[row]] is 0:  z = -inf, whatever it was
+ * out = z in logits' type; token = the lowest index of out's largest number, -1 where there is none above -inf (NaN is
+ * none).  Each part is left out where its pointers are NULL.  Negative ids in history and bias_ids are padding; ids
+ * of vocab and more are skipped and D3_EINVAL is stored; so it is for lengths and prompts outside 0..n_history (which
+ * count as the nearest bound), and for a mask_of of n_masks and more, which counts as -1: no mask. */
+typedef struct d3_constrain_logits_args {
+  uint32_t struct_size;
+  int32_t dtype;             /* D3_BF16, D3_FP16, D3_FP32                                */
+  int32_t n_rows, vocab;     /* 0..65535; >= 1                                           */
+  int32_t n_history, n_bias, n_masks;
+  const void *logits_dev;
+  void *out_dev;             /* may be logits (with the same stride)                     */
+  int64_t logits_stride, out_stride, history_stride, bias_stride, mask_stride;   /* in elements; any >= the row */
+  const int32_t *history_dev;   /* nullable, [n_rows][n_history]                         */
+  const int32_t *lengths_dev;   /* nullable (all of n_history), [n_rows]                 */
+  const int32_t *prompt_dev;    /* nullable (0), [n_rows]                                */
+  const float *repetition_dev, *frequency_dev, *presence_dev;   /* each nullable, [n_rows] */
+  const int32_t *bias_ids_dev;  /* nullable, [n_rows][n_bias]                            */
+  const float *bias_dev;        /* [n_rows][n_bias], of bias_ids' stride                 */
+  const int32_t *masks_dev;     /* nullable, [n_masks][ceil(vocab / 32)]: token t is bit t % 32 of word t / 32 */
+  const int32_t *mask_of_dev;   /* with masks: [n_rows]                                  */
+  int32_t *token_dev;           /* nullable, [n_rows]                                    */
+  int32_t *status_dev;          /* nullable                                              */
+} d3_constrain_logits_args;
+int32_t d3_constrain_logits(const d3_constrain_logits_args *a, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

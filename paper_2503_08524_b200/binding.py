@@ -30,7 +30,8 @@ EXPORTS = ("d3_depth", "d3_schedule", "d3_workspace_bytes", "d3_load", "d3_prefi
            "d3_stall_next_step", "d3_slot_pos",
            "d3_kv_pages_used", "d3_reset_slot", "d3_sync", "d3_free", "d3_strerror",
            "d3_paged_maps", "d3_page_plan", "d3_paged_append", "d3_rope_table", "d3_paged_attention",
-           "d3_paged_attention_workspace", "d3_paged_set_wait_ns", "d3_paged_stall_next", "d3_paged_view")
+           "d3_paged_attention_workspace", "d3_paged_set_wait_ns", "d3_paged_stall_next", "d3_paged_view",
+           "d3_add_norm", "d3_weight8_map", "d3_quantize_weight", "d3_matmul8", "d3_gated_matmul8", "d3_constrain_logits")
 
 
 class Config(C.Structure):
@@ -110,6 +111,13 @@ def _load() -> C.CDLL:
     lib.d3_paged_set_wait_ns.argtypes = [C.c_uint64]
     lib.d3_paged_stall_next.argtypes = [I32]
     lib.d3_paged_view.argtypes = [P, I32, P, C.POINTER(P), C.POINTER(I32), C.POINTER(I32)]
+    # 8-bit block operators: the argument structs are in block8.py
+    lib.d3_add_norm.argtypes = [P, P]
+    lib.d3_weight8_map.argtypes = [P, P]
+    lib.d3_quantize_weight.argtypes = [P, I32, I64, P, P]
+    lib.d3_matmul8.argtypes = [P, P, P]
+    lib.d3_gated_matmul8.argtypes = [P, P, P, P]
+    lib.d3_constrain_logits.argtypes = [P, P]
     return lib
 
 

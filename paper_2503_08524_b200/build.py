@@ -1,6 +1,6 @@
 """Builds libd3.so (the CUDA library behind the C ABI of include/d3.h) in-tree
-with nvcc for sm_100a, and _paged_call.*.so (the Python side of the paged operators'
-calls, csrc/paged_call.cpp) with g++.  No GPU is needed to build."""
+with nvcc for sm_100a, and _paged_call.*.so and _block_call.*.so (the Python side of the
+paged and of the 8-bit block operators' calls, csrc/*_call.cpp) with g++.  No GPU is needed to build."""
 from __future__ import annotations
 
 import glob
@@ -66,17 +66,20 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
-def call_path() -> str:
-    """Where the extension module lies: it reads torch's objects, so its name says what it was built for."""
+CALLS = ("paged_call", "block_call")      # extension modules, by their source
+
+
+def call_path(name: str = "paged_call") -> str:
+    """Where an extension module lies: it reads torch's objects, so its name says what it was built for."""
     import torch
     made_for = "-".join((sys.implementation.cache_tag, "torch" + torch.__version__, "cxx11abi%d" % torch._C._GLIBCXX_USE_CXX11_ABI))
-    return os.path.join(PKG, "_paged_call." + re.sub(r"[^0-9A-Za-z-]", "_", made_for) + ".so")
+    return os.path.join(PKG, "_" + name + "." + re.sub(r"[^0-9A-Za-z-]", "_", made_for) + ".so")
 
 
-def build_call(force: bool = False) -> str:
-    """Compile and link the extension module that makes the paged operators' calls; returns its path."""
-    src, header = os.path.join(CSRC, "paged_call.cpp"), os.path.join(ROOT, "include", "d3.h")
-    out = call_path()
+def build_call(force: bool = False, name: str = "paged_call") -> str:
+    """Compile and link an extension module that makes operators' calls (default: the paged ones'); returns its path."""
+    src, header = os.path.join(CSRC, name + ".cpp"), os.path.join(ROOT, "include", "d3.h")
+    out = call_path(name)
     if not force and os.path.exists(out) and os.path.getmtime(out) > max(os.path.getmtime(src), os.path.getmtime(header)):
         return out
     import sysconfig
@@ -85,7 +88,7 @@ def build_call(force: bool = False) -> str:
     base = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(NVCC))
     # a file of this process's own until it is whole: ranks that import a fresh checkout build it side by side
-    handle, made = tempfile.mkstemp(dir=os.path.dirname(out), prefix="_paged_call.", suffix=".new")
+    handle, made = tempfile.mkstemp(dir=os.path.dirname(out), prefix="_" + name + ".", suffix=".new")
     os.close(handle)
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(base, "include"),
@@ -103,10 +106,10 @@ def build_call(force: bool = False) -> str:
     return out
 
 
-def load_call():
-    """The extension module, built if need be."""
+def load_call(name: str = "paged_call"):
+    """An extension module, built if need be."""
     import importlib.util
-    spec = importlib.util.spec_from_file_location(__package__ + "._paged_call", build_call())
+    spec = importlib.util.spec_from_file_location(__package__ + "._" + name, build_call(name=name))
     module = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(module)
     return module
@@ -114,4 +117,5 @@ def load_call():
 
 if __name__ == "__main__":
     print(build(force=True, verbose="-v" in sys.argv))
-    print(build_call(force=True))
+    for call in CALLS:
+        print(build_call(force=True, name=call))

@@ -1,0 +1,373 @@
+// 8-bit block operators: residual sum + RMSNorm + quantising, weights to 8 bits, and the C ABI of the products.
+#include <math.h>
+
+#include "d3_block8.cuh"
+
+namespace d3 {
+
+namespace {
+
+// ------------------------------------------------------------------ norm
+struct NormArgs {
+  long long n_rows;
+  int dim, x_dtype, add_dtype, gain_dtype, out_dtype;
+  float eps;
+  const void *x, *add, *gain;
+  void *total, *out;
+  float *scale;
+  long long x_stride, add_stride, total_stride, out_stride, scale_stride;
+};
+
+// A row is held in registers by T threads of the CTA, V pieces of 8 numbers each; T = 32 puts rows side by side, a warp
+// each.  Everything is read before anything is written, so that out and total may lie on x and add.  16 neighbouring
+// threads have one block of 128 numbers and find its largest by shuffles.
+template <int V, bool kWarp>
+__global__ void __launch_bounds__(1024) k_add_norm(const __grid_constant__ NormArgs a) {
+  __shared__ float s_sum[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int T = kWarp ? 32 : blockDim.x, t = kWarp ? lane : threadIdx.x;
+  const long long row = kWarp ? (long long)blockIdx.x * (blockDim.x >> 5) + warp : blockIdx.x;
+  const int pieces = a.dim >> 3;
+  pdl_wait();
+  pdl_trigger();
+  if (kWarp && row >= a.n_rows) return;
+  float v[V][8];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int c = i * T + t;
+    if (c < pieces) {
+      load8(a.x, row * a.x_stride + 8 * c, a.x_dtype, v[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+    }
+  }
+  if (a.add) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int c = i * T + t;
+      if (c < pieces) {
+        float u[8];
+        load8(a.add, row * a.add_stride + 8 * c, a.add_dtype, u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] += u[j];
+      }
+    }
+  }
+  if (a.gain) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      float part = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) part = fmaf(v[i][j], v[i][j], part);
+      sum += part;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (!kWarp) {
+      if (lane == 0) s_sum[warp] = sum;
+      __syncthreads();
+      sum = lane < T / 32 ? s_sum[lane] : 0.f;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    }
+    const float r = 1.f / sqrtf(sum / (float)a.dim + a.eps);
+    if (a.total) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = i * T + t;
+        if (c < pieces) store8(a.total, row * a.total_stride + 8 * c, a.add_dtype, v[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int c = i * T + t;
+      if (c < pieces) {
+        float g[8];
+        load8(a.gain, 8 * c, a.gain_dtype, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * r * g[j];
+      }
+    }
+  } else if (a.total) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int c = i * T + t;
+      if (c < pieces) store8(a.total, row * a.total_stride + 8 * c, a.add_dtype, v[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int c = i * T + t;
+    if (a.out_dtype == D3_E4M3) {
+      float top = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max_nan(top, fabsf(v[i][j]));
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+      float inverse;
+      const float scale = block_scale(top, inverse);
+      if (c < pieces) {
+        const uint32_t lo = pack_e4m3(v[i][0] * inverse, v[i][1] * inverse, v[i][2] * inverse, v[i][3] * inverse);
+        const uint32_t hi = pack_e4m3(v[i][4] * inverse, v[i][5] * inverse, v[i][6] * inverse, v[i][7] * inverse);
+        *reinterpret_cast<uint2 *>(static_cast<char *>(a.out) + row * a.out_stride + 8 * c) = make_uint2(lo, hi);
+        if ((c & 15) == 0) a.scale[row * a.scale_stride + (c >> 4)] = scale;
+      }
+    } else if (c < pieces) {
+      store8(a.out, row * a.out_stride + 8 * c, a.out_dtype, v[i]);
+    }
+  }
+}
+
+template <int V>
+cudaError_t launch_norm(const NormArgs &a, int threads, cudaStream_t st) {
+  if (threads <= 32) {
+    const int rows = a.n_rows < 148 * 4 ? 1 : 8;
+    return launch_pdl(k_add_norm<V, true>, dim3((unsigned)((a.n_rows + rows - 1) / rows)), dim3(32 * rows), 0, st, a);
+  }
+  return launch_pdl(k_add_norm<V, false>, dim3((unsigned)a.n_rows), dim3(threads), 0, st, a);
+}
+
+// ------------------------------------------------------------------ weights to 8 bits
+struct QuantWeightArgs {
+  const void *w;
+  int dtype, n, k;
+  long long stride, q_stride;
+  unsigned char *q;
+  float *scale;
+};
+// One block of 128 x 128 per CTA: thread t has 64 numbers of row t / 2, 8 at a time (k is a multiple of 16).  No trigger for the
+// next kernel: what this one writes, a product may read before it waits.
+__global__ void __launch_bounds__(256) k_quantize_weight(const __grid_constant__ QuantWeightArgs a) {
+  __shared__ float s_top[8];
+  pdl_wait();
+  const int row = blockIdx.y * 128 + (threadIdx.x >> 1), k0 = blockIdx.x * 128 + (threadIdx.x & 1) * 64;
+  float v[8][8];
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (row < a.n && k0 + 8 * i < a.k) {
+      if (a.stride % 8 == 0 && ((uintptr_t)a.w & 15u) == 0) {
+        load8(a.w, row * a.stride + k0 + 8 * i, a.dtype, v[i]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = load1(a.w, row * a.stride + k0 + 8 * i + j, a.dtype);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max_nan(top, fabsf(v[i][j]));
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max_nan(top, s_top[i]);
+  float inverse;
+  const float scale = block_scale(top, inverse);
+  if (threadIdx.x == 0) a.scale[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = scale;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (row < a.n && k0 + 8 * i < a.k) {
+      const uint32_t lo = pack_e4m3(v[i][0] * inverse, v[i][1] * inverse, v[i][2] * inverse, v[i][3] * inverse);
+      const uint32_t hi = pack_e4m3(v[i][4] * inverse, v[i][5] * inverse, v[i][6] * inverse, v[i][7] * inverse);
+      *reinterpret_cast<uint2 *>(a.q + row * a.q_stride + k0 + 8 * i) = make_uint2(lo, hi);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ tensor maps
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+EncodeTiledFn rows_encoder() {
+  static EncodeTiledFn fn = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+
+bool weight_ok(const d3_weight8 *w) {
+  return w && w->struct_size == sizeof(d3_weight8) && w->n >= 1 && w->k >= 16 && w->k % 16 == 0 && w->row_stride >= w->k &&
+         w->row_stride % 16 == 0 && w->row_stride <= ((int64_t)1 << 38) && w->q_dev && on_bytes(w->q_dev, 16) && w->scale_dev &&
+         on_bytes(w->scale_dev, 4);
+}
+bool made_for(const Weight8Map *m, const d3_weight8 &w) {
+  return m->of.n == w.n && m->of.k == w.k && m->of.row_stride == w.row_stride && m->of.q_dev == w.q_dev;
+}
+int64_t scale_blocks(int64_t v) { return (v + kScaleBlock - 1) / kScaleBlock; }
+
+// the checks and the launch that both products share
+int32_t product(const d3_weight8 *const (&w)[2], const d3_matmul8_args *a, cudaStream_t st) {
+  const int mats = w[1] ? 2 : 1;
+  for (int i = 0; i < mats; ++i)
+    if (!weight_ok(w[i])) return D3_EINVAL;
+  if (mats == 2 && (w[0]->n != w[1]->n || w[0]->k != w[1]->k)) return D3_EINVAL;
+  if (!a || a->struct_size != sizeof(d3_matmul8_args) || a->n_rows < 0) return D3_EINVAL;
+  const bool eight = a->out_dtype == D3_E4M3;
+  if (!wide_type(a->out_dtype) && !(eight && mats == 2)) return D3_EINVAL;
+  const int n = w[0]->n, k = w[0]->k, es = type_bytes(a->out_dtype);
+  const int64_t kb = scale_blocks(k), nb = scale_blocks(n);
+  if (!a->a_dev || !on_bytes(a->a_dev, 16) || !a->a_scale_dev || !on_bytes(a->a_scale_dev, 4) || !a->out_dev || !on_bytes(a->out_dev, es))
+    return D3_EINVAL;
+  if (a->n_rows > 1 && (a->a_stride < k || a->a_stride % 16 || a->a_stride > ((int64_t)1 << 38) || a->a_scale_stride < kb ||
+                        a->a_scale_stride > ((int64_t)1 << 38) || a->out_stride < n || a->out_stride > ((int64_t)1 << 38)))
+    return D3_EINVAL;
+  if (eight && (!a->scale_dev || !on_bytes(a->scale_dev, 4) ||
+                (a->n_rows > 1 && (a->scale_stride < nb || a->scale_stride > ((int64_t)1 << 38)))))
+    return D3_EINVAL;
+  if (!eight && a->scale_dev) return D3_EINVAL;
+  if (!on_bytes(a->status_dev, 4)) return D3_EINVAL;
+  for (int i = 0; i < mats; ++i)
+    if (w[i]->map && (((uintptr_t)w[i]->map & 63) || !made_for(static_cast<const Weight8Map *>(w[i]->map), *w[i]))) return D3_EINVAL;
+  if (a->n_rows == 0) return D3_OK;
+  const int64_t rows = a->n_rows;
+  const RowSet out = {a->out_dev, rows, a->out_stride * es, (int64_t)n * es};
+  const RowSet scale = {eight ? a->scale_dev : nullptr, rows, a->scale_stride * 4, nb * 4};
+  const RowSet status = {a->status_dev, 1, 4, 4};
+  RowSet read[6] = {{a->a_dev, rows, a->a_stride, k}, {a->a_scale_dev, rows, a->a_scale_stride * 4, kb * 4}};
+  for (int i = 0; i < mats; ++i) {
+    read[2 + 2 * i] = RowSet{w[i]->q_dev, n, w[i]->row_stride, k};
+    read[3 + 2 * i] = RowSet{w[i]->scale_dev, 1, 0, nb * kb * 4};
+  }
+  for (int i = 0; i < 2 + 2 * mats; ++i)
+    if (rows_common(out, read[i]) || rows_common(scale, read[i]) || rows_common(status, read[i])) return D3_EINVAL;
+  if (rows_common(out, scale) || rows_common(out, status) || rows_common(scale, status)) return D3_EINVAL;
+  if (!have_encoder8()) return D3_ECUDA;
+
+  TMap fresh[2];
+  const TMap *map[2] = {nullptr, nullptr};
+  for (int i = 0; i < mats; ++i) {
+    if (w[i]->map) map[i] = &static_cast<const Weight8Map *>(w[i]->map)->map;
+    else if (encode_rows8(&fresh[i], w[i]->q_dev, n, k, w[i]->row_stride, kScaleBlock)) map[i] = &fresh[i];
+    else return D3_ECUDA;
+  }
+  Mm8Args p;
+  memset(&p, 0, sizeof(p));
+  p.n_rows = a->n_rows; p.n = n; p.k = k; p.n_kb = (int)kb;
+  p.a_scale = a->a_scale_dev; p.a_scale_stride = rows > 1 ? a->a_scale_stride : kb;
+  p.w_scale[0] = w[0]->scale_dev; p.w_scale[1] = mats == 2 ? w[1]->scale_dev : nullptr;
+  p.out = a->out_dev; p.out_stride = rows > 1 ? a->out_stride : n; p.out_dtype = a->out_dtype;
+  p.out_wide = on_bytes(a->out_dev, 4 * es) && (p.out_stride % 4 == 0 || rows == 1);
+  p.scale = a->scale_dev; p.scale_stride = rows > 1 ? a->scale_stride : nb;
+  p.status = a->status_dev;
+  p.wait_ns = kBlock8WaitNs;
+  const int64_t a_stride = rows > 1 ? a->a_stride : (int64_t)k;
+  const cudaError_t e = a->n_rows <= kFewRows ? launch_mm8_few(*map[0], map[1], a->a_dev, a_stride, p, st)
+                                              : launch_mm8_many(*map[0], map[1], a->a_dev, a_stride, p, st);
+  return e == cudaSuccess ? D3_OK : D3_ECUDA;
+}
+
+}  // namespace
+
+bool have_encoder8() { return rows_encoder() != nullptr; }
+
+bool encode_rows8(TMap *out, const void *base, int rows, int k, int64_t stride, int box_rows) {
+  EncodeTiledFn fn = rows_encoder();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
+  cuuint32_t box[2] = {(cuuint32_t)kScaleBlock, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+  return fn(reinterpret_cast<CUtensorMap *>(out), CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace d3
+
+using namespace d3;
+
+extern "C" {
+
+int32_t d3_add_norm(const d3_add_norm_args *a, void *cuda_stream) {
+  if (!a || a->struct_size != sizeof(d3_add_norm_args) || a->n_rows < 0) return D3_EINVAL;
+  if (a->dim < 8 || a->dim > 65536 || a->dim % 8 || !wide_type(a->x_dtype)) return D3_EINVAL;
+  const bool eight = a->out_dtype == D3_E4M3;
+  if (!eight && !wide_type(a->out_dtype)) return D3_EINVAL;
+  if (!(a->eps >= 0.f) || isinf(a->eps)) return D3_EINVAL;
+  const int xs = type_bytes(a->x_dtype), os = type_bytes(a->out_dtype), as = type_bytes(a->add_dtype);
+  const int64_t rows = a->n_rows, dim = a->dim, nb = scale_blocks(dim), most = (int64_t)1 << 38;
+  auto stride_ok = [&](int64_t s, int64_t least, int bytes, int unit) {
+    return rows <= 1 || (s >= least && s <= most && s * bytes % unit == 0);
+  };
+  if (!a->x_dev || !on_bytes(a->x_dev, 16) || !stride_ok(a->x_stride, 0, xs, 16)) return D3_EINVAL;
+  if (!a->out_dev || !on_bytes(a->out_dev, eight ? 8 : 16) || !stride_ok(a->out_stride, dim, os, eight ? 8 : 16)) return D3_EINVAL;
+  if (a->add_dev) {
+    if (a->add_dtype != a->x_dtype && a->add_dtype != D3_FP32) return D3_EINVAL;
+    if (!on_bytes(a->add_dev, 16) || !stride_ok(a->add_stride, 0, as, 16)) return D3_EINVAL;
+    if (a->total_dev && (!on_bytes(a->total_dev, 16) || !stride_ok(a->total_stride, dim, as, 16))) return D3_EINVAL;
+  } else if (a->total_dev) {
+    return D3_EINVAL;
+  }
+  if (a->gain_dev && (!wide_type(a->gain_dtype) || !on_bytes(a->gain_dev, 16))) return D3_EINVAL;
+  if (eight ? (!a->scale_dev || !on_bytes(a->scale_dev, 4) || !stride_ok(a->scale_stride, nb, 4, 4)) : a->scale_dev != nullptr) return D3_EINVAL;
+  if (rows == 0) return D3_OK;
+  const RowSet x = {a->x_dev, rows, a->x_stride * xs, dim * xs}, add = {a->add_dev, rows, a->add_stride * as, dim * as},
+               total = {a->total_dev, rows, a->total_stride * as, dim * as}, out = {a->out_dev, rows, a->out_stride * os, dim * os},
+               gain = {a->gain_dev, 1, 0, dim * type_bytes(a->gain_dtype)}, scale = {a->scale_dev, rows, a->scale_stride * 4, nb * 4};
+  // a row is read whole before any of it is written: out on x, total on add or x, number by number
+  const bool out_on_x = a->out_dtype == a->x_dtype && same_rows(out, x), total_on_add = same_rows(total, add),
+             total_on_x = a->add_dtype == a->x_dtype && same_rows(total, x);
+  if ((rows_common(out, x) && !(out_on_x && !(rows > 1 && !rows_distinct(x)))) || (rows_common(total, add) && !(total_on_add && rows_distinct(add))) ||
+      (rows_common(total, x) && !(total_on_x && rows_distinct(x))) || rows_common(out, add) || rows_common(out, total) || rows_common(out, gain) ||
+      rows_common(total, gain) || rows_common(scale, x) || rows_common(scale, add) || rows_common(scale, total) || rows_common(scale, out) ||
+      rows_common(scale, gain))
+    return D3_EINVAL;
+  NormArgs p;
+  p.n_rows = rows; p.dim = a->dim; p.x_dtype = a->x_dtype; p.add_dtype = a->add_dtype; p.gain_dtype = a->gain_dtype; p.out_dtype = a->out_dtype;
+  p.eps = a->eps; p.x = a->x_dev; p.add = a->add_dev; p.gain = a->gain_dev; p.total = a->total_dev; p.out = a->out_dev; p.scale = a->scale_dev;
+  p.x_stride = a->x_stride; p.add_stride = a->add_stride; p.total_stride = a->total_stride; p.out_stride = a->out_stride;
+  p.scale_stride = a->scale_stride;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const int pieces = a->dim / 8;
+  auto threads_for = [&](int v) { return (pieces + 32 * v - 1) / (32 * v) * 32; };
+  cudaError_t e;
+  if (pieces <= 32) e = launch_norm<1>(p, 32, st);
+  else if (pieces <= 1024 && rows < 148 * 4) e = launch_norm<1>(p, threads_for(1), st);
+  else if (pieces <= 1024) e = launch_norm<2>(p, threads_for(2), st);
+  else if (pieces <= 4096) e = launch_norm<4>(p, threads_for(4), st);
+  else e = launch_norm<8>(p, threads_for(8), st);
+  return e == cudaSuccess ? D3_OK : D3_ECUDA;
+}
+
+int32_t d3_weight8_map(const d3_weight8 *w, void *map) {
+  if (!weight_ok(w) || !map || ((uintptr_t)map & 63)) return D3_EINVAL;
+  Weight8Map *m = static_cast<Weight8Map *>(map);
+  if (!encode_rows8(&m->map, w->q_dev, w->n, w->k, w->row_stride, kScaleBlock)) return D3_ECUDA;
+  m->of = *w;
+  m->of.map = nullptr;
+  m->of.scale_dev = nullptr;
+  return D3_OK;
+}
+
+int32_t d3_quantize_weight(const void *w_dev, int32_t dtype, int64_t row_stride, const d3_weight8 *w8, void *cuda_stream) {
+  if (!weight_ok(w8) || !wide_type(dtype) || !w_dev || !on_bytes(w_dev, type_bytes(dtype))) return D3_EINVAL;
+  if (w8->n > 1 && (row_stride < w8->k || row_stride > ((int64_t)1 << 38))) return D3_EINVAL;
+  const int64_t nb = scale_blocks(w8->n), kb = scale_blocks(w8->k), es = type_bytes(dtype);
+  if (nb > 65535) return D3_EINVAL;
+  const RowSet from = {w_dev, w8->n, row_stride * es, w8->k * es}, to = {w8->q_dev, w8->n, w8->row_stride, w8->k},
+               scale = {w8->scale_dev, 1, 0, nb * kb * 4};
+  if (rows_common(from, to) || rows_common(from, scale) || rows_common(to, scale)) return D3_EINVAL;
+  QuantWeightArgs q;
+  q.w = w_dev; q.dtype = dtype; q.n = w8->n; q.k = w8->k; q.stride = w8->n > 1 ? row_stride : 0; q.q_stride = w8->row_stride;
+  q.q = static_cast<unsigned char *>(const_cast<void *>(w8->q_dev)); q.scale = const_cast<float *>(w8->scale_dev);
+  return launch_pdl(k_quantize_weight, dim3((unsigned)kb, (unsigned)nb), dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), q) == cudaSuccess
+             ? D3_OK : D3_ECUDA;
+}
+
+int32_t d3_matmul8(const d3_weight8 *w, const d3_matmul8_args *a, void *cuda_stream) {
+  return product({w, nullptr}, a, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int32_t d3_gated_matmul8(const d3_weight8 *gate, const d3_weight8 *up, const d3_matmul8_args *a, void *cuda_stream) {
+  if (!up) return D3_EINVAL;
+  return product({gate, up}, a, static_cast<cudaStream_t>(cuda_stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,261 @@
+// Shared by the 8-bit block operators: host-side checks, numbers of every type, and the PTX of the tensor-core products.
+#pragma once
+
+#include <cuda.h>   // CUtensorMap and its enums; the encoder is fetched at run time
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "d3_internal.cuh"
+
+namespace d3 {
+
+constexpr int kScaleBlock = 128;                 // numbers that share a scale
+constexpr float kE4m3Max = 448.f;
+constexpr float kLeastTop = 7.888609e-31f;       // 2^-100: a block's largest number counts as this at least
+constexpr unsigned long long kBlock8WaitNs = 2000000000ull;   // bound of every device-side wait
+
+// ------------------------------------------------------------------ host
+inline int type_bytes(int dtype) { return dtype == D3_FP32 ? 4 : dtype == D3_E4M3 ? 1 : 2; }
+inline bool wide_type(int dtype) { return dtype == D3_BF16 || dtype == D3_FP16 || dtype == D3_FP32; }
+inline bool on_bytes(const void *p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
+// Rows of `width` bytes, `stride` bytes apart.
+struct RowSet {
+  const void *p;
+  int64_t n, stride, width;
+};
+// The rows of a set that is written do not overlap one another.
+inline bool rows_distinct(const RowSet &s) { return s.n <= 1 || s.stride >= s.width; }
+// Two sets have a byte in common, as far as can be told without looking at every row: rows of one stride exactly (columns of one
+// buffer may be written while others are read), others by the memory between their first and last bytes.
+inline bool rows_common(const RowSet &a, const RowSet &b) {
+  if (!a.p || !b.p || a.n < 1 || b.n < 1 || a.width < 1 || b.width < 1) return false;
+  const int64_t a0 = (int64_t)(uintptr_t)a.p, b0 = (int64_t)(uintptr_t)b.p;
+  const int64_t a1 = a0 + (a.n - 1) * a.stride + a.width, b1 = b0 + (b.n - 1) * b.stride + b.width;
+  if (a0 >= b1 || b0 >= a1) return false;
+  const int64_t stride = a.n > 1 ? a.stride : b.stride;
+  if ((a.n > 1 && b.n > 1 && a.stride != b.stride) || stride < a.width || stride < b.width) return true;
+  // row i of a and row j of b: the distance of their starts is delta + (j - i) * stride; only the two multiples next to -delta can meet
+  const int64_t delta = b0 - a0;
+  int64_t q = delta / stride;
+  if (q * stride > delta) --q;
+  for (int t = 0; t < 2; ++t, ++q) {
+    const int64_t off = delta - q * stride;       // start of b's row i - ... relative to a's row that is q rows on
+    if (q > -b.n && q < a.n && off < a.width && -off < b.width) return true;
+  }
+  return false;
+}
+inline bool same_rows(const RowSet &a, const RowSet &b) { return a.p == b.p && a.width == b.width && (a.n <= 1 || a.stride == b.stride); }
+
+// What d3_weight8_map writes.
+struct Weight8Map {
+  TMap map;                  // (k, row), boxes of 128 bytes x 128 rows, 128-byte swizzle, zeros outside
+  d3_weight8 of;             // the matrix it was made for (map and scales left out)
+};
+static_assert(sizeof(Weight8Map) <= D3_WEIGHT8_MAP_BYTES, "room for the map");
+// tensor map of [rows][k] bytes with `stride` bytes between rows; false when the driver refuses or has no encoder
+bool encode_rows8(TMap *out, const void *base, int rows, int k, int64_t stride, int box_rows);
+bool have_encoder8();
+
+// A product as the kernels see it.
+struct Mm8Args {
+  int n_rows, n, k, n_kb;            // n_kb: blocks of 128 along k
+  const float *a_scale;
+  long long a_scale_stride;
+  const float *w_scale[2];           // [ceil(n / 128)][n_kb]
+  void *out;
+  long long out_stride;
+  int out_dtype, out_wide;           // out_wide: four results at a time may be written in one piece
+  float *scale;
+  long long scale_stride;
+  int32_t *status;
+  unsigned long long wait_ns;
+  int n_stages, split;               // few rows: CTAs that share a tile's k blocks, as a cluster
+};
+// each enqueues one kernel; cudaSuccess or what the launch said
+cudaError_t launch_mm8_few(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, Mm8Args &p, cudaStream_t st);
+cudaError_t launch_mm8_many(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, Mm8Args &p, cudaStream_t st);
+constexpr int kFewRows = 128;        // rows that the kernel for few rows takes
+
+// ------------------------------------------------------------------ device
+#ifdef __CUDACC__
+__device__ __forceinline__ float half_lo(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xffffu))); }
+__device__ __forceinline__ float half_hi(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
+// 8 consecutive numbers as floats (16-byte aligned)
+__device__ __forceinline__ void load8(const void *base, long long at, int dtype, float (&v)[8]) {
+  if (dtype == D3_FP32) {
+    const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(base) + at);
+    const float4 a = p[0], b = p[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    return;
+  }
+  const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const char *>(base) + 2 * at);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  if (dtype == D3_BF16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = half_lo(w[i]); v[2 * i + 1] = half_hi(w[i]); }
+  }
+}
+// two floats in a 32-bit word, rounded to nearest even
+__device__ __forceinline__ uint32_t pack2(float a, float b, int dtype) {
+  uint32_t r;
+  if (dtype == D3_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+__device__ __forceinline__ void store8(void *base, long long at, int dtype, const float (&v)[8]) {
+  if (dtype == D3_FP32) {
+    float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(base) + at);
+    p[0] = make_float4(v[0], v[1], v[2], v[3]);
+    p[1] = make_float4(v[4], v[5], v[6], v[7]);
+    return;
+  }
+  *reinterpret_cast<uint4 *>(static_cast<char *>(base) + 2 * at) =
+      make_uint4(pack2(v[0], v[1], dtype), pack2(v[2], v[3], dtype), pack2(v[4], v[5], dtype), pack2(v[6], v[7], dtype));
+}
+__device__ __forceinline__ void store1(void *base, long long at, int dtype, float v) {
+  if (dtype == D3_FP32) static_cast<float *>(base)[at] = v;
+  else if (dtype == D3_BF16) static_cast<bf16 *>(base)[at] = __float2bfloat16_rn(v);
+  else static_cast<__half *>(base)[at] = __float2half_rn(v);
+}
+__device__ __forceinline__ float load1(const void *base, long long at, int dtype) {
+  if (dtype == D3_FP32) return static_cast<const float *>(base)[at];
+  if (dtype == D3_BF16) return __bfloat162float(static_cast<const bf16 *>(base)[at]);
+  return __half2float(static_cast<const __half *>(base)[at]);
+}
+// four floats in 8 bits each (saturating: only a NaN is beyond 448 after the division by the scale)
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+  return (uint32_t)lo | ((uint32_t)hi << 16);
+}
+// the larger one, NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// scale of a block whose largest absolute value is `top`, and what its numbers are multiplied with before they are rounded
+__device__ __forceinline__ float block_scale(float top, float &inverse) {
+  const float scale = max_nan(top, kLeastTop) / kE4m3Max;
+  inverse = 1.f / scale;
+  return scale;
+}
+
+__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint64_t clock_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+// Bounded wait for a barrier's phase; false when the limit ran out (the CTA's flag is then set) or, with `leave`, when another
+// wait of the CTA did.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, unsigned long long limit_ns, bool leave = true) {
+  if (mbar_try(bar, parity)) return true;
+  const uint64_t from = clock_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (mbar_try(bar, parity)) return true;
+    if ((it & 15u) == 0u) {
+      if (leave && *gave_up) return false;
+      if (clock_ns() - from > limit_ns) break;
+    }
+  }
+  *gave_up = 1;
+  return false;
+}
+__device__ __forceinline__ void tma_rows8(uint32_t dst, const void *map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// Shared-memory descriptor of rows of 128 bytes in the 128-byte swizzle, k contiguous: groups of 8 rows are 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_rows8(uint32_t at) {
+  return (uint64_t)((at & 0x3ffffu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+// Instruction descriptor: e4m3 x e4m3 -> fp32, both operands k-contiguous, M x N.
+__host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N) {
+  return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+// one arrival once everything that this thread has given the tensor core so far is done
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// 16 or 32 accumulator columns of this thread's lane, to be read behind tc_ld_wait alone
+__device__ __forceinline__ void tc_ld(uint32_t at, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+               "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                 "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tc_ld(uint32_t at, uint32_t (&r)[32]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+               "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+               "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                 "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+                 "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+                 "=r"(r[30]), "=r"(r[31])
+               : "r"(at) : "memory");
+}
+// silu(g) * u (an exp(-g) that is infinite makes it 0; g = -inf gives NaN)
+__device__ __forceinline__ float gate_of(float g, float u) { return g / (1.f + expf(-g)) * u; }
+// A warp has the 128 results of a row that one tile of weight rows gives, lane l those at n0 = 128 tile + 4 l: rounds and writes
+// them, in 8 bits with the block's scale or in a wider type.  What is behind the last column counts and writes nothing.
+__device__ __forceinline__ void finish4(const Mm8Args &t, long long row, int n0, const float (&y)[4], int tile, int lane) {
+  const long long at = row * t.out_stride + n0;
+  if (t.out_dtype == D3_E4M3) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n0 + i < t.n) top = max_nan(top, fabsf(y[i]));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float inverse;
+    const float scale = block_scale(top, inverse);
+    if (lane == 0) t.scale[row * t.scale_stride + tile] = scale;
+    const uint32_t q = pack_e4m3(y[0] * inverse, y[1] * inverse, y[2] * inverse, y[3] * inverse);
+    unsigned char *o = static_cast<unsigned char *>(t.out) + at;
+    if (t.out_wide && n0 + 3 < t.n) {
+      *reinterpret_cast<uint32_t *>(o) = q;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (n0 + i < t.n) o[i] = (unsigned char)(q >> (8 * i));
+    }
+  } else if (t.out_wide && n0 + 3 < t.n) {
+    if (t.out_dtype == D3_FP32) *reinterpret_cast<float4 *>(static_cast<float *>(t.out) + at) = make_float4(y[0], y[1], y[2], y[3]);
+    else *reinterpret_cast<uint2 *>(static_cast<char *>(t.out) + 2 * at) = make_uint2(pack2(y[0], y[1], t.out_dtype), pack2(y[2], y[3], t.out_dtype));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n0 + i < t.n) store1(t.out, at + i, t.out_dtype, y[i]);
+  }
+}
+#endif
+
+}  // namespace d3
