@@ -258,7 +258,7 @@ int32_t product(const d3_weight8 *const (&w)[2], const d3_matmul8_args *a, cudaS
   p.out_wide = on_bytes(a->out_dev, 4 * es) && (p.out_stride % 4 == 0 || rows == 1);
   p.scale = a->scale_dev; p.scale_stride = rows > 1 ? a->scale_stride : nb;
   p.status = a->status_dev;
-  p.wait_ns = kBlock8WaitNs;
+  p.wait_tries = kWaitTries;
   const int64_t a_stride = rows > 1 ? a->a_stride : (int64_t)k;
   const cudaError_t e = a->n_rows <= kFewRows ? launch_mm8_few(*map[0], map[1], a->a_dev, a_stride, p, st)
                                               : launch_mm8_many(*map[0], map[1], a->a_dev, a_stride, p, st);
@@ -277,6 +277,18 @@ bool encode_rows8(TMap *out, const void *base, int rows, int k, int64_t stride, 
   return fn(reinterpret_cast<CUtensorMap *>(out), CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool encode_results8(TMap *out, void *base, int rows, int n, int dtype, int64_t stride) {
+  EncodeTiledFn fn = rows_encoder();
+  if (!fn) return false;
+  const int es = type_bytes(dtype);
+  cuuint64_t dims[2] = {(cuuint64_t)n, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(stride * es)};
+  cuuint32_t box[2] = {(cuuint32_t)(128 / es), 128}, estr[2] = {1, 1};
+  const CUtensorMapDataType type = dtype == D3_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == D3_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                   : dtype == D3_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+  return fn(reinterpret_cast<CUtensorMap *>(out), type, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace d3

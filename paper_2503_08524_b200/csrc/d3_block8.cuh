@@ -12,7 +12,8 @@ namespace d3 {
 constexpr int kScaleBlock = 128;                 // numbers that share a scale
 constexpr float kE4m3Max = 448.f;
 constexpr float kLeastTop = 7.888609e-31f;       // 2^-100: a block's largest number counts as this at least
-constexpr unsigned long long kBlock8WaitNs = 2000000000ull;   // bound of every device-side wait
+constexpr uint32_t kWaitTries = 40000000u;       // bound of every device-side wait: about two seconds
+constexpr uint32_t kDrainTries = 40000u;         // the least that copies and products in flight are waited for: about two milliseconds
 
 // ------------------------------------------------------------------ host
 inline int type_bytes(int dtype) { return dtype == D3_FP32 ? 4 : dtype == D3_E4M3 ? 1 : 2; }
@@ -54,6 +55,8 @@ struct Weight8Map {
 static_assert(sizeof(Weight8Map) <= D3_WEIGHT8_MAP_BYTES, "room for the map");
 // tensor map of [rows][k] bytes with `stride` bytes between rows; false when the driver refuses or has no encoder
 bool encode_rows8(TMap *out, const void *base, int rows, int k, int64_t stride, int box_rows);
+// tensor map of results [rows][n] of a type: boxes of 128 bytes x 128 rows in the 128-byte swizzle
+bool encode_results8(TMap *out, void *base, int rows, int n, int dtype, int64_t stride);
 bool have_encoder8();
 
 // A product as the kernels see it.
@@ -68,7 +71,7 @@ struct Mm8Args {
   float *scale;
   long long scale_stride;
   int32_t *status;
-  unsigned long long wait_ns;
+  uint32_t wait_tries;
   int n_stages, split;               // few rows: CTAs that share a tile's k blocks, as a cluster
 };
 // each enqueues one kernel; cudaSuccess or what the launch said
@@ -146,11 +149,6 @@ __device__ __forceinline__ float block_scale(float top, float &inverse) {
 }
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ uint64_t clock_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
-}
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
@@ -167,19 +165,21 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok;
 }
 // Bounded wait for a barrier's phase; false when the limit ran out (the CTA's flag is then set) or, with `leave`, when another
-// wait of the CTA did.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, unsigned long long limit_ns, bool leave = true) {
-  if (mbar_try(bar, parity)) return true;
-  const uint64_t from = clock_ns();
-  for (uint32_t it = 1;; ++it) {
+// wait of the CTA did.  The limit is a count of tries: one takes 40 to 80 ns where it fails, and a look at a clock in this
+// loop costs the few warps that drive the tensor core more than it tells.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, uint32_t tries, bool leave = true) {
+  for (uint32_t n = 0;; ++n) {
     if (mbar_try(bar, parity)) return true;
-    if ((it & 15u) == 0u) {
-      if (leave && *gave_up) return false;
-      if (clock_ns() - from > limit_ns) break;
-    }
+    if ((n & 255u) == 255u && ((leave && *gave_up) || n >= tries)) break;
   }
   *gave_up = 1;
   return false;
+}
+// one lane of a converged warp, the same one every time
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r;
 }
 __device__ __forceinline__ void tma_rows8(uint32_t dst, const void *map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -195,7 +195,6 @@ __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N) {
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
                ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
@@ -204,7 +203,7 @@ __device__ __forceinline__ void tc_mma_e4m3(uint32_t d, uint64_t a, uint64_t b, 
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// 16 or 32 accumulator columns of this thread's lane, to be read behind tc_ld_wait alone
+// 16 or 32 accumulator columns of this thread's lane, to be read behind tc_ld_wait only
 __device__ __forceinline__ void tc_ld(uint32_t at, uint32_t (&r)[16]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
                "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
@@ -221,6 +220,21 @@ __device__ __forceinline__ void tc_ld(uint32_t at, uint32_t (&r)[32]) {
                  "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
                  "=r"(r[30]), "=r"(r[31])
                : "r"(at) : "memory");
+}
+// waits for the loads so far; nothing may read their registers earlier, which naming them here says
+__device__ __forceinline__ void tc_ld_wait(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :: "memory");
+}
+__device__ __forceinline__ void tc_ld_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]),
+                 "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                 "+r"(r[30]), "+r"(r[31])
+               :: "memory");
 }
 // silu(g) * u (an exp(-g) that is infinite makes it 0; g = -inf gives NaN)
 __device__ __forceinline__ float gate_of(float g, float u) { return g / (1.f + expf(-g)) * u; }

@@ -49,7 +49,7 @@ struct Few {
   static constexpr int kColumns = kBuffers * N * W;
   static constexpr int kStage = W * kTileBytes + N * 128;
   static constexpr int kSums = W * N * 128 * 4;                // one CTA's sums, over the ring when it is empty
-  static constexpr int kScales = 2 * kScaleChunk * N * 4;      // the rows' scales, two chunks
+  static constexpr int kScales = 2 * kScaleChunk * (N + W) * 4;   // the rows' scales and the weights', two chunks
 };
 
 template <int C, int G, int W>
@@ -62,13 +62,13 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
   __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[F::kBuffers], s_read[F::kBuffers], s_tail;
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int S = t.n_stages, split = t.split;
   const int tile = blockIdx.x / split, rank = split > 1 ? (int)cluster_rank() : 0;
   const int row0 = blockIdx.y * N;                             // first row of the call that this CTA multiplies
   const int b0 = (int)((long long)t.n_kb * rank / split), b1 = (int)((long long)t.n_kb * (rank + 1) / split);
   const uint32_t ring = (smem_at(raw) + 1023u) & ~1023u;       // the swizzle goes by the address
-  float *scales = reinterpret_cast<float *>(raw + (ring - smem_at(raw)) + S * F::kStage);   // [2][kScaleChunk][N]
+  float *scales = reinterpret_cast<float *>(raw + (ring - smem_at(raw)) + S * F::kStage);   // [2][kScaleChunk][N], then [2][kScaleChunk][W]
   volatile int *gave_up = &s_gave_up;
 
   if (tid == 0) {
@@ -98,38 +98,40 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
 
   if (warp == 0) {
     // ------------------------------------------------------------ copies
-    if (lane == 0) {
-      int issued = b0;
-      for (int b = b0; b < b1; ++b) {
-        const int it = b - b0, s = it % S, fill = it / S;
-        if (fill > 0 && !mbar_wait(smem_at(&s_empty[s]), (uint32_t)((fill - 1) & 1), gave_up, t.wait_ns)) break;
-        const uint32_t full = smem_at(&s_full[s]), at = ring + (uint32_t)(s * F::kStage);
+    // (the whole warp runs the loops of this branch and the next, so that their arithmetic is the warp's and not a lane's)
+    const bool one = elect_one();
+    int s = 0, phase = 1, b = b0;
+    for (; b < b1; ++b) {
+      if (b - b0 >= S && !mbar_wait(smem_at(&s_empty[s]), (uint32_t)phase, gave_up, t.wait_tries)) break;
+      const uint32_t full = smem_at(&s_full[s]), at = ring + (uint32_t)(s * F::kStage);
+      if (one) {
         mbar_expect(full, F::kStage);
         tma_rows8(at, &map_w0, b * 128, tile * 128, full);
         if (W == 2) tma_rows8(at + kTileBytes, &map_w1, b * 128, tile * 128, full);
         tma_rows8(at + W * kTileBytes, &map_a, b * 128, row0, full);
-        issued = b + 1;
       }
-      if (*gave_up) {   // copies in flight must land before the CTA's shared memory is given back
-        const unsigned long long bound = t.wait_ns > kDrainFloorNs ? t.wait_ns : kDrainFloorNs;
-        for (int b = max(b0, issued - S); b < issued; ++b)
-          mbar_wait(smem_at(&s_full[(b - b0) % S]), (uint32_t)(((b - b0) / S) & 1), gave_up, bound, false);
-      }
+      if (++s == S) { s = 0; phase ^= 1; }
+    }
+    if (*gave_up) {   // copies in flight must land before the CTA's shared memory is given back
+      for (int j = max(b0, b - S); j < b; ++j)
+        mbar_wait(smem_at(&s_full[(j - b0) % S]), (uint32_t)(((j - b0) / S) & 1), gave_up, max(t.wait_tries, kDrainTries), false);
     }
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ products
-    if (lane == 0) {
-      constexpr uint32_t idesc = idesc_e4m3(128, N);
-      bool ok = true;
-      for (int b = b0; b < b1; ++b) {
-        const int it = b - b0, s = it % S, buf = it % F::kBuffers, use = it / F::kBuffers;
-        ok = use == 0 || mbar_wait(smem_at(&s_read[buf]), (uint32_t)((use - 1) & 1), gave_up, t.wait_ns);
-        if (ok) ok = mbar_wait(smem_at(&s_full[s]), (uint32_t)((it / S) & 1), gave_up, t.wait_ns);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t at = ring + (uint32_t)(s * F::kStage);
-        const uint64_t bd = desc_rows8(at + W * kTileBytes);
+    constexpr uint32_t idesc = idesc_e4m3(128, N);
+    const bool one = elect_one();
+    bool ok = true;
+    int s = 0, phase = 0;
+    for (int b = b0; b < b1; ++b) {
+      const int it = b - b0, buf = it % F::kBuffers, use = it / F::kBuffers;
+      ok = mbar_wait(smem_at(&s_full[s]), (uint32_t)phase, gave_up, t.wait_tries);
+      if (ok && use) ok = mbar_wait(smem_at(&s_read[buf]), (uint32_t)((use - 1) & 1), gave_up, t.wait_tries);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t at = ring + (uint32_t)(s * F::kStage);
+      const uint64_t bd = desc_rows8(at + W * kTileBytes);
+      if (one) {
 #pragma unroll
         for (int w = 0; w < W; ++w) {
           const uint64_t ad = desc_rows8(at + w * kTileBytes);
@@ -137,14 +139,14 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
           for (int k = 0; k < 4; ++k)   // 32 numbers = 32 bytes = 2 descriptor units
             tc_mma_e4m3(tmem + (uint32_t)((buf * W + w) * N), ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, k ? 1u : 0u);
         }
-        tc_commit(smem_at(&s_empty[s]));
         tc_commit(smem_at(&s_done[buf]));
+        tc_commit(smem_at(&s_empty[s]));
       }
-      if (!ok) {
-        // what was issued still reads shared memory and writes tensor memory
-        tc_commit(smem_at(&s_tail));
-        mbar_wait(smem_at(&s_tail), 0u, gave_up, t.wait_ns > kDrainFloorNs ? t.wait_ns : kDrainFloorNs, false);
-      }
+      if (++s == S) { s = 0; phase ^= 1; }
+    }
+    if (!ok) {        // what was issued still reads shared memory and writes tensor memory
+      if (one) tc_commit(smem_at(&s_tail));
+      mbar_wait(smem_at(&s_tail), 0u, gave_up, max(t.wait_tries, kDrainTries), false);
     }
     __syncwarp();
   } else {
@@ -154,27 +156,28 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
     const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(g * C);
     // a chunk's scales, read one chunk ahead: entry e = row (e / kScaleChunk), block (e % kScaleChunk)
     constexpr int kMine = N * kScaleChunk / (128 * G);
-    float ahead[kMine];
+    float ahead[kMine], w_ahead = 0.f;
+    float *w_scales = scales + 2 * kScaleChunk * N;
     auto fetch = [&](int from) {
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         const int e = i * 128 * G + et, row = row0 + e / kScaleChunk, b = from + e % kScaleChunk;
         ahead[i] = row < t.n_rows && b < b1 ? t.a_scale[row * t.a_scale_stride + b] : 0.f;
       }
+      const int b = from + et / W;
+      if (et < kScaleChunk * W) w_ahead = b < b1 ? t.w_scale[et % W][(size_t)tile * t.n_kb + b] : 0.f;
     };
-    auto keep = [&](float *to) {
+    auto keep = [&](int half) {
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         const int e = i * 128 * G + et;
-        to[(e % kScaleChunk) * N + e / kScaleChunk] = ahead[i];
+        scales[(half * kScaleChunk + e % kScaleChunk) * N + e / kScaleChunk] = ahead[i];
       }
+      if (et < kScaleChunk * W) w_scales[half * kScaleChunk * W + et] = w_ahead;
     };
     fetch(b0);
-    keep(scales);
+    keep(0);
     asm volatile("bar.sync 1, %0;" ::"n"(128 * G) : "memory");
-    const float *ws[W];
-#pragma unroll
-    for (int w = 0; w < W; ++w) ws[w] = t.w_scale[w] + (size_t)tile * t.n_kb;
     for (int c0 = b0, half = 0; c0 < b1; c0 += kScaleChunk, half ^= 1) {
       const int c1 = min(b1, c0 + kScaleChunk);
       fetch(c0 + kScaleChunk);
@@ -182,8 +185,8 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
         const int it = b - b0, buf = it % F::kBuffers;
         float wsb[W];
 #pragma unroll
-        for (int w = 0; w < W; ++w) wsb[w] = __ldg(ws[w] + b);
-        mbar_wait(smem_at(&s_done[buf]), (uint32_t)((it / F::kBuffers) & 1), gave_up, t.wait_ns);   // (given up: numbers without meaning)
+        for (int w = 0; w < W; ++w) wsb[w] = w_scales[(half * kScaleChunk + b - c0) * W + w];
+        mbar_wait(smem_at(&s_done[buf]), (uint32_t)((it / F::kBuffers) & 1), gave_up, t.wait_tries);   // (given up: numbers without meaning)
         __syncwarp();
         tc_fence_after();
         const float *as = scales + (half * kScaleChunk + (b - c0)) * N + g * C;
@@ -194,7 +197,7 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
           for (int p = 0; p < C; p += P) {
             uint32_t d[P];
             tc_ld(lanes + (uint32_t)((buf * W + w) * N + p), d);
-            tc_ld_wait();
+            tc_ld_wait(d);
             if (w == W - 1 && p == C - P) {
               tc_fence_before();
               mbar_arrive(smem_at(&s_read[buf]));
@@ -210,7 +213,7 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
           }
         }
       }
-      keep(scales + (half ^ 1) * kScaleChunk * N);
+      keep(half ^ 1);
       asm volatile("bar.sync 1, %0;" ::"n"(128 * G) : "memory");
     }
     // every copy has landed and every product is done: the ring holds the sums now, [matrix][row of the call][weight row]

@@ -2,11 +2,13 @@
 //
 //   y[row][r] = sum_b as[row][b] ws[r / 128][b] sum_{k in block b} a[row][k] w[r][k]
 //
-// Bound by the tensor cores: 2 flops for every (row, weight row, k).  A CTA has 128 rows (the tensor core's M) times 256
-// weight rows (N; the gated form: 128 of each matrix).  A block of 128 k is four tcgen05.mma whose sum, 128 x 256, goes to
-// one of two buffers in tensor memory; while the next block is multiplied, eight epilogue warps fetch the sum, multiply it
-// by the two scales and add it to registers (a thread has one row and 64 columns of each half), because every block has
-// scales of its own.
+// Bound by the tensor cores: 2 flops for every (row, weight row, k).  Two CTAs, a cluster, share a tile of 256 rows x 256 weight
+// rows (gated: 128 of each matrix): one tcgen05.mma of cta_group::2 multiplies both CTAs' 128 rows with the 256 weight
+// rows, of which each CTA has brought half, so a byte of shared memory is read for twice the work.  A block of 128 k is
+// four of them, whose sum, 128 x 256 in each CTA, goes to one of two buffers in tensor memory.  Every block has scales of its own:
+// while the next block is multiplied, eight epilogue warps fetch the sum, multiply it by its two scales and add it to
+// registers (a thread has one row, 64 columns of each half; two numbers an instruction).  The grid is persistent, a pair
+// of CTAs for each pair of SMs; results go through shared memory and leave as bulk copies while the next tile begins.
 #include <atomic>
 
 #include "d3_block8.cuh"
@@ -15,185 +17,364 @@ namespace d3 {
 
 namespace {
 
-constexpr int kM = 128;                          // rows of a tile
 constexpr int kBox = 128 * 128;                  // bytes of 128 rows of a stage
-constexpr int kStage = 3 * kBox;                 // a's rows, and two boxes of weight rows
-constexpr int kStages = 4;
-constexpr int kThreads = 64 + 256;
+constexpr int kStage = 2 * kBox;                 // a CTA's rows, and its half of the weight rows
+constexpr int kStages = 5;
+constexpr int kOutBytes = 32 * 1024;             // results on their way out
+constexpr int kThreads = 384;                    // copies, products and two idle warps; eight epilogue warps
 constexpr int kColumns = 512;
+constexpr int kSmem = kStages * kStage + kOutBytes + 1024;
+constexpr int kChunk = 4, kChunks = 3;           // scales come in chunks of 4 blocks, through a ring of their own
+constexpr int kGroupM = 8;                       // tiles of rows that are taken together (their a and the weights beside them stay in L2)
+// Registers: 384 threads start with 168; the epilogue's two warpgroups take 216 and leave 72 to the third
+// (128 * 72 + 256 * 216 = 384 * 168).
+constexpr int kRegsControl = 72, kRegsSums = 216;
+
+__device__ __forceinline__ uint32_t pair_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t at_first(uint32_t local) {   // the same place in the first CTA of the pair
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(local));
+  return r;
+}
+__device__ __forceinline__ void pair_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_load(uint32_t dst, const void *map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+// an arrival at this place in both CTAs once everything given to the tensor cores so far is done
+__device__ __forceinline__ void pair_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
+               : "memory");
+}
+__device__ __forceinline__ void store_box(const void *map, uint32_t from, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
+               ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(from) : "memory");
+}
+__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ void fma2(uint64_t &acc, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b)); }
+__device__ __forceinline__ float first_of(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float second_of(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ void store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// 4 bytes to shared memory without waiting; zeros where they are not wanted
+__device__ __forceinline__ void copy4(uint32_t to, const void *from, bool wanted) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(wanted ? 4 : 0) : "memory");
+}
+
+struct ManyArgs {
+  Mm8Args m;
+  int tiles_m, tiles_n;
+  int bulk;                // results may leave as bulk copies (their rows lie on 16 bytes)
+};
+
+// A warpgroup's box is written: it leaves for the columns from c0 on.
+__device__ __forceinline__ void copy_out(const ManyArgs &t, const CUtensorMap &map, uint32_t from, int c0, int row0, int g, int warp, int lane) {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory");
+  if ((warp & 3) == 0 && lane == 0 && c0 < t.m.n && row0 < t.m.n_rows) {
+    store_box(&map, from, c0, row0);
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
+}
+
+// tile `i` of the grid's order
+__device__ __forceinline__ void tile_of(const ManyArgs &t, int i, int &tm, int &tn) {
+  const int per = kGroupM * t.tiles_n, group = i / per, in = i - group * per, rows = min(kGroupM, t.tiles_m - group * kGroupM);
+  tn = in / rows;
+  tm = group * kGroupM + in - tn * rows;
+}
 
 template <int W>
 __global__ void __launch_bounds__(kThreads, 1)
 k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ CUtensorMap map_a,
-           const __grid_constant__ Mm8Args t) {
+           const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ManyArgs t) {
   extern __shared__ unsigned char raw[];
-  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_read[2], s_tail;
-  __shared__ float s_top[2][kM];
+  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_read[2], s_there[kChunks], s_used[kChunks], s_tail;
+  __shared__ float s_rows[kChunks][kChunk][128], s_weights[kChunks][kChunk][2];
+  __shared__ float s_top[2][128];
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t ring = (smem_at(raw) + 1023u) & ~1023u;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, rank = (int)pair_rank();
+  const uint32_t ring = (smem_at(raw) + 1023u) & ~1023u, out_at = ring + kStages * kStage;
   volatile int *gave_up = &s_gave_up;
-  // columns of the two halves: neighbouring blocks of weight rows, or the same block of the two matrices
-  const int half_n = W == 2 ? 0 : 128;
-  const int n0 = blockIdx.x * (W == 2 ? 128 : 256), row0 = blockIdx.y * kM;
+  const int n_kb = t.m.n_kb, tiles = t.tiles_m * t.tiles_n, pairs = gridDim.x >> 1, first = blockIdx.x >> 1;
+  const int wide = W == 2 ? 128 : 256;             // result columns of a tile
 
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(smem_at(&s_full[s]), 1); mbar_init(smem_at(&s_empty[s]), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(smem_at(&s_done[b]), 1); mbar_init(smem_at(&s_read[b]), 256); }
+    for (int b = 0; b < 2; ++b) { mbar_init(smem_at(&s_done[b]), 1); mbar_init(smem_at(&s_read[b]), 16); }
+    for (int c = 0; c < kChunks; ++c) { mbar_init(smem_at(&s_there[c]), 32); mbar_init(smem_at(&s_used[c]), 8); }
     mbar_init(smem_at(&s_tail), 1);
     s_gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&s_tmem)), "r"((uint32_t)kColumns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&s_tmem)), "r"((uint32_t)kColumns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
+  pair_sync();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   pdl_wait();
   pdl_trigger();
 
-  if (warp == 0) {
-    if (lane == 0) {
-      int issued = 0;
-      for (int b = 0; b < t.n_kb; ++b) {
-        const int s = b % kStages, fill = b / kStages;
-        if (fill > 0 && !mbar_wait(smem_at(&s_empty[s]), (uint32_t)((fill - 1) & 1), gave_up, t.wait_ns)) break;
-        const uint32_t full = smem_at(&s_full[s]), at = ring + (uint32_t)(s * kStage);
-        mbar_expect(full, kStage);
-        tma_rows8(at, &map_a, b * 128, row0, full);
-        tma_rows8(at + kBox, &map_w0, b * 128, n0, full);
-        tma_rows8(at + 2 * kBox, W == 2 ? &map_w1 : &map_w0, b * 128, n0 + half_n, full);
-        issued = b + 1;
-      }
-      if (*gave_up) {
-        const unsigned long long bound = t.wait_ns > kDrainFloorNs ? t.wait_ns : kDrainFloorNs;
-        for (int b = max(0, issued - kStages); b < issued; ++b)
-          mbar_wait(smem_at(&s_full[b % kStages]), (uint32_t)((b / kStages) & 1), gave_up, bound, false);
-      }
-    }
-    __syncwarp();
-  } else if (warp == 1) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = idesc_e4m3(kM, 256);
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsControl));
+    if (warp == 0) {
+      // ---------------------------------------------------------- copies: this CTA's rows, and its half of the weight rows
+      // (the whole warp runs the loops of this branch and the next, so that their arithmetic is the warp's and not a lane's)
+      const bool one = elect_one();
+      const void *map_w = W == 2 && rank == 1 ? &map_w1 : &map_w0;
+      int it = 0, s = 0, phase = 1;
       bool ok = true;
-      for (int b = 0; b < t.n_kb; ++b) {
-        const int s = b % kStages, buf = b & 1;
-        ok = b < 2 || mbar_wait(smem_at(&s_read[buf]), (uint32_t)(((b >> 1) - 1) & 1), gave_up, t.wait_ns);
-        if (ok) ok = mbar_wait(smem_at(&s_full[s]), (uint32_t)((b / kStages) & 1), gave_up, t.wait_ns);
-        if (!ok) break;
-        tc_fence_after();
-        const uint64_t ad = desc_rows8(ring + (uint32_t)(s * kStage)), bd = desc_rows8(ring + (uint32_t)(s * kStage + kBox));
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          tc_mma_e4m3(tmem + (uint32_t)(buf * 256), ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, k ? 1u : 0u);
-        tc_commit(smem_at(&s_empty[s]));
-        tc_commit(smem_at(&s_done[buf]));
-      }
-      if (!ok) {
-        tc_commit(smem_at(&s_tail));
-        mbar_wait(smem_at(&s_tail), 0u, gave_up, t.wait_ns > kDrainFloorNs ? t.wait_ns : kDrainFloorNs, false);
-      }
-    }
-    __syncwarp();
-  } else {
-    const int g = (warp - 2) >> 2, q = warp & 3;
-    const int row = row0 + q * 32 + lane;
-    const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(g * 64);
-    const bool live = row < t.n_rows;
-    const float *as = t.a_scale + (live ? (long long)row : 0) * t.a_scale_stride;
-    const int last_block = (t.n + 127) / 128 - 1;
-    const float *ws0 = t.w_scale[0] + (size_t)(n0 / 128) * t.n_kb;
-    const float *ws1 = W == 2 ? t.w_scale[1] + (size_t)(n0 / 128) * t.n_kb : t.w_scale[0] + (size_t)min(n0 / 128 + 1, last_block) * t.n_kb;
-    float acc[2][64];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < 64; ++i) acc[h][i] = 0.f;
-    for (int b = 0; b < t.n_kb; ++b) {
-      const int buf = b & 1;
-      const float sa = live ? __ldg(as + b) : 0.f, f[2] = {sa * __ldg(ws0 + b), sa * __ldg(ws1 + b)};
-      mbar_wait(smem_at(&s_done[buf]), (uint32_t)((b >> 1) & 1), gave_up, t.wait_ns);
-      __syncwarp();
-      tc_fence_after();
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int p = 0; p < 64; p += 32) {
-          uint32_t d[32];
-          tc_ld(lanes + (uint32_t)(buf * 256 + h * 128 + p), d);
-          tc_ld_wait();
-          if (h == 1 && p == 32) {
-            tc_fence_before();
-            mbar_arrive(smem_at(&s_read[buf]));
+      for (int i = first; i < tiles && ok; i += pairs) {
+        int tm, tn;
+        tile_of(t, i, tm, tn);
+        const int y_a = tm * 256 + rank * 128, y_w = W == 2 ? tn * 128 : tn * 256 + rank * 128;
+        for (int b = 0; b < n_kb; ++b, ++it) {
+          if (it >= kStages && !(ok = mbar_wait(smem_at(&s_empty[s]), (uint32_t)phase, gave_up, t.m.wait_tries))) break;
+          const uint32_t at = ring + (uint32_t)(s * kStage), full = at_first(smem_at(&s_full[s]));
+          if (one) {
+            if (rank == 0) mbar_expect(smem_at(&s_full[s]), 2 * kStage);
+            pair_load(at, &map_a, b * 128, y_a, full);
+            pair_load(at + kBox, map_w, b * 128, y_w, full);
           }
-#pragma unroll
-          for (int i = 0; i < 32; ++i) acc[h][p + i] = fmaf(__uint_as_float(d[i]), f[h], acc[h][p + i]);
+          if (++s == kStages) { s = 0; phase ^= 1; }
         }
       }
-    }
-    // ------------------------------------------------------------ results
-    if constexpr (W == 2) {
+      if (*gave_up && rank == 0) {   // copies in flight must land before either CTA's shared memory is given back
+        for (int j = max(0, it - kStages); j < it; ++j)
+          mbar_wait(smem_at(&s_full[j % kStages]), (uint32_t)((j / kStages) & 1), gave_up, max(t.m.wait_tries, kDrainTries), false);
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // ---------------------------------------------------------- products, by the first CTA
+      if (rank == 0) {
+        constexpr uint32_t idesc = idesc_e4m3(256, 256);
+        const bool one = elect_one();
+        bool ok = true;
+        int it = 0, s = 0, phase = 0;
+        for (int i = first; i < tiles && ok; i += pairs) {
+          for (int b = 0; b < n_kb; ++b, ++it) {
+            const int buf = it & 1;
+            ok = mbar_wait(smem_at(&s_full[s]), (uint32_t)phase, gave_up, t.m.wait_tries);
+            if (ok && it >= 2) ok = mbar_wait(smem_at(&s_read[buf]), (uint32_t)(((it >> 1) - 1) & 1), gave_up, t.m.wait_tries);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t ad = desc_rows8(ring + (uint32_t)(s * kStage)), bd = desc_rows8(ring + (uint32_t)(s * kStage + kBox));
+            if (one) {
 #pragma unroll
-      for (int i = 0; i < 64; ++i) acc[0][i] = gate_of(acc[0][i], acc[1][i]);
-      if (t.out_dtype == D3_E4M3) {   // the block of scales is 128 columns: two threads have a row's
+              for (int k = 0; k < 4; ++k)
+                pair_mma(tmem + (uint32_t)(buf * 256), ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, k ? 1u : 0u);
+              pair_commit(smem_at(&s_done[buf]));
+              pair_commit(smem_at(&s_empty[s]));
+            }
+            if (++s == kStages) { s = 0; phase ^= 1; }
+          }
+        }
+        if (!ok) {   // what was issued still reads shared memory and writes tensor memory
+          if (one) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(&s_tail)) : "memory");
+          mbar_wait(smem_at(&s_tail), 0u, gave_up, max(t.m.wait_tries, kDrainTries), false);
+        }
+      }
+      __syncwarp();
+    } else if (warp == 2) {
+      // ---------------------------------------------------------- scales: of this CTA's rows, and of both halves' weight rows
+      const int last_block = (t.m.n + 127) / 128 - 1;
+      int ch = 0;
+      bool ok = true;
+      for (int i = first; i < tiles && ok; i += pairs) {
+        int tm, tn;
+        tile_of(t, i, tm, tn);
+        const int row0 = tm * 256 + rank * 128, wb = tn * wide / 128;
+        const float *ws[2] = {t.m.w_scale[0] + (size_t)wb * n_kb,
+                              W == 2 ? t.m.w_scale[1] + (size_t)wb * n_kb : t.m.w_scale[0] + (size_t)min(wb + 1, last_block) * n_kb};
+        for (int b = 0; b < n_kb; b += kChunk, ++ch) {
+          const int c = ch % kChunks, fill = ch / kChunks;
+          if (fill > 0 && !(ok = mbar_wait(smem_at(&s_used[c]), (uint32_t)((fill - 1) & 1), gave_up, t.m.wait_tries))) break;
+          const int kb = b + (lane & 3);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {       // 4 blocks of 8 rows at a time; what is behind the end is zeros
+            const int r = e * 8 + (lane >> 2);
+            const bool in = kb < n_kb && row0 + r < t.m.n_rows;
+            copy4(smem_at(&s_rows[c][lane & 3][r]), t.m.a_scale + (in ? (long long)(row0 + r) * t.m.a_scale_stride + kb : 0ll), in);
+          }
+          if (lane < 2 * kChunk) copy4(smem_at(&s_weights[c][lane & 3][lane >> 2]), ws[lane >> 2] + min(kb, n_kb - 1), true);
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_at(&s_there[c])) : "memory");
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+  } else {
+    // ------------------------------------------------------------ sums
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSums));
+    const int g = (warp - 4) >> 2, q = warp & 3, r = q * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(g * 64);
+    const uint32_t read_bar[2] = {at_first(smem_at(&s_read[0])), at_first(smem_at(&s_read[1]))};
+    const int dtype = t.m.out_dtype, es = dtype == D3_FP32 ? 4 : dtype == D3_E4M3 ? 1 : 2;
+    int it = 0, ch = 0;
+    for (int i = first; i < tiles; i += pairs) {
+      int tm, tn;
+      tile_of(t, i, tm, tn);
+      const int row0 = tm * 256 + rank * 128, row = row0 + r, n0 = tn * wide;
+      const bool live = row < t.m.n_rows;
+      uint64_t acc[2][32];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) acc[h][j] = 0ull;
+      for (int b = 0; b < n_kb; ++b, ++it) {
+        const int buf = it & 1;
+        const int in = b % kChunk, c = ch % kChunks;
+        if (in == 0) mbar_wait(smem_at(&s_there[c]), (uint32_t)((ch / kChunks) & 1), gave_up, t.m.wait_tries);
+        const float sa = s_rows[c][in][r], f0 = sa * s_weights[c][in][0], f1 = sa * s_weights[c][in][1];
+        if (in == kChunk - 1 || b == n_kb - 1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_at(&s_used[c]));
+          ++ch;
+        }
+        const uint64_t f[2] = {pair_of(__float_as_uint(f0), __float_as_uint(f0)), pair_of(__float_as_uint(f1), __float_as_uint(f1))};
+        mbar_wait(smem_at(&s_done[buf]), (uint32_t)((it >> 1) & 1), gave_up, t.m.wait_tries);   // (given up: numbers without meaning)
+        __syncwarp();
+        tc_fence_after();
+        uint32_t d[2][32];
+        tc_ld(lanes + (uint32_t)(buf * 256), d[0]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {        // 32 columns: halves 0, 0, 1, 1
+          tc_ld_wait(d[c & 1]);
+          if (c < 3) {
+            tc_ld(lanes + (uint32_t)(buf * 256 + ((c + 1) >> 1) * 128 + ((c + 1) & 1) * 32), d[(c + 1) & 1]);
+          } else {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) pair_arrive(read_bar[buf]);
+          }
+#pragma unroll
+          for (int j = 0; j < 16; ++j) fma2(acc[c >> 1][(c & 1) * 16 + j], pair_of(d[c & 1][2 * j], d[c & 1][2 * j + 1]), f[c >> 1]);
+        }
+      }
+      // ---------------------------------------------------------- results
+      if constexpr (W == 2) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          acc[0][j] = pair_of(__float_as_uint(gate_of(first_of(acc[0][j]), first_of(acc[1][j]))),
+                              __float_as_uint(gate_of(second_of(acc[0][j]), second_of(acc[1][j]))));
+      }
+      // what the last tile left must be out of the staging area
+      if (t.bulk) {
+        if ((warp & 3) == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        if (W == 2 && dtype == D3_E4M3) asm volatile("bar.sync 3, 256;" ::: "memory");
+        else asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory");
+      }
+      if (W == 2 && dtype == D3_E4M3) {   // the block of scales is 128 columns: two threads have a row's
+        const int c0 = n0 + g * 64;
         float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 64; ++i)
-          if (n0 + g * 64 + i < t.n) top = max_nan(top, fabsf(acc[0][i]));
-        s_top[g][q * 32 + lane] = top;
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        top = max_nan(top, s_top[g ^ 1][q * 32 + lane]);
+        for (int j = 0; j < 32; ++j) {
+          if (c0 + 2 * j < t.m.n) top = max_nan(top, fabsf(first_of(acc[0][j])));
+          if (c0 + 2 * j + 1 < t.m.n) top = max_nan(top, fabsf(second_of(acc[0][j])));
+        }
+        s_top[g][r] = top;
+        asm volatile("bar.sync 3, 256;" ::: "memory");
+        top = max_nan(top, s_top[g ^ 1][r]);
         float inverse;
         const float scale = block_scale(top, inverse);
-        if (live) {
-          if (g == 0) t.scale[row * t.scale_stride + n0 / 128] = scale;
-          unsigned char *o = static_cast<unsigned char *>(t.out) + row * t.out_stride + n0 + g * 64;
+        if (live && g == 0) t.m.scale[row * t.m.scale_stride + n0 / 128] = scale;
+        uint32_t v[16];
 #pragma unroll
-          for (int i = 0; i < 64; i += 4) {
-            const uint32_t v = pack_e4m3(acc[0][i] * inverse, acc[0][i + 1] * inverse, acc[0][i + 2] * inverse, acc[0][i + 3] * inverse);
-            if (t.out_wide && n0 + g * 64 + i + 3 < t.n) {
-              *reinterpret_cast<uint32_t *>(o + i) = v;
-            } else {
+        for (int j = 0; j < 16; ++j)
+          v[j] = pack_e4m3(first_of(acc[0][2 * j]) * inverse, second_of(acc[0][2 * j]) * inverse, first_of(acc[0][2 * j + 1]) * inverse,
+                           second_of(acc[0][2 * j + 1]) * inverse);
+        if (t.bulk) {                     // one box: rows of 128 bytes in the 128-byte swizzle
 #pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (n0 + g * 64 + i + j < t.n) o[i + j] = (unsigned char)(v >> (8 * j));
+          for (int j = 0; j < 4; ++j)
+            store16(out_at + (uint32_t)(r * 128 + (((g * 4 + j) ^ (r & 7)) << 4)), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          asm volatile("bar.sync 3, 256;" ::: "memory");
+          if (warp == 4 && lane == 0 && row0 < t.m.n_rows) {
+            store_box(&map_out, out_at, n0, row0);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        } else {
+          if (live) {
+            unsigned char *o = static_cast<unsigned char *>(t.m.out) + row * t.m.out_stride + c0;
+#pragma unroll
+            for (int j = 0; j < 64; ++j)
+              if (c0 + j < t.m.n) o[j] = (unsigned char)(v[j >> 2] >> (8 * (j & 3)));
+          }
+          asm volatile("bar.sync 3, 256;" ::: "memory");   // s_top is written again
+        }
+      } else {
+        const uint32_t mine = out_at + (uint32_t)(g * (kOutBytes / 2));
+#pragma unroll
+        for (int h = 0; h < (W == 2 ? 1 : 2); ++h) {
+          const int c0 = n0 + h * 128 + g * 64;
+          if (t.bulk) {
+            if (h == 1) {                 // the second half takes the first one's place
+              if ((warp & 3) == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+              asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory");
             }
+            if (es == 2) {                // a box of 64 columns: rows of 128 bytes
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                uint32_t v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = pack2(first_of(acc[h][4 * j + e]), second_of(acc[h][4 * j + e]), dtype);
+                store16(mine + (uint32_t)(r * 128 + ((j ^ (r & 7)) << 4)), v[0], v[1], v[2], v[3]);
+              }
+              copy_out(t, map_out, mine, c0, row0, g, warp, lane);
+            } else {                      // boxes of 32 columns, one behind the other
+#pragma unroll
+              for (int part = 0; part < 2; ++part) {
+                if (part == 1) {
+                  if ((warp & 3) == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                  asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory");
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  store16(mine + (uint32_t)(r * 128 + ((j ^ (r & 7)) << 4)), (uint32_t)acc[h][16 * part + 2 * j], (uint32_t)(acc[h][16 * part + 2 * j] >> 32),
+                          (uint32_t)acc[h][16 * part + 2 * j + 1], (uint32_t)(acc[h][16 * part + 2 * j + 1] >> 32));
+                copy_out(t, map_out, mine, c0 + 32 * part, row0, g, warp, lane);
+              }
+            }
+          } else if (live) {
+#pragma unroll
+            for (int j = 0; j < 64; ++j)
+              if (c0 + j < t.m.n) store1(t.m.out, row * t.m.out_stride + c0 + j, dtype, (j & 1) ? second_of(acc[h][j >> 1]) : first_of(acc[h][j >> 1]));
           }
         }
       }
     }
-    if (live && t.out_dtype != D3_E4M3) {
-#pragma unroll
-      for (int h = 0; h < (W == 2 ? 1 : 2); ++h) {
-#pragma unroll
-        for (int i = 0; i < 64; i += 4) {
-          const int c = n0 + h * 128 + g * 64 + i;
-          const long long at = row * t.out_stride + c;
-          if (t.out_wide && c + 3 < t.n) {
-            if (t.out_dtype == D3_FP32)
-              *reinterpret_cast<float4 *>(static_cast<float *>(t.out) + at) = make_float4(acc[h][i], acc[h][i + 1], acc[h][i + 2], acc[h][i + 3]);
-            else
-              *reinterpret_cast<uint2 *>(static_cast<char *>(t.out) + 2 * at) =
-                  make_uint2(pack2(acc[h][i], acc[h][i + 1], t.out_dtype), pack2(acc[h][i + 2], acc[h][i + 3], t.out_dtype));
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (c + j < t.n) store1(t.out, at + j, t.out_dtype, acc[h][i + j]);
-          }
-        }
-      }
-    }
+    if ((warp & 3) == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
-  if (tid == 0 && *gave_up && t.status) *t.status = D3_ETIMEOUT;
-  tc_fence_before();
   __syncthreads();
+  if (tid == 0 && *gave_up && t.m.status) *t.m.status = D3_ETIMEOUT;
+  tc_fence_before();
+  pair_sync();   // neither CTA goes while the other one's products read its shared memory or arrive at its barriers
   if (warp == 1)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kColumns) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kColumns) : "memory");
 }
 
 template <int W>
@@ -202,24 +383,50 @@ cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, Mm8Args &p, c
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  constexpr int smem = kStages * kStage + 1024;
-  static std::atomic<bool> ready[64];
-  if (!ready[dev].load(std::memory_order_acquire)) {
-    if ((e = cudaFuncSetAttribute(k_mm8_many<W>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return e;
-    ready[dev].store(true, std::memory_order_release);
+  static std::atomic<int> sms[64];   // SMs of a device whose attribute is set (setting it twice is harmless)
+  int n_sm = sms[dev].load(std::memory_order_acquire);
+  if (n_sm == 0) {
+    if ((e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(k_mm8_many<W>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem)) != cudaSuccess) return e;
+    sms[dev].store(n_sm, std::memory_order_release);
   }
+  ManyArgs t;
+  t.m = p;
   const int wide = W == 2 ? 128 : 256;
+  t.tiles_m = (p.n_rows + 255) / 256;
+  t.tiles_n = (p.n + wide - 1) / wide;
+  const long long tiles = (long long)t.tiles_m * t.tiles_n;
+  if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
+  // results as bulk copies: boxes of 128 bytes x 128 rows
+  TMap mo = ma;
+  const int es = type_bytes(p.out_dtype);
+  t.bulk = on_bytes(p.out, 16) && (p.out_stride * es) % 16 == 0 && encode_results8(&mo, p.out, p.n_rows, p.n, p.out_dtype, p.out_stride);
+  const long long pairs = tiles < n_sm / 2 ? tiles : n_sm / 2;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((unsigned)(2 * pairs));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
   const CUtensorMap *m0 = reinterpret_cast<const CUtensorMap *>(&w0), *m1 = reinterpret_cast<const CUtensorMap *>(&w1),
-                    *m = reinterpret_cast<const CUtensorMap *>(&ma);
-  return launch_pdl(k_mm8_many<W>, dim3((unsigned)((p.n + wide - 1) / wide), (unsigned)((p.n_rows + kM - 1) / kM)), dim3(kThreads), smem, st,
-                    *m0, *m1, *m, p);
+                    *m = reinterpret_cast<const CUtensorMap *>(&ma), *out = reinterpret_cast<const CUtensorMap *>(&mo);
+  return cudaLaunchKernelEx(&cfg, k_mm8_many<W>, *m0, *m1, *m, *out, static_cast<const ManyArgs>(t));
 }
 
 }  // namespace
 
 cudaError_t launch_mm8_many(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, Mm8Args &p, cudaStream_t st) {
   TMap ma;
-  if (!encode_rows8(&ma, a, p.n_rows, p.k, a_stride, kM)) return cudaErrorInvalidValue;
+  if (!encode_rows8(&ma, a, p.n_rows, p.k, a_stride, 128)) return cudaErrorInvalidValue;
   return w1 ? launch<2>(w0, *w1, ma, p, st) : launch<1>(w0, w0, ma, p, st);
 }
 
