@@ -236,8 +236,18 @@ __device__ __forceinline__ void tc_ld_wait(uint32_t (&r)[32]) {
                  "+r"(r[30]), "+r"(r[31])
                :: "memory");
 }
-// silu(g) * u (an exp(-g) that is infinite makes it 0; g = -inf gives NaN)
-__device__ __forceinline__ float gate_of(float g, float u) { return g / (1.f + expf(-g)) * u; }
+// silu(g) * u = g / (1 + exp(-g)) * u, with 2^x and 1/x of the special function unit.  2^x is as good as its argument: the product
+// -g log2(e) is rounded, by up to 2^-20 where |g| is 16, so what the rounding left out, which a fused multiply-add gives, is put
+// back by 2^(hi + lo) = 2^hi (1 + lo ln 2) (log2(e) itself in 32 bits is 2^-26 off: 2^-22 at 16).  An exp(-g) that is infinite gives 0.
+__device__ __forceinline__ float gate_of(float g, float u) {
+  constexpr float kLog2e = 1.44269504f;
+  const float hi = g * -kLog2e, lo = fmaf(g, -kLog2e, -hi);
+  float t, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(hi));
+  if (fabsf(hi) < 126.f) t = fmaf(t, lo * 0.693147181f, t);      // (beyond, t is next to 0 or to infinity, and lo may be NaN)
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + t));
+  return g * r * u;
+}
 // A warp has the 128 results of a row that one tile of weight rows gives, lane l those at n0 = 128 tile + 4 l: rounds and writes
 // them, in 8 bits with the block's scale or in a wider type.  What is behind the last column counts and writes nothing.
 __device__ __forceinline__ void finish4(const Mm8Args &t, long long row, int n0, const float (&y)[4], int tile, int lane) {

@@ -109,7 +109,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
            const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ManyArgs t) {
   extern __shared__ unsigned char raw[];
   __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_read[2], s_there[kChunks], s_used[kChunks], s_tail;
-  __shared__ float s_rows[kChunks][kChunk][128], s_weights[kChunks][kChunk][2];
+  __shared__ __align__(8) float s_rows[kChunks][kChunk][128], s_weights[kChunks][kChunk][2];
   __shared__ float s_top[2][128];
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
@@ -234,7 +234,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
     const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(g * 64);
     const uint32_t read_bar[2] = {at_first(smem_at(&s_read[0])), at_first(smem_at(&s_read[1]))};
     const int dtype = t.m.out_dtype, es = dtype == D3_FP32 ? 4 : dtype == D3_E4M3 ? 1 : 2;
-    int it = 0, ch = 0;
+    int it = 0, chunk = 0, there = 0;
     for (int i = first; i < tiles; i += pairs) {
       int tm, tn;
       tile_of(t, i, tm, tn);
@@ -245,22 +245,31 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < 32; ++j) acc[h][j] = 0ull;
-      for (int b = 0; b < n_kb; ++b, ++it) {
-        const int buf = it & 1;
-        const int in = b % kChunk, c = ch % kChunks;
-        if (in == 0) mbar_wait(smem_at(&s_there[c]), (uint32_t)((ch / kChunks) & 1), gave_up, t.m.wait_tries);
-        const float sa = s_rows[c][in][r], f0 = sa * s_weights[c][in][0], f1 = sa * s_weights[c][in][1];
+      // the scales of block b: this row's, and those of the two halves' weights
+      float sa;
+      float2 sw;
+      auto next_scales = [&](int b) {
+        const int in = b % kChunk;
+        if (in == 0) mbar_wait(smem_at(&s_there[chunk]), (uint32_t)there, gave_up, t.m.wait_tries);
+        sa = s_rows[chunk][in][r];
+        sw = *reinterpret_cast<const float2 *>(s_weights[chunk][in]);
         if (in == kChunk - 1 || b == n_kb - 1) {
           __syncwarp();
-          if (lane == 0) mbar_arrive(smem_at(&s_used[c]));
-          ++ch;
+          if (lane == 0) mbar_arrive(smem_at(&s_used[chunk]));
+          if (++chunk == kChunks) { chunk = 0; there ^= 1; }
         }
+      };
+      next_scales(0);
+      for (int b = 0; b < n_kb; ++b, ++it) {
+        const int buf = it & 1;
+        const float f0 = sa * sw.x, f1 = sa * sw.y;
         const uint64_t f[2] = {pair_of(__float_as_uint(f0), __float_as_uint(f0)), pair_of(__float_as_uint(f1), __float_as_uint(f1))};
         mbar_wait(smem_at(&s_done[buf]), (uint32_t)((it >> 1) & 1), gave_up, t.m.wait_tries);   // (given up: numbers without meaning)
         __syncwarp();
         tc_fence_after();
         uint32_t d[2][32];
         tc_ld(lanes + (uint32_t)(buf * 256), d[0]);
+        if (b + 1 < n_kb) next_scales(b + 1);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {        // 32 columns: halves 0, 0, 1, 1
           tc_ld_wait(d[c & 1]);
@@ -293,8 +302,8 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
         float top = 0.f;
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-          if (c0 + 2 * j < t.m.n) top = max_nan(top, fabsf(first_of(acc[0][j])));
-          if (c0 + 2 * j + 1 < t.m.n) top = max_nan(top, fabsf(second_of(acc[0][j])));
+          top = max_nan(top, fabsf(first_of(acc[0][j])));     // (columns behind the last one are of zero weights)
+          top = max_nan(top, fabsf(second_of(acc[0][j])));
         }
         s_top[g][r] = top;
         asm volatile("bar.sync 3, 256;" ::: "memory");
