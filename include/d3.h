@@ -603,7 +603,7 @@ int32_t d3_matmul8(const d3_weight8 *w, const d3_matmul8_args *a, void *cuda_str
 int32_t d3_gated_matmul8(const d3_weight8 *gate, const d3_weight8 *up, const d3_matmul8_args *a, void *cuda_stream);
 
 /* Row by row, z the row's logits in fp32, each step rounded once:
- *   of a token among the first lengths[row] of history[row]:  z = z > 0 ? z / repetition : z * repetition
+ *   of a token among the first lengths[row] of history[row]:  z *= z > 0 ? 1 / repetition : repetition
  *   of one that occurs c > 0 times behind the first prompt[row] of them:  z -= frequency * c,  then z -= presence
  *   of a token in bias_ids[row]:  z += bias (of an id that is there twice the later entry counts)
  *   of a token whose bit in masks[mask_of[row]] is 0:  z = -inf, whatever it was

@@ -222,7 +222,8 @@ def test_no_rows():
 # -------------------------------------------------------------------------------------------- logits
 def logits_form(z, history=None, lengths=None, prompt=None, repetition=None, frequency=None, presence=None, bias_ids=None, bias=None, masks=None,
                 mask_of=None):
-    """Row by row in 64 bits: (values, how far fp32 may be off: a rounding for each of five steps, of the numbers that take part)."""
+    """Row by row in 64 bits: (values, how far fp32 may be off: a rounding for each of six steps (1 / repetition is one), of
+    the numbers that take part)."""
     y = z.double().cpu().clone()
     size = y.abs()
     rows, vocab = y.shape
@@ -255,7 +256,7 @@ def logits_form(z, history=None, lengths=None, prompt=None, repetition=None, fre
             for t in range(vocab):
                 if not (words[t // 32] >> (t % 32)) & 1:
                     y[b, t] = float("-inf")
-    return y, size * 5 * 2.0 ** -24
+    return y, size * 6 * 2.0 ** -24
 
 
 def check_logits(out, token, y, dy):
@@ -299,13 +300,25 @@ def test_logits(rows, vocab, n, m, states, dtype):
     y, dy = logits_form(z, **kw)
     out, token = K.d3_constrain_logits(z, **kw)
     check_logits(out, token, y, dy)
-    buf, view = strided(rows, vocab, dtype, 8)
-    view.copy_(z)
-    out2, token2 = K.d3_constrain_logits(view, out=view, **kw)
-    assert torch.equal(view, out) and torch.equal(token, token2)
-    rest = buf.clone()
-    rest[:rows, :vocab] = 7
-    assert (rest == 7).all()
+    for extra in (8, 1, 3):                  # in place, and from rows that start anywhere to rows that start elsewhere
+        buf, view = strided(rows, vocab, dtype, extra)
+        view.copy_(z)
+        other, there = (buf, view) if extra != 3 else strided(rows, vocab, dtype, 6)
+        out2, token2 = K.d3_constrain_logits(view, out=there, **kw)
+        assert torch.equal(there, out) and torch.equal(token, token2)
+        rest = other.clone()
+        rest[:rows, :vocab] = 7
+        assert (rest == 7).all()
+
+
+@pytest.mark.parametrize("n,m", [(32767, 3), (32768, 3), (5, 65535), (5, 65536), (70000, 70000)])
+def test_logits_with_long_lists(n, m):
+    z, kw = some_logits(2, 9000, n, m, 2, FP32, n + m)
+    kw["history"][1] = 17                    # one token, as often as the row is long
+    kw["lengths"][:] = n
+    kw["prompt"][:] = torch.tensor([n // 2, 0], dtype=torch.int32)
+    y, dy = logits_form(z, **kw)
+    check_logits(*K.d3_constrain_logits(z, **kw), y, dy)
 
 
 def test_logits_that_are_not_numbers_and_ties():
