@@ -255,7 +255,6 @@ int32_t product(const d3_weight8 *const (&w)[2], const d3_matmul8_args *a, cudaS
   p.a_scale = a->a_scale_dev; p.a_scale_stride = rows > 1 ? a->a_scale_stride : kb;
   p.w_scale[0] = w[0]->scale_dev; p.w_scale[1] = mats == 2 ? w[1]->scale_dev : nullptr;
   p.out = a->out_dev; p.out_stride = rows > 1 ? a->out_stride : n; p.out_dtype = a->out_dtype;
-  p.out_wide = on_bytes(a->out_dev, 4 * es) && (p.out_stride % 4 == 0 || rows == 1);
   p.scale = a->scale_dev; p.scale_stride = rows > 1 ? a->scale_stride : nb;
   p.status = a->status_dev;
   p.wait_tries = kWaitTries;

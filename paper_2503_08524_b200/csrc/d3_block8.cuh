@@ -67,16 +67,15 @@ struct Mm8Args {
   const float *w_scale[2];           // [ceil(n / 128)][n_kb]
   void *out;
   long long out_stride;
-  int out_dtype, out_wide;           // out_wide: four results at a time may be written in one piece
+  int out_dtype;
   float *scale;
   long long scale_stride;
   int32_t *status;
   uint32_t wait_tries;
-  int n_stages, split;               // few rows: CTAs that share a tile's k blocks, as a cluster
 };
-// each enqueues one kernel; cudaSuccess or what the launch said
-cudaError_t launch_mm8_few(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, Mm8Args &p, cudaStream_t st);
-cudaError_t launch_mm8_many(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, Mm8Args &p, cudaStream_t st);
+// each enqueues one kernel; cudaSuccess or what the launch said (w1: the second matrix of the gated form)
+cudaError_t launch_mm8_few(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, const Mm8Args &p, cudaStream_t st);
+cudaError_t launch_mm8_many(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, const Mm8Args &p, cudaStream_t st);
 constexpr int kFewRows = 128;        // rows that the kernel for few rows takes
 
 // ------------------------------------------------------------------ device
@@ -181,6 +180,10 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
   return r;
 }
+// 4 bytes to shared memory without waiting
+__device__ __forceinline__ void copy4(uint32_t to, const void *from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
 __device__ __forceinline__ void tma_rows8(uint32_t dst, const void *map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
@@ -203,6 +206,15 @@ __device__ __forceinline__ void tc_mma_e4m3(uint32_t d, uint64_t a, uint64_t b, 
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+// two floats in a register pair, multiplied and added by one instruction
+__device__ __forceinline__ uint64_t two_of(uint32_t low, uint32_t high) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(low), "r"(high));
+  return r;
+}
+__device__ __forceinline__ void fma_two(uint64_t &acc, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b)); }
+__device__ __forceinline__ float low_of(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float high_of(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
 // 16 or 32 accumulator columns of this thread's lane, to be read behind tc_ld_wait only
 __device__ __forceinline__ void tc_ld(uint32_t at, uint32_t (&r)[16]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -247,38 +259,6 @@ __device__ __forceinline__ float gate_of(float g, float u) {
   if (fabsf(hi) < 126.f) t = fmaf(t, lo * 0.693147181f, t);      // (beyond, t is next to 0 or to infinity, and lo may be NaN)
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + t));
   return g * r * u;
-}
-// A warp has the 128 results of a row that one tile of weight rows gives, lane l those at n0 = 128 tile + 4 l: rounds and writes
-// them, in 8 bits with the block's scale or in a wider type.  What is behind the last column counts and writes nothing.
-__device__ __forceinline__ void finish4(const Mm8Args &t, long long row, int n0, const float (&y)[4], int tile, int lane) {
-  const long long at = row * t.out_stride + n0;
-  if (t.out_dtype == D3_E4M3) {
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (n0 + i < t.n) top = max_nan(top, fabsf(y[i]));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float inverse;
-    const float scale = block_scale(top, inverse);
-    if (lane == 0) t.scale[row * t.scale_stride + tile] = scale;
-    const uint32_t q = pack_e4m3(y[0] * inverse, y[1] * inverse, y[2] * inverse, y[3] * inverse);
-    unsigned char *o = static_cast<unsigned char *>(t.out) + at;
-    if (t.out_wide && n0 + 3 < t.n) {
-      *reinterpret_cast<uint32_t *>(o) = q;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (n0 + i < t.n) o[i] = (unsigned char)(q >> (8 * i));
-    }
-  } else if (t.out_wide && n0 + 3 < t.n) {
-    if (t.out_dtype == D3_FP32) *reinterpret_cast<float4 *>(static_cast<float *>(t.out) + at) = make_float4(y[0], y[1], y[2], y[3]);
-    else *reinterpret_cast<uint2 *>(static_cast<char *>(t.out) + 2 * at) = make_uint2(pack2(y[0], y[1], t.out_dtype), pack2(y[2], y[3], t.out_dtype));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (n0 + i < t.n) store1(t.out, at + i, t.out_dtype, y[i]);
-  }
 }
 #endif
 

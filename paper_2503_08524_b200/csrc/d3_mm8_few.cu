@@ -2,15 +2,26 @@
 //
 //   y[row][r] = sum_b as[row][b] ws[r / 128][b] sum_{k in block b} a[row][k] w[r][k]
 //
-// Few rows leave 2 * rows flops for a byte of weight: the kernel is bound by reading the weights once.  The weight tile is
-// the tensor core's 128-row operand (M), the rows are its narrow one (N = 16..128, rows beyond n_rows are zeros), so a
-// block of 128 k is four tcgen05.mma and its sum, 128 x N in tensor memory, is small: the epilogue threads (one weight row
-// each) fetch it, multiply by the two scales and add it to registers while the next block is multiplied.
+// Few rows leave 2 * rows flops for a byte of weight: the kernel is bound by reading the weights once.  A tile of 128 weight rows is
+// the tensor core's M and the rows of the call are its N (16..128, rows beyond n_rows are zeros): all 128 lanes of the sums
+// are in use, and an epilogue thread (one weight row) has no more columns than there are rows.  (With the rows as M, tiles can be as
+// narrow as 16 weight rows and k need not be cut, but an instruction takes 40 cycles for its 128 lanes whatever its N, and
+// one warp has all the sums to fetch: 32 rows, 11008 -> 4096, took 15 us.)
 //
-// A CTA takes one tile of 128 weight rows (two matrices' tiles for the gated form) and a share of the k blocks; the CTAs of
-// a tile are a cluster, whose sums meet in distributed shared memory in the order of their ranks.  Every CTA of the
-// cluster finishes every split-th row: a warp has the 128 results of a row, four neighbouring ones a lane, which is also
-// one block of scales where the result goes to 8 bits.
+// A block of 128 k is four tcgen05.mma.  Every block has scales of its own, so its sum is fetched from tensor memory, multiplied by
+// the two scales and added to registers; that is handed over a unit of U blocks at a time, while the next unit is
+// multiplied into the other half of the tensor memory.
+//
+// A CTA has one tile (gated: of both matrices).  Some 96 of them keep the memory busy; where there are fewer, k is cut between the
+// CTAs of a cluster, whose sums meet in distributed shared memory in the order of their ranks.  More CTAs cost more than they
+// give (clusters are started one after another).  us by the number of CTAs: 1 row, 4096 -> 12288: 96 11.9, 192 12.8, 288 17.6;
+// 32 rows, 11008 -> 4096: 32 24.4, 64 16.0, 128 12.5, 256 13.7; 4 rows, 8192 -> 10240: 80 19.6, 160 17.1, 320 21.8; gated,
+// 8 rows, 5120 -> 13824: 108 25.9, 216 26.3.
+//
+// What is left over the time of the weights at the memory's rate is some 4 us a call: the last sums and results 1.2, the step from
+// one call to the next 1 to 1.4, the first copies' way 1.5.  A CTA takes at most half of an SM (but for more than 64 rows),
+// so the next call's CTAs are set up beside it.  Letting them ask for weights ahead of their turn gave nothing (copies
+// into the ring 12.5 us where this takes 11.9) or cost (into L2 box by box 14.0, row by row 18.4).
 #include <atomic>
 
 #include "d3_block8.cuh"
@@ -19,10 +30,11 @@ namespace d3 {
 
 namespace {
 
-constexpr int kTileBytes = 128 * 128;      // a stage's share of a weight matrix
-constexpr int kMaxStages = 8;
-constexpr int kScaleChunk = 8;             // k blocks whose scales are staged at a time
-constexpr int kPairSmem = 113 * 1024 - 512;   // two CTAs of an SM side by side
+constexpr int kTileBytes = 128 * 128;            // a block's share of a weight matrix
+constexpr int kMaxStages = 12;
+constexpr int kChunk = 8, kChunks = 3;           // scales come in chunks of 8 blocks, through a ring of their own
+constexpr int kMostSplit = 8, kEnoughTiles = 96;
+constexpr int kHalfSmem = 112 * 1024, kWholeSmem = 213 * 1024;      // dynamic shared memory, of one of two CTAs on an SM or a CTA alone
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -39,48 +51,99 @@ __device__ __forceinline__ float4 cluster_load4(uint32_t at, uint32_t rank) {
   asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
   return v;
 }
+__device__ __forceinline__ uint64_t mul_two(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 
-// C: rows (accumulator columns) of an epilogue thread, G: warpgroups that share the rows, W: weight matrices (2: gated)
-template <int C, int G, int W>
+// C: rows (accumulator columns) of an epilogue thread, G: warpgroups that share the rows, W: weight matrices (2: gated), U: blocks of a unit
+template <int C, int G, int W, int U>
 struct Few {
   static constexpr int N = C * G;                              // padded rows
-  static constexpr int kThreads = 64 + 128 * G;
-  static constexpr int kBuffers = N * W <= 64 ? 4 : 2;         // of sums in tensor memory: 64 to 256 columns, 512 with N W = 256
-  static constexpr int kColumns = kBuffers * N * W;
-  static constexpr int kStage = W * kTileBytes + N * 128;
+  static constexpr int kThreads = 128 + 128 * G;               // copies, products, scales, an idle warp; epilogue warps
+  static constexpr int kColumns = U * W * N;                   // accumulator columns of a unit, of which there are two
+  static constexpr bool kHalf = 2 * kColumns <= 256;           // two CTAs fit on an SM
+  static constexpr int kStage = W * kTileBytes + N * 128;      // a block
   static constexpr int kSums = W * N * 128 * 4;                // one CTA's sums, over the ring when it is empty
-  static constexpr int kScales = 2 * kScaleChunk * (N + W) * 4;   // the rows' scales and the weights', two chunks
+  // 256 threads start with 128 registers, 384 with 168; the epilogue takes 200 (216) of them and leaves 56 (72) to the others
+  // (128 * 56 + 128 * 200 = 256 * 128, 128 * 72 + 256 * 216 = 384 * 168)
+  static constexpr int kRegsControl = G == 1 ? 56 : 72, kRegsSums = G == 1 ? 200 : 216;
+  static_assert(kColumns <= 256, "tensor memory");
 };
 
-template <int C, int G, int W>
-__global__ void __launch_bounds__(Few<C, G, W>::kThreads)
+struct FewArgs {
+  Mm8Args m;
+  int stages, split;
+  int wide;                // four results at a time may be written in one piece
+};
+
+// A warp has the 128 results of a row that one tile of weight rows gives, lane l those at n0 = 128 tile + 4 l: rounds and writes
+// them, in 8 bits with the block's scale or in a wider type.  What is behind the last column counts and writes nothing.
+__device__ __forceinline__ void finish4(const FewArgs &t, long long row, int n0, const float (&y)[4], int tile, int lane) {
+  const Mm8Args &m = t.m;
+  const long long at = row * m.out_stride + n0;
+  if (m.out_dtype == D3_E4M3) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n0 + i < m.n) top = max_nan(top, fabsf(y[i]));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float inverse;
+    const float scale = block_scale(top, inverse);
+    if (lane == 0) m.scale[row * m.scale_stride + tile] = scale;
+    const uint32_t q = pack_e4m3(y[0] * inverse, y[1] * inverse, y[2] * inverse, y[3] * inverse);
+    unsigned char *o = static_cast<unsigned char *>(m.out) + at;
+    if (t.wide && n0 + 3 < m.n) {
+      *reinterpret_cast<uint32_t *>(o) = q;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (n0 + i < m.n) o[i] = (unsigned char)(q >> (8 * i));
+    }
+  } else if (t.wide && n0 + 3 < m.n) {
+    if (m.out_dtype == D3_FP32) *reinterpret_cast<float4 *>(static_cast<float *>(m.out) + at) = make_float4(y[0], y[1], y[2], y[3]);
+    else *reinterpret_cast<uint2 *>(static_cast<char *>(m.out) + 2 * at) = make_uint2(pack2(y[0], y[1], m.out_dtype), pack2(y[2], y[3], m.out_dtype));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n0 + i < m.n) store1(m.out, at + i, m.out_dtype, y[i]);
+  }
+}
+
+template <int C, int G, int W, int U>
+__global__ void __launch_bounds__(Few<C, G, W, U>::kThreads, G == 1 ? 2 : 1)
 k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ CUtensorMap map_a,
-          const __grid_constant__ Mm8Args t) {
-  using F = Few<C, G, W>;
+          const __grid_constant__ FewArgs t) {
+  using F = Few<C, G, W, U>;
   constexpr int N = F::N;
   extern __shared__ unsigned char raw[];
-  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[F::kBuffers], s_read[F::kBuffers], s_tail;
+  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[2], s_read[2], s_there[kChunks], s_used[kChunks], s_tail;
+  __shared__ __align__(16) float s_rows[kChunks][kChunk][N], s_weights[kChunks][kChunk][2];
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const int S = t.n_stages, split = t.split;
-  const int tile = blockIdx.x / split, rank = split > 1 ? (int)cluster_rank() : 0;
-  const int row0 = blockIdx.y * N;                             // first row of the call that this CTA multiplies
-  const int b0 = (int)((long long)t.n_kb * rank / split), b1 = (int)((long long)t.n_kb * (rank + 1) / split);
+  const int S = t.stages, split = t.split;
+  const int tile = blockIdx.x / split, rank = split > 1 ? (int)cluster_rank() : 0, row0 = blockIdx.y * N;
+  // this CTA's blocks of k: whole chunks of scales, but for the end
+  const int chunks = (t.m.n_kb + kChunk - 1) / kChunk;
+  const int b0 = min(chunks * rank / split * kChunk, t.m.n_kb), b1 = min(chunks * (rank + 1) / split * kChunk, t.m.n_kb);
+  const int units = (b1 - b0 + U - 1) / U;
   const uint32_t ring = (smem_at(raw) + 1023u) & ~1023u;       // the swizzle goes by the address
-  float *scales = reinterpret_cast<float *>(raw + (ring - smem_at(raw)) + S * F::kStage);   // [2][kScaleChunk][N], then [2][kScaleChunk][W]
   volatile int *gave_up = &s_gave_up;
-
-  if (tid == 0) {
+  if (tid == 32) {
     for (int s = 0; s < S; ++s) { mbar_init(smem_at(&s_full[s]), 1); mbar_init(smem_at(&s_empty[s]), 1); }
-    for (int b = 0; b < F::kBuffers; ++b) { mbar_init(smem_at(&s_done[b]), 1); mbar_init(smem_at(&s_read[b]), 128 * G); }
+    for (int b = 0; b < 2; ++b) { mbar_init(smem_at(&s_done[b]), 1); mbar_init(smem_at(&s_read[b]), 4 * G); }
+    for (int c = 0; c < kChunks; ++c) { mbar_init(smem_at(&s_there[c]), 32); mbar_init(smem_at(&s_used[c]), 4 * G); }
     mbar_init(smem_at(&s_tail), 1);
     s_gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&s_tmem)), "r"((uint32_t)F::kColumns) : "memory");
+    __syncwarp();
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&s_tmem)), "r"(F::kHalf ? 256u : 512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
@@ -90,156 +153,158 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
   pdl_wait();
   pdl_trigger();
 
-  float acc[W][C];
-#pragma unroll
-  for (int w = 0; w < W; ++w)
-#pragma unroll
-    for (int i = 0; i < C; ++i) acc[w][i] = 0.f;
-
-  if (warp == 0) {
-    // ------------------------------------------------------------ copies
-    // (the whole warp runs the loops of this branch and the next, so that their arithmetic is the warp's and not a lane's)
-    const bool one = elect_one();
-    int s = 0, phase = 1, b = b0;
-    for (; b < b1; ++b) {
-      if (b - b0 >= S && !mbar_wait(smem_at(&s_empty[s]), (uint32_t)phase, gave_up, t.wait_tries)) break;
-      const uint32_t full = smem_at(&s_full[s]), at = ring + (uint32_t)(s * F::kStage);
-      if (one) {
-        mbar_expect(full, F::kStage);
-        tma_rows8(at, &map_w0, b * 128, tile * 128, full);
-        if (W == 2) tma_rows8(at + kTileBytes, &map_w1, b * 128, tile * 128, full);
-        tma_rows8(at + W * kTileBytes, &map_a, b * 128, row0, full);
-      }
-      if (++s == S) { s = 0; phase ^= 1; }
-    }
-    if (*gave_up) {   // copies in flight must land before the CTA's shared memory is given back
-      for (int j = max(b0, b - S); j < b; ++j)
-        mbar_wait(smem_at(&s_full[(j - b0) % S]), (uint32_t)(((j - b0) / S) & 1), gave_up, max(t.wait_tries, kDrainTries), false);
-    }
-    __syncwarp();
-  } else if (warp == 1) {
-    // ------------------------------------------------------------ products
-    constexpr uint32_t idesc = idesc_e4m3(128, N);
-    const bool one = elect_one();
-    bool ok = true;
-    int s = 0, phase = 0;
-    for (int b = b0; b < b1; ++b) {
-      const int it = b - b0, buf = it % F::kBuffers, use = it / F::kBuffers;
-      ok = mbar_wait(smem_at(&s_full[s]), (uint32_t)phase, gave_up, t.wait_tries);
-      if (ok && use) ok = mbar_wait(smem_at(&s_read[buf]), (uint32_t)((use - 1) & 1), gave_up, t.wait_tries);
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t at = ring + (uint32_t)(s * F::kStage);
-      const uint64_t bd = desc_rows8(at + W * kTileBytes);
-      if (one) {
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-          const uint64_t ad = desc_rows8(at + w * kTileBytes);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)   // 32 numbers = 32 bytes = 2 descriptor units
-            tc_mma_e4m3(tmem + (uint32_t)((buf * W + w) * N), ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), idesc, k ? 1u : 0u);
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kRegsControl));
+    // (a whole warp runs each of the loops below, so that their arithmetic is the warp's and not a lane's)
+    if (warp == 0) {
+      // ---------------------------------------------------------- copies
+      const bool one = elect_one();
+      int s = 0, phase = 1, b = b0;
+      for (; b < b1; ++b) {
+        if (b - b0 >= S && !mbar_wait(smem_at(&s_empty[s]), (uint32_t)phase, gave_up, t.m.wait_tries)) break;
+        const uint32_t full = smem_at(&s_full[s]), at = ring + (uint32_t)(s * F::kStage);
+        if (one) {
+          mbar_expect(full, F::kStage);
+          tma_rows8(at, &map_w0, b * 128, tile * 128, full);
+          if (W == 2) tma_rows8(at + kTileBytes, &map_w1, b * 128, tile * 128, full);
+          tma_rows8(at + W * kTileBytes, &map_a, b * 128, row0, full);
         }
-        tc_commit(smem_at(&s_done[buf]));
-        tc_commit(smem_at(&s_empty[s]));
+        if (++s == S) { s = 0; phase ^= 1; }
       }
-      if (++s == S) { s = 0; phase ^= 1; }
+      if (*gave_up) {   // copies in flight must land before the CTA's shared memory is given back
+        for (int j = max(b0, b - S); j < b; ++j)
+          mbar_wait(smem_at(&s_full[(j - b0) % S]), (uint32_t)(((j - b0) / S) & 1), gave_up, max(t.m.wait_tries, kDrainTries), false);
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // ---------------------------------------------------------- products
+      constexpr uint32_t idesc = idesc_e4m3(128, N);
+      const bool one = elect_one();
+      bool ok = true;
+      int s = 0, phase = 0;
+      for (int u = 0; u < units && ok; ++u) {
+        const int buf = u & 1, blocks = min(U, b1 - b0 - u * U);
+        if (u >= 2) ok = mbar_wait(smem_at(&s_read[buf]), (uint32_t)(((u >> 1) - 1) & 1), gave_up, t.m.wait_tries);
+#pragma unroll 1
+        for (int b = 0; b < blocks && ok; ++b) {
+          ok = mbar_wait(smem_at(&s_full[s]), (uint32_t)phase, gave_up, t.m.wait_tries);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t at = ring + (uint32_t)(s * F::kStage), to = tmem + (uint32_t)(buf * F::kColumns + b * W * N);
+          const uint64_t ad = desc_rows8(at + W * kTileBytes);
+          if (one) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+              const uint64_t wd = desc_rows8(at + w * kTileBytes);
+#pragma unroll
+              for (int k = 0; k < 4; ++k)   // 32 numbers = 32 bytes = 2 descriptor units
+                tc_mma_e4m3(to + (uint32_t)(w * N), wd + (uint64_t)(2 * k), ad + (uint64_t)(2 * k), idesc, k ? 1u : 0u);
+            }
+            if (b == blocks - 1) tc_commit(smem_at(&s_done[buf]));
+            tc_commit(smem_at(&s_empty[s]));
+          }
+          if (++s == S) { s = 0; phase ^= 1; }
+        }
+      }
+      if (!ok) {        // what was issued still reads shared memory and writes tensor memory
+        if (one) tc_commit(smem_at(&s_tail));
+        mbar_wait(smem_at(&s_tail), 0u, gave_up, max(t.m.wait_tries, kDrainTries), false);
+      }
+      __syncwarp();
+    } else if (warp == 2) {
+      // ---------------------------------------------------------- scales: of the rows, and of the tile's weight rows
+      const int rows = min(N, t.m.n_rows - row0);
+      const float *as = t.m.a_scale + row0 * t.m.a_scale_stride;
+      for (int c = 0, b = b0; b < b1; ++c, b += kChunk) {
+        const int slot = c % kChunks, fill = c / kChunks;
+        if (fill > 0 && !mbar_wait(smem_at(&s_used[slot]), (uint32_t)((fill - 1) & 1), gave_up, t.m.wait_tries)) break;
+        const int in = lane & 7, kb = min(b + in, b1 - 1);
+        for (int r = lane >> 3; r < rows; r += 4) copy4(smem_at(&s_rows[slot][in][r]), as + r * t.m.a_scale_stride + kb);
+        if (lane < 8 * W) copy4(smem_at(&s_weights[slot][in][lane >> 3]), t.m.w_scale[lane >> 3] + (size_t)tile * t.m.n_kb + kb);
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_at(&s_there[slot])) : "memory");
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
-    if (!ok) {        // what was issued still reads shared memory and writes tensor memory
-      if (one) tc_commit(smem_at(&s_tail));
-      mbar_wait(smem_at(&s_tail), 0u, gave_up, max(t.wait_tries, kDrainTries), false);
-    }
-    __syncwarp();
   } else {
     // ------------------------------------------------------------ sums
-    const int et = tid - 64, g = (warp - 2) >> 2, q = warp & 3;   // a warp reads the quarter of the lanes that its number names
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::kRegsSums));
+    const int g = (warp - 4) >> 2, q = warp & 3;                  // a warp reads the quarter of the lanes that its number names
     const int r = q * 32 + lane;                                  // weight row of the tile
     const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(g * C);
-    // a chunk's scales, read one chunk ahead: entry e = row (e / kScaleChunk), block (e % kScaleChunk)
-    constexpr int kMine = N * kScaleChunk / (128 * G);
-    float ahead[kMine], w_ahead = 0.f;
-    float *w_scales = scales + 2 * kScaleChunk * N;
-    auto fetch = [&](int from) {
+    constexpr int P = C < 32 ? C : 32;                            // columns of a load
+    uint64_t acc[W][C / 2];                                       // two rows each
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        const int e = i * 128 * G + et, row = row0 + e / kScaleChunk, b = from + e % kScaleChunk;
-        ahead[i] = row < t.n_rows && b < b1 ? t.a_scale[row * t.a_scale_stride + b] : 0.f;
-      }
-      const int b = from + et / W;
-      if (et < kScaleChunk * W) w_ahead = b < b1 ? t.w_scale[et % W][(size_t)tile * t.n_kb + b] : 0.f;
-    };
-    auto keep = [&](int half) {
+    for (int w = 0; w < W; ++w)
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        const int e = i * 128 * G + et;
-        scales[(half * kScaleChunk + e % kScaleChunk) * N + e / kScaleChunk] = ahead[i];
-      }
-      if (et < kScaleChunk * W) w_scales[half * kScaleChunk * W + et] = w_ahead;
-    };
-    fetch(b0);
-    keep(0);
-    asm volatile("bar.sync 1, %0;" ::"n"(128 * G) : "memory");
-    for (int c0 = b0, half = 0; c0 < b1; c0 += kScaleChunk, half ^= 1) {
-      const int c1 = min(b1, c0 + kScaleChunk);
-      fetch(c0 + kScaleChunk);
-      for (int b = c0; b < c1; ++b) {
-        const int it = b - b0, buf = it % F::kBuffers;
-        float wsb[W];
-#pragma unroll
-        for (int w = 0; w < W; ++w) wsb[w] = w_scales[(half * kScaleChunk + b - c0) * W + w];
-        mbar_wait(smem_at(&s_done[buf]), (uint32_t)((it / F::kBuffers) & 1), gave_up, t.wait_tries);   // (given up: numbers without meaning)
-        __syncwarp();
-        tc_fence_after();
-        const float *as = scales + (half * kScaleChunk + (b - c0)) * N + g * C;
-        constexpr int P = C < 32 ? C : 32;
+      for (int i = 0; i < C / 2; ++i) acc[w][i] = 0ull;
+    int slot = 0, there = 0, in = 0;
+    for (int u = 0; u < units; ++u) {
+      const int buf = u & 1, blocks = min(U, b1 - b0 - u * U);
+      if (in == 0) mbar_wait(smem_at(&s_there[slot]), (uint32_t)there, gave_up, t.m.wait_tries);
+      mbar_wait(smem_at(&s_done[buf]), (uint32_t)((u >> 1) & 1), gave_up, t.m.wait_tries);   // (given up: numbers without meaning)
+      __syncwarp();
+      tc_fence_after();
+#pragma unroll 1
+      for (int b = 0; b < blocks; ++b) {
+        const uint32_t from = lanes + (uint32_t)(buf * F::kColumns + b * W * N);
+        const float *as = &s_rows[slot][in + b][g * C], *ws = s_weights[slot][in + b];
 #pragma unroll
         for (int w = 0; w < W; ++w) {
+          const uint64_t f = two_of(__float_as_uint(ws[w]), __float_as_uint(ws[w]));
 #pragma unroll
           for (int p = 0; p < C; p += P) {
             uint32_t d[P];
-            tc_ld(lanes + (uint32_t)((buf * W + w) * N + p), d);
+            tc_ld(from + (uint32_t)(w * N + p), d);
             tc_ld_wait(d);
-            if (w == W - 1 && p == C - P) {
-              tc_fence_before();
-              mbar_arrive(smem_at(&s_read[buf]));
-            }
 #pragma unroll
             for (int i = 0; i < P; i += 4) {
-              const float4 f = *reinterpret_cast<const float4 *>(as + p + i);
-              acc[w][p + i] = fmaf(__uint_as_float(d[i]), f.x * wsb[w], acc[w][p + i]);
-              acc[w][p + i + 1] = fmaf(__uint_as_float(d[i + 1]), f.y * wsb[w], acc[w][p + i + 1]);
-              acc[w][p + i + 2] = fmaf(__uint_as_float(d[i + 2]), f.z * wsb[w], acc[w][p + i + 2]);
-              acc[w][p + i + 3] = fmaf(__uint_as_float(d[i + 3]), f.w * wsb[w], acc[w][p + i + 3]);
+              const uint4 a = *reinterpret_cast<const uint4 *>(as + p + i);
+              fma_two(acc[w][(p + i) / 2], two_of(d[i], d[i + 1]), mul_two(two_of(a.x, a.y), f));
+              fma_two(acc[w][(p + i) / 2 + 1], two_of(d[i + 2], d[i + 3]), mul_two(two_of(a.z, a.w), f));
             }
           }
         }
       }
-      keep(half ^ 1);
-      asm volatile("bar.sync 1, %0;" ::"n"(128 * G) : "memory");
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_at(&s_read[buf]));
+      in += U;
+      if (in == kChunk || u == units - 1) {
+        if (lane == 0) mbar_arrive(smem_at(&s_used[slot]));
+        in = 0;
+        if (++slot == kChunks) { slot = 0; there ^= 1; }
+      }
     }
     // every copy has landed and every product is done: the ring holds the sums now, [matrix][row of the call][weight row]
     float *sums = reinterpret_cast<float *>(raw + (ring - smem_at(raw)));
+    asm volatile("bar.sync 1, %0;" ::"n"(128 * G) : "memory");
 #pragma unroll
     for (int w = 0; w < W; ++w)
 #pragma unroll
-      for (int i = 0; i < C; ++i) sums[(w * N + g * C + i) * 128 + r] = acc[w][i];
+      for (int i = 0; i < C; ++i) sums[(w * N + g * C + i) * 128 + r] = i & 1 ? high_of(acc[w][i / 2]) : low_of(acc[w][i / 2]);
   }
 
   if (split > 1) cluster_sync();
   else __syncthreads();
-  const int rows = min(N, t.n_rows - row0), n0 = tile * 128 + 4 * lane;
+  const int rows = min(N, t.m.n_rows - row0), n0 = tile * 128 + 4 * lane;
   for (int j = rank + split * warp; j < rows; j += split * (F::kThreads / 32)) {
     float y[W][4];
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const uint32_t at = ring + (uint32_t)(((w * N + j) * 128 + 4 * lane) * 4);
-      float4 part[8];
+      float4 sum;
+      if (split == 1) {
+        sum = *reinterpret_cast<const float4 *>(raw + (at - smem_at(raw)));
+      } else {
+        float4 part[kMostSplit];
 #pragma unroll
-      for (int p = 0; p < 8; ++p)
-        if (p < split) part[p] = cluster_load4(at, (uint32_t)p);
-      float4 sum = part[0];
+        for (int p = 0; p < kMostSplit; ++p)
+          if (p < split) part[p] = cluster_load4(at, (uint32_t)p);
+        sum = part[0];
 #pragma unroll
-      for (int p = 1; p < 8; ++p)
-        if (p < split) { sum.x += part[p].x; sum.y += part[p].y; sum.z += part[p].z; sum.w += part[p].w; }
+        for (int p = 1; p < kMostSplit; ++p)
+          if (p < split) { sum.x += part[p].x; sum.y += part[p].y; sum.z += part[p].z; sum.w += part[p].w; }
+      }
       y[w][0] = sum.x; y[w][1] = sum.y; y[w][2] = sum.z; y[w][3] = sum.w;
     }
     if constexpr (W == 2) {
@@ -248,50 +313,44 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
     }
     finish4(t, row0 + j, n0, y[0], tile, lane);
   }
-  if (split > 1) cluster_sync();   // no CTA's sums go while another one reads them
-  if (tid == 0 && *gave_up && t.status) *t.status = D3_ETIMEOUT;
+  if (tid == 0 && *gave_up && t.m.status) *t.m.status = D3_ETIMEOUT;
   tc_fence_before();
-  __syncthreads();
+  if (split > 1) cluster_sync();   // no CTA's sums go while another one reads them
+  else __syncthreads();
   if (warp == 1)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)F::kColumns) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(F::kHalf ? 256u : 512u) : "memory");
 }
 
-template <int C, int G, int W>
-cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, Mm8Args &p, cudaStream_t st) {
-  using F = Few<C, G, W>;
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  static std::atomic<int> sms[64];   // SMs of a device whose attribute is set (setting it twice is harmless)
-  int n_sm = sms[dev].load(std::memory_order_acquire);
-  if (n_sm == 0) {
-    if ((e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-    if ((e = cudaFuncSetAttribute(k_mm8_few<C, G, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024)) != cudaSuccess) return e;
-    sms[dev].store(n_sm, std::memory_order_release);
+template <int C, int G, int W, int U>
+cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args &p, int dev, cudaStream_t st) {
+  using F = Few<C, G, W, U>;
+  static std::atomic<bool> ready[64];   // the shared-memory attribute is per device; setting it twice is harmless
+  if (!ready[dev].load(std::memory_order_acquire)) {
+    const cudaError_t e = cudaFuncSetAttribute(k_mm8_few<C, G, W, U>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWholeSmem);
+    if (e != cudaSuccess) return e;
+    ready[dev].store(true, std::memory_order_release);
   }
-  // Two CTAs an SM where three stages of each fit side by side; one with a longer ring otherwise.
-  const int fixed = F::kScales + 1024;
-  int per_sm = 2, stages = (kPairSmem - fixed) / F::kStage;
-  if (stages < 3 || F::kColumns > 256) { per_sm = 1; stages = (224 * 1024 - fixed) / F::kStage; }
-  const int least = (F::kSums + F::kStage - 1) / F::kStage;    // the ring holds the sums in the end
-  // As many CTAs as the GPU holds at once, so that they share its memory rate from the first to the last byte.
-  const int tiles = (p.n + 127) / 128;
-  int split = n_sm * per_sm / tiles;
-  if (split > 8) split = 8;
-  if (split > p.n_kb) split = p.n_kb;
-  if (split < 1) split = 1;
-  const int most = (p.n_kb + split - 1) / split;               // blocks of a CTA
-  if (stages > most) stages = most;
-  if (stages < least) stages = least;
+  FewArgs t;
+  t.m = p;
+  const int fixed = kChunks * kChunk * (F::N + 2) * 4 + 1024 + 1024;      // static shared memory, and the alignment of the ring
+  int stages = (kHalfSmem - fixed) / F::kStage;
+  if (!F::kHalf || G > 1 || stages < 4) stages = (kWholeSmem - fixed) / F::kStage;
   if (stages > kMaxStages) stages = kMaxStages;
-  p.n_stages = stages;
-  p.split = split;
+  const int least = (F::kSums + F::kStage - 1) / F::kStage;               // the ring holds the sums in the end
+  if (stages < least) stages = least;
+  // k is cut only where there are fewer tiles than keep the memory busy
+  const int tiles = (p.n + 127) / 128, chunks = (p.n_kb + kChunk - 1) / kChunk;
+  int split = 1;
+  while (split < kMostSplit && tiles * split < kEnoughTiles && split * 2 <= chunks) split *= 2;
+  t.stages = stages;
+  t.split = split;
+  const int es = type_bytes(p.out_dtype);
+  t.wide = on_bytes(p.out, 4 * es) && (p.n_rows == 1 || p.out_stride % 4 == 0);
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3((unsigned)(tiles * split), (unsigned)((p.n_rows + F::N - 1) / F::N));
   cfg.blockDim = dim3(F::kThreads);
-  cfg.dynamicSmemBytes = (size_t)stages * F::kStage + fixed;
+  cfg.dynamicSmemBytes = (size_t)stages * F::kStage + 1024;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -304,26 +363,33 @@ cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, Mm8Args &p, c
   cfg.numAttrs = split > 1 ? 2 : 1;
   const CUtensorMap *m0 = reinterpret_cast<const CUtensorMap *>(&w0), *m1 = reinterpret_cast<const CUtensorMap *>(&w1),
                     *m = reinterpret_cast<const CUtensorMap *>(&ma);
-  return cudaLaunchKernelEx(&cfg, k_mm8_few<C, G, W>, *m0, *m1, *m, static_cast<const Mm8Args>(p));
-}
-
-template <int W>
-cudaError_t choose(const TMap &w0, const TMap &w1, const void *a, int64_t a_stride, Mm8Args &p, cudaStream_t st) {
-  const int padded = p.n_rows <= 16 ? 16 : p.n_rows <= 32 ? 32 : p.n_rows <= 64 ? 64 : 128;
-  TMap ma;
-  if (!encode_rows8(&ma, a, p.n_rows, p.k, a_stride, padded)) return cudaErrorInvalidValue;
-  switch (padded) {
-    case 16: return launch<16, 1, W>(w0, w1, ma, p, st);
-    case 32: return launch<32, 1, W>(w0, w1, ma, p, st);
-    case 64: return launch<64, 1, W>(w0, w1, ma, p, st);
-    default: return launch<64, 2, W>(w0, w1, ma, p, st);
-  }
+  return cudaLaunchKernelEx(&cfg, k_mm8_few<C, G, W, U>, *m0, *m1, *m, static_cast<const FewArgs>(t));
 }
 
 }  // namespace
 
-cudaError_t launch_mm8_few(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, Mm8Args &p, cudaStream_t st) {
-  return w1 ? choose<2>(w0, *w1, a, a_stride, p, st) : choose<1>(w0, w0, a, a_stride, p, st);
+cudaError_t launch_mm8_few(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, const Mm8Args &p, cudaStream_t st) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  const int padded = p.n_rows <= 16 ? 16 : p.n_rows <= 32 ? 32 : p.n_rows <= 64 ? 64 : 128;
+  TMap ma;
+  if (!encode_rows8(&ma, a, p.n_rows, p.k, a_stride, padded)) return cudaErrorInvalidValue;
+  if (w1) {
+    switch (padded) {
+      case 16: return launch<16, 1, 2, 4>(w0, *w1, ma, p, dev, st);
+      case 32: return launch<32, 1, 2, 2>(w0, *w1, ma, p, dev, st);
+      case 64: return launch<64, 1, 2, 1>(w0, *w1, ma, p, dev, st);
+      default: return launch<64, 2, 2, 1>(w0, *w1, ma, p, dev, st);
+    }
+  }
+  switch (padded) {
+    case 16: return launch<16, 1, 1, 4>(w0, w0, ma, p, dev, st);
+    case 32: return launch<32, 1, 1, 4>(w0, w0, ma, p, dev, st);
+    case 64: return launch<64, 1, 1, 2>(w0, w0, ma, p, dev, st);
+    default: return launch<64, 2, 1, 1>(w0, w0, ma, p, dev, st);
+  }
 }
 
 }  // namespace d3

@@ -24,7 +24,7 @@ constexpr int kOutBytes = 32 * 1024;             // results on their way out
 constexpr int kThreads = 384;                    // copies, products and two idle warps; eight epilogue warps
 constexpr int kColumns = 512;
 constexpr int kSmem = kStages * kStage + kOutBytes + 1024;
-constexpr int kChunk = 4, kChunks = 3;           // scales come in chunks of 4 blocks, through a ring of their own
+constexpr int kChunk = 4, kChunks = 8;           // scales come in chunks of 4 blocks, through a ring of their own, and are taken 4 at a time
 constexpr int kGroupM = 8;                       // tiles of rows that are taken together (their a and the weights beside them stay in L2)
 // Registers: 384 threads start with 168; the epilogue's two warpgroups take 216 and leave 72 to the third
 // (128 * 72 + 256 * 216 = 384 * 168).
@@ -63,21 +63,8 @@ __device__ __forceinline__ void store_box(const void *map, uint32_t from, int x,
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
                ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(from) : "memory");
 }
-__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-  return r;
-}
-__device__ __forceinline__ void fma2(uint64_t &acc, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b)); }
-__device__ __forceinline__ float first_of(uint64_t v) { return __uint_as_float((uint32_t)v); }
-__device__ __forceinline__ float second_of(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
 __device__ __forceinline__ void store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
-
-// 4 bytes to shared memory without waiting; zeros where they are not wanted
-__device__ __forceinline__ void copy4(uint32_t to, const void *from, bool wanted) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(wanted ? 4 : 0) : "memory");
 }
 
 struct ManyArgs {
@@ -109,7 +96,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
            const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ManyArgs t) {
   extern __shared__ unsigned char raw[];
   __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_read[2], s_there[kChunks], s_used[kChunks], s_tail;
-  __shared__ __align__(8) float s_rows[kChunks][kChunk][128], s_weights[kChunks][kChunk][2];
+  __shared__ __align__(16) float s_rows[kChunks][128][kChunk], s_weights[kChunks][2][kChunk];
   __shared__ float s_top[2][128];
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
@@ -214,14 +201,13 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
         for (int b = 0; b < n_kb; b += kChunk, ++ch) {
           const int c = ch % kChunks, fill = ch / kChunks;
           if (fill > 0 && !(ok = mbar_wait(smem_at(&s_used[c]), (uint32_t)((fill - 1) & 1), gave_up, t.m.wait_tries))) break;
-          const int kb = b + (lane & 3);
+          const int kb = min(b + (lane & 3), n_kb - 1);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {       // 4 blocks of 8 rows at a time; what is behind the end is zeros
+          for (int e = 0; e < 16; ++e) {       // 4 blocks of 8 rows at a time
             const int r = e * 8 + (lane >> 2);
-            const bool in = kb < n_kb && row0 + r < t.m.n_rows;
-            copy4(smem_at(&s_rows[c][lane & 3][r]), t.m.a_scale + (in ? (long long)(row0 + r) * t.m.a_scale_stride + kb : 0ll), in);
+            if (row0 + r < t.m.n_rows) copy4(smem_at(&s_rows[c][r][lane & 3]), t.m.a_scale + (long long)(row0 + r) * t.m.a_scale_stride + kb);
           }
-          if (lane < 2 * kChunk) copy4(smem_at(&s_weights[c][lane & 3][lane >> 2]), ws[lane >> 2] + min(kb, n_kb - 1), true);
+          if (lane < 2 * kChunk) copy4(smem_at(&s_weights[c][lane >> 2][lane & 3]), ws[lane >> 2] + kb);
           asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_at(&s_there[c])) : "memory");
         }
       }
@@ -245,51 +231,57 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < 32; ++j) acc[h][j] = 0ull;
-      // the scales of block b: this row's, and those of the two halves' weights
-      float sa;
-      float2 sw;
-      auto next_scales = [&](int b) {
-        const int in = b % kChunk;
-        if (in == 0) mbar_wait(smem_at(&s_there[chunk]), (uint32_t)there, gave_up, t.m.wait_tries);
-        sa = s_rows[chunk][in][r];
-        sw = *reinterpret_cast<const float2 *>(s_weights[chunk][in]);
-        if (in == kChunk - 1 || b == n_kb - 1) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_at(&s_used[chunk]));
-          if (++chunk == kChunks) { chunk = 0; there ^= 1; }
-        }
-      };
-      next_scales(0);
-      for (int b = 0; b < n_kb; ++b, ++it) {
-        const int buf = it & 1;
-        const float f0 = sa * sw.x, f1 = sa * sw.y;
-        const uint64_t f[2] = {pair_of(__float_as_uint(f0), __float_as_uint(f0)), pair_of(__float_as_uint(f1), __float_as_uint(f1))};
-        mbar_wait(smem_at(&s_done[buf]), (uint32_t)((it >> 1) & 1), gave_up, t.m.wait_tries);   // (given up: numbers without meaning)
+      // Scales of four blocks at a time, this row's times those of the two halves' weights (fetched block by block they took a third of
+      // the epilogue's time).
+      float f0[kChunk], f1[kChunk];
+      // A block's first columns are asked for before the last ones of the block before are added.
+      uint32_t d[2][32];
+      auto begin = [&]() {
+        mbar_wait(smem_at(&s_done[it & 1]), (uint32_t)((it >> 1) & 1), gave_up, t.m.wait_tries);   // (given up: numbers without meaning)
         __syncwarp();
         tc_fence_after();
-        uint32_t d[2][32];
-        tc_ld(lanes + (uint32_t)(buf * 256), d[0]);
-        if (b + 1 < n_kb) next_scales(b + 1);
+        tc_ld(lanes + (uint32_t)((it & 1) * 256), d[0]);
+      };
+      begin();
+      for (int b0 = 0; b0 < n_kb; b0 += kChunk) {
+        mbar_wait(smem_at(&s_there[chunk]), (uint32_t)there, gave_up, t.m.wait_tries);
+        const float4 sa = *reinterpret_cast<const float4 *>(s_rows[chunk][r]), w0 = *reinterpret_cast<const float4 *>(s_weights[chunk][0]),
+                     w1 = *reinterpret_cast<const float4 *>(s_weights[chunk][1]);
+        f0[0] = sa.x * w0.x; f0[1] = sa.y * w0.y; f0[2] = sa.z * w0.z; f0[3] = sa.w * w0.w;
+        f1[0] = sa.x * w1.x; f1[1] = sa.y * w1.y; f1[2] = sa.z * w1.z; f1[3] = sa.w * w1.w;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_at(&s_used[chunk]));
+        if (++chunk == kChunks) { chunk = 0; there ^= 1; }
+#pragma unroll 1                               // (the loop's code has to stay within reach: four blocks unrolled took 563 us where this takes 502)
+        for (int j = 0; j < kChunk; ++j) {
+          if (b0 + j >= n_kb) break;
+          const uint32_t at = lanes + (uint32_t)((it & 1) * 256), read = read_bar[it & 1];
+          const uint64_t f[2] = {two_of(__float_as_uint(f0[0]), __float_as_uint(f0[0])), two_of(__float_as_uint(f1[0]), __float_as_uint(f1[0]))};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {        // 32 columns: halves 0, 0, 1, 1
-          tc_ld_wait(d[c & 1]);
-          if (c < 3) {
-            tc_ld(lanes + (uint32_t)(buf * 256 + ((c + 1) >> 1) * 128 + ((c + 1) & 1) * 32), d[(c + 1) & 1]);
-          } else {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) pair_arrive(read_bar[buf]);
+          for (int e = 0; e + 1 < kChunk; ++e) { f0[e] = f0[e + 1]; f1[e] = f1[e + 1]; }
+          ++it;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {        // 32 columns: halves 0, 0, 1, 1
+            tc_ld_wait(d[c & 1]);
+            if (c < 3) {
+              tc_ld(at + (uint32_t)(((c + 1) >> 1) * 128 + ((c + 1) & 1) * 32), d[(c + 1) & 1]);
+            } else {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) pair_arrive(read);
+              if (b0 + j + 1 < n_kb) begin();
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) fma_two(acc[c >> 1][(c & 1) * 16 + e], two_of(d[c & 1][2 * e], d[c & 1][2 * e + 1]), f[c >> 1]);
           }
-#pragma unroll
-          for (int j = 0; j < 16; ++j) fma2(acc[c >> 1][(c & 1) * 16 + j], pair_of(d[c & 1][2 * j], d[c & 1][2 * j + 1]), f[c >> 1]);
         }
       }
       // ---------------------------------------------------------- results
       if constexpr (W == 2) {
 #pragma unroll
         for (int j = 0; j < 32; ++j)
-          acc[0][j] = pair_of(__float_as_uint(gate_of(first_of(acc[0][j]), first_of(acc[1][j]))),
-                              __float_as_uint(gate_of(second_of(acc[0][j]), second_of(acc[1][j]))));
+          acc[0][j] = two_of(__float_as_uint(gate_of(low_of(acc[0][j]), low_of(acc[1][j]))),
+                              __float_as_uint(gate_of(high_of(acc[0][j]), high_of(acc[1][j]))));
       }
       // what the last tile left must be out of the staging area
       if (t.bulk) {
@@ -302,8 +294,8 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
         float top = 0.f;
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-          top = max_nan(top, fabsf(first_of(acc[0][j])));     // (columns behind the last one are of zero weights)
-          top = max_nan(top, fabsf(second_of(acc[0][j])));
+          top = max_nan(top, fabsf(low_of(acc[0][j])));     // (columns behind the last one are of zero weights)
+          top = max_nan(top, fabsf(high_of(acc[0][j])));
         }
         s_top[g][r] = top;
         asm volatile("bar.sync 3, 256;" ::: "memory");
@@ -314,8 +306,8 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
         uint32_t v[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-          v[j] = pack_e4m3(first_of(acc[0][2 * j]) * inverse, second_of(acc[0][2 * j]) * inverse, first_of(acc[0][2 * j + 1]) * inverse,
-                           second_of(acc[0][2 * j + 1]) * inverse);
+          v[j] = pack_e4m3(low_of(acc[0][2 * j]) * inverse, high_of(acc[0][2 * j]) * inverse, low_of(acc[0][2 * j + 1]) * inverse,
+                           high_of(acc[0][2 * j + 1]) * inverse);
         if (t.bulk) {                     // one box: rows of 128 bytes in the 128-byte swizzle
 #pragma unroll
           for (int j = 0; j < 4; ++j)
@@ -350,7 +342,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
               for (int j = 0; j < 8; ++j) {
                 uint32_t v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = pack2(first_of(acc[h][4 * j + e]), second_of(acc[h][4 * j + e]), dtype);
+                for (int e = 0; e < 4; ++e) v[e] = pack2(low_of(acc[h][4 * j + e]), high_of(acc[h][4 * j + e]), dtype);
                 store16(mine + (uint32_t)(r * 128 + ((j ^ (r & 7)) << 4)), v[0], v[1], v[2], v[3]);
               }
               copy_out(t, map_out, mine, c0, row0, g, warp, lane);
@@ -371,7 +363,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
           } else if (live) {
 #pragma unroll
             for (int j = 0; j < 64; ++j)
-              if (c0 + j < t.m.n) store1(t.m.out, row * t.m.out_stride + c0 + j, dtype, (j & 1) ? second_of(acc[h][j >> 1]) : first_of(acc[h][j >> 1]));
+              if (c0 + j < t.m.n) store1(t.m.out, row * t.m.out_stride + c0 + j, dtype, (j & 1) ? high_of(acc[h][j >> 1]) : low_of(acc[h][j >> 1]));
           }
         }
       }
@@ -387,7 +379,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
 }
 
 template <int W>
-cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, Mm8Args &p, cudaStream_t st) {
+cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args &p, cudaStream_t st) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -433,7 +425,7 @@ cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, Mm8Args &p, c
 
 }  // namespace
 
-cudaError_t launch_mm8_many(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, Mm8Args &p, cudaStream_t st) {
+cudaError_t launch_mm8_many(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, const Mm8Args &p, cudaStream_t st) {
   TMap ma;
   if (!encode_rows8(&ma, a, p.n_rows, p.k, a_stride, 128)) return cudaErrorInvalidValue;
   return w1 ? launch<2>(w0, *w1, ma, p, st) : launch<1>(w0, w0, ma, p, st);
