@@ -18,49 +18,130 @@ struct NormArgs {
   long long x_stride, add_stride, total_stride, out_stride, scale_stride;
 };
 
-// A row is held in registers by T threads of the CTA, V pieces of 8 numbers each; T = 32 puts rows side by side, a warp
-// each.  Everything is read before anything is written, so that out and total may lie on x and add.  16 neighbouring
-// threads have one block of 128 numbers and find its largest by shuffles.
-template <int V, bool kWarp>
+// A thread of the kernels below has K = 8 or 16 numbers of a block of 128, in pieces of E = 4 or 8 that are 16 bytes of x, so that
+// neighbouring threads' pieces lie side by side; the 128 / K threads of the block find its largest by shuffles.  Many rows are
+// bound by the memory, if no more than a few instructions are spent on a number: with types told apart at run time, 8 numbers a
+// thread and two divisions each, 8-bit rows of 4097 x 11008 took 44 us (now 22).  Few rows are bound by the launch.
+template <int kType, int K>
+struct Piece {
+  static constexpr int E = kType == D3_FP32 ? 4 : 8, kGroups = K / E, kLanes = 128 / K;
+  // first number of group j of thread t of a row
+  static __device__ __forceinline__ int at(int t, int j) { return t / kLanes * 128 + j * (kLanes * E) + t % kLanes * E; }
+};
+// E numbers (16-byte aligned, or 8 where four 16-bit ones are asked for)
+template <int kType, int E>
+__device__ __forceinline__ void read_some(const char *p, float *v) {
+  if constexpr (E == 8) {
+    float u[8];
+    load8(p, 0, kType, u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = u[j];
+  } else if constexpr (kType == D3_FP32) {
+    const float4 u = *reinterpret_cast<const float4 *>(p);
+    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    if (kType == D3_BF16) {
+      v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u); v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
+    } else {
+      v[0] = half_lo(u.x); v[1] = half_hi(u.x); v[2] = half_lo(u.y); v[3] = half_hi(u.y);
+    }
+  }
+}
+template <int E>
+__device__ __forceinline__ void write_some(char *p, int dtype, const float *v) {
+#pragma unroll
+  for (int j = 0; j < E; j += 4) {
+    if (dtype == D3_FP32) *reinterpret_cast<float4 *>(p + 4 * j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+    else if (E == 4) *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(v[0], v[1], dtype), pack2(v[2], v[3], dtype));
+  }
+  if (E == 8 && dtype != D3_FP32)
+    *reinterpret_cast<uint4 *>(p) = make_uint4(pack2(v[0], v[1], dtype), pack2(v[2], v[3], dtype), pack2(v[4], v[5], dtype), pack2(v[6], v[7], dtype));
+}
+// a thread's numbers of one of its blocks, zeros behind the end of the row
+template <int kType, int K, int kOf>
+__device__ __forceinline__ void read_row(const char *row, int t, int dim, float (&v)[K]) {
+  using P = Piece<kOf, K>;                      // (the pieces are those of x, whatever is read)
+  constexpr int kSize = kType == D3_FP32 ? 4 : 2;
+#pragma unroll
+  for (int j = 0; j < P::kGroups; ++j) {
+    const int at = P::at(t, j);
+    if (at < dim) {
+      read_some<kType, P::E>(row + at * kSize, v + j * P::E);
+    } else {
+#pragma unroll
+      for (int e = 0; e < P::E; ++e) v[j * P::E + e] = 0.f;
+    }
+  }
+}
+template <int K, int kOf>
+__device__ __forceinline__ void write_row(char *row, int t, int dim, int dtype, const float (&v)[K]) {
+  using P = Piece<kOf, K>;
+  const int size = dtype == D3_FP32 ? 4 : 2;
+#pragma unroll
+  for (int j = 0; j < P::kGroups; ++j) {
+    const int at = P::at(t, j);
+    if (at < dim) write_some<P::E>(row + at * size, dtype, v + j * P::E);
+  }
+}
+// the same in 8 bits with the block's scale (all threads of the warp take part)
+template <int K, int kOf>
+__device__ __forceinline__ void write_row_e4m3(char *row, float *scales, int t, int dim, const float (&v)[K]) {
+  using P = Piece<kOf, K>;
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < K; ++j) top = max_nan(top, fabsf(v[j]));
+#pragma unroll
+  for (int o = P::kLanes / 2; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+  float inverse;
+  const float scale = block_scale(top, inverse);
+#pragma unroll
+  for (int j = 0; j < P::kGroups; ++j) {
+    const int at = P::at(t, j);
+    if (at < dim) {
+      const float *u = v + j * P::E;
+      const uint32_t lo = pack_e4m3(u[0] * inverse, u[1] * inverse, u[2] * inverse, u[3] * inverse);
+      if constexpr (P::E == 4) *reinterpret_cast<uint32_t *>(row + at) = lo;
+      else *reinterpret_cast<uint2 *>(row + at) = make_uint2(lo, pack_e4m3(u[4] * inverse, u[5] * inverse, u[6] * inverse, u[7] * inverse));
+    }
+  }
+  if (t % P::kLanes == 0 && t / P::kLanes * 128 < dim) scales[t / P::kLanes] = scale;
+}
+
+// A row is held in registers by the threads of a CTA, V times K numbers each; kWarp puts rows side by side, a warp each.
+// Everything is read before anything is written, so that out and total may lie on x and add.  kAdd: the type of add, -1 for none.
+template <int V, int K, bool kWarp, int kType, int kAdd>
 __global__ void __launch_bounds__(1024) k_add_norm(const __grid_constant__ NormArgs a) {
   __shared__ float s_sum[32];
+  constexpr int kSize = kType == D3_FP32 ? 4 : 2, kAddSize = kAdd == D3_FP32 ? 4 : 2;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int T = kWarp ? 32 : blockDim.x, t = kWarp ? lane : threadIdx.x;
   const long long row = kWarp ? (long long)blockIdx.x * (blockDim.x >> 5) + warp : blockIdx.x;
-  const int pieces = a.dim >> 3;
   pdl_wait();
   pdl_trigger();
   if (kWarp && row >= a.n_rows) return;
-  float v[V][8];
+  float v[V][K];
+  const char *x = static_cast<const char *>(a.x) + row * a.x_stride * kSize;
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int c = i * T + t;
-    if (c < pieces) {
-      load8(a.x, row * a.x_stride + 8 * c, a.x_dtype, v[i]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-    }
-  }
-  if (a.add) {
+  for (int i = 0; i < V; ++i) read_row<kType, K, kType>(x, i * T + t, a.dim, v[i]);
+  if constexpr (kAdd >= 0) {
+    const char *add = static_cast<const char *>(a.add) + row * a.add_stride * kAddSize;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int c = i * T + t;
-      if (c < pieces) {
-        float u[8];
-        load8(a.add, row * a.add_stride + 8 * c, a.add_dtype, u);
+      float u[K];
+      read_row<kAdd, K, kType>(add, i * T + t, a.dim, u);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] += u[j];
-      }
+      for (int j = 0; j < K; ++j) v[i][j] += u[j];
     }
   }
+  float r = 0.f;
   if (a.gain) {
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float part = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) part = fmaf(v[i][j], v[i][j], part);
+      for (int j = 0; j < K; ++j) part = fmaf(v[i][j], v[i][j], part);
       sum += part;
     }
 #pragma unroll
@@ -72,61 +153,85 @@ __global__ void __launch_bounds__(1024) k_add_norm(const __grid_constant__ NormA
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     }
-    const float r = 1.f / sqrtf(sum / (float)a.dim + a.eps);
-    if (a.total) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int c = i * T + t;
-        if (c < pieces) store8(a.total, row * a.total_stride + 8 * c, a.add_dtype, v[i]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = i * T + t;
-      if (c < pieces) {
-        float g[8];
-        load8(a.gain, 8 * c, a.gain_dtype, g);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * r * g[j];
-      }
-    }
-  } else if (a.total) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = i * T + t;
-      if (c < pieces) store8(a.total, row * a.total_stride + 8 * c, a.add_dtype, v[i]);
-    }
+    r = 1.f / sqrtf(sum / (float)a.dim + a.eps);
   }
+  if (kAdd >= 0 && a.total) {
+    char *total = static_cast<char *>(a.total) + row * a.total_stride * kAddSize;
+#pragma unroll
+    for (int i = 0; i < V; ++i) write_row<K, kType>(total, i * T + t, a.dim, kAdd, v[i]);
+  }
+  char *out = static_cast<char *>(a.out) + row * a.out_stride * (a.out_dtype == D3_E4M3 ? 1 : a.out_dtype == D3_FP32 ? 4 : 2);
+  float *scales = a.scale + row * a.scale_stride;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int c = i * T + t;
-    if (a.out_dtype == D3_E4M3) {
-      float top = 0.f;
+    if (a.gain) {
+      float g[K];
+      const char *gain = static_cast<const char *>(a.gain);
+      if (a.gain_dtype == D3_BF16) read_row<D3_BF16, K, kType>(gain, i * T + t, a.dim, g);
+      else if (a.gain_dtype == D3_FP16) read_row<D3_FP16, K, kType>(gain, i * T + t, a.dim, g);
+      else read_row<D3_FP32, K, kType>(gain, i * T + t, a.dim, g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) top = max_nan(top, fabsf(v[i][j]));
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-      float inverse;
-      const float scale = block_scale(top, inverse);
-      if (c < pieces) {
-        const uint32_t lo = pack_e4m3(v[i][0] * inverse, v[i][1] * inverse, v[i][2] * inverse, v[i][3] * inverse);
-        const uint32_t hi = pack_e4m3(v[i][4] * inverse, v[i][5] * inverse, v[i][6] * inverse, v[i][7] * inverse);
-        *reinterpret_cast<uint2 *>(static_cast<char *>(a.out) + row * a.out_stride + 8 * c) = make_uint2(lo, hi);
-        if ((c & 15) == 0) a.scale[row * a.scale_stride + (c >> 4)] = scale;
-      }
-    } else if (c < pieces) {
-      store8(a.out, row * a.out_stride + 8 * c, a.out_dtype, v[i]);
+      for (int j = 0; j < K; ++j) v[i][j] = v[i][j] * r * g[j];
     }
+    if (a.out_dtype == D3_E4M3) write_row_e4m3<K, kType>(out, scales, i * T + t, a.dim, v[i]);
+    else write_row<K, kType>(out, i * T + t, a.dim, a.out_dtype, v[i]);
   }
 }
 
-template <int V>
-cudaError_t launch_norm(const NormArgs &a, int threads, cudaStream_t st) {
-  if (threads <= 32) {
-    const int rows = a.n_rows < 148 * 4 ? 1 : 8;
-    return launch_pdl(k_add_norm<V, true>, dim3((unsigned)((a.n_rows + rows - 1) / rows)), dim3(32 * rows), 0, st, a);
+// The 8 bits alone: blocks of 128 have nothing to do with one another, so they are dealt out whatever row they are in, kQuant
+// to a thread (of 8 that share a block).
+constexpr int kQuant = 2, kQuantThreads = 256, kQuantBlocks = kQuantThreads / 8;
+template <int kType>
+__global__ void __launch_bounds__(kQuantThreads) k_quantize(const __grid_constant__ NormArgs a) {
+  constexpr int kSize = kType == D3_FP32 ? 4 : 2;
+  const uint32_t wide = (uint32_t)(a.dim + 127) / 128;
+  pdl_wait();
+  pdl_trigger();
+  // (fewer than 2^31 blocks)
+  const uint32_t b = blockIdx.x * (uint32_t)(kQuant * kQuantBlocks) + threadIdx.x / 8;
+  uint32_t row = b / wide, c = b - row * wide;
+  float v[kQuant][16];
+  uint32_t rows[kQuant];
+  int ts[kQuant];
+#pragma unroll
+  for (int i = 0; i < kQuant; ++i) {
+    rows[i] = row;
+    ts[i] = (int)(8 * c + threadIdx.x % 8);
+    read_row<kType, 16, kType>(static_cast<const char *>(a.x) + row * a.x_stride * kSize, ts[i], row < a.n_rows ? a.dim : 0, v[i]);
+    c += kQuantBlocks;
+    while (c >= wide) { c -= wide; ++row; }
   }
-  return launch_pdl(k_add_norm<V, false>, dim3((unsigned)a.n_rows), dim3(threads), 0, st, a);
+#pragma unroll
+  for (int i = 0; i < kQuant; ++i)
+    write_row_e4m3<16, kType>(static_cast<char *>(a.out) + rows[i] * a.out_stride, a.scale + rows[i] * a.scale_stride, ts[i], rows[i] < a.n_rows ? a.dim : 0, v[i]);
+}
+
+// threads of a row, V times K numbers each
+inline int norm_threads(int dim, int v, int k) { return ((dim + 127) / 128 * (128 / k) + 32 * v - 1) / (32 * v) * 32; }
+template <int V, int K, int kType, int kAdd>
+cudaError_t launch_norm(const NormArgs &a, cudaStream_t st) {
+  const int threads = norm_threads(a.dim, V, K);
+  if constexpr (V == 1) {
+    if (threads <= 32) {
+      const int rows = a.n_rows < 148 * 4 ? 1 : 8;
+      return launch_pdl(k_add_norm<V, K, true, kType, kAdd>, dim3((unsigned)((a.n_rows + rows - 1) / rows)), dim3(32 * rows), 0, st, a);
+    }
+  }
+  return launch_pdl(k_add_norm<V, K, false, kType, kAdd>, dim3((unsigned)a.n_rows), dim3(threads), 0, st, a);
+}
+template <int kType, int kAdd>
+cudaError_t launch_norm_k(const NormArgs &a, cudaStream_t st) {
+  // (us with 8 / 16 numbers a thread: 4096 x 4096 in 16 bits 23.9 / 28.8, 32 x 5120 2.4 / 2.7, 8191 x 8192 130 / 128)
+  if (a.dim <= 8192) return launch_norm<1, 8, kType, kAdd>(a, st);
+  if (a.dim <= 16384) return launch_norm<1, 16, kType, kAdd>(a, st);
+  if (a.dim <= 32768) return launch_norm<2, 16, kType, kAdd>(a, st);
+  return launch_norm<4, 16, kType, kAdd>(a, st);
+}
+template <int kType>
+cudaError_t launch_norm_add(const NormArgs &a, cudaStream_t st) {
+  if (!a.add) return launch_norm_k<kType, -1>(a, st);
+  if (a.add_dtype == D3_FP32) return launch_norm_k<kType, D3_FP32>(a, st);
+  return launch_norm_k<kType, kType>(a, st);
 }
 
 // ------------------------------------------------------------------ weights to 8 bits
@@ -336,14 +441,14 @@ int32_t d3_add_norm(const d3_add_norm_args *a, void *cuda_stream) {
   p.x_stride = a->x_stride; p.add_stride = a->add_stride; p.total_stride = a->total_stride; p.out_stride = a->out_stride;
   p.scale_stride = a->scale_stride;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int pieces = a->dim / 8;
-  auto threads_for = [&](int v) { return (pieces + 32 * v - 1) / (32 * v) * 32; };
   cudaError_t e;
-  if (pieces <= 32) e = launch_norm<1>(p, 32, st);
-  else if (pieces <= 1024 && rows < 148 * 4) e = launch_norm<1>(p, threads_for(1), st);
-  else if (pieces <= 1024) e = launch_norm<2>(p, threads_for(2), st);
-  else if (pieces <= 4096) e = launch_norm<4>(p, threads_for(4), st);
-  else e = launch_norm<8>(p, threads_for(8), st);
+  const long long quant = (rows * nb + kQuant * kQuantBlocks - 1) / (kQuant * kQuantBlocks);
+  if (eight && !a->add_dev && !a->gain_dev && quant * kQuant * kQuantBlocks <= 0x7fffffffll) {
+    void (*kernel)(NormArgs) = a->x_dtype == D3_FP32 ? k_quantize<D3_FP32> : a->x_dtype == D3_BF16 ? k_quantize<D3_BF16> : k_quantize<D3_FP16>;
+    e = launch_pdl(kernel, dim3((unsigned)quant), dim3(kQuantThreads), 0, st, p);
+  } else {
+    e = a->x_dtype == D3_FP32 ? launch_norm_add<D3_FP32>(p, st) : a->x_dtype == D3_BF16 ? launch_norm_add<D3_BF16>(p, st) : launch_norm_add<D3_FP16>(p, st);
+  }
   return e == cudaSuccess ? D3_OK : D3_ECUDA;
 }
 

@@ -140,11 +140,14 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-// scale of a block whose largest absolute value is `top`, and what its numbers are multiplied with before they are rounded
+// Scale of a block whose largest absolute value is `top`, and what its numbers are multiplied with before they are rounded: 448 / top
+// to 2^-22, which the rounding to 2^-4 does not see.
 __device__ __forceinline__ float block_scale(float top, float &inverse) {
-  const float scale = max_nan(top, kLeastTop) / kE4m3Max;
-  inverse = 1.f / scale;
-  return scale;
+  top = max_nan(top, kLeastTop);
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(top));
+  inverse = kE4m3Max * r;
+  return top / kE4m3Max;
 }
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
