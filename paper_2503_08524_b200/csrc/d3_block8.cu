@@ -364,8 +364,12 @@ int32_t product(const d3_weight8 *const (&w)[2], const d3_matmul8_args *a, cudaS
   p.status = a->status_dev;
   p.wait_tries = kWaitTries;
   const int64_t a_stride = rows > 1 ? a->a_stride : (int64_t)k;
-  const cudaError_t e = a->n_rows <= kFewRows ? launch_mm8_few(*map[0], map[1], a->a_dev, a_stride, p, st)
-                                              : launch_mm8_many(*map[0], map[1], a->a_dev, a_stride, p, st);
+  // Two kernels: one reads the weights for up to 128 rows at a time, one multiplies 256 rows by 256 weight rows at the tensor cores'
+  // rate, if there are tiles enough for every pair of SMs.
+  FewPlan plan;
+  const bool few = plan_mm8_few(p, mats, plan) <= estimate_mm8_many(p, mats);
+  const cudaError_t e = few ? launch_mm8_few(*map[0], map[1], a->a_dev, a_stride, p, plan, st)
+                            : launch_mm8_many(*map[0], map[1], a->a_dev, a_stride, p, st);
   return e == cudaSuccess ? D3_OK : D3_ECUDA;
 }
 

@@ -74,9 +74,12 @@ struct Mm8Args {
   uint32_t wait_tries;
 };
 // each enqueues one kernel; cudaSuccess or what the launch said (w1: the second matrix of the gated form)
-cudaError_t launch_mm8_few(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, const Mm8Args &p, cudaStream_t st);
+struct FewPlan { int rows, split; };   // rows of a CTA, CTAs that share the k of a tile
+cudaError_t launch_mm8_few(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, const Mm8Args &p, const FewPlan &plan, cudaStream_t st);
 cudaError_t launch_mm8_many(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, const Mm8Args &p, cudaStream_t st);
-constexpr int kFewRows = 128;        // rows that the kernel for few rows takes
+// estimates of what the kernels take, in us; `plan`: the best way of the kernel for few rows
+float plan_mm8_few(const Mm8Args &p, int mats, FewPlan &plan);
+float estimate_mm8_many(const Mm8Args &p, int mats);
 
 // ------------------------------------------------------------------ device
 #ifdef __CUDACC__

@@ -1,4 +1,4 @@
-// Products of up to kFewRows rows in 8 bits with a weight matrix in 8 bits: weights stream, rows ride along.
+// Products of few rows in 8 bits with a weight matrix in 8 bits: weights stream, rows ride along.
 //
 //   y[row][r] = sum_b as[row][b] ws[r / 128][b] sum_{k in block b} a[row][k] w[r][k]
 //
@@ -12,9 +12,9 @@
 // the two scales and added to registers; that is handed over a unit of U blocks at a time, while the next unit is
 // multiplied into the other half of the tensor memory.
 //
-// A CTA has one tile (gated: of both matrices).  Some 96 of them keep the memory busy; where there are fewer, k is cut between the
-// CTAs of a cluster, whose sums meet in distributed shared memory in the order of their ranks.  More CTAs cost more than they
-// give (clusters are started one after another).  us by the number of CTAs: 1 row, 4096 -> 12288: 96 11.9, 192 12.8, 288 17.6;
+// A CTA has one tile (gated: of both matrices) for N rows.  Where that makes too few CTAs, k is cut between those of a cluster, whose
+// sums meet in distributed shared memory in the order of their ranks; more CTAs cost more than they give (clusters are
+// started one after another).  us by the number of CTAs: 1 row, 4096 -> 12288: 96 11.9, 192 12.8, 288 17.6;
 // 32 rows, 11008 -> 4096: 32 24.4, 64 16.0, 128 12.5, 256 13.7; 4 rows, 8192 -> 10240: 80 19.6, 160 17.1, 320 21.8; gated,
 // 8 rows, 5120 -> 13824: 108 25.9, 216 26.3.
 //
@@ -22,6 +22,8 @@
 // one call to the next 1 to 1.4, the first copies' way 1.5.  A CTA takes at most half of an SM (but for more than 64 rows),
 // so the next call's CTAs are set up beside it.  Letting them ask for weights ahead of their turn gave nothing (copies
 // into the ring 12.5 us where this takes 11.9) or cost (into L2 box by box 14.0, row by row 18.4).
+#include <math.h>
+
 #include <atomic>
 
 #include "d3_block8.cuh"
@@ -33,7 +35,7 @@ namespace {
 constexpr int kTileBytes = 128 * 128;            // a block's share of a weight matrix
 constexpr int kMaxStages = 12;
 constexpr int kChunk = 8, kChunks = 3;           // scales come in chunks of 8 blocks, through a ring of their own
-constexpr int kMostSplit = 8, kEnoughTiles = 96;
+constexpr int kMostSplit = 8;
 constexpr int kHalfSmem = 112 * 1024, kWholeSmem = 213 * 1024;      // dynamic shared memory, of one of two CTAs on an SM or a CTA alone
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -322,7 +324,7 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
 }
 
 template <int C, int G, int W, int U>
-cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args &p, int dev, cudaStream_t st) {
+cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args &p, int split, int dev, cudaStream_t st) {
   using F = Few<C, G, W, U>;
   static std::atomic<bool> ready[64];   // the shared-memory attribute is per device; setting it twice is harmless
   if (!ready[dev].load(std::memory_order_acquire)) {
@@ -338,10 +340,7 @@ cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args
   if (stages > kMaxStages) stages = kMaxStages;
   const int least = (F::kSums + F::kStage - 1) / F::kStage;               // the ring holds the sums in the end
   if (stages < least) stages = least;
-  // k is cut only where there are fewer tiles than keep the memory busy
-  const int tiles = (p.n + 127) / 128, chunks = (p.n_kb + kChunk - 1) / kChunk;
-  int split = 1;
-  while (split < kMostSplit && tiles * split < kEnoughTiles && split * 2 <= chunks) split *= 2;
+  const int tiles = (p.n + 127) / 128;
   t.stages = stages;
   t.split = split;
   const int es = type_bytes(p.out_dtype);
@@ -366,29 +365,63 @@ cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args
   return cudaLaunchKernelEx(&cfg, k_mm8_few<C, G, W, U>, *m0, *m1, *m, static_cast<const FewArgs>(t));
 }
 
+// What a call takes with N rows a CTA and k cut in `split`, in us, as measured: a block of k takes a CTA 0.24 us (N = 16, 32), 0.315
+// (64) or 0.48 (128), gated 0.33, 0.5 and 0.9; two CTAs on an SM 1.35 times that (N = 64: 1.8); the memory gives 6.3 TB/s, L2 13;
+// a call costs 3.3 us, clusters of 2, 4 and 8 CTAs 0.5, 1 and 3.5 more.  (rows x k x n, estimate / measured, and the other
+// kernel: 128 x 8192 x 1024: N 32 in 4 8.1 / 7.8; 256 x 8192 x 1024: 64 in 4 9.3 / 9.9, 32; 300 x 28672 x 500: 64 in 4 21.9 / 23.7,
+// 136; 512 x 4096 x 512: 64 in 4 6.8 / 7.0, 18.4; 2000 x 11008 x 300: 128 in 2 24.4 / 28.8, 80; 200 x 11008 x 4096: 128 in 2
+// 24.4 / 28.5, 44.)
+float few_us(const Mm8Args &p, int mats, int N, int split) {
+  constexpr float kSms = 148.f;
+  const float rows = (float)((p.n_rows + N - 1) / N), tiles = (float)((p.n + 127) / 128), ctas = rows * tiles * split;
+  const float blocks = (float)((((p.n_kb + kChunk - 1) / kChunk + split - 1) / split) * kChunk), kb = blocks < p.n_kb ? blocks : (float)p.n_kb;
+  const float each = mats == 2 ? (N <= 32 ? 0.33f : N == 64 ? 0.5f : 0.9f) : (N <= 32 ? 0.24f : N == 64 ? 0.315f : 0.48f);
+  const bool shared = mats == 1 && N <= 64;                      // two CTAs fit on an SM
+  const float on_sm = ceilf(ctas / kSms);
+  float work = kb * each;
+  if (on_sm > 1.f) work *= shared ? ceilf(on_sm / 2.f) * (N == 64 ? 1.8f : 1.35f) : on_sm;
+  if (!shared && split == kMostSplit && ctas > 64.f) work *= 2.f; // (eight SMs at a time do not come out even)
+  const float memory = (float)p.n * p.k * mats / 6.3e6f, l2 = ctas * kb * (mats * 16384.f + N * 128.f) / 13e6f;
+  const float most = work > memory ? (work > l2 ? work : l2) : (memory > l2 ? memory : l2);
+  return most + 3.3f + (split == 1 ? 0.f : split == 2 ? 0.5f : split == 4 ? 1.f : 3.5f);
+}
+
 }  // namespace
 
-cudaError_t launch_mm8_few(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, const Mm8Args &p, cudaStream_t st) {
+float plan_mm8_few(const Mm8Args &p, int mats, FewPlan &plan) {
+  float best = INFINITY;
+  for (int N = 16; N <= 128; N *= 2) {
+    if (N > 16 && N / 2 >= p.n_rows) break;                      // half of it would do
+    if ((p.n_rows + N - 1) / N > 65535) continue;
+    for (int split = 1; split <= kMostSplit && split <= (p.n_kb + kChunk - 1) / kChunk; split *= 2) {
+      const float us = few_us(p, mats, N, split);
+      if (us < best) { best = us; plan.rows = N; plan.split = split; }
+    }
+  }
+  return best;
+}
+
+cudaError_t launch_mm8_few(const TMap &w0, const TMap *w1, const void *a, int64_t a_stride, const Mm8Args &p, const FewPlan &plan, cudaStream_t st) {
   int dev = 0;
   const cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  const int padded = p.n_rows <= 16 ? 16 : p.n_rows <= 32 ? 32 : p.n_rows <= 64 ? 64 : 128;
   TMap ma;
-  if (!encode_rows8(&ma, a, p.n_rows, p.k, a_stride, padded)) return cudaErrorInvalidValue;
+  if (!encode_rows8(&ma, a, p.n_rows, p.k, a_stride, plan.rows)) return cudaErrorInvalidValue;
+  const int s = plan.split;
   if (w1) {
-    switch (padded) {
-      case 16: return launch<16, 1, 2, 4>(w0, *w1, ma, p, dev, st);
-      case 32: return launch<32, 1, 2, 2>(w0, *w1, ma, p, dev, st);
-      case 64: return launch<64, 1, 2, 1>(w0, *w1, ma, p, dev, st);
-      default: return launch<64, 2, 2, 1>(w0, *w1, ma, p, dev, st);
+    switch (plan.rows) {
+      case 16: return launch<16, 1, 2, 4>(w0, *w1, ma, p, s, dev, st);
+      case 32: return launch<32, 1, 2, 2>(w0, *w1, ma, p, s, dev, st);
+      case 64: return launch<64, 1, 2, 1>(w0, *w1, ma, p, s, dev, st);
+      default: return launch<64, 2, 2, 1>(w0, *w1, ma, p, s, dev, st);
     }
   }
-  switch (padded) {
-    case 16: return launch<16, 1, 1, 4>(w0, w0, ma, p, dev, st);
-    case 32: return launch<32, 1, 1, 4>(w0, w0, ma, p, dev, st);
-    case 64: return launch<64, 1, 1, 2>(w0, w0, ma, p, dev, st);
-    default: return launch<64, 2, 1, 1>(w0, w0, ma, p, dev, st);
+  switch (plan.rows) {
+    case 16: return launch<16, 1, 1, 4>(w0, w0, ma, p, s, dev, st);
+    case 32: return launch<32, 1, 1, 4>(w0, w0, ma, p, s, dev, st);
+    case 64: return launch<64, 1, 1, 2>(w0, w0, ma, p, s, dev, st);
+    default: return launch<64, 2, 1, 1>(w0, w0, ma, p, s, dev, st);
   }
 }
 
