@@ -366,20 +366,19 @@ cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args
 }
 
 // What a call takes with N rows a CTA and k cut in `split`, in us, as measured: a block of k takes a CTA 0.24 us (N = 16, 32), 0.315
-// (64) or 0.48 (128), gated 0.33, 0.5 and 0.9; two CTAs on an SM 1.35 times that (N = 64: 1.8); the memory gives 6.3 TB/s, L2 13;
-// a call costs 3.3 us, clusters of 2, 4 and 8 CTAs 0.5, 1 and 3.5 more.  (rows x k x n, estimate / measured, and the other
-// kernel: 128 x 8192 x 1024: N 32 in 4 8.1 / 7.8; 256 x 8192 x 1024: 64 in 4 9.3 / 9.9, 32; 300 x 28672 x 500: 64 in 4 21.9 / 23.7,
-// 136; 512 x 4096 x 512: 64 in 4 6.8 / 7.0, 18.4; 2000 x 11008 x 300: 128 in 2 24.4 / 28.8, 80; 200 x 11008 x 4096: 128 in 2
-// 24.4 / 28.5, 44.)
+// (64) or 0.48 (128), gated 0.335, 0.42, 0.76 and 0.95; two CTAs on an SM 1.35 times that (N = 64: 1.8); CTAs that find no
+// place at first 6 us more; the memory gives 6.3 TB/s, L2 13; a call costs 3.3 us, clusters of 2, 4 and 8 CTAs 0.5, 1 and 3.5
+// more.  (rows x k x n, estimate / measured, and the other kernel: 128 x 8192 x 1024: N 32 in 4 8.1 / 7.9, 32; 256 x 8192 x 1024:
+// 64 in 4 9.3 / 9.9, 32; 300 x 28672 x 500: 64 in 4 21.9 / 23.7, 136; 512 x 4096 x 512: 64 in 4 6.8 / 7.0, 18.4; 2000 x 11008 x
+// 300: 128 in 2 24.4 / 28.8, 80; gated 64 x 4096 x 11008: 64 27.6 / 29.0, 37.6; 128 rows of it: 128 33.7 / 35.0, 38.1.)
 float few_us(const Mm8Args &p, int mats, int N, int split) {
   constexpr float kSms = 148.f;
   const float rows = (float)((p.n_rows + N - 1) / N), tiles = (float)((p.n + 127) / 128), ctas = rows * tiles * split;
   const float blocks = (float)((((p.n_kb + kChunk - 1) / kChunk + split - 1) / split) * kChunk), kb = blocks < p.n_kb ? blocks : (float)p.n_kb;
-  const float each = mats == 2 ? (N <= 32 ? 0.33f : N == 64 ? 0.5f : 0.9f) : (N <= 32 ? 0.24f : N == 64 ? 0.315f : 0.48f);
+  const float each = mats == 2 ? (N == 16 ? 0.335f : N == 32 ? 0.42f : N == 64 ? 0.76f : 0.95f) : (N <= 32 ? 0.24f : N == 64 ? 0.315f : 0.48f);
   const bool shared = mats == 1 && N <= 64;                      // two CTAs fit on an SM
-  const float on_sm = ceilf(ctas / kSms);
-  float work = kb * each;
-  if (on_sm > 1.f) work *= shared ? ceilf(on_sm / 2.f) * (N == 64 ? 1.8f : 1.35f) : on_sm;
+  const float on_sm = ceilf(ctas / kSms), waves = shared ? (on_sm > 2.f ? on_sm / 2.f : 1.f) : on_sm;
+  float work = waves * kb * each * (shared && on_sm > 1.f ? (N == 64 ? 1.8f : 1.35f) : 1.f) + 6.f * (waves - 1.f);
   if (!shared && split == kMostSplit && ctas > 64.f) work *= 2.f; // (eight SMs at a time do not come out even)
   const float memory = (float)p.n * p.k * mats / 6.3e6f, l2 = ctas * kb * (mats * 16384.f + N * 128.f) / 13e6f;
   const float most = work > memory ? (work > l2 ? work : l2) : (memory > l2 ? memory : l2);

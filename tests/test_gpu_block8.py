@@ -350,3 +350,16 @@ def test_logits_report_bad_entries_and_go_on():
         y, dy = logits_form(z, **bad)
         check_logits(out, token, y, dy)
         assert int(status) == (-1 if name else 0), name
+
+
+# the ways a product can take (rows of a CTA, k cut between CTAs, either kernel), whatever the sizes that choose them
+@pytest.mark.parametrize("rows,k,n", [(1, 28672, 16), (20, 4096, 256), (40, 11008, 130), (100, 2064, 1000), (128, 8192, 1024), (256, 8192, 1024), (300, 8192, 500),
+                                      (1000, 4096, 260), (3000, 1040, 200), (257, 4096, 2304), (520, 272, 3000)])
+def test_products_of_middling_sizes(rows, k, n):
+    g = gen(rows + k + n)
+    a, s = F.some_rows(rows, k, g)
+    gate, up = F.some_weight(n, k, g), F.some_weight(n, k, g)
+    y, dy = F.product(a, s, *gate)
+    F.check_wide(K.d3_matmul8(a, s, K.Weight8(*gate), dtype=FP32), y, dy)
+    h, dh = F.gated(y, dy, *F.product(a, s, *up))
+    F.check_8_bits(*K.d3_gated_matmul8(a, s, K.Weight8(*gate), K.Weight8(*up)), h, dh)
