@@ -601,6 +601,15 @@ typedef struct d3_matmul8_args {
 } d3_matmul8_args;
 int32_t d3_matmul8(const d3_weight8 *w, const d3_matmul8_args *a, void *cuda_stream);
 int32_t d3_gated_matmul8(const d3_weight8 *gate, const d3_weight8 *up, const d3_matmul8_args *a, void *cuda_stream);
+/* Failure detection, as d3_paged_set_wait_ns.  Every wait inside the two products gives up after about `ns` nanoseconds
+ * (default 2e9; it is counted in tries of 40 to 80 ns): the call stores D3_ETIMEOUT, lets what is in flight land (some
+ * milliseconds at least) and ends; nothing traps, and the next call is not affected.  Process-wide, for calls made from now
+ * on (a captured call keeps the limit it was captured with).  ns >= 1. */
+int32_t d3_matmul8_set_wait_ns(uint64_t ns);
+/* Drill for the above: in the first CTA of the next product with rows, every stage of copies expects one arrival more than
+ * comes, so the waits for them can only end by their limit (set a short one first).  0 takes a drill back.  That call's
+ * outputs are undefined; if it is captured, every replay of it stalls. */
+int32_t d3_matmul8_stall_next(int32_t on);
 
 /* Row by row, z the row's logits in fp32, each step rounded once:
  *   of a token among the first lengths[row] of history[row]:  z *= z > 0 ? 1 / repetition : repetition

@@ -27,7 +27,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import build as _build
-from .binding import LIB, OK, D3Error
+from .binding import EINVAL, LIB, OK, D3Error
 from .paged import _TYPES, _on_stream, _refuse
 
 _block_call = _build.load_call("block_call")
@@ -159,6 +159,20 @@ def d3_gated_matmul8(a: torch.Tensor, a_scale: torch.Tensor, gate: Weight8, up: 
         return _on_stream(lambda: d3_gated_matmul8(a, a_scale, gate, up, out=out, scale=scale, dtype=dtype, status=status), gate.index, stream,
                           "d3_gated_matmul8")
     return _block_call.product(gate._at, up._at, gate.index, a, a_scale, out, scale, dtype, status)
+
+
+def d3_matmul8_set_wait_ns(ns: int) -> None:
+    """Limit of every wait inside the products of this process from now on (default 2e9)."""
+    rc = LIB.d3_matmul8_set_wait_ns(int(ns)) if int(ns) >= 0 else EINVAL
+    if rc != OK:
+        raise D3Error(rc, "d3_matmul8_set_wait_ns")
+
+
+def d3_matmul8_stall_next(on: int) -> None:
+    """Drill: the waits for copies of the next product cannot be satisfied (1; 0: none)."""
+    rc = LIB.d3_matmul8_stall_next(int(on))
+    if rc != OK:
+        raise D3Error(rc, "d3_matmul8_stall_next")
 
 
 def d3_constrain_logits(logits: torch.Tensor, *, history: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,

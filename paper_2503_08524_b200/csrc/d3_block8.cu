@@ -1,6 +1,8 @@
 // 8-bit block operators: residual sum + RMSNorm + quantising, weights to 8 bits, and the C ABI of the products.
 #include <math.h>
 
+#include <atomic>
+
 #include "d3_block8.cuh"
 
 namespace d3 {
@@ -309,6 +311,9 @@ bool made_for(const Weight8Map *m, const d3_weight8 &w) {
 }
 int64_t scale_blocks(int64_t v) { return (v + kScaleBlock - 1) / kScaleBlock; }
 
+std::atomic<uint32_t> wait_tries{kWaitTries};
+std::atomic<int> stall_next{0};
+
 // the checks and the launch that both products share
 int32_t product(const d3_weight8 *const (&w)[2], const d3_matmul8_args *a, cudaStream_t st) {
   const int mats = w[1] ? 2 : 1;
@@ -362,7 +367,8 @@ int32_t product(const d3_weight8 *const (&w)[2], const d3_matmul8_args *a, cudaS
   p.out = a->out_dev; p.out_stride = rows > 1 ? a->out_stride : n; p.out_dtype = a->out_dtype;
   p.scale = a->scale_dev; p.scale_stride = rows > 1 ? a->scale_stride : nb;
   p.status = a->status_dev;
-  p.wait_tries = kWaitTries;
+  p.wait_tries = wait_tries.load(std::memory_order_relaxed);
+  p.stall = stall_next.exchange(0, std::memory_order_relaxed);
   const int64_t a_stride = rows > 1 ? a->a_stride : (int64_t)k;
   // Two kernels: one reads the weights for up to 128 rows at a time, one multiplies 256 rows by 256 weight rows at the tensor cores'
   // rate, if there are tiles enough for every pair of SMs.
@@ -479,6 +485,19 @@ int32_t d3_quantize_weight(const void *w_dev, int32_t dtype, int64_t row_stride,
   q.q = static_cast<unsigned char *>(const_cast<void *>(w8->q_dev)); q.scale = const_cast<float *>(w8->scale_dev);
   return launch_pdl(k_quantize_weight, dim3((unsigned)kb, (unsigned)nb), dim3(256), 0, static_cast<cudaStream_t>(cuda_stream), q) == cudaSuccess
              ? D3_OK : D3_ECUDA;
+}
+
+int32_t d3_matmul8_set_wait_ns(uint64_t ns) {
+  if (ns < 1) return D3_EINVAL;
+  const uint64_t tries = ns / kTryNs + 1;
+  wait_tries.store(tries < 0x7fffffffull ? (uint32_t)tries : 0x7fffffffu, std::memory_order_relaxed);
+  return D3_OK;
+}
+
+int32_t d3_matmul8_stall_next(int32_t on) {
+  if (on != 0 && on != 1) return D3_EINVAL;
+  stall_next.store(on, std::memory_order_relaxed);
+  return D3_OK;
 }
 
 int32_t d3_matmul8(const d3_weight8 *w, const d3_matmul8_args *a, void *cuda_stream) {

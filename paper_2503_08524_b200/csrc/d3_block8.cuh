@@ -12,6 +12,7 @@ namespace d3 {
 constexpr int kScaleBlock = 128;                 // numbers that share a scale
 constexpr float kE4m3Max = 448.f;
 constexpr float kLeastTop = 7.888609e-31f;       // 2^-100: a block's largest number counts as this at least
+constexpr uint32_t kTryNs = 50;                  // a try of a wait that fails takes 40 to 80 ns
 constexpr uint32_t kWaitTries = 40000000u;       // bound of every device-side wait: about two seconds
 constexpr uint32_t kDrainTries = 40000u;         // the least that copies and products in flight are waited for: about two milliseconds
 
@@ -72,6 +73,7 @@ struct Mm8Args {
   long long scale_stride;
   int32_t *status;
   uint32_t wait_tries;
+  int stall;                         // drill: the first CTA's copies seem never to land
 };
 // each enqueues one kernel; cudaSuccess or what the launch said (w1: the second matrix of the gated form)
 struct FewPlan { int rows, split; };   // rows of a CTA, CTAs that share the k of a tile

@@ -121,7 +121,7 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
   using F = Few<C, G, W, U>;
   constexpr int N = F::N;
   extern __shared__ unsigned char raw[];
-  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[2], s_read[2], s_there[kChunks], s_used[kChunks], s_tail;
+  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[2], s_read[2], s_there[kChunks], s_used[kChunks], s_tail, s_never;
   __shared__ __align__(16) float s_rows[kChunks][kChunk][N], s_weights[kChunks][kChunk][2];
   __shared__ uint32_t s_tmem;
   __shared__ int s_gave_up;
@@ -135,10 +135,12 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
   const uint32_t ring = (smem_at(raw) + 1023u) & ~1023u;       // the swizzle goes by the address
   volatile int *gave_up = &s_gave_up;
   if (tid == 32) {
-    for (int s = 0; s < S; ++s) { mbar_init(smem_at(&s_full[s]), 1); mbar_init(smem_at(&s_empty[s]), 1); }
+    const uint32_t copies = t.m.stall && blockIdx.x == 0 && blockIdx.y == 0 ? 2 : 1;
+    for (int s = 0; s < S; ++s) { mbar_init(smem_at(&s_full[s]), copies); mbar_init(smem_at(&s_empty[s]), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(smem_at(&s_done[b]), 1); mbar_init(smem_at(&s_read[b]), 4 * G); }
     for (int c = 0; c < kChunks; ++c) { mbar_init(smem_at(&s_there[c]), 32); mbar_init(smem_at(&s_used[c]), 4 * G); }
     mbar_init(smem_at(&s_tail), 1);
+    mbar_init(smem_at(&s_never), 1);
     s_gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -172,10 +174,6 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
           tma_rows8(at + W * kTileBytes, &map_a, b * 128, row0, full);
         }
         if (++s == S) { s = 0; phase ^= 1; }
-      }
-      if (*gave_up) {   // copies in flight must land before the CTA's shared memory is given back
-        for (int j = max(b0, b - S); j < b; ++j)
-          mbar_wait(smem_at(&s_full[(j - b0) % S]), (uint32_t)(((j - b0) / S) & 1), gave_up, max(t.m.wait_tries, kDrainTries), false);
       }
       __syncwarp();
     } else if (warp == 1) {
@@ -315,7 +313,10 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
     }
     finish4(t, row0 + j, n0, y[0], tile, lane);
   }
-  if (tid == 0 && *gave_up && t.m.status) *t.m.status = D3_ETIMEOUT;
+  if (*gave_up && warp == 0) {     // copies may be in flight, which must land before the CTA's shared memory is given back
+    mbar_wait(smem_at(&s_never), 0u, gave_up, kDrainTries, false);
+    if (lane == 0 && t.m.status) *t.m.status = D3_ETIMEOUT;
+  }
   tc_fence_before();
   if (split > 1) cluster_sync();   // no CTA's sums go while another one reads them
   else __syncthreads();

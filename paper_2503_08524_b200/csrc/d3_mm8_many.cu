@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ CUtensorMap map_a,
            const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ManyArgs t) {
   extern __shared__ unsigned char raw[];
-  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_read[2], s_there[kChunks], s_used[kChunks], s_tail;
+  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_read[2], s_there[kChunks], s_used[kChunks], s_tail, s_never;
   __shared__ __align__(16) float s_rows[kChunks][128][kChunk], s_weights[kChunks][2][kChunk];
   __shared__ float s_top[2][128];
   __shared__ uint32_t s_tmem;
@@ -109,10 +109,12 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
   const int wide = W == 2 ? 128 : 256;             // result columns of a tile
 
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(smem_at(&s_full[s]), 1); mbar_init(smem_at(&s_empty[s]), 1); }
+    const uint32_t copies = t.m.stall && blockIdx.x == 0 ? 2 : 1;
+    for (int s = 0; s < kStages; ++s) { mbar_init(smem_at(&s_full[s]), copies); mbar_init(smem_at(&s_empty[s]), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(smem_at(&s_done[b]), 1); mbar_init(smem_at(&s_read[b]), 16); }
     for (int c = 0; c < kChunks; ++c) { mbar_init(smem_at(&s_there[c]), 32); mbar_init(smem_at(&s_used[c]), 8); }
     mbar_init(smem_at(&s_tail), 1);
+    mbar_init(smem_at(&s_never), 1);
     s_gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -152,10 +154,6 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
           }
           if (++s == kStages) { s = 0; phase ^= 1; }
         }
-      }
-      if (*gave_up && rank == 0) {   // copies in flight must land before either CTA's shared memory is given back
-        for (int j = max(0, it - kStages); j < it; ++j)
-          mbar_wait(smem_at(&s_full[j % kStages]), (uint32_t)((j / kStages) & 1), gave_up, max(t.m.wait_tries, kDrainTries), false);
       }
       __syncwarp();
     } else if (warp == 1) {
@@ -370,7 +368,10 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
     if ((warp & 3) == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   __syncthreads();
-  if (tid == 0 && *gave_up && t.m.status) *t.m.status = D3_ETIMEOUT;
+  if (*gave_up && warp == 0) {     // copies may be in flight, which must land before the CTA's shared memory is given back
+    mbar_wait(smem_at(&s_never), 0u, gave_up, kDrainTries, false);
+    if (lane == 0 && t.m.status) *t.m.status = D3_ETIMEOUT;
+  }
   tc_fence_before();
   pair_sync();   // neither CTA goes while the other one's products read its shared memory or arrive at its barriers
   if (warp == 1)
