@@ -581,7 +581,8 @@ typedef struct d3_weight8 {
 #define D3_WEIGHT8_MAP_BYTES 256
 int32_t d3_weight8_map(const d3_weight8 *w, void *map);
 
-/* w [n][k] (D3_BF16, D3_FP16, D3_FP32; row stride in elements) to w8's q and scales (which the call writes). */
+/* w [n][k] (D3_BF16, D3_FP16, D3_FP32; row stride in elements) to w8's q and scales (which the call writes); n up to
+ * 65535 * 128. */
 int32_t d3_quantize_weight(const void *w_dev, int32_t dtype, int64_t row_stride, const d3_weight8 *w8, void *cuda_stream);
 
 /* out[row][n] = sum_k a[row][k] w[n][k]: the products of a block of 128 k are summed by the tensor core in fp32, each
@@ -623,8 +624,8 @@ int32_t d3_matmul8_stall_next(int32_t on);
 typedef struct d3_constrain_logits_args {
   uint32_t struct_size;
   int32_t dtype;             /* D3_BF16, D3_FP16, D3_FP32                                */
-  int32_t n_rows, vocab;     /* 0..65535; >= 1                                           */
-  int32_t n_history, n_bias, n_masks;
+  int32_t n_rows, vocab;     /* 0..65535; 1..2^30                                        */
+  int32_t n_history, n_bias, n_masks;   /* >= 0, the first two up to 2^30                */
   const void *logits_dev;
   void *out_dev;             /* may be logits (with the same stride)                     */
   int64_t logits_stride, out_stride, history_stride, bias_stride, mask_stride;   /* in elements; any >= the row */

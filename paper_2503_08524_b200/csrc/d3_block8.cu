@@ -244,11 +244,11 @@ struct QuantWeightArgs {
   unsigned char *q;
   float *scale;
 };
-// One block of 128 x 128 per CTA: thread t has 64 numbers of row t / 2, 8 at a time (k is a multiple of 16).  No trigger for the
-// next kernel: what this one writes, a product may read before it waits.
+// One block of 128 x 128 per CTA: thread t has 64 numbers of row t / 2, 8 at a time (k is a multiple of 16).
 __global__ void __launch_bounds__(256) k_quantize_weight(const __grid_constant__ QuantWeightArgs a) {
   __shared__ float s_top[8];
   pdl_wait();
+  pdl_trigger();
   const int row = blockIdx.y * 128 + (threadIdx.x >> 1), k0 = blockIdx.x * 128 + (threadIdx.x & 1) * 64;
   float v[8][8];
   float top = 0.f;

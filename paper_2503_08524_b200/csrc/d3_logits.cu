@@ -317,6 +317,7 @@ extern "C" {
 int32_t d3_constrain_logits(const d3_constrain_logits_args *a, void *cuda_stream) {
   if (!a || a->struct_size != sizeof(d3_constrain_logits_args) || !wide_type(a->dtype)) return D3_EINVAL;
   if (a->n_rows < 0 || a->n_rows > 65535 || a->vocab < 1 || a->n_history < 0 || a->n_bias < 0 || a->n_masks < 0) return D3_EINVAL;
+  if (a->n_history > (1 << 30) || a->n_bias > (1 << 30)) return D3_EINVAL;
   const int es = type_bytes(a->dtype);
   const int64_t rows = a->n_rows, vocab = a->vocab, words = (vocab + 31) / 32, most = (int64_t)1 << 38;
   auto stride_ok = [&](int64_t s, int64_t least) { return rows <= 1 || (s >= least && s <= most); };

@@ -109,7 +109,7 @@ def test_weights_that_are_not_quantized(dtype, stride, at):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(struct_size=1), dict(dtype=E4M3), dict(n_rows=-1), dict(n_rows=65536), dict(vocab=0), dict(vocab=(1 << 30) + 1), dict(n_history=-1), dict(n_bias=-1),
+    dict(struct_size=1), dict(dtype=E4M3), dict(n_rows=-1), dict(n_rows=65536), dict(vocab=0), dict(vocab=(1 << 30) + 1), dict(n_history=-1), dict(n_bias=-1), dict(n_history=(1 << 30) + 1), dict(n_bias=(1 << 30) + 1),
     dict(n_masks=-1), dict(logits_dev=None), dict(out_dev=None), dict(logits_dev=FAKE + 2), dict(out_dev=FAKE + MB + 1), dict(out_stride=999),
     dict(history_dev=None), dict(bias_dev=None), dict(bias_ids_dev=None), dict(masks_dev=None), dict(mask_of_dev=None), dict(history_stride=-1),
     dict(bias_stride=-4), dict(mask_stride=-1), dict(token_dev=FAKE + 2), dict(status_dev=FAKE + 3), dict(lengths_dev=FAKE + 1),

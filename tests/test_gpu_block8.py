@@ -153,7 +153,7 @@ def test_gated(rows, k, n, dtype):
 
 
 @pytest.mark.parametrize("rows", [1, 30, 120, 140, 400])
-@pytest.mark.parametrize("extra", [1, 4, 16])
+@pytest.mark.parametrize("extra", [1, 3, 4, 16])
 def test_products_between_strides(rows, extra):
     k, n = 400, 333
     g = gen(rows)
@@ -335,6 +335,21 @@ def test_logits_that_are_not_numbers_and_ties():
     out, token = K.d3_constrain_logits(z, masks=masks, mask_of=mask_of)
     assert token.tolist() == [0, -1, -1, 39999, 20000, -1]
     assert float(out[0, 7]) == float("-inf") and torch.isnan(out[1]).all()
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 32000), (300, 1000)])
+def test_logits_without_a_token(rows, vocab):
+    """The C ABI's form that wants no token, and parts that are left out one by one."""
+    import ctypes as C
+    z, kw = some_logits(rows, vocab, 40, 3, 2, FP32, vocab)
+    out = torch.zeros_like(z)
+    args = K.ConstrainLogitsArgs(C.sizeof(K.ConstrainLogitsArgs), 2, rows, vocab, 0, 0, 0, z.data_ptr(), out.data_ptr(), vocab, vocab, 0, 0, 0)
+    assert K.LIB.d3_constrain_logits(C.byref(args), torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(out, z)
+    for left in (("history", "lengths", "prompt", "repetition", "frequency", "presence"), ("lengths",), ("prompt", "repetition"), ("frequency",), ("presence",),
+                 ("bias_ids", "bias"), ("masks", "mask_of")):
+        some = {k: v for k, v in kw.items() if k not in left}
+        check_logits(*K.d3_constrain_logits(z, **some), *logits_form(z, **some))
 
 
 def test_logits_report_bad_entries_and_go_on():
