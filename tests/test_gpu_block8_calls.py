@@ -200,3 +200,38 @@ def test_weights_without_a_map_of_their_own(rows):
     out = torch.zeros((rows, 260), dtype=BF16, device="cuda")
     args = K.Matmul8Args(C.sizeof(K.Matmul8Args), rows, P.BF16, a[0].data_ptr(), a[1].data_ptr(), out.data_ptr(), None, 272, 3, 260, 0, None)
     assert K.LIB.d3_matmul8(C.byref(bare), C.byref(args), None) == -1       # a map that was not made for this matrix
+
+
+FIRST = """
+import sys
+sys.path[:0] = [{root!r}, {tests!r}]
+import torch, block8_forms as F
+from paper_2503_08524_b200 import block8 as K
+g = torch.Generator(device="cuda").manual_seed(1)
+ws = [K.Weight8(*F.some_weight(n, 1040, g)) for n in (300, 5000)]
+a = [F.some_rows(r, 1040, g) for r in (3, 50, 2000)]
+x, gain, z = torch.randn((5, 1040), generator=g, device="cuda"), torch.ones(1040, device="cuda"), torch.randn((5, 40000), generator=g, device="cuda")
+h = torch.randint(0, 40000, (5, 40000), generator=g, device="cuda").to(torch.int32)
+def calls():
+    out = [K.d3_matmul8(*i, w) for i in a for w in ws] + [t for i in a for w in ws for t in K.d3_gated_matmul8(*i, w, w)]
+    out += list(K.d3_add_norm(x, gain, add=x)) + list(K.d3_quantize(x)) + list(K.d3_constrain_logits(z, history=h)) + list(K.d3_constrain_logits(z, history=h[:, :9]))
+    return [t.view(torch.uint8) for t in out]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):          # nothing of this process has run a kernel of these before
+    got = calls()
+for _ in range(2):
+    graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(p, q) for p, q in zip(got, calls()))
+print("same")
+"""
+
+
+def test_first_calls_under_capture():
+    import os
+    import subprocess
+    import sys
+    tests = os.path.dirname(os.path.abspath(__file__))
+    p = subprocess.run([sys.executable, "-c", FIRST.format(root=os.path.dirname(tests), tests=tests)], capture_output=True, text=True, timeout=300)
+    assert p.returncode == 0 and p.stdout.strip().endswith("same"), p.stderr[-2000:]
