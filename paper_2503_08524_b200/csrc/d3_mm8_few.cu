@@ -78,6 +78,7 @@ struct FewArgs {
   Mm8Args m;
   int stages, split;
   int wide;                // four results at a time may be written in one piece
+  int late;                // the next call may begin when this one's copies are asked for, and not at once
 };
 
 // A warp has the 128 results of a row that one tile of weight rows gives, lane l those at n0 = 128 tile + 4 l: rounds and writes
@@ -155,7 +156,7 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   pdl_wait();
-  pdl_trigger();
+  if (!t.late) pdl_trigger();
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kRegsControl));
@@ -176,6 +177,7 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
         if (++s == S) { s = 0; phase ^= 1; }
       }
       __syncwarp();
+      if (t.late) pdl_trigger();
     } else if (warp == 1) {
       // ---------------------------------------------------------- products
       constexpr uint32_t idesc = idesc_e4m3(128, N);
@@ -344,6 +346,9 @@ cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args
   const int tiles = (p.n + 127) / 128;
   t.stages = stages;
   t.split = split;
+  // Where some SMs have two CTAs, those of a call that begins early take places that even them out (4 rows, 8192 -> 10240, call
+  // after call: 20.4 us, begun late 18.2; 1 row, 4096 -> 12288, one CTA an SM: 11.8, late 12.0).
+  t.late = (long long)tiles * split * ((p.n_rows + F::N - 1) / F::N) > 148;
   const int es = type_bytes(p.out_dtype);
   t.wide = on_bytes(p.out, 4 * es) && (p.n_rows == 1 || p.out_stride % 4 == 0);
   cudaLaunchConfig_t cfg;
