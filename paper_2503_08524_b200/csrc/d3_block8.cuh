@@ -146,12 +146,13 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 // Scale of a block whose largest absolute value is `top`, and what its numbers are multiplied with before they are rounded: 448 / top
-// to 2^-22, which the rounding to 2^-4 does not see.
+// to 2^-22, which the rounding to 2^-4 does not see.  (The reciprocal is taken of top / 2^9: that of a top above 2^126 is no normal
+// number, and 0 here.)
 __device__ __forceinline__ float block_scale(float top, float &inverse) {
   top = max_nan(top, kLeastTop);
   float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(top));
-  inverse = kE4m3Max * r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(top * 0x1p-9f));
+  inverse = kE4m3Max * 0x1p-9f * r;
   return top / kE4m3Max;
 }
 
