@@ -543,7 +543,8 @@ int32_t d3_paged_view(const d3_model *m, int32_t layer, d3_paged_kv *kv, const i
  * Numbers in 8 bits: D3_E4M3 q[row][k] with fp32 scale[row][k / 128] (rows of activations) or
  * scale[row / 128][k / 128] (weights); the value is q times its scale.  A scale that these calls write is
  * max(largest absolute value of its block, 2^-100) / 448; NaN or infinite where the block holds a NaN or an infinity,
- * which makes what is computed from that block NaN.  Rounding to 8 bits is to nearest even. */
+ * which makes what is computed from that block NaN.  A number in 8 bits is its quotient by the scale, rounded to fp32 as division
+ * rounds it and then to nearest even. */
 
 /* y[row] = s / sqrt(mean(s^2) + eps) * gain with s = x + add, fp32 throughout (s is not rounded in between);
  * total = s in add's type.  gain_dev NULL: no norm, y = s.  Rows are `dim` contiguous numbers, strides in elements. */

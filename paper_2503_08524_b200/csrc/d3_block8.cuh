@@ -132,7 +132,7 @@ __device__ __forceinline__ float load1(const void *base, long long at, int dtype
   if (dtype == D3_BF16) return __bfloat162float(static_cast<const bf16 *>(base)[at]);
   return __half2float(static_cast<const __half *>(base)[at]);
 }
-// four floats in 8 bits each (saturating: only a NaN is beyond 448 after the division by the scale)
+// four floats in 8 bits each (saturating: only a NaN, or the rounding of a quotient, is beyond 448 after the division by the scale)
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
   uint16_t lo, hi;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
@@ -145,17 +145,6 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-// Scale of a block whose largest absolute value is `top`, and what its numbers are multiplied with before they are rounded: 448 / top
-// to 2^-22, which the rounding to 2^-4 does not see.  (The reciprocal is taken of top / 2^9: that of a top above 2^126 is no normal
-// number, and 0 here.)
-__device__ __forceinline__ float block_scale(float top, float &inverse) {
-  top = max_nan(top, kLeastTop);
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(top * 0x1p-9f));
-  inverse = kE4m3Max * 0x1p-9f * r;
-  return top / kE4m3Max;
-}
-
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -224,6 +213,49 @@ __device__ __forceinline__ uint64_t two_of(uint32_t low, uint32_t high) {
 __device__ __forceinline__ void fma_two(uint64_t &acc, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b)); }
 __device__ __forceinline__ float low_of(uint64_t v) { return __uint_as_float((uint32_t)v); }
 __device__ __forceinline__ float high_of(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+// Scale of a block whose largest absolute value is `top`, and what quotients by it are made of.
+struct BlockScale {
+  float scale, inverse, divisor;
+};
+__device__ __forceinline__ BlockScale block_scale(float top) {
+  BlockScale b;
+  top = max_nan(top, kLeastTop);
+  constexpr float kPart = 1.f / kE4m3Max;              // (top / 448, rounded as the quotients below are; every top's is the division's)
+  const float q = top * kPart, s = fmaf(fmaf(-q, kE4m3Max, top), kPart, q);
+  const bool infinite = top == INFINITY;
+  b.scale = infinite ? top : s;
+  b.inverse = __frcp_rn(b.scale);                      // (2^-109 <= scale < 2^120: normal numbers both)
+  b.divisor = infinite ? 0.f : s;                      // (beside an infinity finite numbers become 0, not 0 * inf)
+  return b;
+}
+// Blocks whose remainders would fall below the smallest number are divided 2^64 times larger: this says so of a scale and sets it up,
+// the numbers are the caller's to multiply.
+constexpr float kLift = 0x1p64f;
+__device__ __forceinline__ bool lift(BlockScale &b) {
+  if (!(b.scale < 0x1p-90f)) return false;
+  b.inverse *= 1.f / kLift;
+  b.divisor *= kLift;
+  return true;
+}
+// Two numbers divided by their block's scale, as fp32 division rounds it: v * inverse with the remainder's share put back
+// (Markstein's division: correct where the inverse is the rounded reciprocal; checked for every divisor next to each border between two
+// codes of 8 bits, where with an inverse that is 2^-23 off some numbers get the other code).  The remainder is exact, so its rounding
+// downwards says nothing but that one of nothing is -0, which leaves a quotient of -0 as it is.
+__device__ __forceinline__ uint64_t quotient_two(float v0, float v1, const BlockScale &b) {
+  const uint64_t v = two_of(__float_as_uint(v0), __float_as_uint(v1)), i = two_of(__float_as_uint(b.inverse), __float_as_uint(b.inverse)),
+                 d = two_of(__float_as_uint(-b.divisor), __float_as_uint(-b.divisor));
+  uint64_t q, r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(q) : "l"(v), "l"(i));
+  asm("fma.rm.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(q), "l"(d), "l"(v));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(q) : "l"(r), "l"(i), "l"(q));
+  return q;
+}
+// four numbers of a block in 8 bits
+__device__ __forceinline__ uint32_t quantize4(float v0, float v1, float v2, float v3, const BlockScale &b) {
+  const uint64_t lo = quotient_two(v0, v1, b), hi = quotient_two(v2, v3, b);
+  return pack_e4m3(low_of(lo), high_of(lo), low_of(hi), high_of(hi));
+}
+
 // 16, 32 or 64 accumulator columns of this thread's lane, to be read behind tc_ld_wait only
 __device__ __forceinline__ void tc_ld(uint32_t at, uint32_t (&r)[16]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "

@@ -93,10 +93,10 @@ __device__ __forceinline__ void finish4(const FewArgs &t, long long row, int n0,
       if (n0 + i < m.n) top = max_nan(top, fabsf(y[i]));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float inverse;
-    const float scale = block_scale(top, inverse);
-    if (lane == 0) m.scale[row * m.scale_stride + tile] = scale;
-    const uint32_t q = pack_e4m3(y[0] * inverse, y[1] * inverse, y[2] * inverse, y[3] * inverse);
+    BlockScale b = block_scale(top);
+    if (lane == 0) m.scale[row * m.scale_stride + tile] = b.scale;
+    const float up = lift(b) ? kLift : 1.f;
+    const uint32_t q = quantize4(y[0] * up, y[1] * up, y[2] * up, y[3] * up, b);
     unsigned char *o = static_cast<unsigned char *>(m.out) + at;
     if (t.wide && n0 + 3 < m.n) {
       *reinterpret_cast<uint32_t *>(o) = q;

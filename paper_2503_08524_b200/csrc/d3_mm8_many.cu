@@ -321,14 +321,16 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
         s_top[g][r] = top;
         asm volatile("bar.sync 3, 256;" ::: "memory");
         top = max_nan(top, s_top[g ^ 1][r]);
-        float inverse;
-        const float scale = block_scale(top, inverse);
-        if (live && g == 0) t.m.scale[row * t.m.scale_stride + n0 / 128] = scale;
+        BlockScale b = block_scale(top);
+        if (live && g == 0) t.m.scale[row * t.m.scale_stride + n0 / 128] = b.scale;
+        if (lift(b)) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            acc[0][j] = two_of(__float_as_uint(low_of(acc[0][j]) * kLift), __float_as_uint(high_of(acc[0][j]) * kLift));
+        }
         uint32_t v[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          v[j] = pack_e4m3(low_of(acc[0][2 * j]) * inverse, high_of(acc[0][2 * j]) * inverse, low_of(acc[0][2 * j + 1]) * inverse,
-                           high_of(acc[0][2 * j + 1]) * inverse);
+        for (int j = 0; j < 16; ++j) v[j] = quantize4(low_of(acc[0][2 * j]), high_of(acc[0][2 * j]), low_of(acc[0][2 * j + 1]), high_of(acc[0][2 * j + 1]), b);
         // one box: rows of 128 bytes in the 128-byte swizzle
 #pragma unroll
         for (int j = 0; j < 4; ++j)
