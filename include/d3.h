@@ -570,7 +570,7 @@ int32_t d3_add_norm(const d3_add_norm_args *a, void *cuda_stream);
 /* A weight matrix [n][k] in 8 bits (k contiguous: W of y = W x) with its scales. */
 typedef struct d3_weight8 {
   uint32_t struct_size;
-  int32_t n, k;              /* k a multiple of 16                                       */
+  int32_t n, k;              /* up to 2^31 - 256; k a multiple of 16                     */
   int64_t row_stride;        /* in bytes, a multiple of 16, >= k                         */
   const void *q_dev;         /* 16-byte aligned                                          */
   const float *scale_dev;    /* [ceil(n / 128)][ceil(k / 128)], contiguous               */
@@ -592,7 +592,7 @@ int32_t d3_quantize_weight(const void *w_dev, int32_t dtype, int64_t row_stride,
  * rounded to out_dtype, or (D3_E4M3) to 8 bits with scales. */
 typedef struct d3_matmul8_args {
   uint32_t struct_size;
-  int32_t n_rows;            /* >= 0                                                     */
+  int32_t n_rows;            /* 0..2^31 - 256                                            */
   int32_t out_dtype;
   const void *a_dev;         /* D3_E4M3 [n_rows][k]; base and stride multiples of 16     */
   const float *a_scale_dev;  /* [n_rows][ceil(k / 128)]                                  */

@@ -309,8 +309,11 @@ EncodeTiledFn rows_encoder() {
   return fn;
 }
 
+// the largest n_rows, n and k: whole tiles of 256 end within 32 bits
+constexpr int kMostOfOne = 0x7fffff00;
 bool weight_ok(const d3_weight8 *w) {
-  return w && w->struct_size == sizeof(d3_weight8) && w->n >= 1 && w->k >= 16 && w->k % 16 == 0 && w->row_stride >= w->k &&
+  return w && w->struct_size == sizeof(d3_weight8) && w->n >= 1 && w->n <= kMostOfOne && w->k >= 16 && w->k <= kMostOfOne && w->k % 16 == 0 &&
+         w->row_stride >= w->k &&
          w->row_stride % 16 == 0 && w->row_stride <= ((int64_t)1 << 38) && w->q_dev && on_bytes(w->q_dev, 16) && w->scale_dev &&
          on_bytes(w->scale_dev, 4);
 }
@@ -328,7 +331,7 @@ int32_t product(const d3_weight8 *const (&w)[2], const d3_matmul8_args *a, cudaS
   for (int i = 0; i < mats; ++i)
     if (!weight_ok(w[i])) return D3_EINVAL;
   if (mats == 2 && (w[0]->n != w[1]->n || w[0]->k != w[1]->k)) return D3_EINVAL;
-  if (!a || a->struct_size != sizeof(d3_matmul8_args) || a->n_rows < 0) return D3_EINVAL;
+  if (!a || a->struct_size != sizeof(d3_matmul8_args) || a->n_rows < 0 || a->n_rows > kMostOfOne) return D3_EINVAL;
   const bool eight = a->out_dtype == D3_E4M3;
   if (!wide_type(a->out_dtype) && !(eight && mats == 2)) return D3_EINVAL;
   const int n = w[0]->n, k = w[0]->k, es = type_bytes(a->out_dtype);
