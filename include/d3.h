@@ -621,7 +621,8 @@ int32_t d3_matmul8_stall_next(int32_t on);
  * out = z in logits' type; token = the lowest index of out's largest number, -1 where there is none above -inf (NaN is
  * none).  Each part is left out where its pointers are NULL.  Negative ids in history and bias_ids are padding; ids
  * of vocab and more are skipped and D3_EINVAL is stored; so it is for lengths and prompts outside 0..n_history (which
- * count as the nearest bound), and for a mask_of of n_masks and more, which counts as -1: no mask. */
+ * count as the nearest bound), and for a mask_of of n_masks and more, which counts as -1: no mask.  A list of no entries
+ * (n_history or n_bias 0) needs no address, whatever else of its part is given. */
 typedef struct d3_constrain_logits_args {
   uint32_t struct_size;
   int32_t dtype;             /* D3_BF16, D3_FP16, D3_FP32                                */

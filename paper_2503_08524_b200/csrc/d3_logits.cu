@@ -142,7 +142,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_constrain_logits(const __grid_c
         if (v < 0 || v > a.n_history) bad = true;
         return min(max(v, 0), a.n_history);
       };
-      if (a.history) { length = bounded(a.lengths, a.n_history); prompt = bounded(a.prompt, 0); }
+      length = bounded(a.lengths, a.n_history);          // (a history of no entries: checked alike)
+      prompt = bounded(a.prompt, 0);
       if (a.repetition) { rep = a.repetition[row]; per_rep = __fdiv_rn(1.f, rep); }
       if (a.frequency) freq = a.frequency[row];
       if (a.presence) pres = a.presence[row];
@@ -329,9 +330,11 @@ int32_t d3_constrain_logits(const d3_constrain_logits_args *a, void *cuda_stream
                           a->bias_dev, a->masks_dev, a->mask_of_dev, a->token_dev, a->status_dev};
   for (const void *p : words4)
     if (!on_bytes(p, 4)) return D3_EINVAL;
-  if (!a->history_dev && (a->lengths_dev || a->prompt_dev || a->repetition_dev || a->frequency_dev || a->presence_dev)) return D3_EINVAL;
+  // (lists of no entries may have no address)
+  if (!a->history_dev && a->n_history > 0 && (a->lengths_dev || a->prompt_dev || a->repetition_dev || a->frequency_dev || a->presence_dev))
+    return D3_EINVAL;
   if (history && !stride_ok(a->history_stride, 0)) return D3_EINVAL;
-  if ((a->bias_ids_dev != nullptr) != (a->bias_dev != nullptr) || (biased && !stride_ok(a->bias_stride, 0))) return D3_EINVAL;
+  if ((a->n_bias > 0 && (a->bias_ids_dev != nullptr) != (a->bias_dev != nullptr)) || (biased && !stride_ok(a->bias_stride, 0))) return D3_EINVAL;
   if ((a->masks_dev != nullptr) != (a->mask_of_dev != nullptr) ||
       (a->masks_dev && a->n_masks > 1 && (a->mask_stride < 0 || a->mask_stride > most)))
     return D3_EINVAL;
@@ -351,7 +354,7 @@ int32_t d3_constrain_logits(const d3_constrain_logits_args *a, void *cuda_stream
 
   LogitsArgs p;
   memset(&p, 0, sizeof(p));
-  p.n_rows = a->n_rows; p.vocab = a->vocab; p.n_history = a->n_history; p.n_bias = biased ? a->n_bias : 0; p.n_masks = a->n_masks; p.dtype = a->dtype;
+  p.n_rows = a->n_rows; p.vocab = a->vocab; p.n_history = history ? a->n_history : 0; p.n_bias = biased ? a->n_bias : 0; p.n_masks = a->n_masks; p.dtype = a->dtype;
   p.logits = a->logits_dev; p.out = a->out_dev;
   p.logits_stride = rows > 1 ? a->logits_stride : 0; p.out_stride = rows > 1 ? a->out_stride : 0;
   p.history_stride = rows > 1 ? a->history_stride : 0; p.bias_stride = rows > 1 ? a->bias_stride : 0;
