@@ -614,7 +614,7 @@ int32_t d3_matmul8_set_wait_ns(uint64_t ns);
 int32_t d3_matmul8_stall_next(int32_t on);
 
 /* Row by row, z the row's logits in fp32, each step rounded once:
- *   of a token among the first lengths[row] of history[row]:  z *= z > 0 ? 1 / repetition : repetition
+ *   of a token among the first lengths[row] of history[row]:  z = z > 0 ? z / repetition : z * repetition
  *   of one that occurs c > 0 times behind the first prompt[row] of them:  z -= frequency * c,  then z -= presence
  *   of a token in bias_ids[row]:  z += bias (of an id that is there twice the later entry counts)
  *   of a token whose bit in masks[mask_of[row]] is 0:  z = -inf, whatever it was
