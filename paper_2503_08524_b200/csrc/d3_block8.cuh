@@ -310,16 +310,17 @@ __device__ __forceinline__ void tc_ld_wait(uint32_t (&r)[64]) {
     asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]) :: "memory");
 }
 // silu(g) * u = g / (1 + exp(-g)) * u, with 2^x and 1/x of the special function unit.  2^x is as good as its argument: the product
-// -g log2(e) is rounded, by up to 2^-20 where |g| is 16, so what the rounding left out, which a fused multiply-add gives, is put
-// back by 2^(hi + lo) = 2^hi (1 + lo ln 2) (log2(e) itself in 32 bits is 2^-26 off: 2^-22 at 16).  An exp(-g) that is infinite gives 0.
+// -g log2(e) is rounded, by up to 2^-18 where |g| is 88, and log2(e) itself is 2^-26 off in 32 bits, so what both left out, which
+// fused multiply-adds give, is put back by 2^(hi + lo) = 2^hi (1 + lo ln 2).  From 1 + exp(-g) = 2^126 on the reciprocal is below the normal
+// numbers, where the unit gives 0, so far out a quarter of both sides is divided.  An exp(-g) that is infinite (g below -88.72) gives 0.
 __device__ __forceinline__ float gate_of(float g, float u) {
-  constexpr float kLog2e = 1.44269504f;
-  const float hi = g * -kLog2e, lo = fmaf(g, -kLog2e, -hi);
+  constexpr float kLog2e = 1.44269504f, kRest = 1.925963e-8f;    // log2(e) = 1.44269502162933 in 32 bits + 0.00000001925963
+  const float hi = g * -kLog2e, lo = fmaf(g, -kRest, fmaf(g, -kLog2e, -hi)), part = hi > 100.f ? 0.25f : 1.f;
   float t, r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(hi));
-  if (fabsf(hi) < 126.f) t = fmaf(t, lo * 0.693147181f, t);      // (beyond, t is next to 0 or to infinity, and lo may be NaN)
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + t));
-  return g * r * u;
+  if (fabsf(hi) < 128.f) t = fmaf(t, lo * 0.693147181f, t);      // (beyond, t is 0 or infinite, and lo may be NaN)
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fmaf(t, part, part)));
+  return g * part * r * u;
 }
 #endif
 
