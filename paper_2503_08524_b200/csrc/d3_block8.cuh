@@ -172,6 +172,23 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   *gave_up = 1;
   return false;
 }
+// Barriers that the lanes of a warp have to reach together.  Loops of unlike lengths or a branch of one lane may have left them apart.
+__device__ __forceinline__ void group_sync(int barrier, int threads) {
+  __syncwarp();
+  asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+  cluster_arrive();
+  cluster_wait();
+}
 // one lane of a converged warp, the same one every time
 __device__ __forceinline__ bool elect_one() {
   uint32_t r;

@@ -102,8 +102,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_constrain_logits(const __grid_c
       if (rank == 0) mbar_expect(smem_at(&s_bar), 8u * (uint32_t)(a.split - 1));
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    cluster_arrive();
   }
   clear();
   pdl_wait();
@@ -278,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_constrain_logits(const __grid_c
   }
   if (bad && a.status) *a.status = D3_EINVAL;
   if (!a.token) {                            // (the same for every thread of the cluster)
-    if (a.split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (a.split > 1) cluster_wait();
     return;
   }
   // The best token: of the warps, then of the CTAs.  Each CTA but the first writes what it found to the first one's shared memory and
@@ -289,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_constrain_logits(const __grid_c
   for (int o = 16; o > 0; o >>= 1) take(best, at, __shfl_xor_sync(0xffffffffu, best, o), __shfl_xor_sync(0xffffffffu, at, o));
   if (lane == 0) { s_best[warp] = best; s_at[warp] = at; }
   __syncthreads();
-  if (a.split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (a.split > 1) cluster_wait();
   if (warp != 0) return;
   best = lane < kThreads / 32 ? s_best[lane] : -INFINITY;
   at = lane < kThreads / 32 ? s_at[lane] : 0x7fffffff;

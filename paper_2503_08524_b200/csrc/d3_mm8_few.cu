@@ -43,9 +43,6 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ float4 cluster_load4(uint32_t at, uint32_t rank) {
   uint32_t remote;
   float4 v;
@@ -279,7 +276,7 @@ k_mm8_few(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CU
     }
     // every copy has landed and every product is done: the ring holds the sums now, [matrix][row of the call][weight row]
     float *sums = reinterpret_cast<float *>(raw + (ring - smem_at(raw)));
-    asm volatile("bar.sync 1, %0;" ::"n"(128 * G) : "memory");
+    group_sync(1, 128 * G);
 #pragma unroll
     for (int w = 0; w < W; ++w)
 #pragma unroll

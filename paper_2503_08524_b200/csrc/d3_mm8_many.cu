@@ -37,9 +37,6 @@ __device__ __forceinline__ uint32_t pair_rank() {
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ void pair_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ uint32_t at_first(uint32_t local) {   // the same place in the first CTA of the pair
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(local));
@@ -78,7 +75,7 @@ struct ManyArgs {
 // A warpgroup's box is written: it leaves for the columns from c0 on.
 __device__ __forceinline__ void copy_out(const ManyArgs &t, const CUtensorMap &map, uint32_t from, int c0, int row0, int g, int warp, int lane) {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory");
+  group_sync(1 + g, 128);
   if ((warp & 3) == 0 && lane == 0 && c0 < t.m.n && row0 < t.m.n_rows) {
     store_box(&map, from, c0, row0);
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
@@ -149,7 +146,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
   }
   tc_fence_before();
   __syncthreads();
-  pair_sync();
+  cluster_sync();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   pdl_wait();
@@ -275,6 +272,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
         f1[0] = sa.x * w1.x; f1[1] = sa.y * w1.y; f1[2] = sa.z * w1.z; f1[3] = sa.w * w1.w;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_at(&s_used[chunk]));
+        __syncwarp();
         if (++chunk == kChunks) { chunk = 0; there ^= 1; }
 #pragma unroll 1                               // (the loop's code has to stay within reach: four blocks unrolled took 563 us where this takes 502)
         for (int j = 0; j < kChunk; ++j) {
@@ -307,8 +305,8 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
       // what the last tile left must be out of the staging area
       if (t.bulk) {
         if ((warp & 3) == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-        if (W == 2 && dtype == D3_E4M3) asm volatile("bar.sync 3, 256;" ::: "memory");
-        else asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory");
+        if (W == 2 && dtype == D3_E4M3) group_sync(3, 256);
+        else group_sync(1 + g, 128);
       }
       if (W == 2 && dtype == D3_E4M3) {   // the block of scales is 128 columns: two threads have a row's
         const int c0 = n0 + g * 64;
@@ -319,7 +317,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
           top = max_nan(top, fabsf(high_of(acc[0][j])));
         }
         s_top[g][r] = top;
-        asm volatile("bar.sync 3, 256;" ::: "memory");
+        group_sync(3, 256);
         top = max_nan(top, s_top[g ^ 1][r]);
         BlockScale b = block_scale(top);
         if (live && g == 0) t.m.scale[row * t.m.scale_stride + n0 / 128] = b.scale;
@@ -337,14 +335,14 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
           store16(out_at + (uint32_t)(r * 128 + (((g * 4 + j) ^ (r & 7)) << 4)), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
         if (t.bulk) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          asm volatile("bar.sync 3, 256;" ::: "memory");
+          group_sync(3, 256);
           if (warp == 4 && lane == 0 && row0 < t.m.n_rows) {
             store_box(&map_out, out_at, n0, row0);
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
         } else {
           copy_lines<unsigned char, 64>(t, out_at, g * 64, c0, row0, q, lane);
-          asm volatile("bar.sync 3, 256;" ::: "memory");   // s_top is written again
+          group_sync(3, 256);   // s_top is written again
         }
       } else {
         const uint32_t mine = out_at + (uint32_t)(g * (kOutBytes / 2));
@@ -353,7 +351,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
           const int c0 = n0 + h * 128 + g * 64;
           if (t.bulk && h == 1) {         // the second half takes the first one's place
             if ((warp & 3) == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory");
+            group_sync(1 + g, 128);
           }
           if (es == 2) {                  // a box of 64 columns: rows of 128 bytes
 #pragma unroll
@@ -370,7 +368,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
             for (int part = 0; part < 2; ++part) {
               if (t.bulk && part == 1) {
                 if ((warp & 3) == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory");
+                group_sync(1 + g, 128);
               }
 #pragma unroll
               for (int j = 0; j < 8; ++j)
@@ -391,7 +389,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
     if (lane == 0 && t.m.status) *t.m.status = D3_ETIMEOUT;
   }
   tc_fence_before();
-  pair_sync();   // neither CTA goes while the other one's products read its shared memory or arrive at its barriers
+  cluster_sync();   // neither CTA goes while the other one's products read its shared memory or arrive at its barriers
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kColumns) : "memory");
 }
