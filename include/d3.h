@@ -389,7 +389,7 @@ typedef struct d3_paged_kv {
   const float *k_scale_dev, *v_scale_dev; /* E4M3 only: fp32 [n_kv_heads], the stored number times
                                 the scale is the value; NULL = 1                         */
   const void *maps;          /* HOST, nullable: what d3_paged_maps wrote for this pool; without it
-                                every d3_paged_attention encodes its tensor map anew    */
+                                every d3_paged_attention encodes its tensor maps anew   */
 } d3_paged_kv;
 /* Encodes the tensor maps of a pool once, to D3_PAGED_MAPS_BYTES of caller-owned HOST memory (64-byte aligned) that
  * kv->maps may then point to.  They hold for the fields of `kv` as they are now (scales aside): a call with
