@@ -70,16 +70,36 @@ struct ManyArgs {
   Mm8Args m;
   int tiles_m, tiles_n;
   int bulk;                // results may leave as bulk copies (their rows lie on 16 bytes)
+  int whole;               // the columns that do: whole pieces of 16 bytes, behind which such a copy would write the rest of the last piece
 };
 
 // A warpgroup's box is written: it leaves for the columns from c0 on.
 __device__ __forceinline__ void copy_out(const ManyArgs &t, const CUtensorMap &map, uint32_t from, int c0, int row0, int g, int warp, int lane) {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   group_sync(1 + g, 128);
-  if ((warp & 3) == 0 && lane == 0 && c0 < t.m.n && row0 < t.m.n_rows) {
+  if ((warp & 3) == 0 && lane == 0 && c0 < t.whole && row0 < t.m.n_rows) {
     store_box(&map, from, c0, row0);
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
+}
+
+// a number of a box, at row r and `byte` of its 128
+template <typename T>
+__device__ __forceinline__ T box_number(uint32_t from, int r, uint32_t byte) {
+  const uint32_t at = from + (uint32_t)(r * 128) + (((byte >> 4) ^ (uint32_t)(r & 7)) << 4) + (byte & 15u);
+  uint32_t v;
+  if (sizeof(T) == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  else if (sizeof(T) == 2) asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(v) : "r"(at) : "memory");
+  else asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return (T)v;
+}
+// The columns that no bulk copy takes, fewer than 16 bytes of a row: a thread writes those that it has put into the box itself.
+template <typename T, int kColumns>
+__device__ __forceinline__ void copy_rest(const ManyArgs &t, uint32_t from, int first_byte, int c0, int row, int r) {
+  if (t.whole == t.m.n || row >= t.m.n_rows) return;
+#pragma unroll 1
+  for (int c = max(t.whole - c0, 0); c < min(t.m.n - c0, kColumns); ++c)
+    static_cast<T *>(t.m.out)[row * t.m.out_stride + c0 + c] = box_number<T>(from, r, (uint32_t)(first_byte + c * (int)sizeof(T)));
 }
 
 // The same for results whose rows do not lie on 16 bytes: every warp writes the rows that its lanes have put into shared memory,
@@ -95,12 +115,8 @@ __device__ __forceinline__ void copy_lines(const ManyArgs &t, uint32_t from, int
     T *out = static_cast<T *>(t.m.out) + (row0 + r) * t.m.out_stride + c0;
 #pragma unroll
     for (int c = lane; c < kColumns; c += 32) {
-      const uint32_t byte = (uint32_t)(first_byte + c * (int)sizeof(T)), at = from + (uint32_t)(r * 128) + (((byte >> 4) ^ (uint32_t)(r & 7)) << 4) + (byte & 15u);
-      uint32_t v;
-      if (sizeof(T) == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-      else if (sizeof(T) == 2) asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(v) : "r"(at) : "memory");
-      else asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-      if (c0 + c < t.m.n) out[c] = (T)v;
+      const T v = box_number<T>(from, r, (uint32_t)(first_byte + c * (int)sizeof(T)));
+      if (c0 + c < t.m.n) out[c] = v;
     }
   }
   __syncwarp();
@@ -334,9 +350,10 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
         for (int j = 0; j < 4; ++j)
           store16(out_at + (uint32_t)(r * 128 + (((g * 4 + j) ^ (r & 7)) << 4)), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
         if (t.bulk) {
+          copy_rest<unsigned char, 64>(t, out_at, g * 64, c0, row, r);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           group_sync(3, 256);
-          if (warp == 4 && lane == 0 && row0 < t.m.n_rows) {
+          if (warp == 4 && lane == 0 && n0 < t.whole && row0 < t.m.n_rows) {
             store_box(&map_out, out_at, n0, row0);
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
@@ -361,6 +378,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
               for (int e = 0; e < 4; ++e) v[e] = pack2(low_of(acc[h][4 * j + e]), high_of(acc[h][4 * j + e]), dtype);
               store16(mine + (uint32_t)(r * 128 + ((j ^ (r & 7)) << 4)), v[0], v[1], v[2], v[3]);
             }
+            if (t.bulk) copy_rest<unsigned short, 64>(t, mine, 0, c0, row, r);
             if (t.bulk) copy_out(t, map_out, mine, c0, row0, g, warp, lane);
             else copy_lines<unsigned short, 64>(t, mine, 0, c0, row0, q, lane);
           } else {                        // boxes of 32 columns, one behind the other
@@ -374,6 +392,7 @@ k_mm8_many(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ C
               for (int j = 0; j < 8; ++j)
                 store16(mine + (uint32_t)(r * 128 + ((j ^ (r & 7)) << 4)), (uint32_t)acc[h][16 * part + 2 * j], (uint32_t)(acc[h][16 * part + 2 * j] >> 32),
                         (uint32_t)acc[h][16 * part + 2 * j + 1], (uint32_t)(acc[h][16 * part + 2 * j + 1] >> 32));
+              if (t.bulk) copy_rest<unsigned int, 32>(t, mine, 0, c0 + 32 * part, row, r);
               if (t.bulk) copy_out(t, map_out, mine, c0 + 32 * part, row0, g, warp, lane);
               else copy_lines<unsigned int, 32>(t, mine, 0, c0 + 32 * part, row0, q, lane);
             }
@@ -417,7 +436,9 @@ cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args
   // results as bulk copies: boxes of 128 bytes x 128 rows
   TMap mo = ma;
   const int es = type_bytes(p.out_dtype);
-  t.bulk = on_bytes(p.out, 16) && (p.out_stride * es) % 16 == 0 && encode_results8(&mo, p.out, p.n_rows, p.n, p.out_dtype, p.out_stride);
+  t.whole = p.n - p.n % (16 / es);
+  t.bulk = t.whole > 0 && on_bytes(p.out, 16) && (p.out_stride * es) % 16 == 0 &&
+           encode_results8(&mo, p.out, p.n_rows, t.whole, p.out_dtype, p.out_stride);
   const long long pairs = tiles < n_sm / 2 ? tiles : n_sm / 2;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
