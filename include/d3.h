@@ -603,6 +603,10 @@ typedef struct d3_matmul8_args {
 } d3_matmul8_args;
 int32_t d3_matmul8(const d3_weight8 *w, const d3_matmul8_args *a, void *cuda_stream);
 int32_t d3_gated_matmul8(const d3_weight8 *gate, const d3_weight8 *up, const d3_matmul8_args *a, void *cuda_stream);
+/* How a product of these sizes (n_rows >= 1; gated 0 or 1) is done: plan[0] = rows of a tile, 16, 32, 64 or 128 in the kernel that streams
+ * the weights past few rows, 256 in the one for many; plan[1] = CTAs that share a tile's k.  The rule's rates were measured on one kind of
+ * GPU; results differ in the order of their sums alone. */
+int32_t d3_matmul8_plan(int32_t n_rows, int32_t n, int32_t k, int32_t gated, int32_t *plan);
 /* Failure detection, as d3_paged_set_wait_ns.  Every wait inside the two products gives up after about `ns` nanoseconds
  * (default 2e9; it is counted in tries of 40 to 80 ns): the call stores D3_ETIMEOUT, lets what is in flight land (some
  * milliseconds at least) and ends; nothing traps, and the next call is not affected.  Process-wide, for calls made from now

@@ -31,7 +31,8 @@ EXPORTS = ("d3_depth", "d3_schedule", "d3_workspace_bytes", "d3_load", "d3_prefi
            "d3_kv_pages_used", "d3_reset_slot", "d3_sync", "d3_free", "d3_strerror",
            "d3_paged_maps", "d3_page_plan", "d3_paged_append", "d3_rope_table", "d3_paged_attention",
            "d3_paged_attention_workspace", "d3_paged_set_wait_ns", "d3_paged_stall_next", "d3_paged_view",
-           "d3_add_norm", "d3_weight8_map", "d3_quantize_weight", "d3_matmul8", "d3_gated_matmul8", "d3_matmul8_set_wait_ns", "d3_matmul8_stall_next", "d3_constrain_logits")
+           "d3_add_norm", "d3_weight8_map", "d3_quantize_weight", "d3_matmul8", "d3_gated_matmul8", "d3_matmul8_plan", "d3_matmul8_set_wait_ns",
+           "d3_matmul8_stall_next", "d3_constrain_logits")
 
 
 class Config(C.Structure):
@@ -117,6 +118,7 @@ def _load() -> C.CDLL:
     lib.d3_quantize_weight.argtypes = [P, I32, I64, P, P]
     lib.d3_matmul8.argtypes = [P, P, P]
     lib.d3_gated_matmul8.argtypes = [P, P, P, P]
+    lib.d3_matmul8_plan.argtypes = [I32, I32, I32, I32, P]
     lib.d3_matmul8_set_wait_ns.argtypes = [C.c_uint64]
     lib.d3_matmul8_stall_next.argtypes = [I32]
     lib.d3_constrain_logits.argtypes = [P, P]

@@ -161,6 +161,15 @@ def d3_gated_matmul8(a: torch.Tensor, a_scale: torch.Tensor, gate: Weight8, up: 
     return _block_call.product(gate._at, up._at, gate.index, a, a_scale, out, scale, dtype, status)
 
 
+def d3_matmul8_plan(rows: int, n: int, k: int, gated: bool = False) -> Tuple[int, int]:
+    """How a product of these sizes is done: (rows of a tile: 16 to 128, or 256 in the kernel for many rows; CTAs that share its k)."""
+    plan = (_I32 * 2)()
+    rc = LIB.d3_matmul8_plan(rows, n, k, int(bool(gated)), plan)
+    if rc != OK:
+        raise D3Error(rc, "d3_matmul8_plan")
+    return plan[0], plan[1]
+
+
 def d3_matmul8_set_wait_ns(ns: int) -> None:
     """Limit of every wait inside the products of this process from now on (default 2e9)."""
     rc = LIB.d3_matmul8_set_wait_ns(int(ns)) if int(ns) >= 0 else EINVAL

@@ -325,6 +325,10 @@ int64_t scale_blocks(int64_t v) { return (v + kScaleBlock - 1) / kScaleBlock; }
 std::atomic<uint32_t> wait_tries{kWaitTries};
 std::atomic<int> stall_next{0};
 
+// Two kernels: one reads the weights for up to 128 rows at a time (true; as `plan` says), one multiplies 256 rows by 256 weight rows at the
+// tensor cores' rate, if there are tiles enough for every pair of SMs.
+bool choose(const Mm8Args &p, int mats, FewPlan &plan) { return plan_mm8_few(p, mats, plan) <= estimate_mm8_many(p, mats); }
+
 // the checks and the launch that both products share
 int32_t product(const d3_weight8 *const (&w)[2], const d3_matmul8_args *a, cudaStream_t st) {
   const int mats = w[1] ? 2 : 1;
@@ -381,10 +385,8 @@ int32_t product(const d3_weight8 *const (&w)[2], const d3_matmul8_args *a, cudaS
   p.wait_tries = wait_tries.load(std::memory_order_relaxed);
   p.stall = stall_next.exchange(0, std::memory_order_relaxed);
   const int64_t a_stride = rows > 1 ? a->a_stride : (int64_t)k;
-  // Two kernels: one reads the weights for up to 128 rows at a time, one multiplies 256 rows by 256 weight rows at the tensor cores'
-  // rate, if there are tiles enough for every pair of SMs.
   FewPlan plan;
-  const bool few = plan_mm8_few(p, mats, plan) <= estimate_mm8_many(p, mats);
+  const bool few = choose(p, mats, plan);
   const cudaError_t e = few ? launch_mm8_few(*map[0], map[1], a->a_dev, a_stride, p, plan, st)
                             : launch_mm8_many(*map[0], map[1], a->a_dev, a_stride, p, st);
   return e == cudaSuccess ? D3_OK : D3_ECUDA;
@@ -508,6 +510,19 @@ int32_t d3_matmul8_set_wait_ns(uint64_t ns) {
 int32_t d3_matmul8_stall_next(int32_t on) {
   if (on != 0 && on != 1) return D3_EINVAL;
   stall_next.store(on, std::memory_order_relaxed);
+  return D3_OK;
+}
+
+int32_t d3_matmul8_plan(int32_t n_rows, int32_t n, int32_t k, int32_t gated, int32_t *plan) {
+  if (n_rows < 1 || n_rows > kMostOfOne || n < 1 || n > kMostOfOne || k < 16 || k > kMostOfOne || k % 16 || gated < 0 || gated > 1 || !plan)
+    return D3_EINVAL;
+  Mm8Args p;
+  memset(&p, 0, sizeof(p));
+  p.n_rows = n_rows; p.n = n; p.k = k; p.n_kb = (int)scale_blocks(k);
+  FewPlan few;
+  const bool is_few = choose(p, gated ? 2 : 1, few);
+  plan[0] = is_few ? few.rows : 256;
+  plan[1] = is_few ? few.split : 1;
   return D3_OK;
 }
 
