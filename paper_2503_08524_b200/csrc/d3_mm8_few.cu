@@ -19,8 +19,9 @@
 // 8 rows, 5120 -> 13824: 108 25.9, 216 26.3.
 //
 // What is left over the time of the weights at the memory's rate is some 4 us a call: the last sums and results 1.2, the step from
-// one call to the next 1 to 1.4, the first copies' way 1.5.  A CTA takes at most half of an SM (but for more than 64 rows),
-// so the next call's CTAs are set up beside it.  Letting them ask for weights ahead of their turn gave nothing (copies
+// one call to the next 1 to 1.4, the first copies' way 1.5.  A CTA of one matrix and up to 64 rows takes at most half of an SM, so the
+// next call's CTAs are set up beside it; one of two matrices (three stages in half of an SM would be too few) or of 128 rows takes
+// a whole one.  Letting them ask for weights ahead of their turn gave nothing (copies
 // into the ring 12.5 us where this takes 11.9) or cost (into L2 box by box 14.0, row by row 18.4).
 #include <math.h>
 
@@ -62,7 +63,7 @@ struct Few {
   static constexpr int N = C * G;                              // padded rows
   static constexpr int kThreads = 128 + 128 * G;               // copies, products, scales, an idle warp; epilogue warps
   static constexpr int kColumns = U * W * N;                   // accumulator columns of a unit, of which there are two
-  static constexpr bool kHalf = 2 * kColumns <= 256;           // two CTAs fit on an SM
+  static constexpr bool kHalf = 2 * kColumns <= 256;           // two CTAs' columns fit into an SM's tensor memory
   static constexpr int kStage = W * kTileBytes + N * 128;      // a block
   static constexpr int kSums = W * N * 128 * 4;                // one CTA's sums, over the ring when it is empty
   // 256 threads start with 128 registers, 384 with 168; the epilogue takes 200 (216) of them and leaves 56 (72) to the others
@@ -336,7 +337,8 @@ cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args
   t.m = p;
   const int fixed = kChunks * kChunk * (F::N + 2) * 4 + 1024 + 1024;      // static shared memory, and the alignment of the ring
   int stages = (kHalfSmem - fixed) / F::kStage;
-  if (!F::kHalf || G > 1 || stages < 4) stages = (kWholeSmem - fixed) / F::kStage;
+  const bool shared = F::kHalf && G == 1 && stages >= 4;                  // two CTAs fit on an SM (one matrix, up to 64 rows)
+  if (!shared) stages = (kWholeSmem - fixed) / F::kStage;
   if (stages > kMaxStages) stages = kMaxStages;
   const int least = (F::kSums + F::kStage - 1) / F::kStage;               // the ring holds the sums in the end
   if (stages < least) stages = least;
@@ -344,8 +346,9 @@ cudaError_t launch(const TMap &w0, const TMap &w1, const TMap &ma, const Mm8Args
   t.stages = stages;
   t.split = split;
   // Where some SMs have two CTAs, those of a call that begins early take places that even them out (4 rows, 8192 -> 10240, call
-  // after call: 20.4 us, begun late 18.2; 1 row, 4096 -> 12288, one CTA an SM: 11.8, late 12.0).
-  t.late = (long long)tiles * split * ((p.n_rows + F::N - 1) / F::N) > 148;
+  // after call: 20.4 us, begun late 18.2; 1 row, 4096 -> 12288, one CTA an SM: 11.8, late 12.0).  Where a CTA has an SM to itself there is
+  // no place to take (gated 8 x 8192 -> 28672, call after call: 74.0, late 74.0; 32 rows of it 78.9 and 79.0).
+  t.late = shared && (long long)tiles * split * ((p.n_rows + F::N - 1) / F::N) > 148;
   const int es = type_bytes(p.out_dtype);
   t.wide = on_bytes(p.out, 4 * es) && (p.n_rows == 1 || p.out_stride % 4 == 0);
   cudaLaunchConfig_t cfg;
