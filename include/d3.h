@@ -547,7 +547,9 @@ int32_t d3_paged_view(const d3_model *m, int32_t layer, d3_paged_kv *kv, const i
  * rounds it and then to nearest even. */
 
 /* y[row] = s / sqrt(mean(s^2) + eps) * gain with s = x + add, fp32 throughout (s is not rounded in between);
- * total = s in add's type.  gain_dev NULL: no norm, y = s.  Rows are `dim` contiguous numbers, strides in elements. */
+ * total = s in add's type.  gain_dev NULL: no norm, y = s.  Rows are `dim` contiguous numbers, strides in elements.  Squares are
+ * fp32 too: a mean of theirs above its largest number (numbers of 1.8e19) is infinite, and y 0.  A number of
+ * a row above 32768 takes 1.4 times as long. */
 typedef struct d3_add_norm_args {
   uint32_t struct_size;
   int32_t n_rows;            /* >= 0                                                     */
@@ -587,7 +589,8 @@ int32_t d3_weight8_map(const d3_weight8 *w, void *map);
 int32_t d3_quantize_weight(const void *w_dev, int32_t dtype, int64_t row_stride, const d3_weight8 *w8, void *cuda_stream);
 
 /* out[row][n] = sum_k a[row][k] w[n][k]: the products of a block of 128 k are summed by the tensor core in fp32, each
- * block's sum is multiplied by the two scales and added in fp32; one rounding to out_dtype (D3_BF16, D3_FP16, D3_FP32).
+ * block's sum is multiplied by the product of the two scales and added, all in fp32; one rounding to out_dtype (D3_BF16,
+ * D3_FP16, D3_FP32).
  * d3_gated_matmul8: g and u are such sums over `gate` and `up` (one shape), h = g / (1 + exp(-g)) * u in fp32, then
  * rounded to out_dtype, or (D3_E4M3) to 8 bits with scales. */
 typedef struct d3_matmul8_args {
@@ -644,7 +647,7 @@ typedef struct d3_constrain_logits_args {
   const int32_t *masks_dev;     /* nullable, [n_masks][ceil(vocab / 32)]: token t is bit t % 32 of word t / 32 */
   const int32_t *mask_of_dev;   /* with masks: [n_rows]                                  */
   int32_t *token_dev;           /* nullable, [n_rows]                                    */
-  int32_t *status_dev;          /* nullable                                              */
+  int32_t *status_dev;          /* nullable; D3_ETIMEOUT: a row's parts were waited for in vain, its token is undefined */
 } d3_constrain_logits_args;
 int32_t d3_constrain_logits(const d3_constrain_logits_args *a, void *cuda_stream);
 

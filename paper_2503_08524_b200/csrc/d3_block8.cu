@@ -233,6 +233,7 @@ cudaError_t launch_norm(const NormArgs &a, cudaStream_t st) {
 template <int kType, int kAdd>
 cudaError_t launch_norm_k(const NormArgs &a, cudaStream_t st) {
   // (us with 8 / 16 numbers a thread: 4096 x 4096 in 16 bits 23.9 / 28.8, 32 x 5120 2.4 / 2.7, 8191 x 8192 130 / 128)
+  // (64 numbers a thread do not fit into its registers: 250 x 65536 takes 65 us where 500 x 32768 takes 46)
   if (a.dim <= 8192) return launch_norm<1, 8, kType, kAdd>(a, st);
   if (a.dim <= 16384) return launch_norm<1, 16, kType, kAdd>(a, st);
   if (a.dim <= 32768) return launch_norm<2, 16, kType, kAdd>(a, st);
@@ -253,7 +254,9 @@ struct QuantWeightArgs {
   unsigned char *q;
   float *scale;
 };
-// One block of 128 x 128 per CTA: thread t has 64 numbers of row t / 2, 8 at a time (k is a multiple of 16).
+// One block of 128 x 128 per CTA: thread t has 64 numbers of row t / 2, 8 at a time (k is a multiple of 16).  A warp's load
+// takes 16 bytes from each of 32 lines, and L2 moves 530 MB where 151 are read and written: 12288 x 4096 bf16 takes 53 us, 44 % of the
+// copy rate.  (A weight is brought to 8 bits once.)
 __global__ void __launch_bounds__(256) k_quantize_weight(const __grid_constant__ QuantWeightArgs a) {
   __shared__ float s_top[8];
   pdl_wait();

@@ -9,6 +9,9 @@
 // while the next block is multiplied, eight epilogue warps fetch the sum, multiply it by its two scales and add it to
 // registers (a thread has one row, 64 columns of each half; two numbers an instruction).  The grid is persistent, a pair
 // of CTAs for each pair of SMs; results go through shared memory and leave as bulk copies while the next tile begins.
+//
+// Times in this file are those of short runs at full clock; in a loop of such calls the power cap (990 W, 1.48 GHz) takes a sixth more
+// (8191 x 8192 x 8192: 464 us, in a loop 540 to 575).
 #include <math.h>
 
 #include <atomic>
