@@ -57,3 +57,20 @@ def test_gated_results_of_large_numbers(rows, k, n):
     assert 2.0 ** 127.9 < float(h.abs().max()) < 2.0 ** 128
     out, scale = K.d3_gated_matmul8(a, s, K.Weight8(*gate), K.Weight8(*up))
     F.check_8_bits(out, scale, h, dh)
+
+
+@pytest.mark.parametrize("rows,k,n", [(1, 256, 384), (20, 512, 300), (100, 256, 384), (600, 1024, 2000)])
+@pytest.mark.parametrize("power", [-40, -85, -95, -105, -120])
+def test_gated_results_of_small_numbers(rows, k, n, power):
+    """Down to blocks that count as 2^-100 and keep a few of their bits, or none."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    a, s = F.some_rows(rows, k, g)
+    gate, up = F.some_weight(n, k, g), F.some_weight(n, k, g)
+    up = (up[0], up[1] * 2.0 ** power)
+    h, dh = F.gated(*F.product(a, s, *gate), *F.product(a, s, *up))
+    out, scale = K.d3_gated_matmul8(a, s, K.Weight8(*gate), K.Weight8(*up))
+    F.check_8_bits(out, scale, h, dh)
+    if power == -120:                 # (a number of 2^-118.8 and more, half the least one's 2^-9 of that scale, is not 0)
+        assert float(h.abs().max()) < 2.0 ** -100 and (scale == 2.0 ** -100 / 448).all()
+    elif power >= -95:
+        assert (out.float().abs().amax(1) >= 256).all()
